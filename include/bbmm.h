@@ -380,6 +380,90 @@ int bbmm_predict_mean(bbmm_ctx* ctx, const float* Xstar, int64_t ns, const float
 int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns, float* var,
                      int64_t* iters_run, double* max_resid);
 
+/* ------------------------------------------------------------------------
+ * Attention: reading values at queries off the inputs of another, longer or shorter sequence with the normalised
+ * exponential kernel (the kernel smoother beside bbmm_predict_mean), and its learned bias by buckets of the
+ * position difference (a stationary log-kernel by pieces), with gradients.  None of these calls needs bbmm_setup
+ * or touches the problem it set.
+ *
+ *   s_ij = scale q_i.k_j + T[h][bucket(j - i - start_b)]   over the keys j < k_len_b with key_mask_bj != 0,
+ *   o_i  = sum_j exp(s_ij - lse_i) v_j,     lse_i = log sum_j exp(s_ij).
+ * A row that nothing is left for (no keys, all masked, all scores -infinity) has o_i = 0, lse_i = -infinity and no part in any
+ * gradient.  Masked keys, and queries and keys behind their lengths, may hold anything, infinities and NaN
+ * included; rows of O at or behind q_len_b are zero (lse -infinity), and so are rows of the gradients behind the lengths and
+ * of masked keys.
+ *
+ *   bucket(r), with edges e_1 < .. < e_E and c(x) the number of edges that are at most x:
+ *       two_sided:  c(|r|) + (r > 0 ? E + 1 : 0)     2 (E + 1) buckets
+ *       otherwise:  c(max(-r, 0))                        E + 1 buckets
+ *
+ *   type          BBMM_TYPE_F32, _F16 or _BF16: of Q, K, V, O, the table and all gradients.  lse is fp32.  Scores, softmax statistics
+ *                 and sums are fp32; weights (and dS) are rounded to `type` once as operands of the second products.
+ *   heads         query heads; kv_heads divides it, head h reads keys and values of head h / (heads / kv_heads)
+ *   d, dv         features of queries and keys, and of values: 1 .. 128
+ *   scale         finite and > 0
+ *   Q, K, V       device; element [b][row][head][feature] at b stride[0] + row stride[1] + head stride[2] + feature
+ *                 (strides in elements, none negative; 0 shares an input, its gradient is then returned for every use)
+ *   q_len, k_len  device, batch entries (taken as within [0, nq] and [0, nk]), or NULL: all rows
+ *   key_mask      device, batch x nk bytes, or NULL
+ *   table         device, heads x buckets, or NULL (no bias).  Entries may be -infinity (pairs excluded); finite entries below
+ *                 -2.3e38 count as that
+ *   edges         host, n_edges entries, 1 <= e_1 < .. <= 1024; 0 <= n_edges <= 63; only read during the call
+ *   q_start       device, batch entries: position of query 0 on the keys' axis, or NULL (0)
+ * Limits: batch, heads and kv_heads <= 65535, nq and nk <= 2^30; zero sizes are allowed for batch, nq and nk.
+ * Outputs are dense, [batch][row][head][feature]; lse [batch][heads][nq].  Outputs must not overlap inputs or each other.
+ * The calls only queue work on the context's stream, allocate nothing and keep nothing: their workspace is the
+ * caller's, so they may be recorded in a graph, and two graphs (or streams) may run together if their
+ * buffers and workspaces differ.  Results are the same from call to call (no sums in an order that changes).
+ * ---------------------------------------------------------------------- */
+enum { BBMM_TYPE_F32 = 0, BBMM_TYPE_F16 = 1, BBMM_TYPE_BF16 = 2 };
+
+typedef struct {
+  int32_t type;
+  int32_t two_sided;
+  int64_t batch, heads, kv_heads, nq, nk, d, dv;
+  double scale;
+  const void* Q;
+  const void* K;
+  const void* V;
+  int64_t q_stride[3];
+  int64_t k_stride[3];
+  int64_t v_stride[3];
+  const int32_t* q_len;
+  const int32_t* k_len;
+  const uint8_t* key_mask;
+  const void* table;
+  int64_t n_edges;
+  const int32_t* edges;
+  const int64_t* q_start;
+} bbmm_attention;
+
+/* Bytes of device workspace (16-byte aligned) that bbmm_attend (grad 0) or bbmm_attend_grad (grad 1) needs for these sizes;
+ * may be 0.  bytes: host.  Pointers of `in` are not read, only whether a table is there. */
+int bbmm_attend_workspace(bbmm_ctx* ctx, const bbmm_attention* in, int32_t grad, int64_t* bytes);
+
+/* O (device, batch x nq x heads x dv) and lse (device, batch x heads x nq float). */
+int bbmm_attend(bbmm_ctx* ctx, const bbmm_attention* in, void* O, float* lse, void* work, int64_t work_bytes);
+
+/* Gradients of sum(dO . O): dQ, dK, dV (device, dense, shapes of Q, K, V) and dtable (device, heads x buckets; NULL without a
+ * table).  O, lse: as bbmm_attend left them for the same `in`; dO: device, strides like Q's.  The table's gradient
+ * is summed over batch, queries and keys, those of K and V over the heads that share them. */
+int bbmm_attend_grad(bbmm_ctx* ctx, const bbmm_attention* in, const void* O, const float* lse, const void* dO,
+                     const int64_t* do_stride, void* dQ, void* dK, void* dV, void* dtable, void* work, int64_t work_bytes);
+
+/* The bias as a matrix: B[h][i][j] = table[h][bucket(j - i - start)], device, heads x nq x nk, dense. */
+int bbmm_bucket_bias(bbmm_ctx* ctx, int32_t type, const void* table, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges,
+                     const int32_t* edges, int32_t two_sided, int64_t start, void* B);
+
+/* Gradient of the table from that of the matrix, summed over the batch that the matrix was broadcast to:
+ * dtable[h][n] = sum over b and all (i, j) of bucket n of dB[b][h][i][j].  dB: device, batch x heads x nq x nk, dense.
+ * work: device, bbmm_bucket_bias_workspace bytes. */
+int bbmm_bucket_bias_workspace(bbmm_ctx* ctx, int64_t batch, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges,
+                               int32_t two_sided, int64_t* bytes);
+int bbmm_bucket_bias_grad(bbmm_ctx* ctx, int32_t type, const void* dB, int64_t batch, int64_t heads, int64_t nq, int64_t nk,
+                          int64_t n_edges, const int32_t* edges, int32_t two_sided, int64_t start, void* dtable, void* work,
+                          int64_t work_bytes);
+
 #ifdef __cplusplus
 }
 #endif

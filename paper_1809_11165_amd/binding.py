@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libbbmm.so")
 
 KERNEL_RBF, KERNEL_MATERN52 = 0, 1
 MODE_MATERIALISED, MODE_ONTHEFLY, MODE_SGPR = 0, 1, 2
+TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
 OK, EINVAL, ENOMEM, ENOTPD, ENONFINITE, EHIP, ENOCONV = 0, 1, 2, 3, 4, 5, 6
 MAX_ITERS = 256
 
@@ -30,6 +31,8 @@ EXPORTS = [
     "bbmm_precond_setup", "bbmm_precond_solve", "bbmm_make_probes", "bbmm_mbcg",
     "bbmm_tridiag_eig_batched", "bbmm_tridiag_eig_batched_noalloc", "bbmm_slq_logdet", "bbmm_slq_from_coeffs", "bbmm_dk_traces",
     "bbmm_predict_mean", "bbmm_predict_var",
+    "bbmm_attend_workspace", "bbmm_attend", "bbmm_attend_grad",
+    "bbmm_bucket_bias", "bbmm_bucket_bias_workspace", "bbmm_bucket_bias_grad",
 ]
 
 
@@ -60,6 +63,16 @@ class _Result(C.Structure):
                 ("alpha", C.POINTER(C.c_double)), ("beta", C.POINTER(C.c_double)),
                 ("resid", C.POINTER(C.c_double)), ("pivots", C.POINTER(C.c_int64)),
                 ("slq_terms", C.POINTER(C.c_double))]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("type", C.c_int32), ("two_sided", C.c_int32),
+                ("batch", C.c_int64), ("heads", C.c_int64), ("kv_heads", C.c_int64), ("nq", C.c_int64),
+                ("nk", C.c_int64), ("d", C.c_int64), ("dv", C.c_int64), ("scale", C.c_double),
+                ("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("q_len", C.c_void_p), ("k_len", C.c_void_p), ("key_mask", C.c_void_p), ("table", C.c_void_p),
+                ("n_edges", C.c_int64), ("edges", C.POINTER(C.c_int32)), ("q_start", C.c_void_p)]
 
 
 _lib = None
@@ -112,6 +125,18 @@ def load_library() -> C.CDLL:
     lib.bbmm_predict_mean.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
     lib.bbmm_predict_var.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
                                      C.POINTER(C.c_int64), C.POINTER(C.c_double)]
+    lib.bbmm_attend_workspace.argtypes = [C.c_void_p, C.POINTER(_Attention), C.c_int32, C.POINTER(C.c_int64)]
+    lib.bbmm_attend.argtypes = [C.c_void_p, C.POINTER(_Attention), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]
+    lib.bbmm_attend_grad.argtypes = [C.c_void_p, C.POINTER(_Attention), C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.POINTER(C.c_int64), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_int64]
+    lib.bbmm_bucket_bias.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
+                                     C.POINTER(C.c_int32), C.c_int32, C.c_int64, C.c_void_p]
+    lib.bbmm_bucket_bias_workspace.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
+                                               C.c_int32, C.POINTER(C.c_int64)]
+    lib.bbmm_bucket_bias_grad.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
+                                          C.c_int64, C.POINTER(C.c_int32), C.c_int32, C.c_int64, C.c_void_p, C.c_void_p,
+                                          C.c_int64]
     _lib = lib
     return lib
 
@@ -192,6 +217,114 @@ class Problem:
             _check_dev(self.Uind, (self.Uind.shape[0], d), "Uind")
             p.m, p.Uind, p.jitter_rel = int(self.Uind.shape[0]), self.Uind.data_ptr(), float(self.jitter_rel)
         return p
+
+
+def _type_of(tensor, name):
+    import torch
+    codes = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}
+    if not isinstance(tensor, torch.Tensor) or tensor.dtype not in codes:
+        raise TypeError("%s must be a float32, float16 or bfloat16 tensor" % name)
+    return codes[tensor.dtype]
+
+
+def _check_same(tensor, shape, dtypes, device, name, dense=True):
+    """A tensor of this shape, one of these types and on this device; dense, or with its last dimension contiguous."""
+    import torch
+    if not isinstance(tensor, torch.Tensor) or tensor.dtype not in dtypes:
+        raise TypeError("%s must be a tensor of type %s" % (name, " or ".join(str(t) for t in dtypes)))
+    if tensor.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, tensor.device, device))
+    if tuple(tensor.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(tensor.shape), tuple(shape)))
+    if dense and not tensor.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if not dense and tensor.shape[-1] > 1 and tensor.stride(-1) != 1 and tensor.numel():
+        raise ValueError("the last dimension of %s must be contiguous" % name)
+
+
+def bucket_edges(num_buckets: int, max_distance: int, two_sided: bool = True):
+    """Edges of the usual buckets: unit steps up to half of a side's buckets, then equal steps of the logarithm up to
+    max_distance, which opens the last one.  An edge is the first whole distance at or beyond its step, found in whole
+    numbers (x^n against powers), so nothing is rounded at a border.  Steps that fall on the same distance move up by one."""
+    side = num_buckets // 2 if two_sided else num_buckets
+    if side < 1 or (two_sided and num_buckets % 2) or max_distance < 1:
+        raise ValueError("num_buckets must be positive (even when two_sided) and max_distance at least 1")
+    near = max(1, side // 2)
+    far = max(int(max_distance), near + 1)
+    n = side - near
+    edges = list(range(1, near + 1))
+    for k in range(1, n):
+        want = near ** (n - k) * far ** k
+        lo, hi = edges[-1] + 1, max(far, edges[-1] + 1)
+        while lo < hi:
+            mid = (lo + hi) // 2
+            lo, hi = (lo, mid) if mid ** n >= want else (mid + 1, hi)
+        edges.append(lo)
+    return edges[:side - 1]
+
+
+def _edges(edges):
+    """Edges as the C array that a call takes (range and order are checked by the library)."""
+    e = [int(x) for x in (edges if edges is not None else ())]
+    if any(x < -2 ** 31 or x >= 2 ** 31 for x in e):
+        raise ValueError("bucket edges must ascend within [1, 1024]")
+    return (C.c_int32 * len(e))(*e)
+
+
+@dataclass
+class Attention:
+    """One attention call (see include/bbmm.h, "Attention").  Q (batch, nq, heads, d), K (batch, nk, kv_heads, d), V (batch,
+    nk, kv_heads, dv): device tensors of one type, any strides with the last dimension contiguous.  scale: default
+    d^-1/2.  q_len, k_len: int32 (batch,); key_mask: bool or uint8 (batch, nk), true takes part; table: (heads, buckets)
+    of Q's type with edges (see bucket_edges); q_start: int64 (batch,)."""
+    Q: "object"
+    K: "object"
+    V: "object"
+    scale: Optional[float] = None
+    q_len: "object" = None
+    k_len: "object" = None
+    key_mask: "object" = None
+    table: "object" = None
+    edges: "object" = None
+    two_sided: bool = True
+    q_start: "object" = None
+    _keep: list = field(default_factory=list, repr=False)
+
+    def tensors(self):
+        return [t for t in (self.Q, self.K, self.V, self.q_len, self.k_len, self.key_mask, self.table, self.q_start)
+                if t is not None]
+
+    def to_c(self, device) -> _Attention:
+        import torch
+        a = _Attention()
+        a.type = _type_of(self.Q, "Q")
+        t = (self.Q.dtype,)
+        if self.Q.dim() != 4 or self.K.dim() != 4 or self.V.dim() != 4:
+            raise ValueError("Q, K and V must have four dimensions (batch, row, head, feature)")
+        b, nq, h, d = self.Q.shape
+        nk, hk, dv = self.K.shape[1], self.K.shape[2], self.V.shape[3]
+        _check_same(self.Q, (b, nq, h, d), t, device, "Q", dense=False)
+        _check_same(self.K, (b, nk, hk, d), t, device, "K", dense=False)
+        _check_same(self.V, (b, nk, hk, dv), t, device, "V", dense=False)
+        a.batch, a.heads, a.kv_heads, a.nq, a.nk, a.d, a.dv = b, h, hk, nq, nk, d, dv
+        a.scale = float(d) ** -0.5 if self.scale is None else float(self.scale)
+        a.Q, a.K, a.V = self.Q.data_ptr(), self.K.data_ptr(), self.V.data_ptr()
+        a.q_stride[:], a.k_stride[:], a.v_stride[:] = self.Q.stride()[:3], self.K.stride()[:3], self.V.stride()[:3]
+        for name, shape, dtypes in (("q_len", (b,), (torch.int32,)), ("k_len", (b,), (torch.int32,)),
+                                    ("key_mask", (b, nk), (torch.bool, torch.uint8)), ("q_start", (b,), (torch.int64,))):
+            x = getattr(self, name)
+            if x is not None:
+                _check_same(x, shape, dtypes, device, name)
+                setattr(a, name, x.data_ptr())
+        a.two_sided = int(bool(self.two_sided))
+        if self.table is not None:
+            e = _edges(self.edges)
+            _check_same(self.table, (h, (len(e) + 1) * (2 if self.two_sided else 1)), t, device, "table")
+            self._keep = [e]
+            a.table, a.n_edges, a.edges = self.table.data_ptr(), len(e), e
+        elif self.edges is not None:
+            raise ValueError("edges without a table")
+        return a
 
 
 @dataclass
@@ -429,6 +562,114 @@ class Context:
         self._ck(self.lib.bbmm_predict_var(self.h, mode, _dptr(Xstar), ns, _dptr(var), C.byref(iters),
                                            C.byref(resid)))
         return var, int(iters.value), float(resid.value)
+
+
+    # ---- attention --------------------------------------------------------------------------
+    def _ordered(self, tensors, call):
+        """Runs `call` (which allocates its outputs and queues work) with the context's stream current.  Where that is not
+        the caller's stream, the work waits for what the caller has queued, the caller's stream waits for the work, and
+        no tensor's memory is reused before both are done."""
+        torch = self.torch
+        here = torch.cuda.current_stream(self.device)
+        if here.cuda_stream == self._stream.cuda_stream:
+            with torch.cuda.device(self.device):
+                return call()
+        self._stream.wait_stream(here)
+        with torch.cuda.device(self.device), torch.cuda.stream(self._stream):
+            out = call()
+        for t in tensors:
+            t.record_stream(self._stream)
+        for t in out if isinstance(out, tuple) else (out,):
+            if t is not None:
+                t.record_stream(here)
+        here.wait_stream(self._stream)
+        return out
+
+    def _work(self, nbytes: int):
+        """(tensor to keep, pointer, size) of a workspace from torch's allocator on the current stream."""
+        if nbytes == 0:
+            return None, None, 0
+        w = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
+        return w, _dptr(w), nbytes
+
+    def _attend_bytes(self, a: _Attention, grad: bool) -> int:
+        n = C.c_int64(0)
+        self._ck(self.lib.bbmm_attend_workspace(self.h, C.byref(a), int(grad), C.byref(n)))
+        return n.value
+
+    def bbmm_attend_workspace(self, att: Attention, grad: bool = False) -> int:
+        """Bytes that bbmm_attend (bbmm_attend_grad) takes from torch's allocator besides its outputs."""
+        return self._attend_bytes(att.to_c(self.device), grad)
+
+    def bbmm_attend(self, att: Attention):
+        """(O, lse): (batch, nq, heads, dv) of Q's type and (batch, heads, nq) float32."""
+        a = att.to_c(self.device)
+
+        def call():
+            O = self.torch.empty(a.batch, a.nq, a.heads, a.dv, dtype=att.Q.dtype, device=self.device)
+            lse = self._empty(a.batch, a.heads, a.nq)
+            w, wp, n = self._work(self._attend_bytes(a, False))
+            self._ck(self.lib.bbmm_attend(self.h, C.byref(a), _dptr(O), _dptr(lse), wp, n))
+            return O, lse
+
+        return self._ordered(att.tensors(), call)
+
+    def bbmm_attend_grad(self, att: Attention, O, lse, dO):
+        """(dQ, dK, dV, dtable) of sum(dO * O); dtable is None without a table.  O, lse: from bbmm_attend of the same call."""
+        a = att.to_c(self.device)
+        t = (att.Q.dtype,)
+        shape = (a.batch, a.nq, a.heads, a.dv)
+        _check_same(O, shape, t, self.device, "O")
+        _check_same(lse, (a.batch, a.heads, a.nq), (self.torch.float32,), self.device, "lse")
+        _check_same(dO, shape, t, self.device, "dO", dense=False)
+        stride = (C.c_int64 * 3)(*dO.stride()[:3])
+
+        def call():
+            dQ, dK, dV = (self.torch.empty(x.shape, dtype=x.dtype, device=self.device) for x in (att.Q, att.K, att.V))
+            dtable = None if att.table is None else self.torch.empty_like(att.table)
+            w, wp, n = self._work(self._attend_bytes(a, True))
+            self._ck(self.lib.bbmm_attend_grad(self.h, C.byref(a), _dptr(O), _dptr(lse), _dptr(dO), stride, _dptr(dQ),
+                                               _dptr(dK), _dptr(dV), None if dtable is None else _dptr(dtable), wp, n))
+            return dQ, dK, dV, dtable
+
+        return self._ordered(att.tensors() + [O, lse, dO], call)
+
+    def bbmm_bucket_bias(self, table, edges, nq: int, nk: int, two_sided: bool = True, start: int = 0):
+        """The bias as a matrix (heads, nq, nk) of the table's type: table[h, bucket(j - i - start)]."""
+        kind, e = _type_of(table, "table"), _edges(edges)
+        _check_same(table, (table.shape[0], (len(e) + 1) * (2 if two_sided else 1)), (table.dtype,), self.device, "table")
+
+        def call():
+            B = self.torch.empty(table.shape[0], nq, nk, dtype=table.dtype, device=self.device)
+            self._ck(self.lib.bbmm_bucket_bias(self.h, kind, _dptr(table), table.shape[0], nq, nk, len(e), e,
+                                               int(bool(two_sided)), int(start), _dptr(B)))
+            return B
+
+        return self._ordered([table], call)
+
+    def bbmm_bucket_bias_workspace(self, batch: int, heads: int, nq: int, nk: int, n_edges: int, two_sided: bool = True) -> int:
+        """Bytes that bbmm_bucket_bias_grad takes from torch's allocator besides its output."""
+        n = C.c_int64(0)
+        self._ck(self.lib.bbmm_bucket_bias_workspace(self.h, batch, heads, nq, nk, n_edges, int(bool(two_sided)),
+                                                     C.byref(n)))
+        return n.value
+
+    def bbmm_bucket_bias_grad(self, dB, edges, two_sided: bool = True, start: int = 0):
+        """Gradient (heads, buckets) of the table from that of the matrix, dB (batch, heads, nq, nk), summed over the batch."""
+        kind, e = _type_of(dB, "dB"), _edges(edges)
+        if dB.dim() != 4:
+            raise ValueError("dB must have four dimensions (batch, head, nq, nk)")
+        _check_same(dB, dB.shape, (dB.dtype,), self.device, "dB")
+        b, h, nq, nk = dB.shape
+
+        def call():
+            dtable = self.torch.empty(h, (len(e) + 1) * (2 if two_sided else 1), dtype=dB.dtype, device=self.device)
+            w, wp, n = self._work(self.bbmm_bucket_bias_workspace(b, h, nq, nk, len(e), two_sided))
+            self._ck(self.lib.bbmm_bucket_bias_grad(self.h, kind, _dptr(dB), b, h, nq, nk, len(e), e, int(bool(two_sided)),
+                                                    int(start), _dptr(dtable), wp, n))
+            return dtable
+
+        return self._ordered([dB], call)
 
 
 def problem_from_workload(w, mode: int, device="cuda:0") -> Problem:

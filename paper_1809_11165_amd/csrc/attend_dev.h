@@ -1,0 +1,277 @@
+// Device pieces shared by the attention kernels: types, matrix fragments, LDS tiles, staging and the bias line.
+//
+// All matrix work is done by 32 x 32 MFMA blocks whose first operand comes from an LDS tile and whose second one stays in
+// registers.  The result has its column in lane % 32 and rows 8 (r / 4) + 4 (lane / 32) + r % 4 in registers r = 0 .. 15.  The
+// eight values that a second operand of the next product wants per lane may be ANY eight of its 16 summed indices, as long as the first
+// operand's lane holds the same ones: so registers 8 u .. 8 u + 7 of a result are that operand as they stand (index
+// 16 u + 8 (e / 4) + 4 (lane / 32) + e % 4), and scores turn into weights of the next product without leaving their lane.
+#pragma once
+
+#include "bbmm_attend.h"
+
+namespace att {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int kPad = 64;                                  // the bias line goes this far beyond the last edge
+constexpr int kLine = 2 * (BBMM_ATT_FAR + kPad) + 1;
+
+template <typename T> struct Frag;
+template <> struct Frag<__bf16> {
+  typedef bf16x8 type;
+  static __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<_Float16> {
+  typedef f16x8 type;
+  static __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<float> {
+  typedef f32x8 type;
+  static __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// Eight registers of a result as the second operand of the next product (rounded to T once).
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type pack8(const f32x16& c, int u) {
+  typename Frag<T>::type f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = (T)c[8 * u + e];
+  return f;
+}
+
+// ---- LDS tiles: rows of DP elements; the 16-byte pieces of row r stand in places c ^ swz(r).  Eight rows in a row have eight
+// different swz, and four rows in a row four different swz / 2: no bank conflicts along columns (row_frag) nor in 4 x 16 blocks (col_frag).
+__device__ __forceinline__ int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+// First operand: element e of the lane = tile[rb + lane % 32][16 s + 8 (lane / 32) + e];  rb a multiple of 32.
+template <typename T, int DP>
+__device__ __forceinline__ typename Frag<T>::type row_frag(const char* tile, int rb, int s, int lane) {
+  constexpr int kRow = DP * (int)sizeof(T);
+  int r = lane & 31, half = lane >> 5;
+  const char* p = tile + (rb + r) * kRow;
+  if constexpr (sizeof(T) == 2) {
+    return *(const typename Frag<T>::type*)(p + (((2 * s + half) ^ swz(r)) << 4));
+  } else {
+    f32x4 lo = *(const f32x4*)(p + (((4 * s + 2 * half) ^ swz(r)) << 4));
+    f32x4 hi = *(const f32x4*)(p + (((4 * s + 2 * half + 1) ^ swz(r)) << 4));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+
+// First operand, transposed: element e of the lane = tile[rb + 8 (e / 4) + 4 (lane / 32) + e % 4][cb + lane % 32]; rb a multiple of
+// 16, cb of 32.  Two-byte types by the transposing LDS read: 16 lanes read a block of four rows of 16 elements, eight bytes
+// each (lane L: row L / 4, elements 4 (L % 4) on), and receive a column each.
+template <typename T, int DP>
+__device__ __forceinline__ typename Frag<T>::type col_frag(const char* tile, int rb, int cb, int lane) {
+  constexpr int kRow = DP * (int)sizeof(T);
+  int half = lane >> 5;
+  typename Frag<T>::type f;
+  if constexpr (sizeof(T) == 2) {
+    int L = lane & 15, r4 = L >> 2;
+    int c = (cb >> 3) + 2 * ((lane >> 4) & 1) + ((L & 3) >> 1);
+    const char* p = tile + (rb + 4 * half + r4) * kRow + ((c ^ ((r4 << 1) | half)) << 4) + ((L & 1) << 3);
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRow));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    f = __builtin_bit_cast(typename Frag<T>::type, v);
+  } else {
+    int col = cb + (lane & 31);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      int r = rb + 8 * (e >> 2) + 4 * half + (e & 3);
+      f[e] = *(const float*)(tile + r * kRow + (((col >> 2) ^ (((e & 3) << 1) | half)) << 4) + ((col & 3) << 2));
+    }
+  }
+  return f;
+}
+
+// 16 bytes of a row: elements [c, c + 16 / sizeof(T)) of `row`, zero from element `width` on.
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* row, int c, int width, int vec) {
+  constexpr int E = 16 / (int)sizeof(T);
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (c >= width) return v;
+  if (vec) return *(const u32x4*)(row + c);
+  T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (c + i < width) e[i] = row[c + i];
+  return v;
+}
+
+// A tile of ROWS rows on its way from memory to LDS: 256 threads, 16 bytes each per pass.
+template <typename T, int DP, int ROWS>
+struct Stage {
+  static constexpr int E = 16 / (int)sizeof(T), CH = DP / E, RP = 256 / CH, N = ROWS / RP;
+  u32x4 v[N];
+  // row 0 of the tile at `base`; rows from `rows` on are zero and not read
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int width, int vec, int tid) {
+    int r = tid / CH, c = (tid % CH) * E;
+    const T* p = base + (int64_t)r * stride;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = u32x4{0u, 0u, 0u, 0u};
+      if (r + i * RP < rows) v[i] = load16<T>(p, c, width, vec);
+      p += (int64_t)RP * stride;
+    }
+  }
+  // rows without a bit in `keep` are stored as zeros, whatever they held
+  __device__ __forceinline__ void store(char* tile, uint64_t keep, int tid) const {
+    int r = tid / CH, c = tid % CH;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int row = r + i * RP;
+      u32x4 x = v[i];
+      if (!((keep >> row) & 1)) x = u32x4{0u, 0u, 0u, 0u};
+      *(u32x4*)(tile + row * DP * (int)sizeof(T) + ((c ^ swz(row)) << 4)) = x;
+    }
+  }
+};
+
+// Second operand kept in registers: element e = row[16 s + 8 (lane / 32) + e], zero where there is no row.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type reg_frag(const T* row, bool have, int s, int width, int vec, int lane) {
+  int c = 16 * s + 8 * (lane >> 5);
+  typename Frag<T>::type f;
+  if constexpr (sizeof(T) == 2) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (have) v = load16<T>(row, c, width, vec);
+    f = __builtin_bit_cast(typename Frag<T>::type, v);
+  } else {
+    u32x4 lo = {0u, 0u, 0u, 0u}, hi = lo;
+    if (have) {
+      lo = load16<T>(row, c, width, vec);
+      hi = load16<T>(row, c + 4, width, vec);
+    }
+    f = __builtin_shufflevector(__builtin_bit_cast(f32x4, lo), __builtin_bit_cast(f32x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  return f;
+}
+
+// ---- buckets
+__device__ __forceinline__ int bucket_of(const AttBuckets& bk, int r) {
+  int dist = bk.two_sided ? abs(r) : max(-r, 0);
+  int lo = 0, hi = bk.n_edges;                 // first edge beyond dist
+  while (lo < hi) {
+    int mid = (lo + hi) >> 1;
+    if (bk.edges[mid] <= dist) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo + ((bk.two_sided && r > 0) ? bk.n_edges + 1 : 0);
+}
+
+// Sums by bucket of a workgroup (four waves): diag[r + span] holds the sum of difference r, |r| <= span; `left` and `right` are sums of
+// differences -far and below, far and above.  A wave takes every fourth bucket.
+__device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* diag, int span, float left, float right, float* out, int lane,
+                                            int wave) {
+  for (int n = wave; n < bk.buckets; n += 4) {
+    float s = 0.f;
+    for (int k = lane; k <= 2 * span; k += 64)
+      if (bucket_of(bk, k - span) == n) s += diag[k];
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) s += __shfl_xor(s, x, 64);
+    if (bucket_of(bk, -bk.far) == n) s += left;
+    if (bucket_of(bk, bk.far) == n) s += right;
+    if (lane == 0) out[n] = s;
+  }
+}
+
+// A table entry in units of the base-2 exponent.  Finite entries stay finite: one below -2.3e38 counts as that (the same
+// weight zero beside any other score, and weights of its own where a row holds nothing else).
+template <typename T>
+__device__ __forceinline__ float bias2(T t) {
+  float x = (float)t;
+  float y = x * kLog2e;
+  return (x > -__builtin_inff()) ? fmaxf(y, -3.40282347e38f) : y;
+}
+
+// line[r + far + kPad] = bias of difference r, |r| <= far + kPad, for one head.
+template <typename T>
+__device__ __forceinline__ void fill_line(float* line, const AttArgs& a, int h, int tid, int threads) {
+  int n = 2 * (a.bk.far + kPad) + 1;
+  const T* tab = (const T*)a.table + (size_t)h * a.bk.buckets;
+  for (int i = tid; i < n; i += threads) line[i] = bias2<T>(tab[bucket_of(a.bk, i - a.bk.far - kPad)]);
+}
+
+__device__ __forceinline__ int clamp_rel(int64_t r) {
+  const int64_t lim = 1 << 30;
+  return (int)(r < -lim ? -lim : (r > lim ? lim : r));
+}
+
+// position of a batch's first query: beyond 2^40 everything is far
+__device__ __forceinline__ int64_t start_of(const AttArgs& a, int b) {
+  const int64_t lim = (int64_t)1 << 40;
+  int64_t s = a.q_start ? a.q_start[b] : 0;
+  return s < -lim ? -lim : (s > lim ? lim : s);
+}
+
+// Scores of 32 keys against 32 queries in base-2 exponents, bias added.  KEYS_DOWN: keys in the registers, queries in the lanes, else the
+// other way round.  rel0: j - i - start of the first key and the first query; line: see fill_line (null: no table).  Returns 0 where the
+// differences are mixed, -1 / 1 where all lie beyond the last edge on that side (or there is no table).
+template <bool KEYS_DOWN>
+__device__ __forceinline__ int add_bias(f32x16& s, float c2, const float* line, int far, int rel0, float left, float right, int lane) {
+  int half = lane >> 5;
+  if (!line || rel0 + 31 <= -far || rel0 - 31 >= far) {
+    float cb = !line ? 0.f : (rel0 < 0 ? left : right);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c2, cb);
+    return rel0 < 0 ? -1 : 1;
+  }
+  const float* b = line + (KEYS_DOWN ? rel0 - (lane & 31) + 4 * half : rel0 + (lane & 31) - 4 * half) + far + kPad;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c2, KEYS_DOWN ? b[8 * (r >> 2) + (r & 3)] : b[-(8 * (r >> 2) + (r & 3))]);
+  return 0;
+}
+
+// Four consecutive features of one output row.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int c, int width, int vec, float x0, float x1, float x2, float x3) {
+  T e[4] = {(T)x0, (T)x1, (T)x2, (T)x3};
+  if (c >= width) return;
+  if (vec && c + 4 <= width) {
+    if constexpr (sizeof(T) == 2) *(uint2*)(row + c) = __builtin_bit_cast(uint2, e);
+    else *(u32x4*)(row + c) = __builtin_bit_cast(u32x4, e);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < width) row[c + i] = e[i];
+  }
+}
+
+// the other half of a wave's 32 columns
+__device__ __forceinline__ float other_half(float x) {
+  return __shfl_xor(x, 32, 64);
+}
+
+// keys of a tile that take part: bit i = key j0 + i, i < 64
+__device__ __forceinline__ uint64_t keep_bits(int n_left, const uint8_t* mask_row, uint8_t mask_byte) {
+  uint64_t m = n_left >= 64 ? ~0ull : ((1ull << n_left) - 1);
+  if (mask_row) m &= __ballot(mask_byte != 0);
+  return m;
+}
+
+// Bound on exp2 arguments above the running reference: the reference is moved (and what was summed rescaled) only when a score
+// exceeds it by more than this, so that most tiles leave the accumulators alone.
+constexpr float kSlack = 8.f;
+// fp16 weights are kept this much (log2) above one, away from that type's smallest numbers; 2^(8 + 6) is far from its largest.
+template <typename T> struct Lift { static constexpr float value = 0.f; };
+template <> struct Lift<_Float16> { static constexpr float value = 6.f; };
+
+// Workgroup id -> position such that the eight dies, to which consecutive ids go in turn, get runs of neighbouring positions
+// (workgroups that read the same keys share an L2).
+__device__ __forceinline__ int die_order(int id, int per_die) { return (id & 7) * per_die + (id >> 3); }
+
+}  // namespace att

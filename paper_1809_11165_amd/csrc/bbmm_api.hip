@@ -3,6 +3,7 @@
 // paper's algorithm (App. C preconditioner -> probes -> Alg. 2 -> SLQ / trace terms) and
 // copies the scalar results back with a single stream synchronisation.
 #include "bbmm.h"
+#include "bbmm_attend.h"
 #include "bbmm_dev.h"
 #include "bbmm_plan.h"
 
@@ -2071,6 +2072,315 @@ int bbmm_solve_logdet_grad(bbmm_ctx* c, const bbmm_problem* in, bbmm_result* out
   bool again = false;
   int rc = solve_call(c, in, out, false, &again);
   return again ? solve_call(c, in, out, true, &again) : rc;
+}
+
+// ------------------------------------------------------------------ attention
+}  // extern "C"
+
+namespace {
+
+// The context's device for the length of a call; the caller's comes back afterwards.
+struct OnDevice {
+  int before = -1;
+  hipError_t err;
+  explicit OnDevice(int device) {
+    if (hipGetDevice(&before) != hipSuccess) before = -1;
+    err = before == device ? hipSuccess : hipSetDevice(device);
+    if (before == device) before = -1;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+int set_buckets(bbmm_ctx* c, int64_t n_edges, const int32_t* edges, int32_t two_sided, bool need_edges, AttBuckets* out) {
+  if (n_edges < 0 || n_edges > BBMM_ATT_MAXEDGES || (n_edges > 0 && need_edges && !edges))
+    return fail(c, BBMM_EINVAL, "between 0 and 63 bucket edges are needed");
+  out->n_edges = (int)n_edges;
+  out->two_sided = two_sided != 0;
+  out->buckets = (int)(n_edges + 1) * (two_sided ? 2 : 1);
+  out->far = 1;
+  for (int k = 0; k < BBMM_ATT_MAXEDGES; ++k) out->edges[k] = 0;
+  if (!need_edges) return BBMM_OK;
+  for (int k = 0; k < n_edges; ++k) {
+    if (edges[k] < 1 || edges[k] > BBMM_ATT_FAR || (k && edges[k] <= edges[k - 1]))
+      return fail(c, BBMM_EINVAL, "bucket edges must ascend within [1, 1024]");
+    out->edges[k] = out->far = edges[k];
+  }
+  return BBMM_OK;
+}
+
+// Whether rows at p with these strides (elements) may be read or written `bytes` at a time.
+bool wide_rows(const void* p, const int64_t* stride, int64_t width, size_t elem, size_t bytes) {
+  bool ok = (uintptr_t)p % bytes == 0 && width * elem % bytes == 0;
+  for (int k = 0; k < 3 && stride; ++k) ok = ok && stride[k] * elem % bytes == 0;
+  return ok;
+}
+
+constexpr int64_t kAttMaxLen = (int64_t)1 << 30, kAttMaxHeads = 65535, kAttMaxGrid = (int64_t)1 << 23;   // 2^32 threads of 256 per workgroup, and eight dies
+
+// Sizes and buckets; the pointers only where `pointers` is set.
+int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs* a) {
+  if (!in) return fail(c, BBMM_EINVAL, "attention: no description");
+  if (in->type < BBMM_TYPE_F32 || in->type > BBMM_TYPE_BF16) return fail(c, BBMM_EINVAL, "attention: unknown type");
+  if (in->batch < 0 || in->batch > kAttMaxHeads || in->heads < 1 || in->heads > kAttMaxHeads || in->kv_heads < 1 ||
+      in->heads % in->kv_heads != 0)
+    return fail(c, BBMM_EINVAL, "attention: batch and heads up to 65535, kv_heads must divide heads");
+  if (in->nq < 0 || in->nq > kAttMaxLen || in->nk < 0 || in->nk > kAttMaxLen) return fail(c, BBMM_EINVAL, "attention: nq and nk up to 2^30");
+  if (in->d < 1 || in->d > BBMM_ATT_MAXD || in->dv < 1 || in->dv > BBMM_ATT_MAXD) return fail(c, BBMM_EINVAL, "attention: d and dv from 1 to 128");
+  if (!(in->scale > 0.0) || !isfinite((float)in->scale) || !((float)in->scale > 0.f)) return fail(c, BBMM_EINVAL, "attention: scale must be finite and > 0");
+  memset(a, 0, sizeof *a);
+  int rc = set_buckets(c, in->table ? in->n_edges : 0, in->edges, in->two_sided, pointers && in->table, &a->bk);
+  if (rc) return rc;
+  a->B = (int)in->batch, a->H = (int)in->heads, a->HK = (int)in->kv_heads, a->G = a->H / a->HK;
+  a->nq = (int)in->nq, a->nk = (int)in->nk, a->d = (int)in->d, a->dv = (int)in->dv;
+  a->scale = (float)in->scale, a->c2 = (float)(in->scale * 1.4426950408889634);
+  a->table = in->table;
+  int64_t rows = std::max<int64_t>((in->nq + 127) / 128 * in->heads, (in->nk + 127) / 128 * in->kv_heads);
+  if (in->batch * rows > kAttMaxGrid || in->batch * in->heads * in->nq > 16 * kAttMaxGrid || in->batch * in->kv_heads * in->nk > 16 * kAttMaxGrid)
+    return fail(c, BBMM_EINVAL, "attention: more than 2^27 rows in one call");
+  if (!pointers) return BBMM_OK;
+  size_t e = in->type == BBMM_TYPE_F32 ? 4 : 2;
+  if ((in->batch && in->nq && !in->Q) || (in->batch && in->nk && (!in->K || !in->V))) return fail(c, BBMM_EINVAL, "attention: Q, K and V are required");
+  if (((uintptr_t)in->Q | (uintptr_t)in->K | (uintptr_t)in->V | (uintptr_t)in->table) % e) return fail(c, BBMM_EINVAL, "attention: pointer not aligned to its type");
+  for (int k = 0; k < 3; ++k)
+    if (in->q_stride[k] < 0 || in->k_stride[k] < 0 || in->v_stride[k] < 0) return fail(c, BBMM_EINVAL, "attention: negative stride");
+  a->Q = in->Q, a->K = in->K, a->V = in->V;
+  memcpy(a->qs, in->q_stride, sizeof a->qs);
+  memcpy(a->ks, in->k_stride, sizeof a->ks);
+  memcpy(a->vs, in->v_stride, sizeof a->vs);
+  a->q_len = in->q_len, a->k_len = in->k_len, a->mask = in->key_mask, a->mask_s = in->nk, a->q_start = in->q_start;
+  a->qvec = wide_rows(a->Q, a->qs, a->d, e, 16), a->kvec = wide_rows(a->K, a->ks, a->d, e, 16), a->vvec = wide_rows(a->V, a->vs, a->dv, e, 16);
+  return BBMM_OK;
+}
+
+// How the forward pass is laid out.  Few rows per shared head (kAttFewRows): the kernel that packs them and splits the keys over its
+// waves; else 128 queries of a head per workgroup.  The keys are split over workgroups while those do not fill the device twice and
+// a part keeps at least kAttFewPart (kAttPart) keys.
+constexpr int64_t kAttFewRows = 32, kAttFewPart = 256, kAttPart = 512;
+struct AttPlan {
+  bool few;
+  int nsplit;
+};
+AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
+  AttPlan p;
+  int64_t rows = (int64_t)a.nq * a.G;
+  p.few = rows <= kAttFewRows;
+  int64_t wgs = p.few ? (int64_t)a.B * a.HK * ((rows + 31) / 32) : (int64_t)a.B * a.H * ((a.nq + 127) / 128);
+  int64_t part = p.few ? kAttFewPart : kAttPart;
+  int64_t want = (2 * c->num_cus + wgs - 1) / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, a.nk / part);
+  p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
+  return p;
+}
+
+// Offsets into the workspace, 256-byte steps.
+size_t step256(size_t n) { return (n + 255) / 256 * 256; }
+struct AttWork {
+  size_t pO, pl, delta, tsum, norms, bytes;
+};
+AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
+  AttWork w{};
+  size_t rows = (size_t)a.B * a.H * a.nq;
+  if (!grad) {
+    AttPlan p = attention_plan(c, a);
+    if (p.nsplit > 1) {
+      w.pO = 0;
+      w.pl = step256(rows * p.nsplit * ((a.dv + 3) / 4 * 4) * sizeof(float));
+      w.bytes = w.pl + step256(rows * p.nsplit * sizeof(float));
+    }
+    return w;
+  }
+  w.norms = 0;
+  w.delta = 256;
+  w.tsum = w.delta + step256(rows * sizeof(float));
+  w.bytes = w.tsum + (a.table ? step256((size_t)a.H * a.B * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float)) : 0);
+  return w;
+}
+
+int check_work(bbmm_ctx* c, const void* work, int64_t have, size_t need) {
+  if (need == 0) return BBMM_OK;
+  if (!work || have < (int64_t)need) return fail(c, BBMM_EINVAL, "workspace too small: " + std::to_string(need) + " bytes are needed");
+  if ((uintptr_t)work % 16) return fail(c, BBMM_EINVAL, "workspace must be 16-byte aligned");
+  return BBMM_OK;
+}
+
+// Rows per workgroup of the bias kernels: enough workgroups to fill the device several times, at most 64 rows each (one line of the
+// table is laid out per workgroup, and the gradient leaves one set of sums per workgroup).
+int bucket_rows(const bbmm_ctx* c, int64_t planes, int64_t nq) {
+  int64_t r = planes * nq / (8 * c->num_cus);
+  return (int)std::max<int64_t>(4, std::min<int64_t>(64, r / 4 * 4));
+}
+
+int bucket_sizes(bbmm_ctx* c, int64_t batch, int64_t heads, int64_t nq, int64_t nk) {
+  if (batch < 0 || batch > kAttMaxHeads || heads < 1 || heads > kAttMaxHeads || nq < 0 || nq > kAttMaxLen / 64 || nk < 0 || nk > kAttMaxLen ||
+      batch * heads * ((nq + 3) / 4) > kAttMaxGrid)
+    return fail(c, BBMM_EINVAL, "bias: batch and heads up to 65535, nq up to 2^24, nk up to 2^30, 2^25 rows in all");
+  return BBMM_OK;
+}
+
+int attend(bbmm_ctx* c, const bbmm_attention* in, void* O, float* lse, void* work, int64_t work_bytes) {
+  AttArgs a;
+  int rc = attention_args(c, in, true, &a);
+  if (rc) return rc;
+  if (a.B == 0 || a.nq == 0) return BBMM_OK;
+  size_t e = in->type == BBMM_TYPE_F32 ? 4 : 2;
+  if (!O || !lse || (uintptr_t)O % e || (uintptr_t)lse % 4) return fail(c, BBMM_EINVAL, "attention: O and lse are required");
+  AttPlan p = attention_plan(c, a);
+  AttWork w = attention_work(c, a, false);
+  rc = check_work(c, work, work_bytes, w.bytes);
+  if (rc) return rc;
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  AttOut o{};
+  o.O = O, o.lse = lse, o.nsplit = p.nsplit, o.dv4 = (a.dv + 3) / 4 * 4;
+  o.os[2] = a.dv, o.os[1] = (int64_t)a.H * a.dv, o.os[0] = o.os[1] * a.nq;
+  o.ovec = wide_rows(O, nullptr, a.dv, e, 4 * e);
+  o.pO = (float*)((char*)work + w.pO), o.pl = (float*)((char*)work + w.pl);
+  if (p.few) launch_attend_few(c->stream, in->type, a, o);
+  else launch_attend(c->stream, in->type, a, o);
+  if (p.nsplit > 1) launch_attend_join(c->stream, in->type, a, o);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const float* lse, const void* dO, const int64_t* do_stride, void* dQ,
+                void* dK, void* dV, void* dtable, void* work, int64_t work_bytes) {
+  AttArgs a;
+  int rc = attention_args(c, in, true, &a);
+  if (rc) return rc;
+  size_t e = in->type == BBMM_TYPE_F32 ? 4 : 2;
+  bool rows = a.B && a.nq, keys = a.B && a.nk;
+  if (rows && (!O || !lse || !dO || !do_stride || !dQ)) return fail(c, BBMM_EINVAL, "attention: O, lse, dO and dQ are required");
+  if (keys && (!dK || !dV)) return fail(c, BBMM_EINVAL, "attention: dK and dV are required");
+  if (a.table && !dtable) return fail(c, BBMM_EINVAL, "attention: a table needs dtable");
+  if (((uintptr_t)O | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV | (uintptr_t)dtable) % e || (uintptr_t)lse % 4)
+    return fail(c, BBMM_EINVAL, "attention: pointer not aligned to its type");
+  AttWork w = attention_work(c, a, true);
+  rc = check_work(c, work, work_bytes, w.bytes);
+  if (rc) return rc;
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  AttGrad g{};
+  g.O = O, g.dO = dO, g.lse = lse, g.dQ = dQ, g.dK = dK, g.dV = dV;
+  for (int k = 0; k < 3 && do_stride; ++k) {
+    if (do_stride[k] < 0) return fail(c, BBMM_EINVAL, "attention: negative stride");
+    g.dos[k] = do_stride[k];
+  }
+  g.ovec = wide_rows(O, nullptr, a.dv, e, 16), g.dovec = wide_rows(dO, g.dos, a.dv, e, 16);
+  g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
+  g.delta = (float*)((char*)work + w.delta), g.tsum = (float*)((char*)work + w.tsum), g.norms = (unsigned*)((char*)work + w.norms);
+  hipStream_t s = c->stream;
+  launch_attend_delta(s, in->type, a, g);
+  if (rows) launch_attend_dq(s, in->type, a, g);
+  if (keys) launch_attend_dkv(s, in->type, a, g);
+  if (a.table) launch_bucket_join(s, in->type, g.tsum, a.B * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+int bucket_bias(bbmm_ctx* c, int32_t type, const void* table, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges, const int32_t* edges,
+                int32_t two_sided, int64_t start, void* B) {
+  if (type < BBMM_TYPE_F32 || type > BBMM_TYPE_BF16) return fail(c, BBMM_EINVAL, "bias: unknown type");
+  int rc = bucket_sizes(c, 1, heads, nq, nk);
+  if (rc) return rc;
+  AttBuckets bk;
+  rc = set_buckets(c, n_edges, edges, two_sided, true, &bk);
+  if (rc) return rc;
+  if (nq == 0 || nk == 0) return BBMM_OK;
+  size_t e = type == BBMM_TYPE_F32 ? 4 : 2;
+  if (!table || !B || ((uintptr_t)table | (uintptr_t)B) % e) return fail(c, BBMM_EINVAL, "bias: table and matrix are required, aligned to their type");
+  if (start < -kAttMaxLen * 1024 || start > kAttMaxLen * 1024) return fail(c, BBMM_EINVAL, "bias: start within 2^40");
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  launch_bucket_bias(c->stream, type, table, bk, start, (int)heads, (int)nq, nk, bucket_rows(c, heads, nq), B);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+size_t bucket_work(const bbmm_ctx* c, int64_t batch, int64_t heads, int64_t nq, int buckets) {
+  int rows = bucket_rows(c, batch * heads, nq);
+  return (size_t)(heads * batch * ((nq + rows - 1) / rows)) * buckets * sizeof(float);
+}
+
+int bucket_bias_grad(bbmm_ctx* c, int32_t type, const void* dB, int64_t batch, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges,
+                     const int32_t* edges, int32_t two_sided, int64_t start, void* dtable, void* work, int64_t work_bytes) {
+  if (type < BBMM_TYPE_F32 || type > BBMM_TYPE_BF16) return fail(c, BBMM_EINVAL, "bias: unknown type");
+  int rc = bucket_sizes(c, batch, heads, nq, nk);
+  if (rc) return rc;
+  AttBuckets bk;
+  rc = set_buckets(c, n_edges, edges, two_sided, true, &bk);
+  if (rc) return rc;
+  bool some = batch && nq && nk;
+  size_t e = type == BBMM_TYPE_F32 ? 4 : 2;
+  if ((some && !dB) || !dtable || ((uintptr_t)dB | (uintptr_t)dtable) % e) return fail(c, BBMM_EINVAL, "bias: matrix and table are required, aligned to their type");
+  if (start < -kAttMaxLen * 1024 || start > kAttMaxLen * 1024) return fail(c, BBMM_EINVAL, "bias: start within 2^40");
+  rc = check_work(c, work, work_bytes, some ? bucket_work(c, batch, heads, nq, bk.buckets) : 0);
+  if (rc) return rc;
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  int rows = bucket_rows(c, batch * heads, nq);
+  if (some) launch_bucket_grad(c->stream, type, dB, bk, start, (int)batch, (int)heads, (int)nq, nk, rows, (float*)work);
+  launch_bucket_join(c->stream, type, (const float*)work, some ? (int)(batch * ((nq + rows - 1) / rows)) : 0, (int)heads, bk.buckets, dtable);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+// A C entry lets no exception out (the only one is a failed allocation of a message).
+template <typename F>
+int guarded(bbmm_ctx* c, F f) {
+  if (!c) return BBMM_EINVAL;
+  try {
+    return f();
+  } catch (...) {
+    return BBMM_ENOMEM;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int bbmm_attend_workspace(bbmm_ctx* c, const bbmm_attention* in, int32_t grad, int64_t* bytes) {
+  return guarded(c, [&] {
+    AttArgs a;
+    int rc = attention_args(c, in, false, &a);
+    if (rc) return rc;
+    if (!bytes) return fail(c, BBMM_EINVAL, "attention: bytes is required");
+    *bytes = a.B == 0 ? (grad ? 256 : 0) : (int64_t)attention_work(c, a, grad != 0).bytes;
+    return (int)BBMM_OK;
+  });
+}
+
+int bbmm_attend(bbmm_ctx* c, const bbmm_attention* in, void* O, float* lse, void* work, int64_t work_bytes) {
+  return guarded(c, [&] { return attend(c, in, O, lse, work, work_bytes); });
+}
+
+int bbmm_attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const float* lse, const void* dO, const int64_t* do_stride, void* dQ,
+                     void* dK, void* dV, void* dtable, void* work, int64_t work_bytes) {
+  return guarded(c, [&] { return attend_grad(c, in, O, lse, dO, do_stride, dQ, dK, dV, dtable, work, work_bytes); });
+}
+
+int bbmm_bucket_bias(bbmm_ctx* c, int32_t type, const void* table, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges, const int32_t* edges,
+                     int32_t two_sided, int64_t start, void* B) {
+  return guarded(c, [&] { return bucket_bias(c, type, table, heads, nq, nk, n_edges, edges, two_sided, start, B); });
+}
+
+int bbmm_bucket_bias_workspace(bbmm_ctx* c, int64_t batch, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges, int32_t two_sided,
+                               int64_t* bytes) {
+  return guarded(c, [&] {
+    AttBuckets bk;
+    int rc = bucket_sizes(c, batch, heads, nq, nk);
+    if (!rc) rc = set_buckets(c, n_edges, nullptr, two_sided, false, &bk);
+    if (rc) return rc;
+    if (!bytes) return fail(c, BBMM_EINVAL, "bias: bytes is required");
+    *bytes = batch && nq && nk ? (int64_t)bucket_work(c, batch, heads, nq, bk.buckets) : 0;
+    return (int)BBMM_OK;
+  });
+}
+
+int bbmm_bucket_bias_grad(bbmm_ctx* c, int32_t type, const void* dB, int64_t batch, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges,
+                          const int32_t* edges, int32_t two_sided, int64_t start, void* dtable, void* work, int64_t work_bytes) {
+  return guarded(c, [&] { return bucket_bias_grad(c, type, dB, batch, heads, nq, nk, n_edges, edges, two_sided, start, dtable, work, work_bytes); });
 }
 
 }  // extern "C"

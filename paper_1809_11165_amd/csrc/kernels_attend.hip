@@ -1,0 +1,418 @@
+// Attention forward: o_i = sum_j p_ij v_j, p_i = softmax_j(scale q_i.k_j + T[h, bucket(j - i - start)]), in one pass over the keys with
+// the running reference and sum of the softmax (fp32), scores never leaving the registers.
+//
+// k_attend: a workgroup of four waves takes 128 queries of one head, 32 per wave.  Transposed scores S^T = K Q^T put a query in
+// a lane, so that maximum, sum, bias offset and rescaling are per-lane scalars and the weights are, as they stand, the
+// second operand of O^T += V^T P^T (see attend_dev.h).  K and V tiles go through LDS, two buffers, the next tile's loads in flight
+// during a tile's products.
+// k_attend_few: up to 32 rows (query, head of the group) of one shared head; the waves split the keys instead, read K straight
+// into registers and V through LDS of their own, and join at the end.  Bound by reading K and V once.
+// Both may split the key axis over workgroups; k_attend_join then weighs the parts.
+#include "attend_dev.h"
+
+using namespace att;
+
+namespace {
+
+__device__ __forceinline__ void drop_keys(f32x16& s, unsigned keep, int lane) {
+  if (keep == 0xffffffffu) return;
+  unsigned k = keep >> (4 * (lane >> 5));
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = ((k >> (8 * (r >> 2) + (r & 3))) & 1) ? s[r] : -__builtin_inff();
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt, int total, int per_die) {
+  typedef typename Frag<T>::type frag;
+  constexpr int BK = sizeof(T) == 2 ? 64 : 32, NB = BK / 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
+  __shared__ __align__(16) char tile[2][2][kTile];
+  __shared__ float line[kLine];
+  int id = die_order(blockIdx.x, per_die);
+  if (id >= total) return;
+  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  int qt = id % nqt, sp = (id / nqt) % o.nsplit, bh = id / nqt / o.nsplit;
+  int h = bh % a.H, b = bh / a.H, hk = h / a.G;
+  int q0 = qt * 128 + wave * 32, i = q0 + (lane & 31);
+  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
+  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  if (qt * 128 >= qn) kn = 0;
+  int tiles = (kn + BK - 1) / BK, per = (tiles + o.nsplit - 1) / o.nsplit;
+  int t0 = min(sp * per, tiles), t1 = min(t0 + per, tiles);
+
+  const T* K = (const T*)a.K + b * a.ks[0] + hk * a.ks[2];
+  const T* V = (const T*)a.V + b * a.vs[0] + hk * a.vs[2];
+  const uint8_t* mrow = a.mask ? a.mask + b * a.mask_s : nullptr;
+  frag q[NS];
+  {
+    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = reg_frag<T>(row, i < qn, s, a.d, a.qvec, lane);
+  }
+  const float* ln = nullptr;
+  if (a.table && t0 < t1) {
+    fill_line<T>(line, a, h, tid, 256);
+    ln = line;
+  }
+  int64_t start = start_of(a, b);
+
+  Stage<T, DP, BK> sk, sv;
+  uint64_t keep = 0;
+  uint8_t mb = 0;
+  auto fetch = [&](int t) {
+    int j0 = t * BK, left = kn - j0;
+    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, a.kvec, tid);
+    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, a.vvec, tid);
+    if (mrow) mb = (lane < BK && lane < left) ? mrow[j0 + lane] : 0;
+  };
+  auto put = [&](int t) {
+    keep = keep_bits(min(kn - t * BK, BK), mrow, mb);
+    sk.store(tile[t & 1][0], ~0ull, tid);
+    sv.store(tile[t & 1][1], keep, tid);
+  };
+  f32x16 acc[ND];
+#pragma unroll
+  for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
+  float m = -__builtin_inff(), l = 0.f;     // reference and sum (this lane's half of the keys)
+  if (t0 < t1) {
+    fetch(t0);
+    put(t0);
+  }
+  __syncthreads();
+  float left = 0.f, right = 0.f;
+  if (ln) {
+    left = line[kPad];
+    right = line[2 * a.bk.far + kPad];
+  }
+  for (int t = t0; t < t1; ++t) {
+    const char *tk = tile[t & 1][0], *tv = tile[t & 1][1];
+    uint64_t kp = keep;
+    if (t + 1 < t1) fetch(t + 1);
+    if (kp) {
+      f32x16 s[NB];
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        s[n] = f32x16{};
+#pragma unroll
+        for (int k = 0; k < NS; ++k) s[n] = Frag<T>::mma(row_frag<T, DP>(tk, 32 * n, k, lane), q[k], s[n]);
+        add_bias<true>(s[n], a.c2, ln, a.bk.far, clamp_rel((int64_t)t * BK + 32 * n - q0 - start), left, right, lane);
+        drop_keys(s[n], (unsigned)(kp >> (32 * n)), lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+      }
+      top = fmaxf(top, other_half(top));
+      bool move = top > m + kSlack;
+      if (__any(move)) {
+        float up = move ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+        m = move ? top : m;
+        l *= up;
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[n][r] *= up;
+      }
+      float ref = (m == -__builtin_inff() ? 0.f : m) - Lift<T>::value;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - ref);
+          l += s[n][r];
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          frag p = pack8<T>(s[n], u);
+#pragma unroll
+          for (int c = 0; c < ND; ++c) acc[c] = Frag<T>::mma(col_frag<T, DP>(tv, 32 * n + 16 * u, 32 * c, lane), p, acc[c]);
+        }
+      }
+    }
+    if (t + 1 < t1) put(t + 1);
+    __syncthreads();
+  }
+  l += other_half(l);
+  bool some = l != 0.f && i < qn;           // NaN counts as something
+  float inv = some ? 1.f / l : 0.f;
+  float lse2 = some ? (m - Lift<T>::value) + __builtin_amdgcn_logf(l) : -__builtin_inff();
+  if (i >= a.nq) return;
+  size_t row = ((size_t)b * a.H + h) * a.nq + i;
+  if (o.nsplit == 1) {
+    if (half == 0) o.lse[row] = lse2 * kLn2;
+    T* out = (T*)o.O + b * o.os[0] + (int64_t)i * o.os[1] + h * o.os[2];
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        store4<T>(out, 32 * n + 8 * r + 4 * half, a.dv, o.ovec, acc[n][4 * r] * inv, acc[n][4 * r + 1] * inv, acc[n][4 * r + 2] * inv,
+                  acc[n][4 * r + 3] * inv);
+  } else {
+    row += (size_t)sp * a.B * a.H * a.nq;
+    if (half == 0) o.pl[row] = lse2;
+    float* out = o.pO + row * o.dv4;
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        int c = 32 * n + 8 * r + 4 * half;
+        if (c < o.dv4) *(f32x4*)(out + c) = f32x4{acc[n][4 * r] * inv, acc[n][4 * r + 1] * inv, acc[n][4 * r + 2] * inv, acc[n][4 * r + 3] * inv};
+      }
+  }
+}
+
+// Rows rho = 32 rb .. of shared head hk: query rho / G, head hk G + rho % G.
+template <typename T, int DP>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttArgs a, AttOut o, int nrb) {
+  typedef typename Frag<T>::type frag;
+  constexpr int ND = DP / 32, NS = DP / 16, E = 16 / (int)sizeof(T), CH = DP / E, NV = 32 * CH / 64;
+  constexpr bool kLds = sizeof(T) == 2;      // V through LDS (four-byte elements are read as the product wants them)
+  constexpr int kVt = 32 * DP * 2, kJoin = 32 * (DP + 4) * 4;
+  __shared__ __align__(16) char buf[4 * (kVt > kJoin ? kVt : kJoin)];
+  __shared__ float tab[32][2 * (BBMM_ATT_MAXEDGES + 1) + 1];
+  __shared__ uint8_t bline[kLine];
+  __shared__ float wm[4][32], wl[4][32];
+  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+  int x = blockIdx.x, rb = x % nrb, sp = (x / nrb) % o.nsplit, bh = x / nrb / o.nsplit, hk = bh % a.HK, b = bh / a.HK;
+  int rows = a.nq * a.G, rho = rb * 32 + col, i = rho / a.G, h = hk * a.G + rho % a.G;
+  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
+  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  bool mine = rho < rows && i < qn;
+  int blocks = (kn + 31) / 32, per = (blocks + o.nsplit - 1) / o.nsplit;
+  int t0 = min(sp * per, blocks), t1 = min(t0 + per, blocks);
+  int i0 = rb * 32 / a.G;                     // first query of the rows
+
+  const T* K = (const T*)a.K + b * a.ks[0] + hk * a.ks[2];
+  const T* V = (const T*)a.V + b * a.vs[0] + hk * a.vs[2];
+  const uint8_t* mrow = a.mask ? a.mask + b * a.mask_s : nullptr;
+  int64_t start = start_of(a, b);
+  frag q[NS], kf[NS];
+  {
+    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = reg_frag<T>(row, mine, s, a.d, a.qvec, lane);
+  }
+  float left = 0.f, right = 0.f;
+  if (a.table) {
+    for (int n = tid; n < 32 * a.bk.buckets; n += 256) {
+      int r = rb * 32 + n / a.bk.buckets, g = r % a.G;
+      tab[n / a.bk.buckets][n % a.bk.buckets] = r < rows ? bias2<T>(((const T*)a.table)[(size_t)(hk * a.G + g) * a.bk.buckets + n % a.bk.buckets]) : 0.f;
+    }
+    for (int n = tid; n < 2 * (a.bk.far + kPad) + 1; n += 256) bline[n] = (uint8_t)bucket_of(a.bk, n - a.bk.far - kPad);
+    __syncthreads();
+    left = tab[col][bline[0]];
+    right = tab[col][bline[2 * (a.bk.far + kPad)]];
+  }
+  char* vt = buf + wave * kVt;
+  u32x4 vr[kLds ? NV : 1];
+  uint8_t mb = 0, mnext = 0;
+  auto fetch_k = [&](int t) {
+    int j = t * 32 + col;
+    const T* row = K + (int64_t)j * a.ks[1];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) kf[s] = reg_frag<T>(row, j < kn, s, a.d, a.kvec, lane);
+    if (mrow) mnext = (lane < 32 && j < kn) ? mrow[j] : 0;
+  };
+  auto fetch_v = [&](int t) {
+    if constexpr (kLds) {
+      int r = lane / CH, c = (lane % CH) * E, j = t * 32 + r;
+      const T* p = V + (int64_t)j * a.vs[1];
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        vr[n] = u32x4{0u, 0u, 0u, 0u};
+        if (j + n * (64 / CH) < kn) vr[n] = load16<T>(p, c, a.dv, a.vvec);
+        p += (int64_t)(64 / CH) * a.vs[1];
+      }
+    }
+  };
+  f32x16 acc[ND];
+#pragma unroll
+  for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
+  float m = -__builtin_inff(), l = 0.f;
+  int t = t0 + wave;
+  if (t < t1) {
+    fetch_k(t);
+    fetch_v(t);
+  }
+  for (; t < t1; t += 4) {
+    mb = mnext;
+    unsigned keep = (unsigned)keep_bits(min(kn - t * 32, 32), mrow, mb);
+    if constexpr (kLds) {
+      int r = lane / CH, c = lane % CH;
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        int row = r + n * (64 / CH);
+        u32x4 v = vr[n];
+        if (!((keep >> row) & 1)) v = u32x4{0u, 0u, 0u, 0u};
+        *(u32x4*)(vt + row * DP * 2 + ((c ^ swz(row)) << 4)) = v;
+      }
+    }
+    f32x16 s = f32x16{};
+#pragma unroll
+    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(kf[k], q[k], s);
+    if (t + 4 < t1) {
+      fetch_k(t + 4);
+      fetch_v(t + 4);
+    }
+    int rel0 = clamp_rel((int64_t)t * 32 - i0 - start);     // of the first key and the first query
+    if (!a.table || rel0 + 31 <= -a.bk.far || rel0 - 31 >= a.bk.far) {
+      float cb = rel0 < 0 ? left : right;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c2, cb);
+    } else {
+      const uint8_t* bl = bline + (rel0 - (min(i, a.nq - 1) - i0) + 4 * half + a.bk.far + kPad);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c2, tab[col][bl[8 * (r >> 2) + (r & 3)]]);
+    }
+    drop_keys(s, keep, lane);
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = fmaxf(top, other_half(top));
+    bool move = top > m + kSlack;
+    if (__any(move)) {
+      float up = move ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+      m = move ? top : m;
+      l *= up;
+#pragma unroll
+      for (int n = 0; n < ND; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[n][r] *= up;
+    }
+    float ref = (m == -__builtin_inff() ? 0.f : m) - Lift<T>::value;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(s[r] - ref);
+      l += s[r];
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      frag p = pack8<T>(s, u);
+#pragma unroll
+      for (int c = 0; c < ND; ++c) {
+        frag v;
+        if constexpr (kLds) {
+          v = col_frag<T, DP>(vt, 16 * u, 32 * c, lane);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            int r = 16 * u + 8 * (e >> 2) + 4 * half + (e & 3), cc = 32 * c + col;
+            v[e] = ((keep >> r) & 1) && cc < a.dv ? V[(int64_t)(t * 32 + r) * a.vs[1] + cc] : (T)0.f;
+          }
+        }
+        acc[c] = Frag<T>::mma(v, p, acc[c]);
+      }
+    }
+    if constexpr (kLds) __builtin_amdgcn_wave_barrier();
+  }
+  // join the four waves: each leaves its sums relative to its own reference
+  l += other_half(l);
+  __syncthreads();
+  float* part = (float*)buf + wave * 32 * (DP + 4) + col * (DP + 4);
+#pragma unroll
+  for (int n = 0; n < ND; ++n)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *(f32x4*)(part + 32 * n + 8 * r + 4 * half) = f32x4{acc[n][4 * r], acc[n][4 * r + 1], acc[n][4 * r + 2], acc[n][4 * r + 3]};
+  if (half == 0) {
+    wm[wave][col] = m;
+    wl[wave][col] = l;
+  }
+  __syncthreads();
+  // eight threads per row
+  int row = tid >> 3, rr = rb * 32 + row, qi = rr / a.G, hh = hk * a.G + rr % a.G;
+  if (rr >= rows) return;
+  float top = fmaxf(fmaxf(wm[0][row], wm[1][row]), fmaxf(wm[2][row], wm[3][row]));
+  float w[4], sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    w[k] = wm[k][row] == -__builtin_inff() && wl[k][row] == 0.f ? 0.f : __builtin_amdgcn_exp2f(wm[k][row] - top);
+    sum += w[k] * wl[k][row];
+  }
+  bool some = sum != 0.f && qi < qn;
+  float inv = some ? 1.f / sum : 0.f;
+  float lse2 = some ? (top - Lift<T>::value) + __builtin_amdgcn_logf(sum) : -__builtin_inff();
+  size_t at = ((size_t)b * a.H + hh) * a.nq + qi;
+  if (o.nsplit > 1) at += (size_t)sp * a.B * a.H * a.nq;
+  if ((tid & 7) == 0) {
+    if (o.nsplit == 1) o.lse[at] = lse2 * kLn2;
+    else o.pl[at] = lse2;
+  }
+  const float* src = (const float*)buf + row * (DP + 4);
+  T* out = (T*)o.O + b * o.os[0] + (int64_t)qi * o.os[1] + hh * o.os[2];
+  for (int c = (tid & 7) * 4; c < DP; c += 32) {
+    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (some) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (w[k] != 0.f) y += (w[k] * inv) * *(const f32x4*)(src + k * 32 * (DP + 4) + c);
+    }
+    if (o.nsplit == 1) store4<T>(out, c, a.dv, o.ovec, y[0], y[1], y[2], y[3]);
+    else if (c < o.dv4) *(f32x4*)(o.pO + at * o.dv4 + c) = y;
+  }
+}
+
+// One wave per row: parts weighed by their sums.  Two features per lane.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_join(AttArgs a, AttOut o) {
+  int lane = threadIdx.x & 63;
+  size_t n = (size_t)a.B * a.H * a.nq, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= n) return;
+  float top = -__builtin_inff();
+  for (int s = lane; s < o.nsplit; s += 64) top = fmaxf(top, o.pl[s * n + row]);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 64));
+  float sum = 0.f, y0 = 0.f, y1 = 0.f;
+  int c = 2 * lane;
+  for (int s = 0; s < o.nsplit; ++s) {
+    float p = o.pl[s * n + row];
+    if (p == -__builtin_inff()) continue;
+    float w = __builtin_amdgcn_exp2f(p - top);
+    sum += w;
+    if (c < o.dv4) {
+      float2 v = *(const float2*)(o.pO + (s * n + row) * o.dv4 + c);
+      y0 = fmaf(w, v.x, y0);
+      y1 = fmaf(w, v.y, y1);
+    }
+  }
+  bool some = sum != 0.f;
+  float inv = some ? 1.f / sum : 0.f;
+  if (lane == 0) o.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+  int i = (int)(row % a.nq), h = (int)(row / a.nq % a.H), b = (int)(row / a.nq / a.H);
+  T* out = (T*)o.O + b * o.os[0] + (int64_t)i * o.os[1] + h * o.os[2];
+  if (c < a.dv) out[c] = (T)(y0 * inv);
+  if (c + 1 < a.dv) out[c + 1] = (T)(y1 * inv);
+}
+
+template <typename T>
+void attend_t(hipStream_t s, const AttArgs& a, const AttOut& o) {
+  int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt * o.nsplit, per = (total + 7) / 8;
+  if (a.d <= 64 && a.dv <= 64) k_attend<T, 64><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
+  else k_attend<T, 128><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
+}
+template <typename T>
+void attend_few_t(hipStream_t s, const AttArgs& a, const AttOut& o) {
+  int nrb = (int)(((int64_t)a.nq * a.G + 31) / 32), total = a.B * a.HK * nrb * o.nsplit;
+  if (a.d <= 64 && a.dv <= 64) k_attend_few<T, 64><<<total, 256, 0, s>>>(a, o, nrb);
+  else k_attend_few<T, 128><<<total, 256, 0, s>>>(a, o, nrb);
+}
+
+}  // namespace
+
+void launch_attend(hipStream_t s, int type, const AttArgs& a, const AttOut& o) {
+  if (type == 0) attend_t<float>(s, a, o);
+  else if (type == 1) attend_t<_Float16>(s, a, o);
+  else attend_t<__bf16>(s, a, o);
+}
+
+void launch_attend_few(hipStream_t s, int type, const AttArgs& a, const AttOut& o) {
+  if (type == 0) attend_few_t<float>(s, a, o);
+  else if (type == 1) attend_few_t<_Float16>(s, a, o);
+  else attend_few_t<__bf16>(s, a, o);
+}
+
+void launch_attend_join(hipStream_t s, int type, const AttArgs& a, const AttOut& o) {
+  size_t n = (size_t)a.B * a.H * a.nq;
+  int g = (int)((n + 3) / 4);
+  if (type == 0) k_attend_join<float><<<g, 256, 0, s>>>(a, o);
+  else if (type == 1) k_attend_join<_Float16><<<g, 256, 0, s>>>(a, o);
+  else k_attend_join<__bf16><<<g, 256, 0, s>>>(a, o);
+}
