@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from dataclasses import dataclass, field
 from typing import Optional
 
@@ -219,26 +220,32 @@ class Problem:
         return p
 
 
+_codes = {}
+
+
 def _type_of(tensor, name):
-    import torch
-    codes = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}
-    if not isinstance(tensor, torch.Tensor) or tensor.dtype not in codes:
+    """The library's code of a tensor's type."""
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16})
+    code = _codes.get(getattr(tensor, "dtype", None))
+    if code is None:
         raise TypeError("%s must be a float32, float16 or bfloat16 tensor" % name)
-    return codes[tensor.dtype]
+    return code
 
 
-def _check_same(tensor, shape, dtypes, device, name, dense=True):
-    """A tensor of this shape, one of these types and on this device; dense, or with its last dimension contiguous."""
-    import torch
-    if not isinstance(tensor, torch.Tensor) or tensor.dtype not in dtypes:
-        raise TypeError("%s must be a tensor of type %s" % (name, " or ".join(str(t) for t in dtypes)))
+def _check_same(tensor, shape, dtype, device, name, dense=True):
+    """A tensor of this shape, type and device; dense, or with its last dimension contiguous."""
+    if getattr(tensor, "dtype", None) is not dtype:
+        raise TypeError("%s must be a tensor of type %s" % (name, dtype))
     if tensor.device != device:
         raise ValueError("%s is on %s, expected %s" % (name, tensor.device, device))
-    if tuple(tensor.shape) != tuple(shape):
+    if tensor.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(tensor.shape), tuple(shape)))
-    if dense and not tensor.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    if not dense and tensor.shape[-1] > 1 and tensor.stride(-1) != 1 and tensor.numel():
+    if dense:
+        if not tensor.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+    elif tensor.stride(-1) != 1 and shape[-1] > 1 and tensor.numel():
         raise ValueError("the last dimension of %s must be contiguous" % name)
 
 
@@ -264,11 +271,12 @@ def bucket_edges(num_buckets: int, max_distance: int, two_sided: bool = True):
 
 
 def _edges(edges):
-    """Edges as the C array that a call takes (range and order are checked by the library)."""
-    e = [int(x) for x in (edges if edges is not None else ())]
-    if any(x < -2 ** 31 or x >= 2 ** 31 for x in e):
-        raise ValueError("bucket edges must ascend within [1, 1024]")
-    return (C.c_int32 * len(e))(*e)
+    """Edges as the C array that a call takes (their range and order are checked by the library)."""
+    try:
+        e = array("i", edges if edges is not None else ())
+    except OverflowError:
+        raise ValueError("bucket edges must ascend within [1, 1024]") from None
+    return (C.c_int32 * len(e)).from_buffer(e) if e else (C.c_int32 * 0)()
 
 
 @dataclass
@@ -288,42 +296,48 @@ class Attention:
     edges: "object" = None
     two_sided: bool = True
     q_start: "object" = None
-    _keep: list = field(default_factory=list, repr=False)
 
     def tensors(self):
         return [t for t in (self.Q, self.K, self.V, self.q_len, self.k_len, self.key_mask, self.table, self.q_start)
                 if t is not None]
 
     def to_c(self, device) -> _Attention:
-        import torch
-        a = _Attention()
-        a.type = _type_of(self.Q, "Q")
-        t = (self.Q.dtype,)
-        if self.Q.dim() != 4 or self.K.dim() != 4 or self.V.dim() != 4:
+        Q, K, V, table = self.Q, self.K, self.V, self.table
+        code, t = _type_of(Q, "Q"), Q.dtype
+        _type_of(K, "K"), _type_of(V, "V")
+        if Q.dim() != 4 or K.dim() != 4 or V.dim() != 4:
             raise ValueError("Q, K and V must have four dimensions (batch, row, head, feature)")
-        b, nq, h, d = self.Q.shape
-        nk, hk, dv = self.K.shape[1], self.K.shape[2], self.V.shape[3]
-        _check_same(self.Q, (b, nq, h, d), t, device, "Q", dense=False)
-        _check_same(self.K, (b, nk, hk, d), t, device, "K", dense=False)
-        _check_same(self.V, (b, nk, hk, dv), t, device, "V", dense=False)
-        a.batch, a.heads, a.kv_heads, a.nq, a.nk, a.d, a.dv = b, h, hk, nq, nk, d, dv
-        a.scale = float(d) ** -0.5 if self.scale is None else float(self.scale)
-        a.Q, a.K, a.V = self.Q.data_ptr(), self.K.data_ptr(), self.V.data_ptr()
-        a.q_stride[:], a.k_stride[:], a.v_stride[:] = self.Q.stride()[:3], self.K.stride()[:3], self.V.stride()[:3]
-        for name, shape, dtypes in (("q_len", (b,), (torch.int32,)), ("k_len", (b,), (torch.int32,)),
-                                    ("key_mask", (b, nk), (torch.bool, torch.uint8)), ("q_start", (b,), (torch.int64,))):
-            x = getattr(self, name)
-            if x is not None:
-                _check_same(x, shape, dtypes, device, name)
-                setattr(a, name, x.data_ptr())
-        a.two_sided = int(bool(self.two_sided))
-        if self.table is not None:
-            e = _edges(self.edges)
-            _check_same(self.table, (h, (len(e) + 1) * (2 if self.two_sided else 1)), t, device, "table")
-            self._keep = [e]
-            a.table, a.n_edges, a.edges = self.table.data_ptr(), len(e), e
+        b, nq, h, d = Q.shape
+        _, nk, hk, dv = V.shape
+        _check_same(Q, (b, nq, h, d), t, device, "Q", dense=False)
+        _check_same(K, (b, nk, hk, d), t, device, "K", dense=False)
+        _check_same(V, (b, nk, hk, dv), t, device, "V", dense=False)
+        two, n, edges = bool(self.two_sided), 0, None
+        if table is not None:
+            edges = _edges(self.edges)
+            n = len(edges)
+            _check_same(table, (h, 2 * n + 2 if two else n + 1), t, device, "table")
         elif self.edges is not None:
             raise ValueError("edges without a table")
+        a = _Attention(code, two, b, h, hk, nq, nk, d, dv, d ** -0.5 if self.scale is None else self.scale, Q.data_ptr(),
+                       K.data_ptr(), V.data_ptr(), Q.stride()[:3], K.stride()[:3], V.stride()[:3])
+        if table is not None:
+            a.table, a.n_edges, a.edges = table.data_ptr(), n, edges
+        if self.q_len is not None or self.k_len is not None or self.key_mask is not None or self.q_start is not None:
+            import torch
+            if self.q_len is not None:
+                _check_same(self.q_len, (b,), torch.int32, device, "q_len")
+                a.q_len = self.q_len.data_ptr()
+            if self.k_len is not None:
+                _check_same(self.k_len, (b,), torch.int32, device, "k_len")
+                a.k_len = self.k_len.data_ptr()
+            if self.key_mask is not None:
+                kind = torch.uint8 if getattr(self.key_mask, "dtype", None) == torch.uint8 else torch.bool
+                _check_same(self.key_mask, (b, nk), kind, device, "key_mask")
+                a.key_mask = self.key_mask.data_ptr()
+            if self.q_start is not None:
+                _check_same(self.q_start, (b,), torch.int64, device, "q_start")
+                a.q_start = self.q_start.data_ptr()
         return a
 
 
@@ -572,10 +586,9 @@ class Context:
         torch = self.torch
         here = torch.cuda.current_stream(self.device)
         if here.cuda_stream == self._stream.cuda_stream:
-            with torch.cuda.device(self.device):
-                return call()
+            return call()
         self._stream.wait_stream(here)
-        with torch.cuda.device(self.device), torch.cuda.stream(self._stream):
+        with torch.cuda.stream(self._stream):
             out = call()
         for t in tensors:
             t.record_stream(self._stream)
@@ -617,10 +630,10 @@ class Context:
     def bbmm_attend_grad(self, att: Attention, O, lse, dO):
         """(dQ, dK, dV, dtable) of sum(dO * O); dtable is None without a table.  O, lse: from bbmm_attend of the same call."""
         a = att.to_c(self.device)
-        t = (att.Q.dtype,)
+        t = att.Q.dtype
         shape = (a.batch, a.nq, a.heads, a.dv)
         _check_same(O, shape, t, self.device, "O")
-        _check_same(lse, (a.batch, a.heads, a.nq), (self.torch.float32,), self.device, "lse")
+        _check_same(lse, (a.batch, a.heads, a.nq), self.torch.float32, self.device, "lse")
         _check_same(dO, shape, t, self.device, "dO", dense=False)
         stride = (C.c_int64 * 3)(*dO.stride()[:3])
 
@@ -637,7 +650,7 @@ class Context:
     def bbmm_bucket_bias(self, table, edges, nq: int, nk: int, two_sided: bool = True, start: int = 0):
         """The bias as a matrix (heads, nq, nk) of the table's type: table[h, bucket(j - i - start)]."""
         kind, e = _type_of(table, "table"), _edges(edges)
-        _check_same(table, (table.shape[0], (len(e) + 1) * (2 if two_sided else 1)), (table.dtype,), self.device, "table")
+        _check_same(table, (table.shape[0], (len(e) + 1) * (2 if two_sided else 1)), table.dtype, self.device, "table")
 
         def call():
             B = self.torch.empty(table.shape[0], nq, nk, dtype=table.dtype, device=self.device)
@@ -659,7 +672,7 @@ class Context:
         kind, e = _type_of(dB, "dB"), _edges(edges)
         if dB.dim() != 4:
             raise ValueError("dB must have four dimensions (batch, head, nq, nk)")
-        _check_same(dB, dB.shape, (dB.dtype,), self.device, "dB")
+        _check_same(dB, dB.shape, dB.dtype, self.device, "dB")
         b, h, nq, nk = dB.shape
 
         def call():

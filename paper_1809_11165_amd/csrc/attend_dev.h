@@ -162,30 +162,33 @@ __device__ __forceinline__ typename Frag<T>::type reg_frag(const T* row, bool ha
 }
 
 // ---- buckets
+// The edges are read at uniform places (scalar loads), eight at a time; places behind the last edge hold the largest int.
 __device__ __forceinline__ int bucket_of(const AttBuckets& bk, int r) {
-  int dist = bk.two_sided ? abs(r) : max(-r, 0);
-  int lo = 0, hi = bk.n_edges;                 // first edge beyond dist
-  while (lo < hi) {
-    int mid = (lo + hi) >> 1;
-    if (bk.edges[mid] <= dist) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo + ((bk.two_sided && r > 0) ? bk.n_edges + 1 : 0);
+  int dist = bk.two_sided ? abs(r) : max(-r, 0), n = 0;
+  for (int k = 0; k < bk.n_edges; k += 8)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) n += bk.edges[k + e] <= dist;
+  return n + ((bk.two_sided && r > 0) ? bk.n_edges + 1 : 0);
 }
 
-// Sums by bucket of a workgroup (four waves): diag[r + span] holds the sum of difference r, |r| <= span; `left` and `right` are sums of
-// differences -far and below, far and above.  A wave takes every fourth bucket.
-__device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* diag, int span, float left, float right, float* out, int lane,
-                                            int wave) {
-  for (int n = wave; n < bk.buckets; n += 4) {
+// Sums by bucket of a workgroup of 256: diag[r + span] holds the sum of difference r, |r| <= span; `left` and `right` are sums of differences
+// -far and below, far and above.  A bucket is an interval of differences on one side; eight lanes take one.
+__device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* diag, int span, float left, float right, float* out, int tid) {
+  int E = bk.n_edges, part = tid & 7;
+  for (int n = tid >> 3; n < bk.buckets; n += 32) {
+    bool ahead = n > E;                                   // two-sided, r > 0
+    int c = ahead ? n - E - 1 : n;
+    int near = c ? bk.edges[c - 1] : 0, beyond = c < E ? bk.edges[c] - 1 : span;
+    beyond = min(beyond, span);
+    int lo = ahead ? max(near, 1) : -beyond, hi = ahead ? beyond : -near;
+    if (!bk.two_sided && n == 0) hi = span;
     float s = 0.f;
-    for (int k = lane; k <= 2 * span; k += 64)
-      if (bucket_of(bk, k - span) == n) s += diag[k];
+    for (int r = lo + part; r <= hi; r += 8) s += diag[r + span];
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) s += __shfl_xor(s, x, 64);
-    if (bucket_of(bk, -bk.far) == n) s += left;
-    if (bucket_of(bk, bk.far) == n) s += right;
-    if (lane == 0) out[n] = s;
+    for (int x = 1; x < 8; x *= 2) s += __shfl_xor(s, x, 64);
+    if (n == E) s += left;
+    if (n == (bk.two_sided ? 2 * E + 1 : 0)) s += right;
+    if (part == 0) out[n] = s;
   }
 }
 

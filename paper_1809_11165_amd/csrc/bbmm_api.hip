@@ -2100,7 +2100,7 @@ int set_buckets(bbmm_ctx* c, int64_t n_edges, const int32_t* edges, int32_t two_
   out->two_sided = two_sided != 0;
   out->buckets = (int)(n_edges + 1) * (two_sided ? 2 : 1);
   out->far = 1;
-  for (int k = 0; k < BBMM_ATT_MAXEDGES; ++k) out->edges[k] = 0;
+  for (int k = 0; k <= BBMM_ATT_MAXEDGES; ++k) out->edges[k] = INT32_MAX;
   if (!need_edges) return BBMM_OK;
   for (int k = 0; k < n_edges; ++k) {
     if (edges[k] < 1 || edges[k] > BBMM_ATT_FAR || (k && edges[k] <= edges[k - 1]))

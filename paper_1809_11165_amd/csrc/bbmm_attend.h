@@ -15,7 +15,7 @@ struct AttBuckets {
   int n_edges, two_sided;
   int far;       // the last edge (1 without edges: then only the sign tells buckets apart)
   int buckets;
-  int edges[BBMM_ATT_MAXEDGES];
+  int edges[BBMM_ATT_MAXEDGES + 1];   // behind the last one: the largest int
 };
 
 struct AttArgs {

@@ -165,11 +165,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   typedef typename Frag<T>::type frag;
   constexpr int ND = DP / 32, NS = DP / 16, E = 16 / (int)sizeof(T), CH = DP / E, NV = 32 * CH / 64;
   constexpr bool kLds = sizeof(T) == 2;      // V through LDS (four-byte elements are read as the product wants them)
-  constexpr int kVt = 32 * DP * 2, kJoin = 32 * (DP + 4) * 4;
-  __shared__ __align__(16) char buf[4 * (kVt > kJoin ? kVt : kJoin)];
-  __shared__ float tab[32][2 * (BBMM_ATT_MAXEDGES + 1) + 1];
-  __shared__ uint8_t bline[kLine];
+  constexpr int kVt = 32 * DP * 2, kPart = 32 * (DP + 4);
+  __shared__ __align__(16) char buf[kLds && 4 * kVt > 8 * kPart ? 4 * kVt : 8 * kPart];
   __shared__ float wm[4][32], wl[4][32];
+  extern __shared__ float dyn[];               // with a table: 32 rows of its entries, then the bucket of every difference (bytes)
   int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
   int x = blockIdx.x, rb = x % nrb, sp = (x / nrb) % o.nsplit, bh = x / nrb / o.nsplit, hk = bh % a.HK, b = bh / a.HK;
   int rows = a.nq * a.G, rho = rb * 32 + col, i = rho / a.G, h = hk * a.G + rho % a.G;
@@ -185,22 +184,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   const uint8_t* mrow = a.mask ? a.mask + b * a.mask_s : nullptr;
   int64_t start = start_of(a, b);
   frag q[NS], kf[NS];
-  {
-    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) q[s] = reg_frag<T>(row, mine, s, a.d, a.qvec, lane);
-  }
-  float left = 0.f, right = 0.f;
-  if (a.table) {
-    for (int n = tid; n < 32 * a.bk.buckets; n += 256) {
-      int r = rb * 32 + n / a.bk.buckets, g = r % a.G;
-      tab[n / a.bk.buckets][n % a.bk.buckets] = r < rows ? bias2<T>(((const T*)a.table)[(size_t)(hk * a.G + g) * a.bk.buckets + n % a.bk.buckets]) : 0.f;
-    }
-    for (int n = tid; n < 2 * (a.bk.far + kPad) + 1; n += 256) bline[n] = (uint8_t)bucket_of(a.bk, n - a.bk.far - kPad);
-    __syncthreads();
-    left = tab[col][bline[0]];
-    right = tab[col][bline[2 * (a.bk.far + kPad)]];
-  }
   char* vt = buf + wave * kVt;
   u32x4 vr[kLds ? NV : 1];
   uint8_t mb = 0, mnext = 0;
@@ -232,6 +215,25 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
     fetch_k(t);
     fetch_v(t);
   }
+  {
+    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = reg_frag<T>(row, mine, s, a.d, a.qvec, lane);
+  }
+  float left = 0.f, right = 0.f;
+  int pitch = a.bk.buckets | 1;
+  const float* tab = dyn + col * pitch;
+  uint8_t* bline = (uint8_t*)(dyn + 32 * pitch);
+  if (a.table) {
+    // entries of the rows' heads, and the bucket of every difference (bytes)
+    int r = rb * 32 + (tid >> 3);
+    const T* src = (const T*)a.table + (size_t)(hk * a.G + r % a.G) * a.bk.buckets;
+    for (int n = tid & 7; n < a.bk.buckets; n += 8) dyn[(tid >> 3) * pitch + n] = r < rows ? bias2<T>(src[n]) : 0.f;
+    for (int n = tid; n < 2 * (a.bk.far + kPad) + 1; n += 256) bline[n] = (uint8_t)bucket_of(a.bk, n - a.bk.far - kPad);
+    __syncthreads();
+    left = tab[bline[0]];
+    right = tab[bline[2 * (a.bk.far + kPad)]];
+  }
   for (; t < t1; t += 4) {
     mb = mnext;
     unsigned keep = (unsigned)keep_bits(min(kn - t * 32, 32), mrow, mb);
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
     } else {
       const uint8_t* bl = bline + (rel0 - (min(i, a.nq - 1) - i0) + 4 * half + a.bk.far + kPad);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c2, tab[col][bl[8 * (r >> 2) + (r & 3)]]);
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c2, tab[bl[8 * (r >> 2) + (r & 3)]]);
     }
     drop_keys(s, keep, lane);
     float top = -__builtin_inff();
@@ -303,30 +305,39 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
     }
     if constexpr (kLds) __builtin_amdgcn_wave_barrier();
   }
-  // join the four waves: each leaves its sums relative to its own reference
+  // join the four waves: each scales its sums to the largest reference; two leave theirs in LDS, the other two add them, all write
   l += other_half(l);
-  __syncthreads();
-  float* part = (float*)buf + wave * 32 * (DP + 4) + col * (DP + 4);
-#pragma unroll
-  for (int n = 0; n < ND; ++n)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      *(f32x4*)(part + 32 * n + 8 * r + 4 * half) = f32x4{acc[n][4 * r], acc[n][4 * r + 1], acc[n][4 * r + 2], acc[n][4 * r + 3]};
   if (half == 0) {
     wm[wave][col] = m;
     wl[wave][col] = l;
   }
   __syncthreads();
+  float top = fmaxf(fmaxf(wm[0][col], wm[1][col]), fmaxf(wm[2][col], wm[3][col]));
+  float w = m == -__builtin_inff() && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - top);
+  float* part = (float*)buf + (wave & 1) * kPart + col * (DP + 4) + 4 * half;
+  if (wave >= 2) {
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(f32x4*)(part + 32 * n + 8 * r) = f32x4{acc[n][4 * r] * w, acc[n][4 * r + 1] * w, acc[n][4 * r + 2] * w, acc[n][4 * r + 3] * w};
+  }
+  __syncthreads();
+  if (wave < 2) {
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(f32x4*)(part + 32 * n + 8 * r) += f32x4{acc[n][4 * r] * w, acc[n][4 * r + 1] * w, acc[n][4 * r + 2] * w, acc[n][4 * r + 3] * w};
+  }
+  __syncthreads();
   // eight threads per row
   int row = tid >> 3, rr = rb * 32 + row, qi = rr / a.G, hh = hk * a.G + rr % a.G;
   if (rr >= rows) return;
-  float top = fmaxf(fmaxf(wm[0][row], wm[1][row]), fmaxf(wm[2][row], wm[3][row]));
-  float w[4], sum = 0.f;
+  top = fmaxf(fmaxf(wm[0][row], wm[1][row]), fmaxf(wm[2][row], wm[3][row]));
+  float sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    w[k] = wm[k][row] == -__builtin_inff() && wl[k][row] == 0.f ? 0.f : __builtin_amdgcn_exp2f(wm[k][row] - top);
-    sum += w[k] * wl[k][row];
-  }
+  for (int k = 0; k < 4; ++k) sum += wm[k][row] == -__builtin_inff() && wl[k][row] == 0.f ? 0.f : __builtin_amdgcn_exp2f(wm[k][row] - top) * wl[k][row];
   bool some = sum != 0.f && qi < qn;
   float inv = some ? 1.f / sum : 0.f;
   float lse2 = some ? (top - Lift<T>::value) + __builtin_amdgcn_logf(sum) : -__builtin_inff();
@@ -339,47 +350,54 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   const float* src = (const float*)buf + row * (DP + 4);
   T* out = (T*)o.O + b * o.os[0] + (int64_t)qi * o.os[1] + hh * o.os[2];
   for (int c = (tid & 7) * 4; c < DP; c += 32) {
-    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (some) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (w[k] != 0.f) y += (w[k] * inv) * *(const f32x4*)(src + k * 32 * (DP + 4) + c);
-    }
+    f32x4 y = (*(const f32x4*)(src + c) + *(const f32x4*)(src + kPart + c)) * inv;
+    if (!some) y = f32x4{0.f, 0.f, 0.f, 0.f};
     if (o.nsplit == 1) store4<T>(out, c, a.dv, o.ovec, y[0], y[1], y[2], y[3]);
     else if (c < o.dv4) *(f32x4*)(o.pO + at * o.dv4 + c) = y;
   }
 }
 
-// One wave per row: parts weighed by their sums.  Two features per lane.
+// A workgroup per row: parts weighed by their sums.  Eight groups of 32 lanes take every eighth part, four features per lane.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(AttArgs a, AttOut o) {
-  int lane = threadIdx.x & 63;
-  size_t n = (size_t)a.B * a.H * a.nq, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= n) return;
+  __shared__ float wsum[4], wtop[4];
+  __shared__ __align__(16) f32x4 part[8][32];
+  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = tid >> 5, c = 4 * (tid & 31);
+  size_t n = (size_t)a.B * a.H * a.nq, row = blockIdx.x;
   float top = -__builtin_inff();
-  for (int s = lane; s < o.nsplit; s += 64) top = fmaxf(top, o.pl[s * n + row]);
+  for (int s = tid; s < o.nsplit; s += 256) top = fmaxf(top, o.pl[s * n + row]);
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 64));
-  float sum = 0.f, y0 = 0.f, y1 = 0.f;
-  int c = 2 * lane;
-  for (int s = 0; s < o.nsplit; ++s) {
+  if (lane == 0) wtop[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(wtop[0], wtop[1]), fmaxf(wtop[2], wtop[3]));
+  float sum = 0.f;
+  f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = g; s < o.nsplit; s += 8) {
     float p = o.pl[s * n + row];
-    if (p == -__builtin_inff()) continue;
-    float w = __builtin_amdgcn_exp2f(p - top);
+    float w = p == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(p - top);
     sum += w;
     if (c < o.dv4) {
-      float2 v = *(const float2*)(o.pO + (s * n + row) * o.dv4 + c);
-      y0 = fmaf(w, v.x, y0);
-      y1 = fmaf(w, v.y, y1);
+      f32x4 v = *(const f32x4*)(o.pO + (s * n + row) * o.dv4 + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(w, v[e], y[e]);
     }
   }
+  part[g][tid & 31] = y;
+  sum += __shfl_xor(sum, 32, 64);
+  if (lane == 0) wsum[wave] = sum;
+  __syncthreads();
+  if (tid >= 32) return;
+  sum = (wsum[0] + wsum[1]) + (wsum[2] + wsum[3]);
+#pragma unroll
+  for (int k = 1; k < 8; ++k) y += part[k][tid];
   bool some = sum != 0.f;
   float inv = some ? 1.f / sum : 0.f;
-  if (lane == 0) o.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+  if (tid == 0) o.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
   int i = (int)(row % a.nq), h = (int)(row / a.nq % a.H), b = (int)(row / a.nq / a.H);
   T* out = (T*)o.O + b * o.os[0] + (int64_t)i * o.os[1] + h * o.os[2];
-  if (c < a.dv) out[c] = (T)(y0 * inv);
-  if (c + 1 < a.dv) out[c + 1] = (T)(y1 * inv);
+  store4<T>(out, c, a.dv, o.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
 template <typename T>
@@ -391,8 +409,9 @@ void attend_t(hipStream_t s, const AttArgs& a, const AttOut& o) {
 template <typename T>
 void attend_few_t(hipStream_t s, const AttArgs& a, const AttOut& o) {
   int nrb = (int)(((int64_t)a.nq * a.G + 31) / 32), total = a.B * a.HK * nrb * o.nsplit;
-  if (a.d <= 64 && a.dv <= 64) k_attend_few<T, 64><<<total, 256, 0, s>>>(a, o, nrb);
-  else k_attend_few<T, 128><<<total, 256, 0, s>>>(a, o, nrb);
+  size_t lds = a.table ? 32 * sizeof(float) * (a.bk.buckets | 1) + 2 * (a.bk.far + kPad) + 1 : 0;
+  if (a.d <= 64 && a.dv <= 64) k_attend_few<T, 64><<<total, 256, lds, s>>>(a, o, nrb);
+  else k_attend_few<T, 128><<<total, 256, lds, s>>>(a, o, nrb);
 }
 
 }  // namespace
@@ -411,7 +430,7 @@ void launch_attend_few(hipStream_t s, int type, const AttArgs& a, const AttOut& 
 
 void launch_attend_join(hipStream_t s, int type, const AttArgs& a, const AttOut& o) {
   size_t n = (size_t)a.B * a.H * a.nq;
-  int g = (int)((n + 3) / 4);
+  int g = (int)n;
   if (type == 0) k_attend_join<float><<<g, 256, 0, s>>>(a, o);
   else if (type == 1) k_attend_join<_Float16><<<g, 256, 0, s>>>(a, o);
   else k_attend_join<__bf16><<<g, 256, 0, s>>>(a, o);

@@ -241,7 +241,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
     }
     __syncthreads();
     float* out = g.tsum + ((size_t)h * a.B * nqt + (size_t)b * nqt + qt) * a.bk.buckets;
-    bucket_sums(a.bk, line, span, side[0] + side[1] + side[2] + side[3], side[4] + side[5] + side[6] + side[7], out, lane, wave);
+    bucket_sums(a.bk, line, span, side[0] + side[1] + side[2] + side[3], side[4] + side[5] + side[6] + side[7], out, tid);
   }
 }
 

@@ -61,9 +61,15 @@ __global__ __launch_bounds__(256) void k_bucket_grad(const T* __restrict__ dB, A
   for (int n = tid; n < 2 * far - 1; n += 256) {
     int64_t r = n - (far - 1) + start;                       // j - i
     int64_t lo = max(i0, -r), hi = min(i1, nk - r);
-    float s = 0.f;
-    for (int64_t i = lo; i < hi; ++i) s += (float)mat[i * nk + i + r];
-    diag[n] = s;
+    int count = (int)max((int64_t)0, hi - lo);
+    const T* p = count ? mat + lo * nk + lo + r : mat;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};        // eight loads in flight
+    for (int i = 0; i < count; i += 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += i + e < count ? (float)p[e * (nk + 1)] : 0.f;
+      p += 8 * (nk + 1);
+    }
+    diag[n] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
   }
   float sl = 0.f, sr = 0.f;
   for (int64_t i = i0 + wave; i < i1; i += 4) {
@@ -79,17 +85,24 @@ __global__ __launch_bounds__(256) void k_bucket_grad(const T* __restrict__ dB, A
     };
     if (lane < lead) one(lane);
     if (tail + lane < nk) one(tail + lane);
-    for (int64_t c = lane; c < body; c += 64) {
-      int64_t j = lead + c * E;
-      int r = clamp_rel(j - off);
-      if (r > -far && r + E - 1 < far) continue;
-      u32x4 v = *(const u32x4*)(row + j);
+    for (int64_t c0 = lane; c0 < body; c0 += 4 * 64) {
+      u32x4 v[4];
+      int r[4];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float x = (float)reinterpret_cast<const T*>(&v)[e];
-        sl += r + e <= -far ? x : 0.f;
-        sr += r + e >= far ? x : 0.f;
+      for (int k = 0; k < 4; ++k) {                         // four loads in flight; what lies between the edges is not read
+        int64_t c = c0 + 64 * k, j = lead + c * E;
+        r[k] = clamp_rel(j - off);
+        v[k] = u32x4{0u, 0u, 0u, 0u};
+        if (c < body && (r[k] <= -far || r[k] + E - 1 >= far)) v[k] = *(const u32x4*)(row + j);
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          float x = (float)reinterpret_cast<const T*>(&v[k])[e];
+          sl += r[k] + e <= -far ? x : 0.f;
+          sr += r[k] + e >= far ? x : 0.f;
+        }
     }
   }
 #pragma unroll
@@ -103,7 +116,7 @@ __global__ __launch_bounds__(256) void k_bucket_grad(const T* __restrict__ dB, A
   }
   __syncthreads();
   float* out = tsum + ((size_t)h * nparts + (size_t)b * gridDim.x + blockIdx.x) * bk.buckets;
-  bucket_sums(bk, diag, far - 1, side[0][0] + side[0][1] + side[0][2] + side[0][3], side[1][0] + side[1][1] + side[1][2] + side[1][3], out, lane, wave);
+  bucket_sums(bk, diag, far - 1, side[0][0] + side[0][1] + side[0][2] + side[0][3], side[1][0] + side[1][1] + side[1][2] + side[1][3], out, tid);
 }
 
 // One wave per (head, bucket): the parts in a fixed order, 64 bits.
