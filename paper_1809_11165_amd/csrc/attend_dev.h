@@ -192,6 +192,38 @@ __device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* d
   }
 }
 
+// Adds the 32 x 32 block s (keys in the registers, queries in the lanes) along its diagonals: line[j - i] += sum, `line` pointing at
+// the difference of the first key and the first query, one line per half of the wave.  Halves first exchange registers so that each
+// has 16 keys in a row; a sum then moves one lane per key, towards higher lanes for keys ahead (what leaves a row of 16 lanes
+// lies behind), towards lower ones for keys behind.  Two LDS additions per block, all lanes of a half at places of their own, instead of
+// sixteen (those made the dQ pass of 8 x 12 x 512 x 640 in bf16, d = 64, 104 us, see there).
+__device__ __forceinline__ float from_lane_below(float x) {   // of the row of 16, zero into the first
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x111, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float from_lane_above(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x101, 0xf, 0xf, true));
+}
+__device__ __forceinline__ void add_diagonals(const f32x16& s, float* line, int lane) {
+  float k[16];                                              // key 16 (lane / 32) + index
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      auto x = __builtin_amdgcn_permlane32_swap(__float_as_int(s[4 * g + e]), __float_as_int(s[4 * (g + 2) + e]), false, false);
+      k[8 * g + e] = __int_as_float(x[0]);
+      k[8 * g + 4 + e] = __int_as_float(x[1]);
+    }
+  float ahead = k[0], behind = k[15];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) {
+    ahead = from_lane_below(ahead) + k[i];
+    behind = from_lane_above(behind) + k[15 - i];
+  }
+  int q = lane & 15, base = 16 * (lane >> 5) - (lane & 16);
+  __hip_atomic_fetch_add(line + base + 15 - q, ahead, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  if (q) __hip_atomic_fetch_add(line + base - q, behind, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
 // A table entry in units of the base-2 exponent.  Finite entries stay finite: one below -2.3e38 counts as that (the same
 // weight zero beside any other score, and weights of its own where a row holds nothing else).
 template <typename T>

@@ -185,11 +185,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
         }
         if (ln) {
           if (where == 0) {
-            // a lane's additions go to its half's line at places of their own: no two lanes of a half meet
-            float* d = diag + (2 * wave + half) * nline + (rel0 - (lane & 31) + 4 * half + span);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              __hip_atomic_fetch_add(d + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            add_diagonals(s, diag + (2 * wave + half) * nline + rel0 + span, lane);
           } else {
             float x = 0.f;
 #pragma unroll
