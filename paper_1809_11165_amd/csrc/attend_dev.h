@@ -50,21 +50,28 @@ __device__ __forceinline__ typename Frag<T>::type pack8(const f32x16& c, int u) 
   return f;
 }
 
-// ---- LDS tiles: rows of DP elements; the 16-byte pieces of row r stand in places c ^ swz(r).  Eight rows in a row have eight
-// different swz, and four rows in a row four different swz / 2: no bank conflicts along columns (row_frag) nor in 4 x 16 blocks (col_frag).
-__device__ __forceinline__ int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// ---- LDS tiles: rows of DP elements; the 16-byte pieces of row r stand in places c ^ swz(r).  A cycle of the LDS serves 256 bytes: 16 lanes
+// of a row_frag (16 rows, one piece each), 32 lanes of a 16-bit col_frag (four rows, four neighbouring pieces) or all 64 of an fp32
+// one (two rows four apart, 128 bytes each).  swz puts each of these on 16 different places of 256 bytes: no bank conflicts.  (With the pieces
+// spread over 128 bytes only, a forward pass of 4096 x 10000, d = 128, spent 40 % of its LDS cycles on conflicts.)
+template <typename T, int DP>
+__device__ __forceinline__ int swz(int r) {
+  if constexpr (sizeof(T) == 4) return (((r >> 2) & 1) << 3) | ((r & 3) << 1) | ((r >> 3) & 1);
+  else if constexpr (DP >= 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+  else return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);      // two rows share 256 bytes
+}
 
 // First operand: element e of the lane = tile[rb + lane % 32][16 s + 8 (lane / 32) + e];  rb a multiple of 32.
 template <typename T, int DP>
 __device__ __forceinline__ typename Frag<T>::type row_frag(const char* tile, int rb, int s, int lane) {
   constexpr int kRow = DP * (int)sizeof(T);
-  int r = lane & 31, half = lane >> 5;
+  int r = lane & 31, half = lane >> 5, f = swz<T, DP>(r);
   const char* p = tile + (rb + r) * kRow;
   if constexpr (sizeof(T) == 2) {
-    return *(const typename Frag<T>::type*)(p + (((2 * s + half) ^ swz(r)) << 4));
+    return *(const typename Frag<T>::type*)(p + (((2 * s + half) ^ f) << 4));
   } else {
-    f32x4 lo = *(const f32x4*)(p + (((4 * s + 2 * half) ^ swz(r)) << 4));
-    f32x4 hi = *(const f32x4*)(p + (((4 * s + 2 * half + 1) ^ swz(r)) << 4));
+    f32x4 lo = *(const f32x4*)(p + (((4 * s + 2 * half) ^ f) << 4));
+    f32x4 hi = *(const f32x4*)(p + (((4 * s + 2 * half + 1) ^ f) << 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 }
@@ -78,12 +85,12 @@ __device__ __forceinline__ typename Frag<T>::type col_frag(const char* tile, int
   int half = lane >> 5;
   typename Frag<T>::type f;
   if constexpr (sizeof(T) == 2) {
-    int L = lane & 15, r4 = L >> 2;
+    int L = lane & 15, r = 4 * half + (L >> 2);
     int c = (cb >> 3) + 2 * ((lane >> 4) & 1) + ((L & 3) >> 1);
-    const char* p = tile + (rb + 4 * half + r4) * kRow + ((c ^ ((r4 << 1) | half)) << 4) + ((L & 1) << 3);
+    const char* p = tile + (rb + r) * kRow + ((L & 1) << 3);
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRow));
+    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + ((c ^ swz<T, DP>(r)) << 4)));
+    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRow + ((c ^ swz<T, DP>(r + 8)) << 4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     f = __builtin_bit_cast(typename Frag<T>::type, v);
@@ -91,12 +98,18 @@ __device__ __forceinline__ typename Frag<T>::type col_frag(const char* tile, int
     int col = cb + (lane & 31);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      int r = rb + 8 * (e >> 2) + 4 * half + (e & 3);
-      f[e] = *(const float*)(tile + r * kRow + (((col >> 2) ^ (((e & 3) << 1) | half)) << 4) + ((col & 3) << 2));
+      int r = 8 * (e >> 2) + 4 * half + (e & 3);
+      f[e] = *(const float*)(tile + (rb + r) * kRow + (((col >> 2) ^ swz<T, DP>(r)) << 4) + ((col & 3) << 2));
     }
   }
   return f;
 }
+
+// Memory from `base` on with hardware bounds: reads at or behind `bytes` give zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bounded(const void* base, unsigned bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
+}
+constexpr unsigned kNowhere = 0x80000000u;   // an offset behind every bound (bounds are below 2^31: wide operands only)
 
 // 16 bytes of a row: elements [c, c + 16 / sizeof(T)) of `row`, zero from element `width` on.
 template <typename T>
@@ -112,31 +125,49 @@ __device__ __forceinline__ u32x4 load16(const T* row, int c, int width, int vec)
   return v;
 }
 
-// A tile of ROWS rows on its way from memory to LDS: 256 threads, 16 bytes each per pass.
-template <typename T, int DP, int ROWS>
+// A tile of ROWS rows on its way from memory to LDS: 256 threads, 16 bytes each per pass.  VEC: rows may be read 16 bytes at a time and a
+// tile spans less than 2^31 bytes.
+template <typename T, int DP, int ROWS, bool VEC>
 struct Stage {
   static constexpr int E = 16 / (int)sizeof(T), CH = DP / E, RP = 256 / CH, N = ROWS / RP;
   u32x4 v[N];
-  // row 0 of the tile at `base`; rows from `rows` on are zero and not read
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int width, int vec, int tid) {
+  // row 0 of the tile at `base`; what is read of rows from `rows` on is within bounds, or zero, and means nothing
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int width, int tid) {
     int r = tid / CH, c = (tid % CH) * E;
-    const T* p = base + (int64_t)r * stride;
+    if constexpr (VEC) {
+      unsigned pitch = (unsigned)stride * (unsigned)sizeof(T);
+      unsigned n = (unsigned)(max(min(rows, ROWS), 1) - 1) * pitch + (unsigned)width * (unsigned)sizeof(T);
+      __amdgpu_buffer_rsrc_t mem = bounded(base, rows > 0 ? n : 0u);
+      unsigned at = c < width ? (unsigned)r * pitch + (unsigned)c * (unsigned)sizeof(T) : kNowhere;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = u32x4{0u, 0u, 0u, 0u};
-      if (r + i * RP < rows) v[i] = load16<T>(p, c, width, vec);
-      p += (int64_t)RP * stride;
+      for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(mem, at + (unsigned)(i * RP) * pitch, 0, 0);
+    } else {
+      const T* p = base + (int64_t)r * stride;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[i] = u32x4{0u, 0u, 0u, 0u};
+        if (r + i * RP < rows) v[i] = load16<T>(p, c, width, 0);
+        p += (int64_t)RP * stride;
+      }
     }
   }
   // rows without a bit in `keep` are stored as zeros, whatever they held
   __device__ __forceinline__ void store(char* tile, uint64_t keep, int tid) const {
     int r = tid / CH, c = tid % CH;
+    if (keep == ~0ull || (ROWS == 32 && keep == 0xffffffffull)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      int row = r + i * RP;
-      u32x4 x = v[i];
-      if (!((keep >> row) & 1)) x = u32x4{0u, 0u, 0u, 0u};
-      *(u32x4*)(tile + row * DP * (int)sizeof(T) + ((c ^ swz(row)) << 4)) = x;
+      for (int i = 0; i < N; ++i) {
+        int row = r + i * RP;
+        *(u32x4*)(tile + row * DP * (int)sizeof(T) + ((c ^ swz<T, DP>(row)) << 4)) = v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        int row = r + i * RP;
+        u32x4 x = v[i];
+        if (!((keep >> row) & 1)) x = u32x4{0u, 0u, 0u, 0u};
+        *(u32x4*)(tile + row * DP * (int)sizeof(T) + ((c ^ swz<T, DP>(row)) << 4)) = x;
+      }
     }
   }
 };
@@ -241,29 +272,65 @@ __device__ __forceinline__ void fill_line(float* line, const AttArgs& a, int h, 
   for (int i = tid; i < n; i += threads) line[i] = bias2<T>(tab[bucket_of(a.bk, i - a.bk.far - kPad)]);
 }
 
+// A value that all lanes hold, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(uniform(__float_as_int(x))); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)(unsigned)uniform((int)(x >> 32)) << 32) | (unsigned)uniform((int)x));
+}
+__device__ __forceinline__ int queries_of(const AttArgs& a, int b) { return a.q_len ? uniform(min(max(a.q_len[b], 0), a.nq)) : a.nq; }
+__device__ __forceinline__ int keys_of(const AttArgs& a, int b) { return a.k_len ? uniform(min(max(a.k_len[b], 0), a.nk)) : a.nk; }
+
+// Waits for all loads issued so far.  Stands before a loop whose operands were loaded ahead of it: without it the compiler's own
+// counting, which meets the loop's loads and those together at the loop's head, waits for the prefetched tile in every turn.
+__device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 __device__ __forceinline__ int clamp_rel(int64_t r) {
   const int64_t lim = 1 << 30;
   return (int)(r < -lim ? -lim : (r > lim ? lim : r));
 }
 
+// x - y + z of a running y (or z) from 0 to 2^30 and a fixed rest r, as 32 bits: differences that leave the line of the bias stay outside.
+__device__ __forceinline__ int rest_below(int64_t r) {      // r + running
+  const int64_t lo = -((int64_t)1 << 30) - 4096, hi = 4096;
+  return (int)(r < lo ? lo : (r > hi ? hi : r));
+}
+__device__ __forceinline__ int rest_above(int64_t r) {      // r - running
+  const int64_t lo = -4096, hi = ((int64_t)1 << 30) + 4096;
+  return (int)(r < lo ? lo : (r > hi ? hi : r));
+}
+
 // position of a batch's first query: beyond 2^40 everything is far
 __device__ __forceinline__ int64_t start_of(const AttArgs& a, int b) {
   const int64_t lim = (int64_t)1 << 40;
-  int64_t s = a.q_start ? a.q_start[b] : 0;
+  int64_t s = a.q_start ? uniform(a.q_start[b]) : 0;
   return s < -lim ? -lim : (s > lim ? lim : s);
 }
 
-// Scores of 32 keys against 32 queries in base-2 exponents, bias added.  KEYS_DOWN: keys in the registers, queries in the lanes, else the
-// other way round.  rel0: j - i - start of the first key and the first query; line: see fill_line (null: no table).  Returns 0 where the
-// differences are mixed, -1 / 1 where all lie beyond the last edge on that side (or there is no table).
+// Scores of 32 keys against 32 queries in base-2 exponents are mul s + add after this: where all differences lie beyond the last edge on one
+// side (or there is no table) s stays as the product left it, else the bias is in s already.  KEYS_DOWN: keys in the registers, queries in
+// the lanes, else the other way round.  rel0: j - i - start of the first key and the first query; line: see fill_line (null: no table).
+// A bias so large that it rounds scores away (a mask by values like the type's lowest) is added first all the same: rows of nothing but such
+// scores then have weights of the rounded ones, as they would have from any other order of the sum.
+// Returns 0 where the differences are mixed, -1 / 1 where all lie beyond the last edge on that side.
+constexpr float kFoldable = 1e6f;
 template <bool KEYS_DOWN>
-__device__ __forceinline__ int add_bias(f32x16& s, float c2, const float* line, int far, int rel0, float left, float right, int lane) {
+__device__ __forceinline__ int add_bias(f32x16& s, float c2, const float* line, int far, int rel0, float left, float right, int lane,
+                                        float& mul, float& add) {
   int half = lane >> 5;
-  if (!line || rel0 + 31 <= -far || rel0 - 31 >= far) {
-    float cb = !line ? 0.f : (rel0 < 0 ? left : right);
+  int side = !line || rel0 + 31 <= -far || rel0 - 31 >= far ? (rel0 < 0 ? -1 : 1) : 0;
+  mul = 1.f;
+  add = 0.f;
+  if (side) {
+    float cb = !line ? 0.f : uniform(side < 0 ? left : right);
+    if (fabsf(cb) < kFoldable) {
+      mul = c2;
+      add = cb;
+    } else {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c2, cb);
-    return rel0 < 0 ? -1 : 1;
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c2, cb);
+    }
+    return side;
   }
   const float* b = line + (KEYS_DOWN ? rel0 - (lane & 31) + 4 * half : rel0 + (lane & 31) - 4 * half) + far + kPad;
 #pragma unroll

@@ -2110,9 +2110,10 @@ int set_buckets(bbmm_ctx* c, int64_t n_edges, const int32_t* edges, int32_t two_
   return BBMM_OK;
 }
 
-// Whether rows at p with these strides (elements) may be read or written `bytes` at a time.
+// Whether rows at p with these strides (elements) may be read or written `bytes` at a time, and 128 of them span less than 2^31 bytes (the
+// kernels' bounded reads).
 bool wide_rows(const void* p, const int64_t* stride, int64_t width, size_t elem, size_t bytes) {
-  bool ok = (uintptr_t)p % bytes == 0 && width * elem % bytes == 0;
+  bool ok = (uintptr_t)p % bytes == 0 && width * elem % bytes == 0 && (!stride || stride[1] < (int64_t)1 << 21);
   for (int k = 0; k < 3 && stride; ++k) ok = ok && stride[k] * elem % bytes == 0;
   return ok;
 }
@@ -2176,7 +2177,7 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
 // Offsets into the workspace, 256-byte steps.
 size_t step256(size_t n) { return (n + 255) / 256 * 256; }
 struct AttWork {
-  size_t pO, pl, delta, tsum, norms, bytes;
+  size_t pO, pl, delta, lo, hi, tsum, norms, bytes;
 };
 AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
   AttWork w{};
@@ -2192,7 +2193,9 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
   }
   w.norms = 0;
   w.delta = 256;
-  w.tsum = w.delta + step256(rows * sizeof(float));
+  w.lo = w.delta + step256(rows * sizeof(float));
+  w.hi = w.lo + step256(rows * sizeof(float));
+  w.tsum = w.hi + step256(rows * sizeof(float));
   w.bytes = w.tsum + (a.table ? step256((size_t)a.H * a.B * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float)) : 0);
   return w;
 }
@@ -2268,7 +2271,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   }
   g.ovec = wide_rows(O, nullptr, a.dv, e, 16), g.dovec = wide_rows(dO, g.dos, a.dv, e, 16);
   g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
-  g.delta = (float*)((char*)work + w.delta), g.tsum = (float*)((char*)work + w.tsum), g.norms = (unsigned*)((char*)work + w.norms);
+  g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (unsigned*)((char*)work + w.norms);
   hipStream_t s = c->stream;
   launch_attend_delta(s, in->type, a, g);
   if (rows) launch_attend_dq(s, in->type, a, g);

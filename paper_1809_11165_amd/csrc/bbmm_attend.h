@@ -47,7 +47,8 @@ struct AttGrad {
   int ovec, dovec, dqvec, dkvec, dvvec;
   const float* lse;
   void *dQ, *dK, *dV;            // dense
-  float* delta;                  // B x H x nq: do_i.o_i
+  // B x H x nq, left by launch_attend_delta: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
+  float *delta, *lo, *hi;
   float* tsum;                   // per workgroup of the dQ pass: sums of dS by bucket (H x (B ceil(nq / 128)) x buckets)
   unsigned* norms;               // fp16: bits of the largest |do_i| and |v_j|
 };

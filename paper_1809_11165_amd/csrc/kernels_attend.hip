@@ -21,7 +21,7 @@ __device__ __forceinline__ void drop_keys(f32x16& s, unsigned keep, int lane) {
   for (int r = 0; r < 16; ++r) s[r] = ((k >> (8 * (r >> 2) + (r & 3))) & 1) ? s[r] : -__builtin_inff();
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt, int total, int per_die) {
   typedef typename Frag<T>::type frag;
   constexpr int BK = sizeof(T) == 2 ? 64 : 32, NB = BK / 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
@@ -29,12 +29,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt,
   __shared__ float line[kLine];
   int id = die_order(blockIdx.x, per_die);
   if (id >= total) return;
-  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int qt = id % nqt, sp = (id / nqt) % o.nsplit, bh = id / nqt / o.nsplit;
   int h = bh % a.H, b = bh / a.H, hk = h / a.G;
   int q0 = qt * 128 + wave * 32, i = q0 + (lane & 31);
-  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
-  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  int qn = queries_of(a, b);
+  int kn = keys_of(a, b);
   if (qt * 128 >= qn) kn = 0;
   int tiles = (kn + BK - 1) / BK, per = (tiles + o.nsplit - 1) / o.nsplit;
   int t0 = min(sp * per, tiles), t1 = min(t0 + per, tiles);
@@ -55,18 +55,18 @@ __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt,
   }
   int64_t start = start_of(a, b);
 
-  Stage<T, DP, BK> sk, sv;
+  Stage<T, DP, BK, VEC> sk, sv;
   uint64_t keep = 0;
   uint8_t mb = 0;
   auto fetch = [&](int t) {
     int j0 = t * BK, left = kn - j0;
-    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, a.kvec, tid);
-    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, a.vvec, tid);
+    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, tid);
+    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, tid);
     if (mrow) mb = (lane < BK && lane < left) ? mrow[j0 + lane] : 0;
   };
   auto put = [&](int t) {
     keep = keep_bits(min(kn - t * BK, BK), mrow, mb);
-    sk.store(tile[t & 1][0], ~0ull, tid);
+    sk.store(tile[t & 1][0], ~0ull, tid);             // scores of masked keys are replaced
     sv.store(tile[t & 1][1], keep, tid);
   };
   f32x16 acc[ND];
@@ -77,28 +77,33 @@ __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt,
     fetch(t0);
     put(t0);
   }
+  settle();
   __syncthreads();
   float left = 0.f, right = 0.f;
   if (ln) {
     left = line[kPad];
     right = line[2 * a.bk.far + kPad];
   }
+  int rel = rest_below(-(int64_t)q0 - start);
   for (int t = t0; t < t1; ++t) {
     const char *tk = tile[t & 1][0], *tv = tile[t & 1][1];
     uint64_t kp = keep;
     if (t + 1 < t1) fetch(t + 1);
     if (kp) {
       f32x16 s[NB];
+      float mul[NB], add[NB];
       float top = -__builtin_inff();
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         s[n] = f32x16{};
 #pragma unroll
         for (int k = 0; k < NS; ++k) s[n] = Frag<T>::mma(row_frag<T, DP>(tk, 32 * n, k, lane), q[k], s[n]);
-        add_bias<true>(s[n], a.c2, ln, a.bk.far, clamp_rel((int64_t)t * BK + 32 * n - q0 - start), left, right, lane);
+        add_bias<true>(s[n], a.c2, ln, a.bk.far, rel + t * BK + 32 * n, left, right, lane, mul[n], add[n]);
         drop_keys(s[n], (unsigned)(kp >> (32 * n)), lane);
+        float big = -__builtin_inff();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, s[n][r]);
+        top = fmaxf(top, fmaf(big, mul[n], add[n]));
       }
       top = fmaxf(top, other_half(top));
       bool move = top > m + kSlack;
@@ -116,7 +121,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt,
       for (int n = 0; n < NB; ++n) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - ref);
+          s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], mul[n], add[n] - ref));
           l += s[n][r];
         }
 #pragma unroll
@@ -160,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt,
 }
 
 // Rows rho = 32 rb .. of shared head hk: query rho / G, head hk G + rho % G.
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttArgs a, AttOut o, int nrb) {
   typedef typename Frag<T>::type frag;
   constexpr int ND = DP / 32, NS = DP / 16, E = 16 / (int)sizeof(T), CH = DP / E, NV = 32 * CH / 64;
@@ -169,11 +174,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   __shared__ __align__(16) char buf[kLds && 4 * kVt > 8 * kPart ? 4 * kVt : 8 * kPart];
   __shared__ float wm[4][32], wl[4][32];
   extern __shared__ float dyn[];               // with a table: 32 rows of its entries, then the bucket of every difference (bytes)
-  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+  int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5, col = lane & 31;
   int x = blockIdx.x, rb = x % nrb, sp = (x / nrb) % o.nsplit, bh = x / nrb / o.nsplit, hk = bh % a.HK, b = bh / a.HK;
   int rows = a.nq * a.G, rho = rb * 32 + col, i = rho / a.G, h = hk * a.G + rho % a.G;
-  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
-  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  int qn = queries_of(a, b);
+  int kn = keys_of(a, b);
   bool mine = rho < rows && i < qn;
   int blocks = (kn + 31) / 32, per = (blocks + o.nsplit - 1) / o.nsplit;
   int t0 = min(sp * per, blocks), t1 = min(t0 + per, blocks);
@@ -187,22 +192,49 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   char* vt = buf + wave * kVt;
   u32x4 vr[kLds ? NV : 1];
   uint8_t mb = 0, mnext = 0;
+  // rows of a 32-key block from memory, with bounds
+  auto block = [&](const T* base, int64_t stride, int t, int width) {
+    unsigned rows = (unsigned)min(kn - t * 32, 32);
+    return bounded(base + (int64_t)t * 32 * stride, (rows - 1) * (unsigned)stride * (unsigned)sizeof(T) + (unsigned)width * (unsigned)sizeof(T));
+  };
   auto fetch_k = [&](int t) {
-    int j = t * 32 + col;
-    const T* row = K + (int64_t)j * a.ks[1];
+    if constexpr (VEC) {
+      __amdgpu_buffer_rsrc_t mem = block(K, a.ks[1], t, a.d);
+      unsigned at = (unsigned)col * (unsigned)a.ks[1] * (unsigned)sizeof(T);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) kf[s] = reg_frag<T>(row, j < kn, s, a.d, a.kvec, lane);
-    if (mrow) mnext = (lane < 32 && j < kn) ? mrow[j] : 0;
+      for (int s = 0; s < NS; ++s) {
+        int c = 16 * s + 8 * half;
+        if constexpr (sizeof(T) == 2) {
+          kf[s] = __builtin_bit_cast(frag, __builtin_amdgcn_raw_buffer_load_b128(mem, c < a.d ? at + 2 * c : kNowhere, 0, 0));
+        } else {
+          f32x4 lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(mem, c < a.d ? at + 4 * c : kNowhere, 0, 0));
+          f32x4 hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(mem, c + 4 < a.d ? at + 4 * c + 16 : kNowhere, 0, 0));
+          kf[s] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+      }
+    } else {
+      const T* row = K + (int64_t)(t * 32 + col) * a.ks[1];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kf[s] = reg_frag<T>(row, t * 32 + col < kn, s, a.d, 0, lane);
+    }
+    if (mrow) mnext = (lane < 32 && t * 32 + col < kn) ? mrow[t * 32 + col] : 0;
   };
   auto fetch_v = [&](int t) {
     if constexpr (kLds) {
-      int r = lane / CH, c = (lane % CH) * E, j = t * 32 + r;
-      const T* p = V + (int64_t)j * a.vs[1];
+      int r = lane / CH, c = (lane % CH) * E;
+      if constexpr (VEC) {
+        __amdgpu_buffer_rsrc_t mem = block(V, a.vs[1], t, a.dv);
+        unsigned pitch = (unsigned)a.vs[1] * 2, at = c < a.dv ? (unsigned)r * pitch + 2 * c : kNowhere;
 #pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        vr[n] = u32x4{0u, 0u, 0u, 0u};
-        if (j + n * (64 / CH) < kn) vr[n] = load16<T>(p, c, a.dv, a.vvec);
-        p += (int64_t)(64 / CH) * a.vs[1];
+        for (int n = 0; n < NV; ++n) vr[n] = __builtin_amdgcn_raw_buffer_load_b128(mem, at + (unsigned)(n * (64 / CH)) * pitch, 0, 0);
+      } else {
+        const T* p = V + (int64_t)(t * 32 + r) * a.vs[1];
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          vr[n] = u32x4{0u, 0u, 0u, 0u};
+          if (t * 32 + r + n * (64 / CH) < kn) vr[n] = load16<T>(p, c, a.dv, 0);
+          p += (int64_t)(64 / CH) * a.vs[1];
+        }
       }
     }
   };
@@ -234,6 +266,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
     left = tab[bline[0]];
     right = tab[bline[2 * (a.bk.far + kPad)]];
   }
+  int rel = rest_below(-(int64_t)i0 - start);
+  settle();
   for (; t < t1; t += 4) {
     mb = mnext;
     unsigned keep = (unsigned)keep_bits(min(kn - t * 32, 32), mrow, mb);
@@ -244,7 +278,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
         int row = r + n * (64 / CH);
         u32x4 v = vr[n];
         if (!((keep >> row) & 1)) v = u32x4{0u, 0u, 0u, 0u};
-        *(u32x4*)(vt + row * DP * 2 + ((c ^ swz(row)) << 4)) = v;
+        *(u32x4*)(vt + row * DP * 2 + ((c ^ swz<T, DP>(row)) << 4)) = v;
       }
     }
     f32x16 s = f32x16{};
@@ -254,7 +288,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
       fetch_k(t + 4);
       fetch_v(t + 4);
     }
-    int rel0 = clamp_rel((int64_t)t * 32 - i0 - start);     // of the first key and the first query
+    int rel0 = rel + t * 32;                   // of the first key and the first query
     if (!a.table || rel0 + 31 <= -a.bk.far || rel0 - 31 >= a.bk.far) {
       float cb = rel0 < 0 ? left : right;
 #pragma unroll
@@ -400,18 +434,28 @@ __global__ __launch_bounds__(256) void k_attend_join(AttArgs a, AttOut o) {
   store4<T>(out, c, a.dv, o.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
+template <typename T, bool VEC>
+void attend_v(hipStream_t s, const AttArgs& a, const AttOut& o) {
+  int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt * o.nsplit, per = (total + 7) / 8;
+  if (a.d <= 64 && a.dv <= 64) k_attend<T, 64, VEC><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
+  else k_attend<T, 128, VEC><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
+}
+template <typename T, bool VEC>
+void attend_few_v(hipStream_t s, const AttArgs& a, const AttOut& o) {
+  int nrb = (int)(((int64_t)a.nq * a.G + 31) / 32), total = a.B * a.HK * nrb * o.nsplit;
+  size_t lds = a.table ? 32 * sizeof(float) * (a.bk.buckets | 1) + 2 * (a.bk.far + kPad) + 1 : 0;
+  if (a.d <= 64 && a.dv <= 64) k_attend_few<T, 64, VEC><<<total, 256, lds, s>>>(a, o, nrb);
+  else k_attend_few<T, 128, VEC><<<total, 256, lds, s>>>(a, o, nrb);
+}
 template <typename T>
 void attend_t(hipStream_t s, const AttArgs& a, const AttOut& o) {
-  int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt * o.nsplit, per = (total + 7) / 8;
-  if (a.d <= 64 && a.dv <= 64) k_attend<T, 64><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
-  else k_attend<T, 128><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
+  if (a.kvec && a.vvec) attend_v<T, true>(s, a, o);
+  else attend_v<T, false>(s, a, o);
 }
 template <typename T>
 void attend_few_t(hipStream_t s, const AttArgs& a, const AttOut& o) {
-  int nrb = (int)(((int64_t)a.nq * a.G + 31) / 32), total = a.B * a.HK * nrb * o.nsplit;
-  size_t lds = a.table ? 32 * sizeof(float) * (a.bk.buckets | 1) + 2 * (a.bk.far + kPad) + 1 : 0;
-  if (a.d <= 64 && a.dv <= 64) k_attend_few<T, 64><<<total, 256, lds, s>>>(a, o, nrb);
-  else k_attend_few<T, 128><<<total, 256, lds, s>>>(a, o, nrb);
+  if (a.kvec && a.vvec) attend_few_v<T, true>(s, a, o);
+  else attend_few_v<T, false>(s, a, o);
 }
 
 }  // namespace

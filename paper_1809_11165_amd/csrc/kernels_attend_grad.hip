@@ -33,7 +33,38 @@ __global__ void k_zero_norms(unsigned* n) {
   if (threadIdx.x < 2) n[threadIdx.x] = 0;
 }
 
-// 16 lanes per row (b, i, h): delta, and the largest |do_i| (finite ones) for fp16.
+// Beyond this, fp32 holds lse too coarsely to recover weights from it (a row of nothing but masks of -1e9 or of the type's lowest value).
+constexpr float kCoarse = 65536.f;
+
+// Largest score and log2 of the sum relative to it, from the row itself: 16 lanes, a key at a time.  Only for rows beyond kCoarse.
+template <typename T>
+__device__ void row_sums(const AttArgs& a, int b, int h, int i, int lane, float& hi, float& lo) {
+  const T* q = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
+  const T* K = (const T*)a.K + b * a.ks[0] + h / a.G * a.ks[2];
+  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  const int64_t lim = (int64_t)1 << 40;
+  int64_t start = a.q_start ? min(max(a.q_start[b], -lim), lim) : 0;
+  float m = -__builtin_inff(), l = 0.f;
+  for (int j = 0; j < kn; ++j) {
+    if (a.mask && !a.mask[b * a.mask_s + j]) continue;
+    float s = 0.f;
+    for (int c = lane; c < a.d; c += 16) s = fmaf((float)q[c], (float)K[(int64_t)j * a.ks[1] + c], s);
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) s += __shfl_xor(s, x, 16);
+    float bias = a.table ? bias2<T>(((const T*)a.table)[(size_t)h * a.bk.buckets + bucket_of(a.bk, clamp_rel((int64_t)j - i - start))]) : 0.f;
+    s = fmaf(s, a.c2, bias);
+    if (s > m) {
+      l = l * __builtin_amdgcn_exp2f(m - s) + 1.f;
+      m = s;
+    } else if (s != -__builtin_inff()) {
+      l += __builtin_amdgcn_exp2f(s - m);
+    }
+  }
+  hi = m;
+  lo = __builtin_amdgcn_logf(l);
+}
+
+// 16 lanes per row (b, i, h): delta, hi and lo, and the largest |do_i| (finite ones) for fp16.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_delta(AttArgs a, AttGrad g) {
   constexpr int E = 16 / (int)sizeof(T);
@@ -43,8 +74,9 @@ __global__ __launch_bounds__(256) void k_attend_delta(AttArgs a, AttGrad g) {
   int h = (int)(row % a.H), i = (int)(row / a.H % a.nq), b = (int)(row / a.H / a.nq);
   int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
   size_t at = ((size_t)b * a.H + h) * a.nq + i;
-  float s = 0.f, q = 0.f;
-  if (i < qn && g.lse[at] != -__builtin_inff()) {
+  float s = 0.f, q = 0.f, hi = 0.f, lo = __builtin_inff();
+  float lse = i < qn ? g.lse[at] : -__builtin_inff();
+  if (lse != -__builtin_inff()) {
     const T* o = (const T*)g.O + row * a.dv;
     const T* d = (const T*)g.dO + b * g.dos[0] + (int64_t)i * g.dos[1] + h * g.dos[2];
     for (int c = lane * E; c < a.dv; c += 16 * E) {
@@ -56,14 +88,18 @@ __global__ __launch_bounds__(256) void k_attend_delta(AttArgs a, AttGrad g) {
         q = fmaf(v, v, q);
       }
     }
+    lo = lse * kLog2e;
+    if (fabsf(lse) > kCoarse && fabsf(lse) < __builtin_inff()) row_sums<T>(a, b, h, i, lane, hi, lo);
   }
 #pragma unroll
   for (int x = 1; x < 16; x *= 2) {
-    s += __shfl_xor(s, x, 64);
-    q += __shfl_xor(q, x, 64);
+    s += __shfl_xor(s, x, 16);
+    q += __shfl_xor(q, x, 16);
   }
   if (lane == 0) {
     g.delta[at] = s;
+    g.lo[at] = lo;
+    g.hi[at] = hi;
     if (__is_same(T, _Float16) && q < __builtin_inff()) atomicMax(&g.norms[0], __float_as_uint(sqrtf(q)));   // a maximum: any order
   }
 }
@@ -88,7 +124,7 @@ __global__ __launch_bounds__(256) void k_attend_vnorm(AttArgs a, AttGrad g) {
   if (lane == 0 && q < __builtin_inff()) atomicMax(&g.norms[1], __float_as_uint(sqrtf(q)));
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttArgs a, AttGrad g, int nqt, int total, int per_die) {
   typedef typename Frag<T>::type frag;
   constexpr int BK = sizeof(T) == 2 ? 64 : 32, NB = BK / 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
@@ -96,11 +132,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
   extern __shared__ float dyn[];               // with a table: bias line, then eight lines of diagonal sums (wave, half)
   int id = die_order(blockIdx.x, per_die);
   if (id >= total) return;
-  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int qt = id % nqt, bh = id / nqt, h = bh % a.H, b = bh / a.H, hk = h / a.G;
   int q0 = qt * 128 + wave * 32, i = q0 + (lane & 31);
-  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
-  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  int qn = queries_of(a, b);
+  int kn = keys_of(a, b);
   if (qt * 128 >= qn) kn = 0;
   int tiles = (kn + BK - 1) / BK;
   int far = a.bk.far, span = far + kPad, nline = 2 * span + 1;
@@ -111,9 +147,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
   const T* V = (const T*)a.V + b * a.vs[0] + hk * a.vs[2];
   const uint8_t* mrow = a.mask ? a.mask + b * a.mask_s : nullptr;
   size_t row = ((size_t)b * a.H + h) * a.nq + i;
-  float lse = i < qn ? g.lse[row] : -__builtin_inff(), delta = i < qn ? g.delta[row] : 0.f;
-  bool some = lse != -__builtin_inff();
-  float lse2 = some ? lse * kLog2e : __builtin_inff();      // nothing left in the row: weights zero
+  float lo = __builtin_inff(), hi = 0.f, delta = 0.f;        // nothing left in the row: weights zero
+  if (i < qn) lo = g.lo[row], hi = g.hi[row], delta = g.delta[row];
+  bool some = lo != __builtin_inff(), coarse = __any(hi != 0.f);
   frag q[NS], dof[NS];
   {
     const T* qr = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
@@ -133,13 +169,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
   int64_t start = start_of(a, b);
   float cs = ds_scale<T>(g);
 
-  Stage<T, DP, BK> sk, sv;
+  Stage<T, DP, BK, VEC> sk, sv;
   uint64_t keep = 0;
   uint8_t mb = 0;
   auto fetch = [&](int t) {
     int j0 = t * BK, left = kn - j0;
-    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, a.kvec, tid);
-    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, a.vvec, tid);
+    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, tid);
+    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, tid);
     if (mrow) mb = (lane < BK && lane < left) ? mrow[j0 + lane] : 0;
   };
   auto put = [&](int t) {
@@ -155,12 +191,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
     fetch(0);
     put(0);
   }
+  settle();
   __syncthreads();
   float left = 0.f, right = 0.f;
   if (ln) {
     left = line[kPad];
     right = line[2 * far + kPad];
   }
+  int rel = rest_below(-(int64_t)q0 - start);
   for (int t = 0; t < tiles; ++t) {
     const char *tk = tile[t & 1][0], *tv = tile[t & 1][1];
     uint64_t kp = keep;
@@ -173,11 +211,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
         for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tk, 32 * n, k, lane), q[k], s);
 #pragma unroll
         for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tv, 32 * n, k, lane), dof[k], dp);
-        int rel0 = clamp_rel((int64_t)t * BK + 32 * n - q0 - start);
-        int where = add_bias<true>(s, a.c2, ln, far, rel0, left, right, lane);
+        int rel0 = rel + t * BK + 32 * n;
+        float mul, add;
+        int where = add_bias<true>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
+        if (coarse && mul == 1.f) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] -= hi;
+        } else {
+          add -= hi;
+        }
+        add -= lo;
         unsigned kb = (unsigned)(kp >> (32 * n));
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] - lse2) * (dp[r] - delta);
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (dp[r] - delta);
         if (kb != 0xffffffffu) {
           unsigned k = kb >> (4 * half);
 #pragma unroll
@@ -241,20 +287,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
   }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt, int total, int per_die) {
   typedef typename Frag<T>::type frag;
   constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NB = BQ / 32, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
   __shared__ __align__(16) char tile[2][2][kTile];
-  __shared__ __align__(16) float stat[2][2][BQ];      // lse (base 2), delta
+  __shared__ __align__(16) float stat[2][3][BQ];      // lo, delta, hi
   extern __shared__ float dyn[];                      // with a table: bias line
   int id = die_order(blockIdx.x, per_die);
   if (id >= total) return;
-  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int kt = id % nkt, bh = id / nkt, hk = bh % a.HK, b = bh / a.HK;
   int k0 = kt * 128 + wave * 32, j = k0 + (lane & 31);
-  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
-  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
+  int qn = queries_of(a, b);
+  int kn = keys_of(a, b);
   if (kt * 128 >= kn) qn = 0;
   int tiles = (qn + BQ - 1) / BQ, steps = tiles * a.G;
   int far = a.bk.far;
@@ -273,35 +319,40 @@ __global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int
   int64_t start = start_of(a, b);
   float cs = ds_scale<T>(g);
 
-  Stage<T, DP, BQ> sq, sd;
-  float lse = 0.f, delta = 0.f;              // of row `lane` of the tile
+  Stage<T, DP, BQ, VEC> sq, sd;
+  float lo = 0.f, delta = 0.f, hi = 0.f;     // of row `lane` of the tile
+  bool coarse = false;
   auto fetch = [&](int t) {
     int h = hk * a.G + t / tiles, i0 = t % tiles * BQ, rows = qn - i0;
-    sq.load((const T*)a.Q + b * a.qs[0] + (int64_t)i0 * a.qs[1] + h * a.qs[2], a.qs[1], rows, a.d, a.qvec, tid);
-    sd.load((const T*)g.dO + b * g.dos[0] + (int64_t)i0 * g.dos[1] + h * g.dos[2], g.dos[1], rows, a.dv, g.dovec, tid);
+    sq.load((const T*)a.Q + b * a.qs[0] + (int64_t)i0 * a.qs[1] + h * a.qs[2], a.qs[1], rows, a.d, tid);
+    sd.load((const T*)g.dO + b * g.dos[0] + (int64_t)i0 * g.dos[1] + h * g.dos[2], g.dos[1], rows, a.dv, tid);
     size_t row = ((size_t)b * a.H + h) * a.nq + i0 + lane;
     bool have = lane < BQ && lane < rows;
-    lse = have ? g.lse[row] : -__builtin_inff();
+    lo = have ? g.lo[row] : __builtin_inff();
     delta = have ? g.delta[row] : 0.f;
+    hi = have ? g.hi[row] : 0.f;
   };
   auto put = [&](int t) {
-    bool some = lse != -__builtin_inff();
-    uint64_t keep = __ballot(some);
+    uint64_t keep = __ballot(lo != __builtin_inff());
+    coarse = __any(hi != 0.f);
     sq.store(tile[t & 1][0], keep, tid);
     sd.store(tile[t & 1][1], keep, tid);
     if (tid < BQ) {
-      stat[t & 1][0][tid] = some ? lse * kLog2e : __builtin_inff();   // nothing left in the row: weights zero
+      stat[t & 1][0][tid] = lo;                // infinite where nothing is left in the row: weights zero
       stat[t & 1][1][tid] = delta;
+      stat[t & 1][2][tid] = hi;
     }
   };
   f32x16 dk[ND], dv[ND];
 #pragma unroll
   for (int n = 0; n < ND; ++n) dk[n] = dv[n] = f32x16{};
   float left = 0.f, right = 0.f;
+  int rel = rest_above((int64_t)k0 - start);
   if (steps) {
     fetch(0);
     put(0);
   }
+  settle();
   for (int t = 0; t < steps; ++t) {
     if (ln && t % tiles == 0) {              // another head: its bias line (nobody reads the old one any more)
       fill_line<T>(dyn, a, hk * a.G + t / tiles, tid, 256);
@@ -312,6 +363,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int
       __syncthreads();
     }
     const char *tq = tile[t & 1][0], *td = tile[t & 1][1];
+    bool wide = coarse;
     if (t + 1 < steps) fetch(t + 1);
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -320,13 +372,25 @@ __global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int
       for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tq, 32 * n, k, lane), kf[k], s);
 #pragma unroll
       for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(td, 32 * n, k, lane), vf[k], dp);
-      add_bias<false>(s, a.c2, ln, far, clamp_rel((int64_t)k0 - (t % tiles * BQ + 32 * n) - start), left, right, lane);
+      float mul, add;
+      add_bias<false>(s, a.c2, ln, far, rel - (t % tiles * BQ + 32 * n), left, right, lane, mul, add);
+      if (wide) {
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          f32x4 h4 = *(const f32x4*)&stat[t & 1][2][32 * n + 8 * r4 + 4 * half];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * r4 + e] = fmaf(s[4 * r4 + e], mul, add - h4[e]);
+        }
+        mul = 1.f;
+        add = 0.f;
+      }
+      add += PLift<T>::value;
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         f32x4 l4 = *(const f32x4*)&stat[t & 1][0][32 * n + 8 * r4 + 4 * half], d4 = *(const f32x4*)&stat[t & 1][1][32 * n + 8 * r4 + 4 * half];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float p = __builtin_amdgcn_exp2f(s[4 * r4 + e] - (l4[e] - PLift<T>::value));
+          float p = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + e], mul, add - l4[e]));
           s[4 * r4 + e] = p;
           dp[4 * r4 + e] = p * (dp[4 * r4 + e] - d4[e]);
           if (PLift<T>::value != 0.f) dp[4 * r4 + e] *= cs * (1.f / (float)(1 << (int)PLift<T>::value));
@@ -373,19 +437,29 @@ void delta_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   }
   if (n) k_attend_delta<T><<<(unsigned)((n + 15) / 16), 256, 0, s>>>(a, g);
 }
-template <typename T>
-void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
+template <typename T, bool VEC>
+void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt, per = (total + 7) / 8;
   size_t lds = a.table ? sizeof(float) * 9 * (2 * (a.bk.far + kPad) + 1) : 0;
-  if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64><<<8 * per, 256, lds, s>>>(a, g, nqt, total, per);
-  else k_attend_dq<T, 128><<<8 * per, 256, lds, s>>>(a, g, nqt, total, per);
+  if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64, VEC><<<8 * per, 256, lds, s>>>(a, g, nqt, total, per);
+  else k_attend_dq<T, 128, VEC><<<8 * per, 256, lds, s>>>(a, g, nqt, total, per);
+}
+template <typename T, bool VEC>
+void dkv_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
+  int nkt = (a.nk + 127) / 128, total = a.B * a.HK * nkt, per = (total + 7) / 8;
+  size_t lds = a.table ? sizeof(float) * (2 * (a.bk.far + kPad) + 1) : 0;
+  if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<8 * per, 256, lds, s>>>(a, g, nkt, total, per);
+  else k_attend_dkv<T, 128, VEC><<<8 * per, 256, lds, s>>>(a, g, nkt, total, per);
+}
+template <typename T>
+void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
+  if (a.kvec && a.vvec) dq_v<T, true>(s, a, g);
+  else dq_v<T, false>(s, a, g);
 }
 template <typename T>
 void dkv_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  int nkt = (a.nk + 127) / 128, total = a.B * a.HK * nkt, per = (total + 7) / 8;
-  size_t lds = a.table ? sizeof(float) * (2 * (a.bk.far + kPad) + 1) : 0;
-  if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64><<<8 * per, 256, lds, s>>>(a, g, nkt, total, per);
-  else k_attend_dkv<T, 128><<<8 * per, 256, lds, s>>>(a, g, nkt, total, per);
+  if (a.qvec && g.dovec) dkv_v<T, true>(s, a, g);
+  else dkv_v<T, false>(s, a, g);
 }
 
 }  // namespace

@@ -158,6 +158,30 @@ def test_tables_of_minus_infinity_and_of_the_lowest_value(ctx, kind, nq):
     _check(O[:, :, :1], {"o": val["o"][:, :, :1]}, {"o": err["o"][:, :, :1]}, "o")
 
 
+@pytest.mark.parametrize("kind,value", [("f32", -3.4028234663852886e38), ("f32", -1e9), ("bf16", -3.3895313892515355e38), ("bf16", -1e9), ("f32", 1e9)])
+@pytest.mark.parametrize("nq", [4, 70])
+@pytest.mark.parametrize("edges", [EDGES, [1]])
+def test_gradients_of_rows_that_a_huge_bias_flattens(ctx, kind, value, nq, edges):
+    """A bias that rounds every score away leaves equal weights: o and dv are means, dS = (dP - delta) / n, and none of it recoverable from an
+    fp32 lse.  Scores are kept below the rounding of 1e9 (64), so that they vanish in it."""
+    rng = np.random.default_rng(17)
+    att, dO = _case(rng, kind, 2, 2, 1, nq, 200, 32, 32, edges=edges, k_len=[200, 131])
+    att.table[:] = value
+    flat = type(att)(att.Q, att.K, att.V, scale=1e-30, k_len=att.k_len)
+    val, err = _oracle(kind, flat, dO)                     # weights 1 / n; dq and dk carry the scale
+    O, lse = ctx.bbmm_attend(att)
+    _check(O, val, err, "o")
+    dQ, dK, dV, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    _check(dV, val, err, "dv")
+    factor = 32 ** -0.5 / 1e-30
+    tiny = {"dq": 0.0, "dk": 0.0}
+    for name, x in (("dq", dQ), ("dk", dK)):
+        _check(x, {name: val[name] * factor}, {name: err[name] * factor + tiny[name]}, name)
+    with_table = A.attend(kind, _host(att.Q), _host(att.K), _host(att.V), 1e-30, dO=_host(dO), k_len=_host(att.k_len),
+                          table=np.zeros(tuple(att.table.shape)), edges=edges)
+    _check(dT, with_table[0], with_table[1], "dtable")
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("nq", [4, 70])
 def test_a_causal_table_has_gradients(ctx, kind, nq):
