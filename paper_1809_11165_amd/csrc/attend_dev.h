@@ -106,8 +106,9 @@ __device__ __forceinline__ typename Frag<T>::type col_frag(const char* tile, int
 }
 
 // Memory from `base` on with hardware bounds: reads at or behind `bytes` give zero.
+// (The bound has to be in a scalar register: a lane's bound would be taken one lane after the other.)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t bounded(const void* base, unsigned bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
 constexpr unsigned kNowhere = 0x80000000u;   // an offset behind every bound (bounds are below 2^31: wide operands only)
 
