@@ -23,6 +23,8 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr int kPad = 64;                                  // the bias line goes this far beyond the last edge
 constexpr int kLine = 2 * (BBMM_ATT_FAR + kPad) + 1;
 
+template <int V> struct Const { static constexpr int value = V; };
+
 template <typename T> struct Frag;
 template <> struct Frag<__bf16> {
   typedef bf16x8 type;
@@ -136,9 +138,9 @@ struct Stage {
   __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int width, int tid) {
     int r = tid / CH, c = (tid % CH) * E;
     if constexpr (VEC) {
-      unsigned pitch = (unsigned)stride * (unsigned)sizeof(T);
-      unsigned n = (unsigned)(max(min(rows, ROWS), 1) - 1) * pitch + (unsigned)width * (unsigned)sizeof(T);
-      __amdgpu_buffer_rsrc_t mem = bounded(base, rows > 0 ? n : 0u);
+      unsigned pitch = (unsigned)stride * (unsigned)sizeof(T), last = (unsigned)width * (unsigned)sizeof(T);
+      unsigned n = rows >= ROWS ? (unsigned)(ROWS - 1) * pitch + last : rows > 0 ? (unsigned)(rows - 1) * pitch + last : 0u;
+      __amdgpu_buffer_rsrc_t mem = bounded(base, n);
       unsigned at = c < width ? (unsigned)r * pitch + (unsigned)c * (unsigned)sizeof(T) : kNowhere;
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(mem, at + (unsigned)(i * RP) * pitch, 0, 0);
@@ -354,9 +356,14 @@ __device__ __forceinline__ void store4(T* row, int c, int width, int vec, float 
   }
 }
 
-// the other half of a wave's 32 columns
-__device__ __forceinline__ float other_half(float x) {
-  return __shfl_xor(x, 32, 64);
+// A column's two halves of a wave: maximum and sum.
+__device__ __forceinline__ float both_max(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
+  return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
+  return __int_as_float(r[0]) + __int_as_float(r[1]);
 }
 
 // keys of a tile that take part: bit i = key j0 + i, i < 64

@@ -3,8 +3,8 @@
 //
 // k_attend: a workgroup of four waves takes 128 queries of one head, 32 per wave.  Transposed scores S^T = K Q^T put a query in
 // a lane, so that maximum, sum, bias offset and rescaling are per-lane scalars and the weights are, as they stand, the
-// second operand of O^T += V^T P^T (see attend_dev.h).  K and V tiles go through LDS, two buffers, the next tile's loads in flight
-// during a tile's products.
+// second operand of O^T += V^T P^T (see attend_dev.h).  K and V tiles of 32 keys go through LDS, two buffers each.  In the turn of a tile its
+// softmax runs on the vector unit while the matrix unit forms the scores of the tile after and adds up the values of the tile before.
 // k_attend_few: up to 32 rows (query, head of the group) of one shared head; the waves split the keys instead, read K straight
 // into registers and V through LDS of their own, and join at the end.  Bound by reading K and V once.
 // Both may split the key axis over workgroups; k_attend_join then weighs the parts.
@@ -14,19 +14,29 @@ using namespace att;
 
 namespace {
 
-__device__ __forceinline__ void drop_keys(f32x16& s, unsigned keep, int lane) {
+// Scores of excluded keys at -infinity, whatever they were.  `limit`: 32 floats in LDS of this wave alone, infinity or -infinity per key; the
+// minimum with it costs one instruction per score (testing bits costs three) and turns NaN into the limit.
+__device__ __forceinline__ void drop_keys(f32x16& s, unsigned keep, float* limit, int lane) {
   if (keep == 0xffffffffu) return;
-  unsigned k = keep >> (4 * (lane >> 5));
+  if (lane < 32) limit[lane] = ((keep >> lane) & 1) ? __builtin_inff() : -__builtin_inff();
+  __builtin_amdgcn_wave_barrier();
+  const float* l = limit + 4 * (lane >> 5);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = ((k >> (8 * (r >> 2) + (r & 3))) & 1) ? s[r] : -__builtin_inff();
+  for (int g = 0; g < 4; ++g) {
+    f32x4 x = *(const f32x4*)(l + 8 * g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) asm("v_min_f32 %0, %0, %1" : "+v"(s[4 * g + e]) : "v"(x[e]));   // fminf would first quiet both
+  }
+  __builtin_amdgcn_wave_barrier();
 }
 
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt, int total, int per_die) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attend(AttArgs a, AttOut o, int nqt, int total, int per_die) {
   typedef typename Frag<T>::type frag;
-  constexpr int BK = sizeof(T) == 2 ? 64 : 32, NB = BK / 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
-  __shared__ __align__(16) char tile[2][2][kTile];
+  constexpr int BK = 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
+  __shared__ __align__(16) char tk[2][kTile], tv[2][kTile];
   __shared__ float line[kLine];
+  __shared__ __align__(16) float limit[4][32];
   int id = die_order(blockIdx.x, per_die);
   if (id >= total) return;
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
@@ -42,100 +52,147 @@ __global__ __launch_bounds__(256, 2) void k_attend(AttArgs a, AttOut o, int nqt,
   const T* K = (const T*)a.K + b * a.ks[0] + hk * a.ks[2];
   const T* V = (const T*)a.V + b * a.vs[0] + hk * a.vs[2];
   const uint8_t* mrow = a.mask ? a.mask + b * a.mask_s : nullptr;
-  frag q[NS];
-  {
-    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) q[s] = reg_frag<T>(row, i < qn, s, a.d, a.qvec, lane);
-  }
-  const float* ln = nullptr;
-  if (a.table && t0 < t1) {
-    fill_line<T>(line, a, h, tid, 256);
-    ln = line;
-  }
   int64_t start = start_of(a, b);
+  int far = a.bk.far, rel = rest_below(-(int64_t)q0 - start);   // + 32 t: difference of the tile's first key and the wave's first query
 
   Stage<T, DP, BK, VEC> sk, sv;
-  uint64_t keep = 0;
   uint8_t mb = 0;
-  auto fetch = [&](int t) {
-    int j0 = t * BK, left = kn - j0;
-    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, tid);
-    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, tid);
-    if (mrow) mb = (lane < BK && lane < left) ? mrow[j0 + lane] : 0;
+  auto fetch_mask = [&](int t) {
+    if (mrow) mb = (lane < BK && t * BK + lane < kn) ? mrow[t * BK + lane] : 0;
   };
-  auto put = [&](int t) {
-    keep = keep_bits(min(kn - t * BK, BK), mrow, mb);
-    sk.store(tile[t & 1][0], ~0ull, tid);             // scores of masked keys are replaced
-    sv.store(tile[t & 1][1], keep, tid);
-  };
-  f32x16 acc[ND];
+  frag q[NS], p[2];
+  f32x16 acc[ND], s = f32x16{};
 #pragma unroll
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[u][e] = (T)0.f;
   float m = -__builtin_inff(), l = 0.f;     // reference and sum (this lane's half of the keys)
-  if (t0 < t1) {
-    fetch(t0);
-    put(t0);
-  }
-  settle();
-  __syncthreads();
   float left = 0.f, right = 0.f;
-  if (ln) {
-    left = line[kPad];
-    right = line[2 * a.bk.far + kPad];
+  const T* kp = K + (int64_t)t0 * BK * a.ks[1];
+  const T* vp = V + (int64_t)t0 * BK * a.vs[1];
+  int64_t kstep = BK * a.ks[1], vstep = BK * a.vs[1];
+  const float* ln = nullptr;
+  if (t0 < t1) {
+    sk.load(kp, a.ks[1], kn - t0 * BK, a.d, tid);
+    sk.store(tk[t0 & 1], ~0ull, tid);
+    kp += kstep;
+    sk.load(kp, a.ks[1], kn - (t0 + 1) * BK, a.d, tid);
+    kp += kstep;
+    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) q[k] = reg_frag<T>(row, i < qn, k, a.d, a.qvec, lane);
+    sk.store(tk[(t0 + 1) & 1], ~0ull, tid);
+    fetch_mask(t0);
+    sv.store(tv[(t0 + 1) & 1], 0, tid);      // the weights of the turn before the first are zero, and so must be what they weigh
+    if (a.table) {
+      fill_line<T>(line, a, h, tid, 256);
+      ln = line;
+    }
+    settle();
+    __syncthreads();
+    if (ln) {
+      left = uniform(line[kPad]);
+      right = uniform(line[2 * far + kPad]);
+    }
+#pragma unroll
+    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tk[t0 & 1], 0, k, lane), q[k], s);
+    __syncthreads();
   }
-  int rel = rest_below(-(int64_t)q0 - start);
+  // A turn per tile.  On entry s holds its scores' products, p the weights of the tile before; LDS holds the keys of the tile after and the
+  // values of the tile before.  Tiles up to `end` are of one kind: plain ones lie beyond the last edge on one side (or have no bias) and all
+  // their keys take part; their scores are mul s + add as they stand.
+  int whole = mrow ? t0 : kn / BK, end = t0;
+  bool plain = false;
+  float side = 0.f;
   for (int t = t0; t < t1; ++t) {
-    const char *tk = tile[t & 1][0], *tv = tile[t & 1][1];
-    uint64_t kp = keep;
-    if (t + 1 < t1) fetch(t + 1);
-    if (kp) {
-      f32x16 s[NB];
-      float mul[NB], add[NB];
-      float top = -__builtin_inff();
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        s[n] = f32x16{};
-#pragma unroll
-        for (int k = 0; k < NS; ++k) s[n] = Frag<T>::mma(row_frag<T, DP>(tk, 32 * n, k, lane), q[k], s[n]);
-        add_bias<true>(s[n], a.c2, ln, a.bk.far, rel + t * BK + 32 * n, left, right, lane, mul[n], add[n]);
-        drop_keys(s[n], (unsigned)(kp >> (32 * n)), lane);
-        float big = -__builtin_inff();
-#pragma unroll
-        for (int r = 0; r < 16; ++r) big = fmaxf(big, s[n][r]);
-        top = fmaxf(top, fmaf(big, mul[n], add[n]));
-      }
-      top = fmaxf(top, other_half(top));
-      bool move = top > m + kSlack;
-      if (__any(move)) {
-        float up = move ? __builtin_amdgcn_exp2f(m - top) : 1.f;
-        m = move ? top : m;
-        l *= up;
-#pragma unroll
-        for (int n = 0; n < ND; ++n)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[n][r] *= up;
-      }
-      float ref = (m == -__builtin_inff() ? 0.f : m) - Lift<T>::value;
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], mul[n], add[n] - ref));
-          l += s[n][r];
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          frag p = pack8<T>(s[n], u);
-#pragma unroll
-          for (int c = 0; c < ND; ++c) acc[c] = Frag<T>::mma(col_frag<T, DP>(tv, 32 * n + 16 * u, 32 * c, lane), p, acc[c]);
+    if (t == end) {
+      int r = rel + t * BK;
+      end = t1;
+      plain = t < whole;
+      if (plain) {
+        end = min(t1, whole);
+        if (ln) {
+          side = r < 0 ? left : right;
+          plain = (r + 31 <= -far || r - 31 >= far) && fabsf(side) < kFoldable;
+          if (r + 31 <= -far) end = min(end, t + (-far - 31 - r) / BK + 1);
+          else if (r - 31 < far) end = min(end, t + (far + 30 - r) / BK + 1);
         }
       }
     }
-    if (t + 1 < t1) put(t + 1);
+    uint64_t keep = ~0ull;
+    float mul = a.c2, add = side;
+    sk.load(kp, a.ks[1], kn - (t + 2) * BK, a.d, tid);
+    sv.load(vp, a.vs[1], kn - t * BK, a.dv, tid);
+    kp += kstep;
+    vp += vstep;
+    if (!plain) {
+      keep = keep_bits(min(kn - t * BK, BK), mrow, mb);
+      fetch_mask(t + 1);
+      add_bias<true>(s, a.c2, ln, far, rel + t * BK, left, right, lane, mul, add);
+      drop_keys(s, (unsigned)keep, limit[wave], lane);
+    }
+    // Steps kept in this order: each reads the operand of the step after next, queues one product of the tile after (scores) or before (values),
+    // and does its share of this tile's softmax meanwhile.
+    f32x16 next = f32x16{};
+    const char *kt = tk[(t + 1) & 1], *vt = tv[(t + 1) & 1];
+    constexpr int M = NS + 2 * ND, E0 = M / 2 - M / 8;
+    auto operand = [&](int z) { return z < NS ? row_frag<T, DP>(kt, 0, z, lane) : col_frag<T, DP>(vt, 16 * ((z - NS) / ND), 32 * ((z - NS) % ND), lane); };
+    frag f[3], pn[2];
+    f[0] = operand(0);
+    f[1] = operand(1);
+    float big = -__builtin_inff(), up = 1.f, ref = 0.f, sum = 0.f;
+    bool move = false;
+#pragma unroll
+    for (int z = 0; z < M; ++z) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (z + 2 < M) f[(z + 2) % 3] = operand(z + 2);
+      if (z < NS) next = Frag<T>::mma(f[z % 3], q[z], next);
+      else acc[(z - NS) % ND] = Frag<T>::mma(f[z % 3], p[(z - NS) / ND], acc[(z - NS) % ND]);
+      if (z < E0) {
+#pragma unroll
+        for (int r = z * 16 / E0; r < (z + 1) * 16 / E0; ++r) big = fmaxf(big, s[r]);
+        if (z == E0 - 1) {
+          float top = both_max(fmaf(big, mul, add));
+          move = top > m + kSlack;
+          up = move ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+          m = move ? top : m;
+          ref = add - ((m == -__builtin_inff() ? 0.f : m) - Lift<T>::value);
+        }
+      } else {
+#pragma unroll
+        for (int r = (z - E0) * 16 / (M - E0); r < (z + 1 - E0) * 16 / (M - E0); ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, ref));
+          sum += s[r];
+          if (r == 7) pn[0] = pack8<T>(s, 0);
+          if (r == 15) pn[1] = pack8<T>(s, 1);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    p[0] = pn[0];
+    p[1] = pn[1];
+    asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(sum));   // the weights are wanted now, not at their use a turn later
+    l = fmaf(l, up, sum);
+    if (__any(move)) {
+#pragma unroll
+      for (int n = 0; n < ND; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[n][r] *= up;
+    }
+    s = next;
+    sk.store(tk[t & 1], ~0ull, tid);           // scores of masked keys are replaced
+    sv.store(tv[t & 1], keep, tid);
     __syncthreads();
   }
-  l += other_half(l);
+  if (t0 < t1) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int c = 0; c < ND; ++c) acc[c] = Frag<T>::mma(col_frag<T, DP>(tv[(t1 + 1) & 1], 16 * u, 32 * c, lane), p[u], acc[c]);
+  }
+  l = both_sum(l);
   bool some = l != 0.f && i < qn;           // NaN counts as something
   float inv = some ? 1.f / l : 0.f;
   float lse2 = some ? (m - Lift<T>::value) + __builtin_amdgcn_logf(l) : -__builtin_inff();
@@ -173,6 +230,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   constexpr int kVt = 32 * DP * 2, kPart = 32 * (DP + 4);
   __shared__ __align__(16) char buf[kLds && 4 * kVt > 8 * kPart ? 4 * kVt : 8 * kPart];
   __shared__ float wm[4][32], wl[4][32];
+  __shared__ __align__(16) float limit[4][32];
   extern __shared__ float dyn[];               // with a table: 32 rows of its entries, then the bucket of every difference (bytes)
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5, col = lane & 31;
   int x = blockIdx.x, rb = x % nrb, sp = (x / nrb) % o.nsplit, bh = x / nrb / o.nsplit, hk = bh % a.HK, b = bh / a.HK;
@@ -298,11 +356,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c2, tab[bl[8 * (r >> 2) + (r & 3)]]);
     }
-    drop_keys(s, keep, lane);
+    drop_keys(s, keep, limit[wave], lane);
     float top = -__builtin_inff();
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
-    top = fmaxf(top, other_half(top));
+    top = both_max(top);
     bool move = top > m + kSlack;
     if (__any(move)) {
       float up = move ? __builtin_amdgcn_exp2f(m - top) : 1.f;
@@ -340,7 +398,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
     if constexpr (kLds) __builtin_amdgcn_wave_barrier();
   }
   // join the four waves: each scales its sums to the largest reference; two leave theirs in LDS, the other two add them, all write
-  l += other_half(l);
+  l = both_sum(l);
   if (half == 0) {
     wm[wave][col] = m;
     wl[wave][col] = l;

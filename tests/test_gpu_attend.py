@@ -131,6 +131,18 @@ def test_rows_that_a_mask_empties_and_garbage_in_masked_places(ctx, kind, nq):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("nq", [2, 100])
+def test_signalling_nan_in_masked_places(ctx, kind, nq):
+    rng = np.random.default_rng(18)
+    att, dO = _case(rng, kind, 2, 2, 1, nq, 130, 64, 64, edges=EDGES, mask=0.7)
+    want = _oracle(kind, att, dO)
+    bits = {"f32": (torch.int32, 0x7f800001), "f16": (torch.int16, 0x7c01), "bf16": (torch.int16, 0x7f81)}[kind]
+    for x in (att.K, att.V):
+        x.view(bits[0])[~att.key_mask] = bits[1]
+    _run_and_check(ctx, kind, att, dO, want)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("nq", [4, 70])
 def test_tables_of_minus_infinity_and_of_the_lowest_value(ctx, kind, nq):
     """-infinity for everything ahead (a causal mask by the table), and buckets at the type's lowest value: weight zero beside any other
