@@ -380,8 +380,14 @@ constexpr float kSlack = 8.f;
 template <typename T> struct Lift { static constexpr float value = 0.f; };
 template <> struct Lift<_Float16> { static constexpr float value = 6.f; };
 
-// Workgroup id -> position such that the eight dies, to which consecutive ids go in turn, get runs of neighbouring positions
-// (workgroups that read the same keys share an L2).
-__device__ __forceinline__ int die_order(int id, int per_die) { return (id & 7) * per_die + (id >> 3); }
+// Workgroup id -> position such that the workgroups that read the same keys (a unit: `per` neighbouring positions) run on one die, to which every
+// eighth id goes, and share its L2.  Units are dealt out one by one where that comes out even, so that batches of unequal length fall on all
+// dies (4 x 16 heads of 1537 .. 961 keys: the dies' work differed by 1.6); else in runs of neighbouring positions.
+__device__ __forceinline__ int die_order(int id, int units, int per) {
+  int die = id & 7, r = id >> 3;
+  if ((units & 7) == 0) return (r / per * 8 + die) * per + r % per;
+  int at = die * ((units * per + 7) / 8) + r;
+  return r < (units * per + 7) / 8 ? at : units * per;
+}
 
 }  // namespace att

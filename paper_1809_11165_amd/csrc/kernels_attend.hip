@@ -31,16 +31,16 @@ __device__ __forceinline__ void drop_keys(f32x16& s, unsigned keep, float* limit
 }
 
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attend(AttArgs a, AttOut o, int nqt, int total, int per_die) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attend(AttArgs a, AttOut o, int nqt) {
   typedef typename Frag<T>::type frag;
   constexpr int BK = 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
   __shared__ __align__(16) char tk[2][kTile], tv[2][kTile];
+  __shared__ __align__(16) float from[2][32];   // what a key's scores start from: 0, or -infinity where it takes no part
   __shared__ float line[kLine];
-  __shared__ __align__(16) float limit[4][32];
-  int id = die_order(blockIdx.x, per_die);
-  if (id >= total) return;
+  int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt * o.nsplit);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int qt = id % nqt, sp = (id / nqt) % o.nsplit, bh = id / nqt / o.nsplit;
+  if (bh >= a.B * a.H) return;
   int h = bh % a.H, b = bh / a.H, hk = h / a.G;
   int q0 = qt * 128 + wave * 32, i = q0 + (lane & 31);
   int qn = queries_of(a, b);
@@ -55,13 +55,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
   int64_t start = start_of(a, b);
   int far = a.bk.far, rel = rest_below(-(int64_t)q0 - start);   // + 32 t: difference of the tile's first key and the wave's first query
 
-  Stage<T, DP, BK, VEC> sk, sv;
+  constexpr int NST = DP == 64 && sizeof(T) == 2 ? 2 : 1;   // sets of loads on their way
+  Stage<T, DP, BK, VEC> sk[NST], sv[NST];
   uint8_t mb = 0;
   auto fetch_mask = [&](int t) {
     if (mrow) mb = (lane < BK && t * BK + lane < kn) ? mrow[t * BK + lane] : 0;
   };
+  uint64_t k0 = 0, k1 = 0, k2 = 0;             // keys of this tile and the next two that take part
+  auto keys = [&](int t) { return keep_bits(min(max(kn - t * BK, 0), BK), mrow, mb); };
+  auto put_keys = [&](int par, uint64_t keep, const Stage<T, DP, BK, VEC>& st) {
+    st.store(tk[par], keep, tid);
+    if (tid < BK) from[par][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
+  };
+  auto scores_start = [&](int par) {
+    f32x16 c;
+    const float* x = from[par] + 4 * half;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f32x4 y = *(const f32x4*)(x + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[4 * g + e] = y[e];
+    }
+    return c;
+  };
   frag q[NS], p[2];
-  f32x16 acc[ND], s = f32x16{};
+  f32x16 acc[ND], sc[2];
+  sc[0] = sc[1] = f32x16{};
 #pragma unroll
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
 #pragma unroll
@@ -75,17 +94,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
   int64_t kstep = BK * a.ks[1], vstep = BK * a.vs[1];
   const float* ln = nullptr;
   if (t0 < t1) {
-    sk.load(kp, a.ks[1], kn - t0 * BK, a.d, tid);
-    sk.store(tk[t0 & 1], ~0ull, tid);
+    fetch_mask(t0);
+    sk[0].load(kp, a.ks[1], kn - t0 * BK, a.d, tid);
+    k0 = keys(t0);
+    put_keys(0, k0, sk[0]);
     kp += kstep;
-    sk.load(kp, a.ks[1], kn - (t0 + 1) * BK, a.d, tid);
+    fetch_mask(t0 + 1);
+    sk[0].load(kp, a.ks[1], kn - (t0 + 1) * BK, a.d, tid);
     kp += kstep;
     const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
 #pragma unroll
     for (int k = 0; k < NS; ++k) q[k] = reg_frag<T>(row, i < qn, k, a.d, a.qvec, lane);
-    sk.store(tk[(t0 + 1) & 1], ~0ull, tid);
-    fetch_mask(t0);
-    sv.store(tv[(t0 + 1) & 1], 0, tid);      // the weights of the turn before the first are zero, and so must be what they weigh
+    k1 = keys(t0 + 1);
+    put_keys(1, k1, sk[0]);
+    sv[0].store(tv[1], 0, tid);              // the weights of the turn before the first are zero, and so must be what they weigh
+    if (NST == 2) {
+      sk[0].load(kp, a.ks[1], kn - (t0 + 2) * BK, a.d, tid);
+      kp += kstep;
+      sv[0].load(vp, a.vs[1], kn - t0 * BK, a.dv, tid);
+      vp += vstep;
+    }
     if (a.table) {
       fill_line<T>(line, a, h, tid, 256);
       ln = line;
@@ -96,47 +124,40 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
       left = uniform(line[kPad]);
       right = uniform(line[2 * far + kPad]);
     }
+    sc[0] = scores_start(0);
 #pragma unroll
-    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tk[t0 & 1], 0, k, lane), q[k], s);
+    for (int k = 0; k < NS; ++k) sc[0] = Frag<T>::mma(row_frag<T, DP>(tk[0], 0, k, lane), q[k], sc[0]);
     __syncthreads();
   }
-  // A turn per tile.  On entry s holds its scores' products, p the weights of the tile before; LDS holds the keys of the tile after and the
-  // values of the tile before.  Tiles up to `end` are of one kind: plain ones lie beyond the last edge on one side (or have no bias) and all
-  // their keys take part; their scores are mul s + add as they stand.
-  int whole = mrow ? t0 : kn / BK, end = t0;
-  bool plain = false;
+  // A turn per tile.  On entry the scores' products of this tile are there, and p holds the weights of the tile before; LDS holds the keys of the
+  // tile after and the values of the tile before.  Tiles up to `end` are of one kind: plain ones lie beyond the last edge on one side (or have no
+  // bias); their scores are c2 s + side as they stand.
+  int end = ln ? t0 : t1;
+  bool plain = !ln;
   float side = 0.f;
-  for (int t = t0; t < t1; ++t) {
+  auto turn = [&](auto par_, int t) {
+    constexpr int PAR = decltype(par_)::value;
+    f32x16& s = sc[PAR];
+    f32x16& next = sc[PAR ^ 1];
     if (t == end) {
       int r = rel + t * BK;
       end = t1;
-      plain = t < whole;
-      if (plain) {
-        end = min(t1, whole);
-        if (ln) {
-          side = r < 0 ? left : right;
-          plain = (r + 31 <= -far || r - 31 >= far) && fabsf(side) < kFoldable;
-          if (r + 31 <= -far) end = min(end, t + (-far - 31 - r) / BK + 1);
-          else if (r - 31 < far) end = min(end, t + (far + 30 - r) / BK + 1);
-        }
-      }
+      side = r < 0 ? left : right;
+      plain = (r + 31 <= -far || r - 31 >= far) && fabsf(side) < kFoldable;
+      if (r + 31 <= -far) end = min(end, t + (-far - 31 - r) / BK + 1);
+      else if (r - 31 < far) end = min(end, t + (far + 30 - r) / BK + 1);
     }
-    uint64_t keep = ~0ull;
-    float mul = a.c2, add = side;
-    sk.load(kp, a.ks[1], kn - (t + 2) * BK, a.d, tid);
-    sv.load(vp, a.vs[1], kn - t * BK, a.dv, tid);
+    fetch_mask(t + 2);
+    sk[NST == 2 ? PAR ^ 1 : 0].load(kp, a.ks[1], kn - (t + NST + 1) * BK, a.d, tid);
+    sv[NST == 2 ? PAR ^ 1 : 0].load(vp, a.vs[1], kn - (t + NST - 1) * BK, a.dv, tid);
     kp += kstep;
     vp += vstep;
-    if (!plain) {
-      keep = keep_bits(min(kn - t * BK, BK), mrow, mb);
-      fetch_mask(t + 1);
-      add_bias<true>(s, a.c2, ln, far, rel + t * BK, left, right, lane, mul, add);
-      drop_keys(s, (unsigned)keep, limit[wave], lane);
-    }
+    float mul = a.c2, add = side;
+    if (!plain) add_bias<true>(s, a.c2, ln, far, rel + t * BK, left, right, lane, mul, add);
     // Steps kept in this order: each reads the operand of the step after next, queues one product of the tile after (scores) or before (values),
     // and does its share of this tile's softmax meanwhile.
-    f32x16 next = f32x16{};
-    const char *kt = tk[(t + 1) & 1], *vt = tv[(t + 1) & 1];
+    next = scores_start(PAR ^ 1);
+    const char *kt = tk[PAR ^ 1], *vt = tv[PAR ^ 1];
     constexpr int M = NS + 2 * ND, E0 = M / 2 - M / 8;
     auto operand = [&](int z) { return z < NS ? row_frag<T, DP>(kt, 0, z, lane) : col_frag<T, DP>(vt, 16 * ((z - NS) / ND), 32 * ((z - NS) % ND), lane); };
     frag f[3], pn[2];
@@ -181,16 +202,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[n][r] *= up;
     }
-    s = next;
-    sk.store(tk[t & 1], ~0ull, tid);           // scores of masked keys are replaced
-    sv.store(tv[t & 1], keep, tid);
+    k2 = keys(t + 2);
+    put_keys(PAR, k2, sk[NST == 2 ? PAR : 0]);
+    sv[NST == 2 ? PAR : 0].store(tv[PAR], k0, tid);
+    k0 = k1;
+    k1 = k2;
     __syncthreads();
+  };
+  for (int t = t0; t < t1; t += 2) {
+    turn(Const<0>{}, t);
+    if (t + 1 < t1) turn(Const<1>{}, t + 1);
   }
   if (t0 < t1) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int c = 0; c < ND; ++c) acc[c] = Frag<T>::mma(col_frag<T, DP>(tv[(t1 + 1) & 1], 16 * u, 32 * c, lane), p[u], acc[c]);
+      for (int c = 0; c < ND; ++c) acc[c] = Frag<T>::mma(col_frag<T, DP>(tv[(t1 - t0 + 1) & 1], 16 * u, 32 * c, lane), p[u], acc[c]);
   }
   l = both_sum(l);
   bool some = l != 0.f && i < qn;           // NaN counts as something
@@ -494,9 +521,9 @@ __global__ __launch_bounds__(256) void k_attend_join(AttArgs a, AttOut o) {
 
 template <typename T, bool VEC>
 void attend_v(hipStream_t s, const AttArgs& a, const AttOut& o) {
-  int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt * o.nsplit, per = (total + 7) / 8;
-  if (a.d <= 64 && a.dv <= 64) k_attend<T, 64, VEC><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
-  else k_attend<T, 128, VEC><<<8 * per, 256, 0, s>>>(a, o, nqt, total, per);
+  int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt * o.nsplit, grid = (total + 7) / 8 * 8;
+  if (a.d <= 64 && a.dv <= 64) k_attend<T, 64, VEC><<<grid, 256, 0, s>>>(a, o, nqt);
+  else k_attend<T, 128, VEC><<<grid, 256, 0, s>>>(a, o, nqt);
 }
 template <typename T, bool VEC>
 void attend_few_v(hipStream_t s, const AttArgs& a, const AttOut& o) {

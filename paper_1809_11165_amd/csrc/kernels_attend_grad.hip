@@ -125,15 +125,15 @@ __global__ __launch_bounds__(256) void k_attend_vnorm(AttArgs a, AttGrad g) {
 }
 
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttArgs a, AttGrad g, int nqt, int total, int per_die) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttArgs a, AttGrad g, int nqt) {
   typedef typename Frag<T>::type frag;
   constexpr int BK = sizeof(T) == 2 ? 64 : 32, NB = BK / 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
   __shared__ __align__(16) char tile[2][2][kTile];
   extern __shared__ float dyn[];               // with a table: bias line, then eight lines of diagonal sums (wave, half)
-  int id = die_order(blockIdx.x, per_die);
-  if (id >= total) return;
+  int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int qt = id % nqt, bh = id / nqt, h = bh % a.H, b = bh / a.H, hk = h / a.G;
+  if (b >= a.B) return;
   int q0 = qt * 128 + wave * 32, i = q0 + (lane & 31);
   int qn = queries_of(a, b);
   int kn = keys_of(a, b);
@@ -288,16 +288,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
 }
 
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt, int total, int per_die) {
+__global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt) {
   typedef typename Frag<T>::type frag;
   constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NB = BQ / 32, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
   __shared__ __align__(16) char tile[2][2][kTile];
   __shared__ __align__(16) float stat[2][3][BQ];      // lo, delta, hi
   extern __shared__ float dyn[];                      // with a table: bias line
-  int id = die_order(blockIdx.x, per_die);
-  if (id >= total) return;
+  int id = die_order(blockIdx.x, a.B * a.HK, nkt);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int kt = id % nkt, bh = id / nkt, hk = bh % a.HK, b = bh / a.HK;
+  if (b >= a.B) return;
   int k0 = kt * 128 + wave * 32, j = k0 + (lane & 31);
   int qn = queries_of(a, b);
   int kn = keys_of(a, b);
@@ -439,17 +439,17 @@ void delta_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
 }
 template <typename T, bool VEC>
 void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  int nqt = (a.nq + 127) / 128, total = a.B * a.H * nqt, per = (total + 7) / 8;
+  int nqt = (a.nq + 127) / 128, grid = (a.B * a.H * nqt + 7) / 8 * 8;
   size_t lds = a.table ? sizeof(float) * 9 * (2 * (a.bk.far + kPad) + 1) : 0;
-  if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64, VEC><<<8 * per, 256, lds, s>>>(a, g, nqt, total, per);
-  else k_attend_dq<T, 128, VEC><<<8 * per, 256, lds, s>>>(a, g, nqt, total, per);
+  if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
+  else k_attend_dq<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
 }
 template <typename T, bool VEC>
 void dkv_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  int nkt = (a.nk + 127) / 128, total = a.B * a.HK * nkt, per = (total + 7) / 8;
+  int nkt = (a.nk + 127) / 128, grid = (a.B * a.HK * nkt + 7) / 8 * 8;
   size_t lds = a.table ? sizeof(float) * (2 * (a.bk.far + kPad) + 1) : 0;
-  if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<8 * per, 256, lds, s>>>(a, g, nkt, total, per);
-  else k_attend_dkv<T, 128, VEC><<<8 * per, 256, lds, s>>>(a, g, nkt, total, per);
+  if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nkt);
+  else k_attend_dkv<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nkt);
 }
 template <typename T>
 void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
