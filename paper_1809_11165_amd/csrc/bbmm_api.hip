@@ -2174,10 +2174,22 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
   return p;
 }
 
+// The gradient's two passes likewise: the keys of the dQ pass and the queries (of all heads of a group) of the dK, dV pass are split while the
+// workgroups do not fill the device and a part keeps at least kGradPart rows.
+constexpr int64_t kGradPart = 256;
+void gradient_plan(const bbmm_ctx* c, const AttArgs& a, int* qsplit, int* ksplit) {
+  auto parts = [&](int64_t wgs, int64_t rows) {
+    int64_t want = wgs > 0 ? (c->num_cus + wgs - 1) / wgs : 1, most = std::max<int64_t>(1, rows / kGradPart);
+    return (int)std::max<int64_t>(1, std::min(want, most));
+  };
+  *qsplit = parts((int64_t)a.B * a.H * ((a.nq + 127) / 128), a.nk);
+  *ksplit = parts((int64_t)a.B * a.HK * ((a.nk + 127) / 128), (int64_t)a.nq * a.G);
+}
+
 // Offsets into the workspace, 256-byte steps.
 size_t step256(size_t n) { return (n + 255) / 256 * 256; }
 struct AttWork {
-  size_t pO, pl, delta, lo, hi, tsum, norms, bytes;
+  size_t pO, pl, delta, lo, hi, tsum, norms, pq, pk, pv, bytes;
 };
 AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
   AttWork w{};
@@ -2191,12 +2203,22 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
     }
     return w;
   }
-  w.norms = 0;
-  w.delta = 256;
-  w.lo = w.delta + step256(rows * sizeof(float));
-  w.hi = w.lo + step256(rows * sizeof(float));
-  w.tsum = w.hi + step256(rows * sizeof(float));
-  w.bytes = w.tsum + (a.table ? step256((size_t)a.H * a.B * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float)) : 0);
+  int qsplit, ksplit;
+  gradient_plan(c, a, &qsplit, &ksplit);
+  auto take = [&](size_t n) {
+    size_t at = w.bytes;
+    w.bytes += step256(n);
+    return at;
+  };
+  w.norms = take(64 * BBMM_ATT_NORM_SLOTS);
+  w.delta = take(rows * sizeof(float));
+  w.lo = take(rows * sizeof(float));
+  w.hi = take(rows * sizeof(float));
+  w.tsum = take(a.table ? (size_t)a.H * a.B * qsplit * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float) : 0);
+  size_t keys = (size_t)a.B * a.HK * a.nk * ksplit * sizeof(float);
+  w.pq = take(qsplit > 1 ? rows * qsplit * a.d * sizeof(float) : 0);
+  w.pk = take(ksplit > 1 ? keys * a.d : 0);
+  w.pv = take(ksplit > 1 ? keys * a.dv : 0);
   return w;
 }
 
@@ -2272,11 +2294,13 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   g.ovec = wide_rows(O, nullptr, a.dv, e, 16), g.dovec = wide_rows(dO, g.dos, a.dv, e, 16);
   g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
   g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (unsigned*)((char*)work + w.norms);
+  g.pq = (float*)((char*)work + w.pq), g.pk = (float*)((char*)work + w.pk), g.pv = (float*)((char*)work + w.pv);
+  gradient_plan(c, a, &g.qsplit, &g.ksplit);
   hipStream_t s = c->stream;
   launch_attend_delta(s, in->type, a, g);
   if (rows) launch_attend_dq(s, in->type, a, g);
   if (keys) launch_attend_dkv(s, in->type, a, g);
-  if (a.table) launch_bucket_join(s, in->type, g.tsum, a.B * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
+  if (a.table) launch_bucket_join(s, in->type, g.tsum, a.B * g.qsplit * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
   HIPCHK(c, hipGetLastError());
   return BBMM_OK;
 }
@@ -2349,7 +2373,7 @@ int bbmm_attend_workspace(bbmm_ctx* c, const bbmm_attention* in, int32_t grad, i
     int rc = attention_args(c, in, false, &a);
     if (rc) return rc;
     if (!bytes) return fail(c, BBMM_EINVAL, "attention: bytes is required");
-    *bytes = a.B == 0 ? (grad ? 256 : 0) : (int64_t)attention_work(c, a, grad != 0).bytes;
+    *bytes = (int64_t)attention_work(c, a, grad != 0).bytes;
     return (int)BBMM_OK;
   });
 }

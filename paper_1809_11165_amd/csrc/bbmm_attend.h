@@ -9,6 +9,7 @@
 #define BBMM_ATT_MAXD 128      // features of Q, K and of V
 #define BBMM_ATT_MAXEDGES 63   // edges of the buckets
 #define BBMM_ATT_FAR 1024      // largest edge
+#define BBMM_ATT_NORM_SLOTS 64
 
 // The buckets of a difference r = j - i - start (edges ascending; further than the last one, everything on a side shares a bucket).
 struct AttBuckets {
@@ -49,8 +50,10 @@ struct AttGrad {
   void *dQ, *dK, *dV;            // dense
   // B x H x nq, left by launch_attend_delta: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
   float *delta, *lo, *hi;
-  float* tsum;                   // per workgroup of the dQ pass: sums of dS by bucket (H x (B ceil(nq / 128)) x buckets)
-  unsigned* norms;               // fp16: bits of the largest |do_i| and |v_j|
+  float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets
+  unsigned* norms;               // fp16: bits of the largest |do_i| and |v_j|, 64 bytes per slot
+  int qsplit, ksplit;            // parts that the keys of the dQ pass, and the queries of the dK, dV pass, are split into
+  float *pq, *pk, *pv;           // their results: parts x the size of dQ, dK, dV
 };
 
 // type: 0 fp32, 1 fp16, 2 bf16

@@ -62,10 +62,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
     if (mrow) mb = (lane < BK && t * BK + lane < kn) ? mrow[t * BK + lane] : 0;
   };
   uint64_t k0 = 0, k1 = 0, k2 = 0;             // keys of this tile and the next two that take part
-  auto keys = [&](int t) { return keep_bits(min(max(kn - t * BK, 0), BK), mrow, mb); };
+  constexpr uint64_t kAll = 0xffffffffull;
+  int whole = mrow ? -1 : kn / BK;             // tiles before this one are kept as a whole
+  auto keys = [&](int t) { return t < whole ? kAll : keep_bits(min(max(kn - t * BK, 0), BK), mrow, mb); };
   auto put_keys = [&](int par, uint64_t keep, const Stage<T, DP, BK, VEC>& st) {
     st.store(tk[par], keep, tid);
-    if (tid < BK) from[par][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
+    if (keep != kAll && tid < BK) from[par][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
   };
   auto scores_start = [&](int par) {
     f32x16 c;
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
       left = uniform(line[kPad]);
       right = uniform(line[2 * far + kPad]);
     }
-    sc[0] = scores_start(0);
+    if (k0 != kAll) sc[0] = scores_start(0);
 #pragma unroll
     for (int k = 0; k < NS; ++k) sc[0] = Frag<T>::mma(row_frag<T, DP>(tk[0], 0, k, lane), q[k], sc[0]);
     __syncthreads();
@@ -156,7 +158,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
     if (!plain) add_bias<true>(s, a.c2, ln, far, rel + t * BK, left, right, lane, mul, add);
     // Steps kept in this order: each reads the operand of the step after next, queues one product of the tile after (scores) or before (values),
     // and does its share of this tile's softmax meanwhile.
-    next = scores_start(PAR ^ 1);
     const char *kt = tk[PAR ^ 1], *vt = tv[PAR ^ 1];
     constexpr int M = NS + 2 * ND, E0 = M / 2 - M / 8;
     auto operand = [&](int z) { return z < NS ? row_frag<T, DP>(kt, 0, z, lane) : col_frag<T, DP>(vt, 16 * ((z - NS) / ND), 32 * ((z - NS) % ND), lane); };
@@ -169,7 +170,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
     for (int z = 0; z < M; ++z) {
       __builtin_amdgcn_sched_barrier(0);
       if (z + 2 < M) f[(z + 2) % 3] = operand(z + 2);
-      if (z < NS) next = Frag<T>::mma(f[z % 3], q[z], next);
+      if (z == 0) {
+        if (k1 == kAll) next = Frag<T>::mma(f[0], q[0], f32x16{});
+        else next = Frag<T>::mma(f[0], q[0], scores_start(PAR ^ 1));
+      } else if (z < NS) next = Frag<T>::mma(f[z % 3], q[z], next);
       else acc[(z - NS) % ND] = Frag<T>::mma(f[z % 3], p[(z - NS) / ND], acc[(z - NS) % ND]);
       if (z < E0) {
 #pragma unroll

@@ -18,19 +18,34 @@ namespace {
 template <typename T> struct PLift { static constexpr float value = 0.f; };
 template <> struct PLift<_Float16> { static constexpr float value = 12.f; };
 
-// Power of two that keeps |dS| <= 2 |do| |v| below 2^15.
+// Largest |do_i| and |v_j| of a call, in kNormSlots slots of 64 bytes (all rows in one place made 64 000 rows of fp16 wait 200 us for each other).
+constexpr int kNormSlots = BBMM_ATT_NORM_SLOTS;
+
+// Power of two that keeps |dS| <= 2 |do| |v| below 2^15.  All lanes of a wave take part.
 template <typename T>
-__device__ __forceinline__ float ds_scale(const AttGrad& g) {
-  if constexpr (sizeof(T) == 2 && __is_same(T, _Float16)) {
-    float x = __uint_as_float(g.norms[0]), y = __uint_as_float(g.norms[1]);
+__device__ __forceinline__ float ds_scale(const AttGrad& g, int lane) {
+  if constexpr (__is_same(T, _Float16)) {
+    float x = __uint_as_float(g.norms[16 * lane]), y = __uint_as_float(g.norms[16 * lane + 1]);
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+      x = fmaxf(x, __shfl_xor(x, k, 64));
+      y = fmaxf(y, __shfl_xor(y, k, 64));
+    }
     float e = (x > 0.f && y > 0.f) ? 14.f - ceilf(__builtin_amdgcn_logf(x) + __builtin_amdgcn_logf(y)) : 0.f;
-    return __builtin_amdgcn_exp2f(fminf(fmaxf(e, -100.f), 100.f));
+    return uniform(__builtin_amdgcn_exp2f(fminf(fmaxf(e, -100.f), 100.f)));
   }
   return 1.f;
 }
+static_assert(kNormSlots == 64, "a slot per lane");
 
-__global__ void k_zero_norms(unsigned* n) {
-  if (threadIdx.x < 2) n[threadIdx.x] = 0;
+__global__ void k_zero_norms(unsigned* n) { n[16 * threadIdx.x] = n[16 * threadIdx.x + 1] = 0; }
+
+// Four rows of a wave, 16 lanes each: one maximum (any order) into the workgroup's slot.  Rows without a finite norm are left out.
+__device__ __forceinline__ void put_norm(unsigned* norms, int which, float square, int lane) {
+  float x = square < __builtin_inff() ? sqrtf(square) : 0.f;
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  x = fmaxf(x, __shfl_xor(x, 32, 64));
+  if (lane == 0 && x > 0.f) atomicMax(&norms[16 * (blockIdx.x % kNormSlots) + which], __float_as_uint(x));
 }
 
 // Beyond this, fp32 holds lse too coarsely to recover weights from it (a row of nothing but masks of -1e9 or of the type's lowest value).
@@ -70,12 +85,13 @@ __global__ __launch_bounds__(256) void k_attend_delta(AttArgs a, AttGrad g) {
   constexpr int E = 16 / (int)sizeof(T);
   int lane = threadIdx.x & 15;
   int64_t n = (int64_t)a.B * a.nq * a.H, row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (row >= n) return;                      // whole groups of 16 lanes
+  bool have = row < n;                       // whole groups of 16 lanes
+  if (!have) row = n - 1;
   int h = (int)(row % a.H), i = (int)(row / a.H % a.nq), b = (int)(row / a.H / a.nq);
   int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
   size_t at = ((size_t)b * a.H + h) * a.nq + i;
   float s = 0.f, q = 0.f, hi = 0.f, lo = __builtin_inff();
-  float lse = i < qn ? g.lse[at] : -__builtin_inff();
+  float lse = i < qn && have ? g.lse[at] : -__builtin_inff();
   if (lse != -__builtin_inff()) {
     const T* o = (const T*)g.O + row * a.dv;
     const T* d = (const T*)g.dO + b * g.dos[0] + (int64_t)i * g.dos[1] + h * g.dos[2];
@@ -96,12 +112,12 @@ __global__ __launch_bounds__(256) void k_attend_delta(AttArgs a, AttGrad g) {
     s += __shfl_xor(s, x, 16);
     q += __shfl_xor(q, x, 16);
   }
-  if (lane == 0) {
+  if (lane == 0 && have) {
     g.delta[at] = s;
     g.lo[at] = lo;
     g.hi[at] = hi;
-    if (__is_same(T, _Float16) && q < __builtin_inff()) atomicMax(&g.norms[0], __float_as_uint(sqrtf(q)));   // a maximum: any order
   }
+  if (__is_same(T, _Float16)) put_norm(g.norms, 0, q, threadIdx.x & 63);
 }
 
 template <typename T>
@@ -109,36 +125,41 @@ __global__ __launch_bounds__(256) void k_attend_vnorm(AttArgs a, AttGrad g) {
   constexpr int E = 16 / (int)sizeof(T);
   int lane = threadIdx.x & 15;
   int64_t n = (int64_t)a.B * a.nk * a.HK, row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (row >= n) return;
+  bool have = row < n;
+  if (!have) row = n - 1;
   int h = (int)(row % a.HK), j = (int)(row / a.HK % a.nk), b = (int)(row / a.HK / a.nk);
-  if ((a.k_len && j >= a.k_len[b]) || (a.mask && !a.mask[b * a.mask_s + j])) return;
+  if ((a.k_len && j >= a.k_len[b]) || (a.mask && !a.mask[b * a.mask_s + j])) have = false;
   const T* v = (const T*)a.V + b * a.vs[0] + (int64_t)j * a.vs[1] + h * a.vs[2];
   float q = 0.f;
-  for (int c = lane * E; c < a.dv; c += 16 * E) {
+  for (int c = lane * E; c < a.dv && have; c += 16 * E) {
     u32x4 x = load16<T>(v, c, a.dv, a.vvec);
 #pragma unroll
     for (int e = 0; e < E; ++e) q = fmaf((float)reinterpret_cast<T*>(&x)[e], (float)reinterpret_cast<T*>(&x)[e], q);
   }
 #pragma unroll
   for (int x = 1; x < 16; x *= 2) q += __shfl_xor(q, x, 64);
-  if (lane == 0 && q < __builtin_inff()) atomicMax(&g.norms[1], __float_as_uint(sqrtf(q)));
+  put_norm(g.norms, 1, q, threadIdx.x & 63);
 }
 
+// 32 keys a turn.  While the matrix unit forms the scores and dP of the next tile, the vector unit turns this one's into dS; then dQ takes it up.
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttArgs a, AttGrad g, int nqt) {
+__global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttArgs a, AttGrad g, int nqt) {
   typedef typename Frag<T>::type frag;
-  constexpr int BK = sizeof(T) == 2 ? 64 : 32, NB = BK / 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
-  __shared__ __align__(16) char tile[2][2][kTile];
-  extern __shared__ float dyn[];               // with a table: bias line, then eight lines of diagonal sums (wave, half)
-  int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt);
+  constexpr int BK = 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
+  __shared__ __align__(16) char tile[3][2][kTile];   // K, V
+  __shared__ __align__(16) float from[3][32];        // what a key's scores start from: 0, or -infinity where it takes no part
+  __shared__ float side[8];
+  extern __shared__ float dyn[];                     // with a table: bias line, then eight lines of diagonal sums (wave, half)
+  int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt * g.qsplit);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
-  int qt = id % nqt, bh = id / nqt, h = bh % a.H, b = bh / a.H, hk = h / a.G;
+  int qt = id % nqt, sp = id / nqt % g.qsplit, bh = id / nqt / g.qsplit, h = bh % a.H, b = bh / a.H, hk = h / a.G;
   if (b >= a.B) return;
   int q0 = qt * 128 + wave * 32, i = q0 + (lane & 31);
   int qn = queries_of(a, b);
   int kn = keys_of(a, b);
   if (qt * 128 >= qn) kn = 0;
-  int tiles = (kn + BK - 1) / BK;
+  int tiles = (kn + BK - 1) / BK, per = (tiles + g.qsplit - 1) / g.qsplit;
+  int t0 = min(sp * per, tiles), t1 = min(t0 + per, tiles);
   int far = a.bk.far, span = far + kPad, nline = 2 * span + 1;
   float* line = dyn;
   float* diag = dyn + nline;
@@ -166,143 +187,170 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttAr
     for (int n = tid; n < 8 * nline; n += 256) diag[n] = 0.f;
     ln = line;
   }
-  int64_t start = start_of(a, b);
-  float cs = ds_scale<T>(g);
+  float cs = ds_scale<T>(g, lane);                 // a power of two: dS is formed times it
+  lo -= __builtin_amdgcn_logf(cs);
 
   Stage<T, DP, BK, VEC> sk, sv;
-  uint64_t keep = 0;
   uint8_t mb = 0;
+  constexpr uint64_t kAll = 0xffffffffull;
+  int whole = mrow ? -1 : kn / BK;           // tiles before this one are kept as a whole
   auto fetch = [&](int t) {
-    int j0 = t * BK, left = kn - j0;
-    sk.load(K + (int64_t)j0 * a.ks[1], a.ks[1], left, a.d, tid);
-    sv.load(V + (int64_t)j0 * a.vs[1], a.vs[1], left, a.dv, tid);
-    if (mrow) mb = (lane < BK && lane < left) ? mrow[j0 + lane] : 0;
+    sk.load(K + (int64_t)t * BK * a.ks[1], a.ks[1], kn - t * BK, a.d, tid);
+    sv.load(V + (int64_t)t * BK * a.vs[1], a.vs[1], kn - t * BK, a.dv, tid);
+    if (mrow) mb = (lane < BK && t * BK + lane < kn) ? mrow[t * BK + lane] : 0;
   };
-  auto put = [&](int t) {
-    keep = keep_bits(min(kn - t * BK, BK), mrow, mb);
-    sk.store(tile[t & 1][0], keep, tid);
-    sv.store(tile[t & 1][1], keep, tid);
+  auto put = [&](int t, int at) {
+    uint64_t keep = t < whole ? kAll : keep_bits(min(max(kn - t * BK, 0), BK), mrow, mb);
+    sk.store(tile[at][0], keep, tid);
+    sv.store(tile[at][1], keep, tid);
+    if (tid < BK) from[at][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
   };
-  f32x16 acc[ND];
+  auto scores_start = [&](int at) {
+    f32x16 c;
+    const float* x = from[at] + 4 * half;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      f32x4 y = *(const f32x4*)(x + 8 * n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[4 * n + e] = y[e];
+    }
+    return c;
+  };
+  f32x16 acc[ND], s = f32x16{}, dp = f32x16{};
 #pragma unroll
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
-  float sl = 0.f, sr = 0.f;
-  if (tiles) {
-    fetch(0);
-    put(0);
+  float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
+  int rel = rest_below(-(int64_t)q0 - start_of(a, b));
+  if (t0 < t1) {
+    fetch(t0);
+    put(t0, 0);
+    fetch(t0 + 1);
+    put(t0 + 1, 1);
   }
   settle();
   __syncthreads();
-  float left = 0.f, right = 0.f;
   if (ln) {
-    left = line[kPad];
-    right = line[2 * far + kPad];
+    left = uniform(line[kPad]);
+    right = uniform(line[2 * far + kPad]);
   }
-  int rel = rest_below(-(int64_t)q0 - start);
-  for (int t = 0; t < tiles; ++t) {
-    const char *tk = tile[t & 1][0], *tv = tile[t & 1][1];
-    uint64_t kp = keep;
-    if (t + 1 < tiles) fetch(t + 1);
-    if (kp) {
+  if (t0 < t1) {
+    s = scores_start(0);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        f32x16 s = f32x16{}, dp = f32x16{};
+    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 0, k, lane), q[k], s);
 #pragma unroll
-        for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tk, 32 * n, k, lane), q[k], s);
+    for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), dof[k], dp);
+  }
+  int now = 0;
+  for (int t = t0; t < t1; ++t) {
+    int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
+    fetch(t + 2);
+    float mul = a.c2, add = 0.f;
+    int where = 1, rel0 = rel + t * BK;
+    if (ln) where = add_bias<true>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
+    if (coarse) {
 #pragma unroll
-        for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tv, 32 * n, k, lane), dof[k], dp);
-        int rel0 = rel + t * BK + 32 * n;
-        float mul, add;
-        int where = add_bias<true>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
-        if (coarse && mul == 1.f) {
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mul, add) - hi;
+      mul = 1.f;
+      add = 0.f;
+    }
+    add -= lo;
+    const char *kt = tile[nxt][0], *vt = tile[nxt][1], *ko = tile[now][0];
+    f32x16 s2 = scores_start(nxt), dp2 = f32x16{};
+    constexpr int A = 2 * NS, M = A + 2 * ND;
+    auto operand = [&](int z) {
+      return z < NS ? row_frag<T, DP>(kt, 0, z, lane) : z < A ? row_frag<T, DP>(vt, 0, z - NS, lane) : col_frag<T, DP>(ko, 16 * ((z - A) / ND), 32 * ((z - A) % ND), lane);
+    };
+    frag f[3], ds[2];
+    f[0] = operand(0);
+    f[1] = operand(1);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] -= hi;
-        } else {
-          add -= hi;
-        }
-        add -= lo;
-        unsigned kb = (unsigned)(kp >> (32 * n));
+    for (int z = 0; z < M; ++z) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (z + 2 < M) f[(z + 2) % 3] = operand(z + 2);
+      if (z < NS) s2 = Frag<T>::mma(f[z % 3], q[z], s2);
+      else if (z < A) dp2 = Frag<T>::mma(f[z % 3], dof[z - NS], dp2);
+      else acc[(z - A) % ND] = Frag<T>::mma(f[z % 3], ds[(z - A) / ND], acc[(z - A) % ND]);
+      if (z < A) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (dp[r] - delta);
-        if (kb != 0xffffffffu) {
-          unsigned k = kb >> (4 * half);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = ((k >> (8 * (r >> 2) + (r & 3))) & 1) ? s[r] : 0.f;
-        }
-        if (ln) {
-          if (where == 0) {
-            add_diagonals(s, diag + (2 * wave + half) * nline + rel0 + span, lane);
-          } else {
-            float x = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x += s[r];
-            if (where < 0) sl += x;
-            else sr += x;
-          }
-        }
-        if (cs != 1.f) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] *= cs;
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          frag p = pack8<T>(s, u);
-#pragma unroll
-          for (int c = 0; c < ND; ++c) acc[c] = Frag<T>::mma(col_frag<T, DP>(tk, 32 * n + 16 * u, 32 * c, lane), p, acc[c]);
+        for (int r = z * 16 / A; r < (z + 1) * 16 / A; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (dp[r] - delta);
+          if (r == 7) ds[0] = pack8<T>(s, 0);
+          if (r == 15) ds[1] = pack8<T>(s, 1);
         }
       }
     }
-    if (t + 1 < tiles) put(t + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (ln) {
+      if (where == 0) {
+        add_diagonals(s, diag + (2 * wave + half) * nline + rel0 + span, lane);
+      } else {
+        float x = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x += s[r];
+        if (where < 0) sl += x;
+        else sr += x;
+      }
+    }
+    s = s2;
+    dp = dp2;
+    put(t + 2, last);
+    now = nxt;
     __syncthreads();
   }
   if (i < a.nq) {
     float f = a.scale / cs;
-    T* out = (T*)g.dQ + (((int64_t)b * a.nq + i) * a.H + h) * a.d;
+    int64_t at = (((int64_t)b * a.nq + i) * a.H + h) * a.d;
+    auto write = [&](auto* out, int vec) {
 #pragma unroll
-    for (int n = 0; n < ND; ++n)
+      for (int n = 0; n < ND; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        store4<T>(out, 32 * n + 8 * r + 4 * half, a.d, g.dqvec, acc[n][4 * r] * f, acc[n][4 * r + 1] * f, acc[n][4 * r + 2] * f, acc[n][4 * r + 3] * f);
+        for (int r = 0; r < 4; ++r)
+          store4(out, 32 * n + 8 * r + 4 * half, a.d, vec, acc[n][4 * r] * f, acc[n][4 * r + 1] * f, acc[n][4 * r + 2] * f, acc[n][4 * r + 3] * f);
+    };
+    if (g.qsplit == 1) write((T*)g.dQ + at, g.dqvec);
+    else write(g.pq + sp * ((int64_t)a.B * a.nq * a.H * a.d) + at, a.d % 4 == 0);
   }
   if (ln) {                                  // the loop's last barrier stands before this
+    float f = 1.f / cs;
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
       sl += __shfl_xor(sl, x, 64);
       sr += __shfl_xor(sr, x, 64);
     }
-    float* side = (float*)tile;
     if (lane == 0) {
       side[wave] = sl;
       side[4 + wave] = sr;
     }
     for (int n = tid; n < nline; n += 256) {
-      float s = 0.f;
+      float x = 0.f;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s += diag[k * nline + n];
-      line[n] = s;
+      for (int k = 0; k < 8; ++k) x += diag[k * nline + n];
+      line[n] = x * f;
     }
     __syncthreads();
-    float* out = g.tsum + ((size_t)h * a.B * nqt + (size_t)b * nqt + qt) * a.bk.buckets;
-    bucket_sums(a.bk, line, span, side[0] + side[1] + side[2] + side[3], side[4] + side[5] + side[6] + side[7], out, tid);
+    float* out = g.tsum + ((((size_t)h * a.B + b) * g.qsplit + sp) * nqt + qt) * a.bk.buckets;
+    bucket_sums(a.bk, line, span, f * (side[0] + side[1] + side[2] + side[3]), f * (side[4] + side[5] + side[6] + side[7]), out, tid);
   }
 }
 
+// 32 queries of one head a turn, the heads of the group one after the other; else like k_attend_dq.
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt) {
+__global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt) {
   typedef typename Frag<T>::type frag;
-  constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NB = BQ / 32, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
-  __shared__ __align__(16) char tile[2][2][kTile];
-  __shared__ __align__(16) float stat[2][3][BQ];      // lo, delta, hi
+  constexpr int BQ = 32, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
+  __shared__ __align__(16) char tile[3][2][kTile];    // Q, dO
+  __shared__ __align__(16) float stat[3][3][BQ];      // lo, delta (scaled like dS), hi
   extern __shared__ float dyn[];                      // with a table: bias line
-  int id = die_order(blockIdx.x, a.B * a.HK, nkt);
+  int id = die_order(blockIdx.x, a.B * a.HK, nkt * g.ksplit);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
-  int kt = id % nkt, bh = id / nkt, hk = bh % a.HK, b = bh / a.HK;
+  int kt = id % nkt, sp = id / nkt % g.ksplit, bh = id / nkt / g.ksplit, hk = bh % a.HK, b = bh / a.HK;
   if (b >= a.B) return;
   int k0 = kt * 128 + wave * 32, j = k0 + (lane & 31);
   int qn = queries_of(a, b);
   int kn = keys_of(a, b);
   if (kt * 128 >= kn) qn = 0;
-  int tiles = (qn + BQ - 1) / BQ, steps = tiles * a.G;
+  int tiles = (qn + BQ - 1) / BQ, steps = tiles * a.G, per = (steps + g.ksplit - 1) / g.ksplit;   // a part: some tiles of some heads
+  int t0 = min(sp * per, steps), t1 = min(t0 + per, steps);
   int far = a.bk.far;
   const float* ln = a.table ? dyn : nullptr;
   bool mine = j < kn && (!a.mask || a.mask[b * a.mask_s + j]);
@@ -316,150 +364,210 @@ __global__ __launch_bounds__(256, 1) void k_attend_dkv(AttArgs a, AttGrad g, int
       vf[s] = reg_frag<T>(vr, mine, s, a.dv, a.vvec, lane);
     }
   }
-  int64_t start = start_of(a, b);
-  float cs = ds_scale<T>(g);
+  constexpr float kLift = PLift<T>::value;
+  float cs = ds_scale<T>(g, lane), unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
 
   Stage<T, DP, BQ, VEC> sq, sd;
   float lo = 0.f, delta = 0.f, hi = 0.f;     // of row `lane` of the tile
-  bool coarse = false;
-  auto fetch = [&](int t) {
-    int h = hk * a.G + t / tiles, i0 = t % tiles * BQ, rows = qn - i0;
-    sq.load((const T*)a.Q + b * a.qs[0] + (int64_t)i0 * a.qs[1] + h * a.qs[2], a.qs[1], rows, a.d, tid);
-    sd.load((const T*)g.dO + b * g.dos[0] + (int64_t)i0 * g.dos[1] + h * g.dos[2], g.dos[1], rows, a.dv, tid);
-    size_t row = ((size_t)b * a.H + h) * a.nq + i0 + lane;
-    bool have = lane < BQ && lane < rows;
-    lo = have ? g.lo[row] : __builtin_inff();
-    delta = have ? g.delta[row] : 0.f;
-    hi = have ? g.hi[row] : 0.f;
+  int h = hk * a.G + (tiles ? t0 / tiles : 0), i0 = tiles ? t0 % tiles * BQ : 0;   // head and first row of the turn's tile
+  int fh = h, fi = i0;                       // and of the tile to fetch next
+  auto fetch = [&]() {
+    int rows = fh < (hk + 1) * a.G ? qn - fi : 0;
+    sq.load((const T*)a.Q + b * a.qs[0] + (int64_t)fi * a.qs[1] + fh * a.qs[2], a.qs[1], rows, a.d, tid);
+    sd.load((const T*)g.dO + b * g.dos[0] + (int64_t)fi * g.dos[1] + fh * g.dos[2], g.dos[1], rows, a.dv, tid);
+    size_t row = ((size_t)b * a.H + fh) * a.nq + fi + lane;
+    lo = __builtin_inff();
+    delta = hi = 0.f;
+    if (lane < BQ && lane < rows) lo = g.lo[row], delta = g.delta[row], hi = g.hi[row];
+    fi += BQ;
+    if (fi >= qn) fi = 0, ++fh;
   };
-  auto put = [&](int t) {
-    uint64_t keep = __ballot(lo != __builtin_inff());
-    coarse = __any(hi != 0.f);
-    sq.store(tile[t & 1][0], keep, tid);
-    sd.store(tile[t & 1][1], keep, tid);
+  auto put = [&](int at) {
+    uint64_t keep = __ballot(lo != __builtin_inff()) & 0xffffffffull;
+    sq.store(tile[at][0], keep, tid);
+    sd.store(tile[at][1], keep, tid);
     if (tid < BQ) {
-      stat[t & 1][0][tid] = lo;                // infinite where nothing is left in the row: weights zero
-      stat[t & 1][1][tid] = delta;
-      stat[t & 1][2][tid] = hi;
+      stat[at][0][tid] = lo;                 // infinite where nothing is left in the row: weights zero
+      stat[at][1][tid] = delta * ck;
+      stat[at][2][tid] = hi;
     }
+    return __any(hi != 0.f);
   };
-  f32x16 dk[ND], dv[ND];
+  f32x16 dk[ND], dv[ND], s = f32x16{}, dp = f32x16{};
 #pragma unroll
   for (int n = 0; n < ND; ++n) dk[n] = dv[n] = f32x16{};
   float left = 0.f, right = 0.f;
-  int rel = rest_above((int64_t)k0 - start);
-  if (steps) {
-    fetch(0);
-    put(0);
+  int rel = rest_above((int64_t)k0 - start_of(a, b));
+  bool c0 = false, c1 = false;               // rows with a `hi` in this tile and the next
+  if (t0 < t1) {
+    fetch();
+    c0 = put(0);
+    fetch();
+    c1 = put(1);
   }
   settle();
-  for (int t = 0; t < steps; ++t) {
-    if (ln && t % tiles == 0) {              // another head: its bias line (nobody reads the old one any more)
-      fill_line<T>(dyn, a, hk * a.G + t / tiles, tid, 256);
+  __syncthreads();
+  if (t0 < t1) {
+#pragma unroll
+    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 0, k, lane), kf[k], s);
+#pragma unroll
+    for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), vf[k], dp);
+  }
+  int now = 0;
+  for (int t = t0; t < t1; ++t) {
+    if (ln && (i0 == 0 || t == t0)) {                     // another head: its bias line (nobody reads the old one any more)
+      fill_line<T>(dyn, a, h, tid, 256);
       __syncthreads();
-      left = ln[kPad];
-      right = ln[2 * far + kPad];
-    } else if (t == 0) {
-      __syncthreads();
+      left = uniform(ln[kPad]);
+      right = uniform(ln[2 * far + kPad]);
     }
-    const char *tq = tile[t & 1][0], *td = tile[t & 1][1];
-    bool wide = coarse;
-    if (t + 1 < steps) fetch(t + 1);
+    int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
+    fetch();
+    float mul = a.c2, add = 0.f;
+    if (ln) add_bias<false>(s, a.c2, ln, far, rel - i0, left, right, lane, mul, add);
+    const float* st = stat[now][0] + 4 * half;
+    f32x4 l4[4], d4[4];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      f32x16 s = f32x16{}, dp = f32x16{};
+    for (int n = 0; n < 4; ++n) {
+      l4[n] = *(const f32x4*)(st + 8 * n);
+      d4[n] = *(const f32x4*)(st + BQ + 8 * n);
+    }
+    if (c0) {
 #pragma unroll
-      for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tq, 32 * n, k, lane), kf[k], s);
+      for (int n = 0; n < 4; ++n) {
+        f32x4 h4 = *(const f32x4*)(st + 2 * BQ + 8 * n);
 #pragma unroll
-      for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(td, 32 * n, k, lane), vf[k], dp);
-      float mul, add;
-      add_bias<false>(s, a.c2, ln, far, rel - (t % tiles * BQ + 32 * n), left, right, lane, mul, add);
-      if (wide) {
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          f32x4 h4 = *(const f32x4*)&stat[t & 1][2][32 * n + 8 * r4 + 4 * half];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[4 * r4 + e] = fmaf(s[4 * r4 + e], mul, add - h4[e]);
-        }
-        mul = 1.f;
-        add = 0.f;
+        for (int e = 0; e < 4; ++e) s[4 * n + e] = fmaf(s[4 * n + e], mul, add) - h4[e];
       }
-      add += PLift<T>::value;
+      mul = 1.f;
+      add = 0.f;
+    }
+    add += kLift;
+    const char *qn1 = tile[nxt][0], *dn1 = tile[nxt][1], *qo = tile[now][0], *od = tile[now][1];
+    f32x16 s2 = f32x16{}, dp2 = f32x16{};
+    constexpr int A = 2 * NS, M = A + 4 * ND;
+    auto operand = [&](int z) {
+      return z < NS ? row_frag<T, DP>(qn1, 0, z, lane)
+             : z < A ? row_frag<T, DP>(dn1, 0, z - NS, lane)
+                     : col_frag<T, DP>((z - A) / ND % 2 ? qo : od, 16 * ((z - A) / (2 * ND)), 32 * ((z - A) % ND), lane);
+    };
+    frag f[3], p[2], ds[2];
+    f[0] = operand(0);
+    f[1] = operand(1);
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        f32x4 l4 = *(const f32x4*)&stat[t & 1][0][32 * n + 8 * r4 + 4 * half], d4 = *(const f32x4*)&stat[t & 1][1][32 * n + 8 * r4 + 4 * half];
+    for (int z = 0; z < M; ++z) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (z + 2 < M) f[(z + 2) % 3] = operand(z + 2);
+      constexpr int N2 = 2 * ND;
+      int y = z - A;
+      if (z < NS) s2 = Frag<T>::mma(f[z % 3], kf[z], s2);
+      else if (z < A) dp2 = Frag<T>::mma(f[z % 3], vf[z - NS], dp2);
+      else if (y / ND % 2 == 0) dv[y % ND] = Frag<T>::mma(f[z % 3], p[y / N2], dv[y % ND]);
+      else dk[y % ND] = Frag<T>::mma(f[z % 3], ds[y / N2], dk[y % ND]);
+      if (z < A) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float p = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + e], mul, add - l4[e]));
-          s[4 * r4 + e] = p;
-          dp[4 * r4 + e] = p * (dp[4 * r4 + e] - d4[e]);
-          if (PLift<T>::value != 0.f) dp[4 * r4 + e] *= cs * (1.f / (float)(1 << (int)PLift<T>::value));
+        for (int r = z * 16 / A; r < (z + 1) * 16 / A; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add - l4[r >> 2][r & 3]));
+          dp[r] = s[r] * fmaf(dp[r], ck, -d4[r >> 2][r & 3]);
+          if (r == 7) p[0] = pack8<T>(s, 0), ds[0] = pack8<T>(dp, 0);
+          if (r == 15) p[1] = pack8<T>(s, 1), ds[1] = pack8<T>(dp, 1);
         }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        frag p = pack8<T>(s, u), ds = pack8<T>(dp, u);
-#pragma unroll
-        for (int c = 0; c < ND; ++c) dv[c] = Frag<T>::mma(col_frag<T, DP>(td, 32 * n + 16 * u, 32 * c, lane), p, dv[c]);
-#pragma unroll
-        for (int c = 0; c < ND; ++c) dk[c] = Frag<T>::mma(col_frag<T, DP>(tq, 32 * n + 16 * u, 32 * c, lane), ds, dk[c]);
       }
     }
-    if (t + 1 < steps) put(t + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    s = s2;
+    dp = dp2;
+    c0 = c1;
+    c1 = put(last);
+    now = nxt;
+    i0 += BQ;
+    if (i0 >= qn) i0 = 0, ++h;
     __syncthreads();
   }
   if (j >= a.nk) return;
-  float fk = mine ? a.scale / cs : 0.f, fv = 1.f / (float)(1 << (int)PLift<T>::value);
-  T* ok = (T*)g.dK + (((int64_t)b * a.nk + j) * a.HK + hk) * a.d;
-  T* ov = (T*)g.dV + (((int64_t)b * a.nk + j) * a.HK + hk) * a.dv;
+  float fk = a.scale / cs;
+  int64_t at = ((int64_t)b * a.nk + j) * a.HK + hk, all = (int64_t)a.B * a.nk * a.HK;
+  auto write = [&](auto* ok, int kvec, auto* ov, int vvec) {
 #pragma unroll
-  for (int n = 0; n < ND; ++n)
+    for (int n = 0; n < ND; ++n)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      int c = 32 * n + 8 * r + 4 * half;
-      f32x4 x, y;
+      for (int r = 0; r < 4; ++r) {
+        int c = 32 * n + 8 * r + 4 * half;
+        f32x4 x, y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = mine ? dk[n][4 * r + e] * fk : 0.f;
-        y[e] = mine ? dv[n][4 * r + e] * fv : 0.f;
+        for (int e = 0; e < 4; ++e) {
+          x[e] = mine ? dk[n][4 * r + e] * fk : 0.f;
+          y[e] = mine ? dv[n][4 * r + e] * unlift : 0.f;
+        }
+        store4(ok, c, a.d, kvec, x[0], x[1], x[2], x[3]);
+        store4(ov, c, a.dv, vvec, y[0], y[1], y[2], y[3]);
       }
-      store4<T>(ok, c, a.d, g.dkvec, x[0], x[1], x[2], x[3]);
-      store4<T>(ov, c, a.dv, g.dvvec, y[0], y[1], y[2], y[3]);
+  };
+  if (g.ksplit == 1) write((T*)g.dK + at * a.d, g.dkvec, (T*)g.dV + at * a.dv, g.dvvec);
+  else write(g.pk + (sp * all + at) * a.d, a.d % 4 == 0, g.pv + (sp * all + at) * a.dv, a.dv % 4 == 0);
+}
+
+// Parts of a split axis added up in order: out[n] = sum over p of part[p][n].
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_sum(const float* __restrict__ part, int parts, int64_t n, T* __restrict__ out) {
+  int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  if (n % 4 == 0) {
+    f32x4 s = *(const f32x4*)(part + i);
+#pragma unroll 4
+    for (int p = 1; p < parts; ++p) s += *(const f32x4*)(part + p * n + i);
+    store4<T>(out + i, 0, 4, (uintptr_t)out % (4 * sizeof(T)) == 0, s[0], s[1], s[2], s[3]);
+  } else {
+    for (int64_t k = i; k < n && k < i + 4; ++k) {
+      float s = 0.f;
+      for (int p = 0; p < parts; ++p) s += part[p * n + k];
+      out[k] = (T)s;
     }
+  }
 }
 
 template <typename T>
 void delta_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int64_t n = (int64_t)a.B * a.nq * a.H, nv = (int64_t)a.B * a.nk * a.HK;
   if (__is_same(T, _Float16)) {
-    k_zero_norms<<<1, 64, 0, s>>>(g.norms);
+    k_zero_norms<<<1, kNormSlots, 0, s>>>(g.norms);
     if (nv) k_attend_vnorm<T><<<(unsigned)((nv + 15) / 16), 256, 0, s>>>(a, g);
   }
   if (n) k_attend_delta<T><<<(unsigned)((n + 15) / 16), 256, 0, s>>>(a, g);
 }
 template <typename T, bool VEC>
 void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  int nqt = (a.nq + 127) / 128, grid = (a.B * a.H * nqt + 7) / 8 * 8;
+  int nqt = (a.nq + 127) / 128, grid = (a.B * a.H * nqt * g.qsplit + 7) / 8 * 8;
   size_t lds = a.table ? sizeof(float) * 9 * (2 * (a.bk.far + kPad) + 1) : 0;
   if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
   else k_attend_dq<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
 }
 template <typename T, bool VEC>
 void dkv_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  int nkt = (a.nk + 127) / 128, grid = (a.B * a.HK * nkt + 7) / 8 * 8;
+  int nkt = (a.nk + 127) / 128, grid = (a.B * a.HK * nkt * g.ksplit + 7) / 8 * 8;
   size_t lds = a.table ? sizeof(float) * (2 * (a.bk.far + kPad) + 1) : 0;
   if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nkt);
   else k_attend_dkv<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nkt);
 }
 template <typename T>
+void sum_t(hipStream_t s, const float* part, int parts, int64_t n, void* out) {
+  k_attend_sum<T><<<(unsigned)((n + 1023) / 1024), 256, 0, s>>>(part, parts, n, (T*)out);
+}
+template <typename T>
 void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   if (a.kvec && a.vvec) dq_v<T, true>(s, a, g);
   else dq_v<T, false>(s, a, g);
+  if (g.qsplit > 1) sum_t<T>(s, g.pq, g.qsplit, (int64_t)a.B * a.nq * a.H * a.d, g.dQ);
 }
 template <typename T>
 void dkv_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   if (a.qvec && g.dovec) dkv_v<T, true>(s, a, g);
   else dkv_v<T, false>(s, a, g);
+  if (g.ksplit > 1) {
+    int64_t n = (int64_t)a.B * a.nk * a.HK;
+    sum_t<T>(s, g.pk, g.ksplit, n * a.d, g.dK);
+    sum_t<T>(s, g.pv, g.ksplit, n * a.dv, g.dV);
+  }
 }
 
 }  // namespace
