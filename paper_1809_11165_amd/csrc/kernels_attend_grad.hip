@@ -141,13 +141,14 @@ __global__ __launch_bounds__(256) void k_attend_vnorm(AttArgs a, AttGrad g) {
   put_norm(g.norms, 1, q, threadIdx.x & 63);
 }
 
-// 32 keys a turn.  While the matrix unit forms the scores and dP of the next tile, the vector unit turns this one's into dS; then dQ takes it up.
+// 64 keys a turn, as two blocks of 32 (fp32: one block a turn).  While the matrix unit forms the scores and dP of the next block, the vector unit turns this one's into dS; then
+// dQ takes it up.
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttArgs a, AttGrad g, int nqt) {
   typedef typename Frag<T>::type frag;
-  constexpr int BK = 32, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
+  constexpr int NB = sizeof(T) == 2 ? 2 : 1, BK = 32 * NB, ND = DP / 32, NS = DP / 16, kTile = BK * DP * (int)sizeof(T);
   __shared__ __align__(16) char tile[3][2][kTile];   // K, V
-  __shared__ __align__(16) float from[3][32];        // what a key's scores start from: 0, or -infinity where it takes no part
+  __shared__ __align__(16) float from[3][BK];        // what a key's scores start from: 0, or -infinity where it takes no part
   __shared__ float side[8];
   extern __shared__ float dyn[];                     // with a table: bias line, then eight lines of diagonal sums (wave, half)
   int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt * g.qsplit);
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
 
   Stage<T, DP, BK, VEC> sk, sv;
   uint8_t mb = 0;
-  constexpr uint64_t kAll = 0xffffffffull;
+  constexpr uint64_t kAll = NB == 2 ? ~0ull : 0xffffffffull;
   int whole = mrow ? -1 : kn / BK;           // tiles before this one are kept as a whole
   auto fetch = [&](int t) {
     sk.load(K + (int64_t)t * BK * a.ks[1], a.ks[1], kn - t * BK, a.d, tid);
@@ -203,11 +204,12 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     uint64_t keep = t < whole ? kAll : keep_bits(min(max(kn - t * BK, 0), BK), mrow, mb);
     sk.store(tile[at][0], keep, tid);
     sv.store(tile[at][1], keep, tid);
-    if (tid < BK) from[at][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
+    if (keep != kAll && tid < BK) from[at][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
+    return keep;
   };
-  auto scores_start = [&](int at) {
+  auto scores_start = [&](int at, int first) {
     f32x16 c;
-    const float* x = from[at] + 4 * half;
+    const float* x = from[at] + first + 4 * half;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       f32x4 y = *(const f32x4*)(x + 8 * n);
@@ -216,16 +218,18 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     }
     return c;
   };
-  f32x16 acc[ND], s = f32x16{}, dp = f32x16{};
+  f32x16 acc[ND], sc[2], pc[2];              // of a turn's two blocks: scores, dP
+  sc[0] = pc[0] = f32x16{};
+  uint64_t k0 = 0, k1 = 0;                   // keys of this tile and the next that take part
 #pragma unroll
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
   float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
   int rel = rest_below(-(int64_t)q0 - start_of(a, b));
   if (t0 < t1) {
     fetch(t0);
-    put(t0, 0);
+    k0 = put(t0, 0);
     fetch(t0 + 1);
-    put(t0 + 1, 1);
+    k1 = put(t0 + 1, 1);
   }
   settle();
   __syncthreads();
@@ -234,18 +238,19 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     right = uniform(line[2 * far + kPad]);
   }
   if (t0 < t1) {
-    s = scores_start(0);
+    if (k0 != kAll) sc[0] = scores_start(0, 0);
 #pragma unroll
-    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 0, k, lane), q[k], s);
+    for (int k = 0; k < NS; ++k) sc[0] = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 0, k, lane), q[k], sc[0]);
 #pragma unroll
-    for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), dof[k], dp);
+    for (int k = 0; k < NS; ++k) pc[0] = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), dof[k], pc[0]);
   }
   int now = 0;
-  for (int t = t0; t < t1; ++t) {
-    int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
-    fetch(t + 2);
+  // Block of the turn at buffer `at`; the next block: rows 32 (block ^ 1) on of buffer `on`, whose tile keeps the keys `keep`.
+  auto block = [&](auto block_, int rel0, int at, int on, uint64_t keep) {
+    constexpr int B = decltype(block_)::value, here = NB == 2 ? 32 * B : 0, there = NB == 2 ? 32 * (B ^ 1) : 0;   // rows in their tiles
+    f32x16 &s = sc[B], &dp = pc[B], &s2 = sc[B ^ 1], &dp2 = pc[B ^ 1];
     float mul = a.c2, add = 0.f;
-    int where = 1, rel0 = rel + t * BK;
+    int where = 1;
     if (ln) where = add_bias<true>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
     if (coarse) {
 #pragma unroll
@@ -254,11 +259,12 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       add = 0.f;
     }
     add -= lo;
-    const char *kt = tile[nxt][0], *vt = tile[nxt][1], *ko = tile[now][0];
-    f32x16 s2 = scores_start(nxt), dp2 = f32x16{};
+    const char *kt = tile[on][0], *vt = tile[on][1], *ko = tile[at][0];
     constexpr int A = 2 * NS, M = A + 2 * ND;
     auto operand = [&](int z) {
-      return z < NS ? row_frag<T, DP>(kt, 0, z, lane) : z < A ? row_frag<T, DP>(vt, 0, z - NS, lane) : col_frag<T, DP>(ko, 16 * ((z - A) / ND), 32 * ((z - A) % ND), lane);
+      return z < NS ? row_frag<T, DP>(kt, there, z, lane)
+             : z < A ? row_frag<T, DP>(vt, there, z - NS, lane)
+                     : col_frag<T, DP>(ko, here + 16 * ((z - A) / ND), 32 * ((z - A) % ND), lane);
     };
     frag f[3], ds[2];
     f[0] = operand(0);
@@ -267,7 +273,11 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int z = 0; z < M; ++z) {
       __builtin_amdgcn_sched_barrier(0);
       if (z + 2 < M) f[(z + 2) % 3] = operand(z + 2);
-      if (z < NS) s2 = Frag<T>::mma(f[z % 3], q[z], s2);
+      if (z == 0) {
+        if (keep == kAll) s2 = Frag<T>::mma(f[0], q[0], f32x16{});
+        else s2 = Frag<T>::mma(f[0], q[0], scores_start(on, there));
+        dp2 = f32x16{};
+      } else if (z < NS) s2 = Frag<T>::mma(f[z % 3], q[z], s2);
       else if (z < A) dp2 = Frag<T>::mma(f[z % 3], dof[z - NS], dp2);
       else acc[(z - A) % ND] = Frag<T>::mma(f[z % 3], ds[(z - A) / ND], acc[(z - A) % ND]);
       if (z < A) {
@@ -291,9 +301,20 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
         else sr += x;
       }
     }
-    s = s2;
-    dp = dp2;
-    put(t + 2, last);
+  };
+  for (int t = t0; t < t1; ++t) {
+    int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
+    fetch(t + 2);
+    if constexpr (NB == 2) {
+      block(Const<0>{}, rel + t * BK, now, now, k0);
+      block(Const<1>{}, rel + t * BK + 32, now, nxt, k1);
+    } else {
+      block(Const<0>{}, rel + t * BK, now, nxt, k1);
+      sc[0] = sc[1];
+      pc[0] = pc[1];
+    }
+    k0 = k1;
+    k1 = put(t + 2, last);
     now = nxt;
     __syncthreads();
   }
@@ -333,11 +354,11 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
 }
 
-// 32 queries of one head a turn, the heads of the group one after the other; else like k_attend_dq.
+// 64 queries of one head a turn, the heads of the group one after the other; else like k_attend_dq.
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt) {
   typedef typename Frag<T>::type frag;
-  constexpr int BQ = 32, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
+  constexpr int NB = sizeof(T) == 2 ? 2 : 1, BQ = 32 * NB, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
   __shared__ __align__(16) char tile[3][2][kTile];    // Q, dO
   __shared__ __align__(16) float stat[3][3][BQ];      // lo, delta (scaled like dS), hi
   extern __shared__ float dyn[];                      // with a table: bias line
@@ -383,7 +404,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     if (fi >= qn) fi = 0, ++fh;
   };
   auto put = [&](int at) {
-    uint64_t keep = __ballot(lo != __builtin_inff()) & 0xffffffffull;
+    uint64_t keep = __ballot(lo != __builtin_inff()) & (NB == 2 ? ~0ull : 0xffffffffull);
     sq.store(tile[at][0], keep, tid);
     sd.store(tile[at][1], keep, tid);
     if (tid < BQ) {
@@ -393,7 +414,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     }
     return __any(hi != 0.f);
   };
-  f32x16 dk[ND], dv[ND], s = f32x16{}, dp = f32x16{};
+  f32x16 dk[ND], dv[ND], sc[2], pc[2];       // of a turn's two blocks: scores, dP
+  sc[0] = pc[0] = f32x16{};
 #pragma unroll
   for (int n = 0; n < ND; ++n) dk[n] = dv[n] = f32x16{};
   float left = 0.f, right = 0.f;
@@ -409,30 +431,25 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   __syncthreads();
   if (t0 < t1) {
 #pragma unroll
-    for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 0, k, lane), kf[k], s);
+    for (int k = 0; k < NS; ++k) sc[0] = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 0, k, lane), kf[k], sc[0]);
 #pragma unroll
-    for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), vf[k], dp);
+    for (int k = 0; k < NS; ++k) pc[0] = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), vf[k], pc[0]);
   }
   int now = 0;
-  for (int t = t0; t < t1; ++t) {
-    if (ln && (i0 == 0 || t == t0)) {                     // another head: its bias line (nobody reads the old one any more)
-      fill_line<T>(dyn, a, h, tid, 256);
-      __syncthreads();
-      left = uniform(ln[kPad]);
-      right = uniform(ln[2 * far + kPad]);
-    }
-    int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
-    fetch();
+  // Block of the turn at buffer `at` (rel0: its differences, wide: whether it has a `hi`); the next block: rows 32 (block ^ 1) on of buffer `on`.
+  auto block = [&](auto block_, int rel0, int at, int on, bool wide) {
+    constexpr int B = decltype(block_)::value, here = NB == 2 ? 32 * B : 0, there = NB == 2 ? 32 * (B ^ 1) : 0;   // rows in their tiles
+    f32x16 &s = sc[B], &dp = pc[B], &s2 = sc[B ^ 1], &dp2 = pc[B ^ 1];
     float mul = a.c2, add = 0.f;
-    if (ln) add_bias<false>(s, a.c2, ln, far, rel - i0, left, right, lane, mul, add);
-    const float* st = stat[now][0] + 4 * half;
+    const float* st = stat[at][0] + here + 4 * half;
     f32x4 l4[4], d4[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       l4[n] = *(const f32x4*)(st + 8 * n);
       d4[n] = *(const f32x4*)(st + BQ + 8 * n);
     }
-    if (c0) {
+    if (ln) add_bias<false>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
+    if (wide) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         f32x4 h4 = *(const f32x4*)(st + 2 * BQ + 8 * n);
@@ -443,13 +460,13 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       add = 0.f;
     }
     add += kLift;
-    const char *qn1 = tile[nxt][0], *dn1 = tile[nxt][1], *qo = tile[now][0], *od = tile[now][1];
-    f32x16 s2 = f32x16{}, dp2 = f32x16{};
+    const char *qt = tile[on][0], *dt = tile[on][1], *qo = tile[at][0], *od = tile[at][1];
+    s2 = dp2 = f32x16{};
     constexpr int A = 2 * NS, M = A + 4 * ND;
     auto operand = [&](int z) {
-      return z < NS ? row_frag<T, DP>(qn1, 0, z, lane)
-             : z < A ? row_frag<T, DP>(dn1, 0, z - NS, lane)
-                     : col_frag<T, DP>((z - A) / ND % 2 ? qo : od, 16 * ((z - A) / (2 * ND)), 32 * ((z - A) % ND), lane);
+      return z < NS ? row_frag<T, DP>(qt, there, z, lane)
+             : z < A ? row_frag<T, DP>(dt, there, z - NS, lane)
+                     : col_frag<T, DP>((z - A) / ND % 2 ? qo : od, here + 16 * ((z - A) / (2 * ND)), 32 * ((z - A) % ND), lane);
     };
     frag f[3], p[2], ds[2];
     f[0] = operand(0);
@@ -475,8 +492,24 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    s = s2;
-    dp = dp2;
+  };
+  for (int t = t0; t < t1; ++t) {
+    if (ln && (i0 == 0 || t == t0)) {        // another head: its bias line (nobody reads the old one any more)
+      fill_line<T>(dyn, a, h, tid, 256);
+      __syncthreads();
+      left = uniform(ln[kPad]);
+      right = uniform(ln[2 * far + kPad]);
+    }
+    int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
+    fetch();
+    if constexpr (NB == 2) {
+      block(Const<0>{}, rel - i0, now, now, c0);
+      block(Const<1>{}, rel - i0 - 32, now, nxt, c0);
+    } else {
+      block(Const<0>{}, rel - i0, now, nxt, c0);
+      sc[0] = sc[1];
+      pc[0] = pc[1];
+    }
     c0 = c1;
     c1 = put(last);
     now = nxt;
