@@ -2155,10 +2155,11 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
   return BBMM_OK;
 }
 
-// How the forward pass is laid out.  Few rows per shared head (kAttFewRows): the kernel that packs them and splits the keys over its
-// waves; else 128 queries of a head per workgroup.  The keys are split over workgroups while those do not fill the device twice and
-// a part keeps at least kAttFewPart (kAttPart) keys.
-constexpr int64_t kAttFewRows = 32, kAttFewPart = 256, kAttPart = 512;
+// How the forward pass is laid out.  Up to kAttFewRows rows per shared head: the kernel that packs them and splits the keys over its
+// waves; else 128 queries of a head per workgroup.  The keys are split over workgroups while those fill the device less than twice over and
+// a part keeps at least kAttPart keys.  (Parts that only round the device up do not pay: 8 x 12 heads, 512 x 640, 384 workgroups, training step in
+// two parts 145 us, in one 103.)
+constexpr int64_t kAttFewRows = 32, kAttPart = 256;
 struct AttPlan {
   bool few;
   int nsplit;
@@ -2168,15 +2169,15 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
   int64_t rows = (int64_t)a.nq * a.G;
   p.few = rows <= kAttFewRows;
   int64_t wgs = p.few ? (int64_t)a.B * a.HK * ((rows + 31) / 32) : (int64_t)a.B * a.H * ((a.nq + 127) / 128);
-  int64_t part = p.few ? kAttFewPart : kAttPart;
-  int64_t want = (2 * c->num_cus + wgs - 1) / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, a.nk / part);
+  int64_t want = 2 * c->num_cus / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, a.nk / kAttPart);
   p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
   return p;
 }
 
 // The gradient's two passes likewise: the keys of the dQ pass and the queries (of all heads of a group) of the dK, dV pass are split while the
-// workgroups do not fill the device and a part keeps at least kGradPart rows.
-constexpr int64_t kGradPart = 256;
+// workgroups do not fill the device and a part keeps at least kGradPart rows (fp32, 2 x 8 heads, 500 x 1000, training step: 239 us with parts of
+// 256 and 512 forward, 165 with these).
+constexpr int64_t kGradPart = 128;
 void gradient_plan(const bbmm_ctx* c, const AttArgs& a, int* qsplit, int* ksplit) {
   auto parts = [&](int64_t wgs, int64_t rows) {
     int64_t want = wgs > 0 ? (c->num_cus + wgs - 1) / wgs : 1, most = std::max<int64_t>(1, rows / kGradPart);

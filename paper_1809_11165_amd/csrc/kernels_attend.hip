@@ -280,6 +280,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
   frag q[NS], kf[NS];
   char* vt = buf + wave * kVt;
   u32x4 vr[kLds ? NV : 1];
+  frag vf[kLds ? 1 : 2][kLds ? 1 : ND];      // fp32: V as the product wants it, straight from memory
   uint8_t mb = 0, mnext = 0;
   // rows of a 32-key block from memory, with bounds
   auto block = [&](const T* base, int64_t stride, int t, int width) {
@@ -325,6 +326,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
           p += (int64_t)(64 / CH) * a.vs[1];
         }
       }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            int r = 16 * u + 8 * (e >> 2) + 4 * half + (e & 3), c = 32 * n + col;
+            if constexpr (VEC) {
+              __amdgpu_buffer_rsrc_t mem = block(V, a.vs[1], t, a.dv);
+              unsigned at = c < a.dv ? (unsigned)r * (unsigned)a.vs[1] * 4 + 4 * c : kNowhere;
+              vf[u][n][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(mem, at, 0, 0));
+            } else {
+              vf[u][n][e] = t * 32 + r < kn && c < a.dv ? V[(int64_t)(t * 32 + r) * a.vs[1] + c] : (T)0.f;
+            }
+          }
     }
   };
   f32x16 acc[ND];
@@ -375,7 +392,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
     for (int k = 0; k < NS; ++k) s = Frag<T>::mma(kf[k], q[k], s);
     if (t + 4 < t1) {
       fetch_k(t + 4);
-      fetch_v(t + 4);
+      if constexpr (kLds) fetch_v(t + 4);
     }
     int rel0 = rel + t * 32;                   // of the first key and the first query
     if (!a.table || rel0 + 31 <= -a.bk.far || rel0 - 31 >= a.bk.far) {
@@ -417,16 +434,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_attend_few(AttA
         if constexpr (kLds) {
           v = col_frag<T, DP>(vt, 16 * u, 32 * c, lane);
         } else {
+          v = vf[u][c];
+          if (keep != 0xffffffffu) {
+            unsigned k = keep >> (16 * u + 4 * half);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            int r = 16 * u + 8 * (e >> 2) + 4 * half + (e & 3), cc = 32 * c + col;
-            v[e] = ((keep >> r) & 1) && cc < a.dv ? V[(int64_t)(t * 32 + r) * a.vs[1] + cc] : (T)0.f;
+            for (int e = 0; e < 8; ++e) v[e] = ((k >> (8 * (e >> 2) + (e & 3))) & 1) ? v[e] : (T)0.f;
           }
         }
         acc[c] = Frag<T>::mma(v, p, acc[c]);
       }
     }
     if constexpr (kLds) __builtin_amdgcn_wave_barrier();
+    else if (t + 4 < t1) fetch_v(t + 4);
   }
   // join the four waves: each scales its sums to the largest reference; two leave theirs in LDS, the other two add them, all write
   l = both_sum(l);
