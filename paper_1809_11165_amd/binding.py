@@ -235,17 +235,23 @@ def _type_of(tensor, name):
 
 
 def _check_same(tensor, shape, dtype, device, name, dense=True):
-    """A tensor of this shape, type and device; dense, or with its last dimension contiguous."""
-    if getattr(tensor, "dtype", None) is not dtype:
+    """A tensor of this shape, type and device; dense, or with its last dimension contiguous.  (The first line is the
+    usual way through: a few tenths of a microsecond of a call's ten.)"""
+    try:
+        if (tensor.dtype is dtype and tensor.shape == shape and tensor.device == device
+                and (tensor.is_contiguous() or (not dense and tensor.stride(-1) == 1))):
+            return
+    except AttributeError:
+        raise TypeError("%s must be a tensor of type %s" % (name, dtype)) from None
+    if tensor.dtype is not dtype:
         raise TypeError("%s must be a tensor of type %s" % (name, dtype))
     if tensor.device != device:
         raise ValueError("%s is on %s, expected %s" % (name, tensor.device, device))
     if tensor.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(tensor.shape), tuple(shape)))
     if dense:
-        if not tensor.is_contiguous():
-            raise ValueError("%s must be contiguous" % name)
-    elif tensor.stride(-1) != 1 and shape[-1] > 1 and tensor.numel():
+        raise ValueError("%s must be contiguous" % name)
+    if shape[-1] > 1 and tensor.numel():
         raise ValueError("the last dimension of %s must be contiguous" % name)
 
 
@@ -304,11 +310,14 @@ class Attention:
     def to_c(self, device) -> _Attention:
         Q, K, V, table = self.Q, self.K, self.V, self.table
         code, t = _type_of(Q, "Q"), Q.dtype
-        _type_of(K, "K"), _type_of(V, "V")
-        if Q.dim() != 4 or K.dim() != 4 or V.dim() != 4:
-            raise ValueError("Q, K and V must have four dimensions (batch, row, head, feature)")
-        b, nq, h, d = Q.shape
-        _, nk, hk, dv = V.shape
+        try:
+            b, nq, h, d = Q.shape
+            _, nk, hk, dv = V.shape
+            _, _, _, _ = K.shape
+        except ValueError:
+            raise ValueError("Q, K and V must have four dimensions (batch, row, head, feature)") from None
+        except AttributeError:
+            raise TypeError("Q, K and V must be tensors") from None
         _check_same(Q, (b, nq, h, d), t, device, "Q", dense=False)
         _check_same(K, (b, nk, hk, d), t, device, "K", dense=False)
         _check_same(V, (b, nk, hk, dv), t, device, "V", dense=False)
@@ -373,6 +382,7 @@ class Context:
         self.torch = torch
         self.device = torch.device("cuda", device)
         self._stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._raw_stream = self._stream.cuda_stream
         handle = C.c_void_p()
         rc = self.lib.bbmm_create(C.byref(handle), device, C.c_void_p(self._stream.cuda_stream))
         if rc != OK:
@@ -584,9 +594,9 @@ class Context:
         the caller's stream, the work waits for what the caller has queued, the caller's stream waits for the work, and
         no tensor's memory is reused before both are done."""
         torch = self.torch
-        here = torch.cuda.current_stream(self.device)
-        if here.cuda_stream == self._stream.cuda_stream:
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
             return call()
+        here = torch.cuda.current_stream(self.device)
         self._stream.wait_stream(here)
         with torch.cuda.stream(self._stream):
             out = call()
@@ -603,7 +613,7 @@ class Context:
         if nbytes == 0:
             return None, None, 0
         w = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
-        return w, _dptr(w), nbytes
+        return w, w.data_ptr(), nbytes
 
     def _attend_bytes(self, a: _Attention, grad: bool) -> int:
         n = C.c_int64(0)
@@ -619,10 +629,11 @@ class Context:
         a = att.to_c(self.device)
 
         def call():
-            O = self.torch.empty(a.batch, a.nq, a.heads, a.dv, dtype=att.Q.dtype, device=self.device)
-            lse = self._empty(a.batch, a.heads, a.nq)
+            b, h, nq = a.batch, a.heads, a.nq
+            O = self.torch.empty((b, nq, h, a.dv), dtype=att.Q.dtype, device=self.device)
+            lse = self.torch.empty((b, h, nq), dtype=self.torch.float32, device=self.device)
             w, wp, n = self._work(self._attend_bytes(a, False))
-            self._ck(self.lib.bbmm_attend(self.h, C.byref(a), _dptr(O), _dptr(lse), wp, n))
+            self._ck(self.lib.bbmm_attend(self.h, C.byref(a), O.data_ptr(), lse.data_ptr(), wp, n))
             return O, lse
 
         return self._ordered(att.tensors(), call)
@@ -641,8 +652,9 @@ class Context:
             dQ, dK, dV = (self.torch.empty(x.shape, dtype=x.dtype, device=self.device) for x in (att.Q, att.K, att.V))
             dtable = None if att.table is None else self.torch.empty_like(att.table)
             w, wp, n = self._work(self._attend_bytes(a, True))
-            self._ck(self.lib.bbmm_attend_grad(self.h, C.byref(a), _dptr(O), _dptr(lse), _dptr(dO), stride, _dptr(dQ),
-                                               _dptr(dK), _dptr(dV), None if dtable is None else _dptr(dtable), wp, n))
+            self._ck(self.lib.bbmm_attend_grad(self.h, C.byref(a), O.data_ptr(), lse.data_ptr(), dO.data_ptr(), stride,
+                                               dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(),
+                                               None if dtable is None else dtable.data_ptr(), wp, n))
             return dQ, dK, dV, dtable
 
         return self._ordered(att.tensors() + [O, lse, dO], call)
@@ -654,8 +666,8 @@ class Context:
 
         def call():
             B = self.torch.empty(table.shape[0], nq, nk, dtype=table.dtype, device=self.device)
-            self._ck(self.lib.bbmm_bucket_bias(self.h, kind, _dptr(table), table.shape[0], nq, nk, len(e), e,
-                                               int(bool(two_sided)), int(start), _dptr(B)))
+            self._ck(self.lib.bbmm_bucket_bias(self.h, kind, table.data_ptr(), table.shape[0], nq, nk, len(e), e,
+                                               int(bool(two_sided)), int(start), B.data_ptr()))
             return B
 
         return self._ordered([table], call)
@@ -678,8 +690,8 @@ class Context:
         def call():
             dtable = self.torch.empty(h, (len(e) + 1) * (2 if two_sided else 1), dtype=dB.dtype, device=self.device)
             w, wp, n = self._work(self.bbmm_bucket_bias_workspace(b, h, nq, nk, len(e), two_sided))
-            self._ck(self.lib.bbmm_bucket_bias_grad(self.h, kind, _dptr(dB), b, h, nq, nk, len(e), e, int(bool(two_sided)),
-                                                    int(start), _dptr(dtable), wp, n))
+            self._ck(self.lib.bbmm_bucket_bias_grad(self.h, kind, dB.data_ptr(), b, h, nq, nk, len(e), e, int(bool(two_sided)),
+                                                    int(start), dtable.data_ptr(), wp, n))
             return dtable
 
         return self._ordered([dB], call)
