@@ -439,7 +439,7 @@ typedef struct {
 } bbmm_attention;
 
 /* Bytes of device workspace (16-byte aligned) that bbmm_attend (grad 0) or bbmm_attend_grad (grad 1) needs for these sizes;
- * may be 0.  bytes: host.  Pointers of `in` are not read, only whether a table is there. */
+ * may be 0.  bytes: host.  What `in` points to is not read, only whether a table and k_len are there. */
 int bbmm_attend_workspace(bbmm_ctx* ctx, const bbmm_attention* in, int32_t grad, int64_t* bytes);
 
 /* O (device, batch x nq x heads x dv) and lse (device, batch x heads x nq float). */

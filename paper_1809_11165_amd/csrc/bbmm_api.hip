@@ -2136,7 +2136,7 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
   a->B = (int)in->batch, a->H = (int)in->heads, a->HK = (int)in->kv_heads, a->G = a->H / a->HK;
   a->nq = (int)in->nq, a->nk = (int)in->nk, a->d = (int)in->d, a->dv = (int)in->dv;
   a->scale = (float)in->scale, a->c2 = (float)(in->scale * 1.4426950408889634);
-  a->table = in->table;
+  a->table = in->table, a->k_len = in->k_len;
   int64_t rows = std::max<int64_t>((in->nq + 127) / 128 * in->heads, (in->nk + 127) / 128 * in->kv_heads);
   if (in->batch * rows > kAttMaxGrid || in->batch * in->heads * in->nq > 16 * kAttMaxGrid || in->batch * in->kv_heads * in->nk > 16 * kAttMaxGrid)
     return fail(c, BBMM_EINVAL, "attention: more than 2^27 rows in one call");
@@ -2150,16 +2150,17 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
   memcpy(a->qs, in->q_stride, sizeof a->qs);
   memcpy(a->ks, in->k_stride, sizeof a->ks);
   memcpy(a->vs, in->v_stride, sizeof a->vs);
-  a->q_len = in->q_len, a->k_len = in->k_len, a->mask = in->key_mask, a->mask_s = in->nk, a->q_start = in->q_start;
+  a->q_len = in->q_len, a->mask = in->key_mask, a->mask_s = in->nk, a->q_start = in->q_start;
   a->qvec = wide_rows(a->Q, a->qs, a->d, e, 16), a->kvec = wide_rows(a->K, a->ks, a->d, e, 16), a->vvec = wide_rows(a->V, a->vs, a->dv, e, 16);
   return BBMM_OK;
 }
 
 // How the forward pass is laid out.  Up to kAttFewRows rows per shared head: the kernel that packs them and splits the keys over its
-// waves; else 128 queries of a head per workgroup.  The keys are split over workgroups while those fill the device less than twice over and
+// waves; else 128 queries of a head per workgroup (64 rows, packed / not, us: 4 x 8 shared heads of 4, 16 x 8000, d = 128, bf16 50 / 78;
+// 4 x 8 heads, 64 x 4000, d = 64, fp32 35 / 54, bf16 20.8 / 19.7; 96 rows: equal).  The keys are split over workgroups while those fill the device less than twice over and
 // a part keeps at least kAttPart keys.  (Parts that only round the device up do not pay: 8 x 12 heads, 512 x 640, 384 workgroups, training step in
 // two parts 145 us, in one 103.)
-constexpr int64_t kAttFewRows = 32, kAttPart = 256;
+constexpr int64_t kAttFewRows = 64, kAttPart = 256, kAttEvenPart = 1024;
 struct AttPlan {
   bool few;
   int nsplit;
@@ -2171,6 +2172,9 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
   int64_t wgs = p.few ? (int64_t)a.B * a.HK * ((rows + 31) / 32) : (int64_t)a.B * a.H * ((a.nq + 127) / 128);
   int64_t want = 2 * c->num_cus / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, a.nk / kAttPart);
   p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
+  // Lengths of the caller's: smaller parts even them out (8 requests of 32773 .. 18437 keys, 8 heads of 128: 170 us in 8 parts each, 155 in 32;
+  // equal lengths of 30000 in fp32 lose: 106 and 177).
+  if (p.few && a.k_len) p.nsplit = (int)std::max<int64_t>(p.nsplit, std::min(8 * c->num_cus / std::max<int64_t>(wgs, 1), a.nk / kAttEvenPart));
   return p;
 }
 
