@@ -26,23 +26,22 @@ __global__ __launch_bounds__(256) void k_bucket_bias(const T* __restrict__ table
   int64_t r1 = min((int64_t)nq, (int64_t)(blockIdx.x + 1) * rows);
   for (int64_t i = (int64_t)blockIdx.x * rows + wave; i < r1; i += 4) {
     T* row = out + ((int64_t)h * nq + i) * nk;
-    int64_t off = i + start;
-    int lead = (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T);
-    if (lead > nk) lead = (int)nk;
-    int64_t body = (nk - lead) / E, tail = lead + body * E;
-    if (lane < lead) row[lane] = line[min(max(clamp_rel(lane - off), -far), far) + far + kPad];
-    if (tail + lane < nk) row[tail + lane] = line[min(max(clamp_rel(tail + lane - off), -far), far) + far + kPad];
-    for (int64_t c = lane; c < body; c += 64) {
-      int64_t j = lead + c * E;
-      int r = clamp_rel(j - off);
-      u32x4 v;
-      if (r + E - 1 <= -far) v = lv;
-      else if (r >= far) v = rv;
-      else {
+    int rest = rest_below(-(i + start)), n = (int)nk;        // difference of column j: j + rest
+    int lead = min((int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T), n);
+    int body = (n - lead) / E, tail = lead + body * E;
+    if (lane < lead) row[lane] = line[min(max(lane + rest, -far), far) + far + kPad];
+    if (tail + lane < n) row[tail + lane] = line[min(max(tail + lane + rest, -far), far) + far + kPad];
+    u32x4* to = (u32x4*)(row + lead);
+    int r0 = lead + rest;
+    const T* from = line + far + kPad;
+    for (int c = lane; c < body; c += 64) {
+      int r = r0 + c * E;
+      u32x4 v = r < 0 ? lv : rv;
+      if (r + E - 1 > -far && r < far) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&v)[e] = line[r + e + far + kPad];
+        for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&v)[e] = from[r + e];
       }
-      *(u32x4*)(row + j) = v;
+      to[c] = v;
     }
   }
 }
@@ -74,26 +73,26 @@ __global__ __launch_bounds__(256) void k_bucket_grad(const T* __restrict__ dB, A
   float sl = 0.f, sr = 0.f;
   for (int64_t i = i0 + wave; i < i1; i += 4) {
     const T* row = mat + i * nk;
-    int64_t off = i + start;
-    int lead = (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T);
-    if (lead > nk) lead = (int)nk;
-    int64_t body = (nk - lead) / E, tail = lead + body * E;
-    auto one = [&](int64_t j) {
-      int r = clamp_rel(j - off);
+    int rest = rest_below(-(i + start)), n = (int)nk;        // difference of column j: j + rest
+    int lead = min((int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T), n);
+    int body = (n - lead) / E, tail = lead + body * E;
+    auto one = [&](int j) {
+      int r = j + rest;
       if (r <= -far) sl += (float)row[j];
       else if (r >= far) sr += (float)row[j];
     };
     if (lane < lead) one(lane);
-    if (tail + lane < nk) one(tail + lane);
-    for (int64_t c0 = lane; c0 < body; c0 += 4 * 64) {
+    if (tail + lane < n) one(tail + lane);
+    const u32x4* at = (const u32x4*)(row + lead);
+    for (int c0 = lane; c0 < body; c0 += 4 * 64) {
       u32x4 v[4];
       int r[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {                         // four loads in flight; what lies between the edges is not read
-        int64_t c = c0 + 64 * k, j = lead + c * E;
-        r[k] = clamp_rel(j - off);
+        int c = c0 + 64 * k;
+        r[k] = lead + c * E + rest;
         v[k] = u32x4{0u, 0u, 0u, 0u};
-        if (c < body && (r[k] <= -far || r[k] + E - 1 >= far)) v[k] = *(const u32x4*)(row + j);
+        if (c < body && (r[k] <= -far || r[k] + E - 1 >= far)) v[k] = at[c];
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
