@@ -2182,13 +2182,26 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
 // workgroups do not fill the device and a part keeps at least kGradPart rows (fp32, 2 x 8 heads, 500 x 1000, training step: 239 us with parts of
 // 256 and 512 forward, 165 with these).
 constexpr int64_t kGradPart = 128;
-void gradient_plan(const bbmm_ctx* c, const AttArgs& a, int* qsplit, int* ksplit) {
+// delta_i = do_i.o_i takes o_i as the forward pass rounded it.  Where a row holds few keys that is off by as much as dS is rounded (its error goes
+// with the square root of sum p^2), and more in the table's gradient, whose far buckets are small sums of large weights.  Rows of up to
+// kWholeRows keys (kWholeRowsTable with a table) form delta in fp32 from all their scores instead, two products more.  Against 64 bits, bf16, 500
+// queries, without / with: 8 keys: dQ 2.7e-3 / 2.4e-3, table 1.3e-2 / 1.8e-3; 32: table 4.3e-3 / 1.7e-3; 128: 2.9e-3 / 1.6e-3.  Left to the rounded o:
+// 500 keys 2.4e-3, 2000 3.2e-3 (of which the plain sum in fp32 has 2.6e-3).
+constexpr int64_t kWholeRows = 128, kWholeRowsTable = 256;
+struct GradPlan {
+  int qsplit, ksplit;
+  bool whole_rows;
+};
+GradPlan gradient_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
   auto parts = [&](int64_t wgs, int64_t rows) {
     int64_t want = wgs > 0 ? (c->num_cus + wgs - 1) / wgs : 1, most = std::max<int64_t>(1, rows / kGradPart);
     return (int)std::max<int64_t>(1, std::min(want, most));
   };
-  *qsplit = parts((int64_t)a.B * a.H * ((a.nq + 127) / 128), a.nk);
-  *ksplit = parts((int64_t)a.B * a.HK * ((a.nk + 127) / 128), (int64_t)a.nq * a.G);
+  GradPlan p;
+  p.whole_rows = two_bytes && a.nk <= (a.table ? kWholeRowsTable : kWholeRows);
+  p.qsplit = p.whole_rows ? 1 : parts((int64_t)a.B * a.H * ((a.nq + 127) / 128), a.nk);
+  p.ksplit = parts((int64_t)a.B * a.HK * ((a.nk + 127) / 128), (int64_t)a.nq * a.G);
+  return p;
 }
 
 // Offsets into the workspace, 256-byte steps.
@@ -2196,7 +2209,7 @@ size_t step256(size_t n) { return (n + 255) / 256 * 256; }
 struct AttWork {
   size_t pO, pl, delta, lo, hi, tsum, norms, pq, pk, pv, bytes;
 };
-AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
+AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_bytes) {
   AttWork w{};
   size_t rows = (size_t)a.B * a.H * a.nq;
   if (!grad) {
@@ -2208,8 +2221,7 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
     }
     return w;
   }
-  int qsplit, ksplit;
-  gradient_plan(c, a, &qsplit, &ksplit);
+  GradPlan p = gradient_plan(c, a, two_bytes);
   auto take = [&](size_t n) {
     size_t at = w.bytes;
     w.bytes += step256(n);
@@ -2219,11 +2231,11 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad) {
   w.delta = take(rows * sizeof(float));
   w.lo = take(rows * sizeof(float));
   w.hi = take(rows * sizeof(float));
-  w.tsum = take(a.table ? (size_t)a.H * a.B * qsplit * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float) : 0);
-  size_t keys = (size_t)a.B * a.HK * a.nk * ksplit * sizeof(float);
-  w.pq = take(qsplit > 1 ? rows * qsplit * a.d * sizeof(float) : 0);
-  w.pk = take(ksplit > 1 ? keys * a.d : 0);
-  w.pv = take(ksplit > 1 ? keys * a.dv : 0);
+  w.tsum = take(a.table ? (size_t)a.H * a.B * p.qsplit * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float) : 0);
+  size_t keys = (size_t)a.B * a.HK * a.nk * p.ksplit * sizeof(float);
+  w.pq = take(p.qsplit > 1 ? rows * p.qsplit * a.d * sizeof(float) : 0);
+  w.pk = take(p.ksplit > 1 ? keys * a.d : 0);
+  w.pv = take(p.ksplit > 1 ? keys * a.dv : 0);
   return w;
 }
 
@@ -2256,7 +2268,7 @@ int attend(bbmm_ctx* c, const bbmm_attention* in, void* O, float* lse, void* wor
   size_t e = in->type == BBMM_TYPE_F32 ? 4 : 2;
   if (!O || !lse || (uintptr_t)O % e || (uintptr_t)lse % 4) return fail(c, BBMM_EINVAL, "attention: O and lse are required");
   AttPlan p = attention_plan(c, a);
-  AttWork w = attention_work(c, a, false);
+  AttWork w = attention_work(c, a, false, e == 2);
   rc = check_work(c, work, work_bytes, w.bytes);
   if (rc) return rc;
   OnDevice dev(c->device);
@@ -2285,7 +2297,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   if (a.table && !dtable) return fail(c, BBMM_EINVAL, "attention: a table needs dtable");
   if (((uintptr_t)O | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV | (uintptr_t)dtable) % e || (uintptr_t)lse % 4)
     return fail(c, BBMM_EINVAL, "attention: pointer not aligned to its type");
-  AttWork w = attention_work(c, a, true);
+  AttWork w = attention_work(c, a, true, e == 2);
   rc = check_work(c, work, work_bytes, w.bytes);
   if (rc) return rc;
   OnDevice dev(c->device);
@@ -2300,7 +2312,8 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
   g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (unsigned*)((char*)work + w.norms);
   g.pq = (float*)((char*)work + w.pq), g.pk = (float*)((char*)work + w.pk), g.pv = (float*)((char*)work + w.pv);
-  gradient_plan(c, a, &g.qsplit, &g.ksplit);
+  GradPlan p = gradient_plan(c, a, e == 2);
+  g.qsplit = p.qsplit, g.ksplit = p.ksplit, g.whole_rows = p.whole_rows;
   hipStream_t s = c->stream;
   launch_attend_delta(s, in->type, a, g);
   if (rows) launch_attend_dq(s, in->type, a, g);
@@ -2378,7 +2391,7 @@ int bbmm_attend_workspace(bbmm_ctx* c, const bbmm_attention* in, int32_t grad, i
     int rc = attention_args(c, in, false, &a);
     if (rc) return rc;
     if (!bytes) return fail(c, BBMM_EINVAL, "attention: bytes is required");
-    *bytes = (int64_t)attention_work(c, a, grad != 0).bytes;
+    *bytes = (int64_t)attention_work(c, a, grad != 0, in->type != BBMM_TYPE_F32).bytes;
     return (int)BBMM_OK;
   });
 }

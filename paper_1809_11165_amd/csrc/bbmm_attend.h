@@ -52,6 +52,7 @@ struct AttGrad {
   float *delta, *lo, *hi;
   float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets
   unsigned* norms;               // fp16: bits of the largest |do_i| and |v_j|, 64 bytes per slot
+  int whole_rows;                // few keys: the dQ pass forms delta from the row itself
   int qsplit, ksplit;            // parts that the keys of the dQ pass, and the queries of the dK, dV pass, are split into
   float *pq, *pk, *pv;           // their results: parts x the size of dQ, dK, dV
 };

@@ -225,6 +225,43 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
   float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
   int rel = rest_below(-(int64_t)q0 - start_of(a, b));
+  if (g.whole_rows) {
+    // delta_i = sum_j p_ij dP_ij from the row itself, for this pass and (in g.delta) the next
+    float total = 0.f, sd = 0.f;
+    for (int t = 0; t < tiles; ++t) {
+      fetch(t);
+      uint64_t keep = put(t, 0);
+      settle();
+      __syncthreads();
+      if (ln) {
+        left = uniform(line[kPad]);
+        right = uniform(line[2 * far + kPad]);
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        f32x16 s = f32x16{}, dp = f32x16{};
+        if (keep != kAll) s = scores_start(0, 32 * n);
+#pragma unroll
+        for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 32 * n, k, lane), q[k], s);
+#pragma unroll
+        for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 32 * n, k, lane), dof[k], dp);
+        float mul = a.c2, add = 0.f;
+        if (ln) add_bias<true>(s, a.c2, ln, far, rel + t * BK + 32 * n, left, right, lane, mul, add);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float x = fmaf(s[r], mul, add) - hi;
+          x = __builtin_amdgcn_exp2f(x - lo);
+          total += x;
+          sd = fmaf(x, dp[r], sd);
+        }
+      }
+      __syncthreads();
+    }
+    total = both_sum(total);
+    sd = both_sum(sd);
+    delta = some && total != 0.f ? sd / total : 0.f;
+    if (half == 0 && i < qn) g.delta[row] = delta;
+  }
   if (t0 < t1) {
     fetch(t0);
     k0 = put(t0, 0);

@@ -275,6 +275,26 @@ def test_small_gradients_and_long_rows_in_fp16(ctx):
         assert np.abs(_host(x) - ref).max() <= 2 * 2.0 ** -24
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("nk", [1, 3, 8, 33, 100, 250])
+def test_short_rows_keep_the_precision_of_their_type(ctx, kind, nk):
+    """delta from the rounded o would cost rows of few keys several roundings in the table's gradient.  With delta from the scores the gradients
+    are off by one rounding of the output and (dQ, dK) one of dS each: 2 roundings of u in the 2-norm bound any mix of them, and 64 u32 the
+    fp32 sums."""
+    rng = np.random.default_rng(19)
+    att, dO = _case(rng, kind, 2, 4, 2, 300, nk, 64, 64, edges=EDGES, start=[-nk, nk // 2])
+    val, _ = _oracle(kind, att, dO)
+    O, lse = ctx.bbmm_attend(att)
+    dQ, dK, dV, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    u = A.UNIT[kind]
+    for name, x, units in (("dq", dQ, 2), ("dk", dK, 2), ("dv", dV, 2), ("dtable", dT, 1)):
+        size = np.linalg.norm(val[name])
+        if nk > 1 or name == "dv":                         # one key: weights one, dS zero
+            assert np.linalg.norm(_host(x) - val[name]) <= (units * u + 64 * A.U32) * size, name
+        else:
+            assert np.abs(_host(x)).max() <= 64 * A.U32 * 300 * 64
+
+
 @pytest.mark.parametrize("nq,nk", [(3, 700), (150, 700)])
 def test_gradients_against_differences(ctx, nq, nk):
     """sum(dO . O) along a random direction of all inputs together, fp32: central differences of step 2^-6 differ from the derivative by
