@@ -226,11 +226,13 @@ __device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* d
   }
 }
 
-// Adds the 32 x 32 block s (keys in the registers, queries in the lanes) along its diagonals: line[j - i] += sum, `line` pointing at
-// the difference of the first key and the first query, one line per half of the wave.  Halves first exchange registers so that each
+// Adds the 32 x 32 block s (keys in the registers, queries in the lanes) along its diagonals: line[j - i] += sum, `line` (the wave's own)
+// pointing at the difference of the first key and the first query.  Halves first exchange registers so that each
 // has 16 keys in a row; a sum then moves one lane per key, towards higher lanes for keys ahead (what leaves a row of 16 lanes
-// lies behind), towards lower ones for keys behind.  Two LDS additions per block, all lanes of a half at places of their own, instead of
-// sixteen (those made the dQ pass of 8 x 12 x 512 x 640 in bf16, d = 64, 104 us, see there).
+// lies behind), towards lower ones for keys behind.  Few LDS additions instead of sixteen of all lanes (dQ pass of 8 x 12 x 512 x 640 in bf16,
+// d = 64, when this was changed: 106 us to 44, with two additions and a line per half).  The halves share the wave's line, one adding after the
+// other and its lanes at places of their own, so that the order is fixed: a line per half left no room in LDS for d = 128 with an edge
+// past about 830, and the training step is no slower so (104.1 us, 105.3 with a line per half).
 __device__ __forceinline__ float from_lane_below(float x) {   // of the row of 16, zero into the first
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x111, 0xf, 0xf, true));
 }
@@ -254,8 +256,13 @@ __device__ __forceinline__ void add_diagonals(const f32x16& s, float* line, int 
     behind = from_lane_above(behind) + k[15 - i];
   }
   int q = lane & 15, base = 16 * (lane >> 5) - (lane & 16);
-  __hip_atomic_fetch_add(line + base + 15 - q, ahead, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-  if (q) __hip_atomic_fetch_add(line + base - q, behind, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if ((lane >> 5) == half) {
+      __hip_atomic_fetch_add(line + base + 15 - q, ahead, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      if (q) __hip_atomic_fetch_add(line + base - q, behind, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+  }
 }
 
 // A table entry in units of the base-2 exponent.  Finite entries stay finite: one below -2.3e38 counts as that (the same

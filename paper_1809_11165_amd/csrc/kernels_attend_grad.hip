@@ -150,7 +150,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   __shared__ __align__(16) char tile[3][2][kTile];   // K, V
   __shared__ __align__(16) float from[3][BK];        // what a key's scores start from: 0, or -infinity where it takes no part
   __shared__ float side[8];
-  extern __shared__ float dyn[];                     // with a table: bias line, then eight lines of diagonal sums (wave, half)
+  static_assert(sizeof tile + sizeof from + sizeof side + 5 * kLine * sizeof(float) <= 160 * 1024, "the longest line fits beside the tiles");
+  extern __shared__ float dyn[];                     // with a table: bias line, then a line of diagonal sums per wave
   int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt * g.qsplit);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int qt = id % nqt, sp = id / nqt % g.qsplit, bh = id / nqt / g.qsplit, h = bh % a.H, b = bh / a.H, hk = h / a.G;
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   const float* ln = nullptr;
   if (a.table) {
     fill_line<T>(line, a, h, tid, 256);
-    for (int n = tid; n < 8 * nline; n += 256) diag[n] = 0.f;
+    for (int n = tid; n < 4 * nline; n += 256) diag[n] = 0.f;
     ln = line;
   }
   float cs = ds_scale<T>(g, lane);                 // a power of two: dS is formed times it
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     __builtin_amdgcn_sched_barrier(0);
     if (ln) {
       if (where == 0) {
-        add_diagonals(s, diag + (2 * wave + half) * nline + rel0 + span, lane);
+        add_diagonals(s, diag + wave * nline + rel0 + span, lane);
       } else {
         float x = 0.f;
 #pragma unroll
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int n = tid; n < nline; n += 256) {
       float x = 0.f;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x += diag[k * nline + n];
+      for (int k = 0; k < 4; ++k) x += diag[k * nline + n];
       line[n] = x * f;
     }
     __syncthreads();
@@ -608,7 +609,7 @@ void delta_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
 template <typename T, bool VEC>
 void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int nqt = (a.nq + 127) / 128, grid = (a.B * a.H * nqt * g.qsplit + 7) / 8 * 8;
-  size_t lds = a.table ? sizeof(float) * 9 * (2 * (a.bk.far + kPad) + 1) : 0;
+  size_t lds = a.table ? sizeof(float) * 5 * (2 * (a.bk.far + kPad) + 1) : 0;
   if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
   else k_attend_dq<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
 }
