@@ -2155,21 +2155,23 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
   return BBMM_OK;
 }
 
-// How the forward pass is laid out.  Up to kAttFewRows rows per shared head: the kernel that packs them and splits the keys over its
-// waves; else 128 queries of a head per workgroup (64 rows, packed / not, us: 4 x 8 shared heads of 4, 16 x 8000, d = 128, bf16 50 / 78;
-// 4 x 8 heads, 64 x 4000, d = 64, fp32 35 / 54, bf16 20.8 / 19.7; 96 rows: equal).  The keys are split over workgroups while those fill the device less than twice over and
+// How the forward pass is laid out: 128 queries of a head per workgroup, or, up to kAttFewQueries queries, the kernel that packs the rows
+// (query, head) of a shared head by 32 and splits the keys over its waves, where its row blocks are no more than the tiles would be
+// (fp32, whose products are slow: twice as many).  us, packed / tiles: bf16, d = 128: 4 x 8 shared heads of 4, 16 x 8000 50 / 78; 4 of 4,
+// 12 x 20000 25 / 33; 2 of 32, 8 x 8000 23 / 45; d = 64: 2 x 1 of 100, 1 x 4000 18 / 60; 4 x 8 heads, 64 x 4000 (twice the tiles) bf16
+// 20.8 / 19.7, fp32 35 / 54.  The keys are split over workgroups while those fill the device less than twice over and
 // a part keeps at least kAttPart keys.  (Parts that only round the device up do not pay: 8 x 12 heads, 512 x 640, 384 workgroups, training step in
 // two parts 145 us, in one 103.)
-constexpr int64_t kAttFewRows = 64, kAttPart = 256, kAttEvenPart = 1024;
+constexpr int64_t kAttFewQueries = 64, kAttPart = 256, kAttEvenPart = 1024;
 struct AttPlan {
   bool few;
   int nsplit;
 };
-AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a) {
+AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
   AttPlan p;
-  int64_t rows = (int64_t)a.nq * a.G;
-  p.few = rows <= kAttFewRows;
-  int64_t wgs = p.few ? (int64_t)a.B * a.HK * ((rows + 31) / 32) : (int64_t)a.B * a.H * ((a.nq + 127) / 128);
+  int64_t blocks = ((int64_t)a.nq * a.G + 31) / 32, tiles = (int64_t)a.G * ((a.nq + 127) / 128);
+  p.few = a.nq <= kAttFewQueries && blocks <= (two_bytes ? 1 : 2) * tiles;
+  int64_t wgs = (int64_t)a.B * a.HK * (p.few ? blocks : tiles);
   int64_t want = 2 * c->num_cus / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, a.nk / kAttPart);
   p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
   // Lengths of the caller's: smaller parts even them out (8 requests of 32773 .. 18437 keys, 8 heads of 128: 170 us in 8 parts each, 155 in 32;
@@ -2213,7 +2215,7 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_
   AttWork w{};
   size_t rows = (size_t)a.B * a.H * a.nq;
   if (!grad) {
-    AttPlan p = attention_plan(c, a);
+    AttPlan p = attention_plan(c, a, two_bytes);
     if (p.nsplit > 1) {
       w.pO = 0;
       w.pl = step256(rows * p.nsplit * ((a.dv + 3) / 4 * 4) * sizeof(float));
@@ -2267,7 +2269,7 @@ int attend(bbmm_ctx* c, const bbmm_attention* in, void* O, float* lse, void* wor
   if (a.B == 0 || a.nq == 0) return BBMM_OK;
   size_t e = in->type == BBMM_TYPE_F32 ? 4 : 2;
   if (!O || !lse || (uintptr_t)O % e || (uintptr_t)lse % 4) return fail(c, BBMM_EINVAL, "attention: O and lse are required");
-  AttPlan p = attention_plan(c, a);
+  AttPlan p = attention_plan(c, a, e == 2);
   AttWork w = attention_work(c, a, false, e == 2);
   rc = check_work(c, work, work_bytes, w.bytes);
   if (rc) return rc;

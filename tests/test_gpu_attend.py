@@ -98,6 +98,8 @@ CASES = {
     "no_edges": (1, 2, 2, 45, 70, 64, 64, dict(edges=[])),
     "far_edges": (1, 1, 1, 200, 1400, 64, 64, dict(edges=[1, 100, 700, 1024], start=[300])),
     "far_edges_wide": (1, 2, 1, 150, 300, 128, 100, dict(edges=[3, 400, 1024], start=[80])),
+    "many_heads_one_query": (2, 100, 1, 1, 400, 64, 64, dict(edges=EDGES, start=[399, 200])),
+    "wide_group": (1, 24, 2, 33, 300, 40, 40, dict(edges=EDGES)),
     "empty_batches": (3, 2, 2, 50, 60, 64, 64, dict(k_len=[0, 60, 1], q_len=[50, 0, 50], edges=EDGES)),
     "empty_batches_few": (3, 2, 2, 2, 300, 64, 64, dict(k_len=[0, 300, 1], q_len=[2, 0, 1], edges=EDGES)),
     "split_rows": (1, 1, 1, 90, 2100, 64, 64, dict(edges=EDGES, start=[2000], k_len=[2050])),
