@@ -401,7 +401,7 @@ int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns
  *                 and sums are fp32; weights (and dS) are rounded to `type` once as operands of the second products.
  *   heads         query heads; kv_heads divides it, head h reads keys and values of head h / (heads / kv_heads)
  *   d, dv         features of queries and keys, and of values: 1 .. 128
- *   scale         finite and > 0
+ *   scale         > 0, scale / log 2 finite in fp32
  *   Q, K, V       device; element [b][row][head][feature] at b stride[0] + row stride[1] + head stride[2] + feature
  *                 (strides in elements, none negative; 0 shares an input, its gradient is then returned for every use)
  *   q_len, k_len  device, batch entries (taken as within [0, nq] and [0, nk]), or NULL: all rows

@@ -285,6 +285,11 @@ def _edges(edges):
     return (C.c_int32 * len(e)).from_buffer(e) if e else (C.c_int32 * 0)()
 
 
+def _int64(x):
+    """A whole number for an int64 argument: beyond that type, its ends (which the library refuses), not what is left of its bits."""
+    return min(max(int(x), -2 ** 63), 2 ** 63 - 1)
+
+
 @dataclass
 class Attention:
     """One attention call (see include/bbmm.h, "Attention").  Q (batch, nq, heads, d), K (batch, nk, kv_heads, d), V (batch,
@@ -328,7 +333,7 @@ class Attention:
             _check_same(table, (h, 2 * n + 2 if two else n + 1), t, device, "table")
         elif self.edges is not None:
             raise ValueError("edges without a table")
-        a = _Attention(code, two, b, h, hk, nq, nk, d, dv, d ** -0.5 if self.scale is None else self.scale, Q.data_ptr(),
+        a = _Attention(code, two, b, h, hk, nq, nk, d, dv, max(d, 1) ** -0.5 if self.scale is None else self.scale, Q.data_ptr(),
                        K.data_ptr(), V.data_ptr(), Q.stride()[:3], K.stride()[:3], V.stride()[:3])
         if table is not None:
             a.table, a.n_edges, a.edges = table.data_ptr(), n, edges
@@ -667,7 +672,7 @@ class Context:
         def call():
             B = self.torch.empty(table.shape[0], nq, nk, dtype=table.dtype, device=self.device)
             self._ck(self.lib.bbmm_bucket_bias(self.h, kind, table.data_ptr(), table.shape[0], nq, nk, len(e), e,
-                                               int(bool(two_sided)), int(start), B.data_ptr()))
+                                               int(bool(two_sided)), _int64(start), B.data_ptr()))
             return B
 
         return self._ordered([table], call)
@@ -691,7 +696,7 @@ class Context:
             dtable = self.torch.empty(h, (len(e) + 1) * (2 if two_sided else 1), dtype=dB.dtype, device=self.device)
             w, wp, n = self._work(self.bbmm_bucket_bias_workspace(b, h, nq, nk, len(e), two_sided))
             self._ck(self.lib.bbmm_bucket_bias_grad(self.h, kind, dB.data_ptr(), b, h, nq, nk, len(e), e, int(bool(two_sided)),
-                                                    int(start), dtable.data_ptr(), wp, n))
+                                                    _int64(start), dtable.data_ptr(), wp, n))
             return dtable
 
         return self._ordered([dB], call)

@@ -2129,7 +2129,8 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
     return fail(c, BBMM_EINVAL, "attention: batch and heads up to 65535, kv_heads must divide heads");
   if (in->nq < 0 || in->nq > kAttMaxLen || in->nk < 0 || in->nk > kAttMaxLen) return fail(c, BBMM_EINVAL, "attention: nq and nk up to 2^30");
   if (in->d < 1 || in->d > BBMM_ATT_MAXD || in->dv < 1 || in->dv > BBMM_ATT_MAXD) return fail(c, BBMM_EINVAL, "attention: d and dv from 1 to 128");
-  if (!(in->scale > 0.0) || !isfinite((float)in->scale) || !((float)in->scale > 0.f)) return fail(c, BBMM_EINVAL, "attention: scale must be finite and > 0");
+  if (!(in->scale > 0.0) || !isfinite((float)(in->scale * 1.4426950408889634)) || !((float)in->scale > 0.f))
+    return fail(c, BBMM_EINVAL, "attention: scale must be > 0, and finite in units of log 2");
   memset(a, 0, sizeof *a);
   int rc = set_buckets(c, in->table ? in->n_edges : 0, in->edges, in->two_sided, pointers && in->table, &a->bk);
   if (rc) return rc;
@@ -2144,6 +2145,7 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
   size_t e = in->type == BBMM_TYPE_F32 ? 4 : 2;
   if ((in->batch && in->nq && !in->Q) || (in->batch && in->nk && (!in->K || !in->V))) return fail(c, BBMM_EINVAL, "attention: Q, K and V are required");
   if (((uintptr_t)in->Q | (uintptr_t)in->K | (uintptr_t)in->V | (uintptr_t)in->table) % e) return fail(c, BBMM_EINVAL, "attention: pointer not aligned to its type");
+  if (((uintptr_t)in->q_len | (uintptr_t)in->k_len) % 4 || (uintptr_t)in->q_start % 8) return fail(c, BBMM_EINVAL, "attention: lengths or starts not aligned to their type");
   for (int k = 0; k < 3; ++k)
     if (in->q_stride[k] < 0 || in->k_stride[k] < 0 || in->v_stride[k] < 0) return fail(c, BBMM_EINVAL, "attention: negative stride");
   a->Q = in->Q, a->K = in->K, a->V = in->V;

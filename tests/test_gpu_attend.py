@@ -456,3 +456,47 @@ def test_refusals_of_the_library(ctx):
     # the context still works
     again = ctx.bbmm_attend(att)
     assert torch.equal(again[0], O) and torch.equal(again[1], lse)
+
+
+def test_refusals_of_scales_lengths_and_starts(ctx):
+    import ctypes as C
+    from paper_1809_11165_amd import binding
+    att, dO = _case(np.random.default_rng(21), "f32", 2, 2, 2, 5, 9, 16, 16)
+    O, lse = ctx.bbmm_attend(att)
+    for change in (dict(scale=3e38), dict(q_len=2), dict(k_len=1), dict(q_start=4)):      # the last three: addresses off by that much
+        a = att.to_c(ctx.device)
+        for name, x in change.items():
+            setattr(a, name, x if name == "scale" else O.data_ptr() + x)
+        rc = ctx.lib.bbmm_attend(ctx.h, C.byref(a), binding._dptr(O), binding._dptr(lse), None, 0)
+        assert rc == binding.EINVAL, change
+    none = binding.Attention(att.Q[..., :0], att.K[..., :0], att.V)
+    with pytest.raises(binding.BbmmError) as e:
+        ctx.bbmm_attend(none)
+    assert e.value.code == binding.EINVAL
+
+
+def test_two_contexts_at_work_at_once():
+    """Each on a stream of its own, their calls queued in turn without a wait between: the results are those of a context alone."""
+    from paper_1809_11165_amd import binding
+    rng = np.random.default_rng(22)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    ctxs = [binding.Context(0, stream=s) for s in streams]
+    cases = [_case(rng, "f16", 2, 4, 2, 300, 700, 64, 64, edges=EDGES), _case(rng, "bf16", 2, 8, 2, 1, 5000, 128, 128, edges=EDGES)]
+
+    def step(k):
+        with torch.cuda.stream(streams[k]):
+            O, lse = ctxs[k].bbmm_attend(cases[k][0])
+            return (O, lse) + ctxs[k].bbmm_attend_grad(cases[k][0], O, lse, cases[k][1])
+
+    torch.cuda.synchronize()
+    want = []
+    for k in (0, 1):
+        want.append(step(k))
+        torch.cuda.synchronize()
+    got = [[step(k) for k in (0, 1)] for _ in range(10)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for k in (0, 1):
+            assert all(torch.equal(x, y) for x, y in zip(pair[k], want[k]))
+    for c in ctxs:
+        c.close()

@@ -114,3 +114,13 @@ def test_the_matrix_is_the_bias_that_the_attention_adds(ctx, kind):
     by_matrix = _host(ctx.bbmm_bucket_bias_grad(dS, edges, start=start))
     mag = A.table_grad(ds, edges, True, start)[1]
     assert np.all(np.abs(_host(dT) - by_matrix) <= err["dtable"] + ((nq + nk) * A.U32 + A.U32) * mag)
+
+
+@pytest.mark.parametrize("start", [1 << 64, (1 << 64) + 5, -(1 << 70)])
+def test_starts_beyond_64_bits_are_refused(ctx, start):
+    from paper_1809_11165_amd import binding
+    table = _rand(np.random.default_rng(5), "f32", 2, 18)
+    with pytest.raises(binding.BbmmError):
+        ctx.bbmm_bucket_bias(table, EDGES, 4, 4, start=start)
+    with pytest.raises(binding.BbmmError):
+        ctx.bbmm_bucket_bias_grad(torch.zeros(1, 2, 4, 4, device=DEV), EDGES, start=start)
