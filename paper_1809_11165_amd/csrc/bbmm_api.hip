@@ -2162,7 +2162,7 @@ int attention_args(bbmm_ctx* c, const bbmm_attention* in, bool pointers, AttArgs
 // (fp32, whose products are slow: twice as many).  us, packed / tiles: bf16, d = 128: 4 x 8 shared heads of 4, 16 x 8000 50 / 78; 4 of 4,
 // 12 x 20000 25 / 33; 2 of 32, 8 x 8000 23 / 45; d = 64: 2 x 1 of 100, 1 x 4000 18 / 60; 4 x 8 heads, 64 x 4000 (twice the tiles) bf16
 // 20.8 / 19.7, fp32 35 / 54.  The keys are split over workgroups while those fill the device less than twice over and
-// a part keeps at least kAttPart keys.  (Parts that only round the device up do not pay: 8 x 12 heads, 512 x 640, 384 workgroups, training step in
+// parts keep about kAttPart keys.  (Parts that only round the device up do not pay: 8 x 12 heads, 512 x 640, 384 workgroups, training step in
 // two parts 145 us, in one 103.)
 constexpr int64_t kAttFewQueries = 64, kAttPart = 256, kAttEvenPart = 1024;
 struct AttPlan {
@@ -2174,7 +2174,7 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
   int64_t blocks = ((int64_t)a.nq * a.G + 31) / 32, tiles = (int64_t)a.G * ((a.nq + 127) / 128);
   p.few = a.nq <= kAttFewQueries && blocks <= (two_bytes ? 1 : 2) * tiles;
   int64_t wgs = (int64_t)a.B * a.HK * (p.few ? blocks : tiles);
-  int64_t want = 2 * c->num_cus / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, a.nk / kAttPart);
+  int64_t want = 2 * c->num_cus / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, (a.nk + kAttPart - 1) / kAttPart);
   p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
   // Lengths of the caller's: smaller parts even them out (8 requests of 32773 .. 18437 keys, 8 heads of 128: 170 us in 8 parts each, 155 in 32;
   // equal lengths of 30000 in fp32 lose: 106 and 177).
@@ -2322,6 +2322,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   launch_attend_delta(s, in->type, a, g);
   if (rows) launch_attend_dq(s, in->type, a, g);
   if (keys) launch_attend_dkv(s, in->type, a, g);
+  launch_attend_sums(s, in->type, a, g);
   if (a.table) launch_bucket_join(s, in->type, g.tsum, a.B * g.qsplit * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
   HIPCHK(c, hipGetLastError());
   return BBMM_OK;

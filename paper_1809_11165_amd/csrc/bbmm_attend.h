@@ -64,6 +64,7 @@ void launch_attend_join(hipStream_t s, int type, const AttArgs& a, const AttOut&
 void launch_attend_delta(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_dq(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_dkv(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
+void launch_attend_sums(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);   // adds up what the two passes left in parts
 
 // The bias as a matrix (heads x nq x nk, `rows` rows per workgroup), and the sums of a matrix's gradient (batch x heads x nq x nk) by bucket:
 // tsum holds heads x (batch ceil(nq / rows)) x buckets floats, which launch_bucket_join adds up.
