@@ -96,19 +96,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
   int64_t kstep = BK * a.ks[1], vstep = BK * a.vs[1];
   const float* ln = nullptr;
   if (t0 < t1) {
+    // all loads are queued before the first is waited for
+    Stage<T, DP, BK, VEC> s0, s1;
+    s0.load(kp, a.ks[1], kn - t0 * BK, a.d, tid);
+    kp += kstep;
+    s1.load(kp, a.ks[1], kn - (t0 + 1) * BK, a.d, tid);
+    kp += kstep;
     fetch_mask(t0);
-    sk[0].load(kp, a.ks[1], kn - t0 * BK, a.d, tid);
-    k0 = keys(t0);
-    put_keys(0, k0, sk[0]);
-    kp += kstep;
+    uint8_t m0 = mb;
     fetch_mask(t0 + 1);
-    sk[0].load(kp, a.ks[1], kn - (t0 + 1) * BK, a.d, tid);
-    kp += kstep;
     const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
 #pragma unroll
     for (int k = 0; k < NS; ++k) q[k] = reg_frag<T>(row, i < qn, k, a.d, a.qvec, lane);
     k1 = keys(t0 + 1);
-    put_keys(1, k1, sk[0]);
+    mb = m0;
+    k0 = keys(t0);
+    put_keys(0, k0, s0);
+    put_keys(1, k1, s1);
     sv[0].store(tv[1], 0, tid);              // the weights of the turn before the first are zero, and so must be what they weigh
     if (NST == 2) {
       sk[0].load(kp, a.ks[1], kn - (t0 + 2) * BK, a.d, tid);

@@ -169,19 +169,51 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   const T* K = (const T*)a.K + b * a.ks[0] + hk * a.ks[2];
   const T* V = (const T*)a.V + b * a.vs[0] + hk * a.vs[2];
   const uint8_t* mrow = a.mask ? a.mask + b * a.mask_s : nullptr;
+  constexpr uint64_t kAll = NB == 2 ? ~0ull : 0xffffffffull;
+  int whole = mrow ? -1 : kn / BK;           // tiles before this one are kept as a whole
+  struct Loads {
+    Stage<T, DP, BK, VEC> k, v;
+    uint8_t mask = 0;
+  };
+  Loads tl;
+  auto fetch = [&](Loads& x, int t) {
+    x.k.load(K + (int64_t)t * BK * a.ks[1], a.ks[1], kn - t * BK, a.d, tid);
+    x.v.load(V + (int64_t)t * BK * a.vs[1], a.vs[1], kn - t * BK, a.dv, tid);
+    if (mrow) x.mask = (lane < BK && t * BK + lane < kn) ? mrow[t * BK + lane] : 0;
+  };
+  auto put = [&](const Loads& x, int t, int at) {
+    uint64_t keep = t < whole ? kAll : keep_bits(min(max(kn - t * BK, 0), BK), mrow, x.mask);
+    x.k.store(tile[at][0], keep, tid);
+    x.v.store(tile[at][1], keep, tid);
+    if (keep != kAll && tid < BK) from[at][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
+    return keep;
+  };
+  // All that the loop needs first is asked for before anything is waited for (one latency instead of four).
+  Loads t2;
+  auto first_tiles = [&]() {
+    if (t0 < t1) {
+      fetch(tl, t0);
+      fetch(t2, t0 + 1);
+    }
+  };
+  if (!g.whole_rows) first_tiles();
   size_t row = ((size_t)b * a.H + h) * a.nq + i;
   float lo = __builtin_inff(), hi = 0.f, delta = 0.f;        // nothing left in the row: weights zero
   if (i < qn) lo = g.lo[row], hi = g.hi[row], delta = g.delta[row];
-  bool some = lo != __builtin_inff(), coarse = __any(hi != 0.f);
   frag q[NS], dof[NS];
   {
     const T* qr = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
     const T* dr = (const T*)g.dO + b * g.dos[0] + (int64_t)i * g.dos[1] + h * g.dos[2];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      q[s] = reg_frag<T>(qr, some, s, a.d, a.qvec, lane);
-      dof[s] = reg_frag<T>(dr, some, s, a.dv, g.dovec, lane);
+      q[s] = reg_frag<T>(qr, i < qn, s, a.d, a.qvec, lane);
+      dof[s] = reg_frag<T>(dr, i < qn, s, a.dv, g.dovec, lane);
     }
+  }
+  bool some = lo != __builtin_inff(), coarse = __any(hi != 0.f);
+  if (!some) {                               // whatever the row holds
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = dof[s] = frag{};
   }
   const float* ln = nullptr;
   if (a.table) {
@@ -192,22 +224,6 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   float cs = ds_scale<T>(g, lane);                 // a power of two: dS is formed times it
   lo -= __builtin_amdgcn_logf(cs);
 
-  Stage<T, DP, BK, VEC> sk, sv;
-  uint8_t mb = 0;
-  constexpr uint64_t kAll = NB == 2 ? ~0ull : 0xffffffffull;
-  int whole = mrow ? -1 : kn / BK;           // tiles before this one are kept as a whole
-  auto fetch = [&](int t) {
-    sk.load(K + (int64_t)t * BK * a.ks[1], a.ks[1], kn - t * BK, a.d, tid);
-    sv.load(V + (int64_t)t * BK * a.vs[1], a.vs[1], kn - t * BK, a.dv, tid);
-    if (mrow) mb = (lane < BK && t * BK + lane < kn) ? mrow[t * BK + lane] : 0;
-  };
-  auto put = [&](int t, int at) {
-    uint64_t keep = t < whole ? kAll : keep_bits(min(max(kn - t * BK, 0), BK), mrow, mb);
-    sk.store(tile[at][0], keep, tid);
-    sv.store(tile[at][1], keep, tid);
-    if (keep != kAll && tid < BK) from[at][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
-    return keep;
-  };
   auto scores_start = [&](int at, int first) {
     f32x16 c;
     const float* x = from[at] + first + 4 * half;
@@ -230,8 +246,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     // delta_i = sum_j p_ij dP_ij from the row itself, for this pass and (in g.delta) the next
     float total = 0.f, sd = 0.f;
     for (int t = 0; t < tiles; ++t) {
-      fetch(t);
-      uint64_t keep = put(t, 0);
+      fetch(tl, t);
+      uint64_t keep = put(tl, t, 0);
       settle();
       __syncthreads();
       if (ln) {
@@ -262,12 +278,11 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     sd = both_sum(sd);
     delta = some && total != 0.f ? sd / total : 0.f;
     if (half == 0 && i < qn) g.delta[row] = delta;
+    first_tiles();
   }
   if (t0 < t1) {
-    fetch(t0);
-    k0 = put(t0, 0);
-    fetch(t0 + 1);
-    k1 = put(t0 + 1, 1);
+    k0 = put(tl, t0, 0);
+    k1 = put(t2, t0 + 1, 1);
   }
   settle();
   __syncthreads();
@@ -342,7 +357,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   };
   for (int t = t0; t < t1; ++t) {
     int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
-    fetch(t + 2);
+    fetch(tl, t + 2);
     if constexpr (NB == 2) {
       block(Const<0>{}, rel + t * BK, now, now, k0);
       block(Const<1>{}, rel + t * BK + 32, now, nxt, k1);
@@ -352,7 +367,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       pc[0] = pc[1];
     }
     k0 = k1;
-    k1 = put(t + 2, last);
+    k1 = put(tl, t + 2, last);
     now = nxt;
     __syncthreads();
   }
@@ -412,7 +427,30 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   int t0 = min(sp * per, steps), t1 = min(t0 + per, steps);
   int far = a.bk.far;
   const float* ln = a.table ? dyn : nullptr;
-  bool mine = j < kn && (!a.mask || a.mask[b * a.mask_s + j]);
+  bool mine = j < kn;
+  struct Loads {
+    Stage<T, DP, BQ, VEC> q, d;
+    float lo, delta, hi;                     // of row `lane` of the tile
+  };
+  Loads tl, t2;
+  int h = hk * a.G + (tiles ? t0 / tiles : 0), i0 = tiles ? t0 % tiles * BQ : 0;   // head and first row of the turn's tile
+  int fh = h, fi = i0;                       // and of the tile to fetch next
+  auto fetch = [&](Loads& x) {
+    int rows = fh < (hk + 1) * a.G ? qn - fi : 0;
+    x.q.load((const T*)a.Q + b * a.qs[0] + (int64_t)fi * a.qs[1] + fh * a.qs[2], a.qs[1], rows, a.d, tid);
+    x.d.load((const T*)g.dO + b * g.dos[0] + (int64_t)fi * g.dos[1] + fh * g.dos[2], g.dos[1], rows, a.dv, tid);
+    size_t row = ((size_t)b * a.H + fh) * a.nq + fi + lane;
+    x.lo = __builtin_inff();
+    x.delta = x.hi = 0.f;
+    if (lane < BQ && lane < rows) x.lo = g.lo[row], x.delta = g.delta[row], x.hi = g.hi[row];
+    fi += BQ;
+    if (fi >= qn) fi = 0, ++fh;
+  };
+  // as in k_attend_dq, ahead of the first wait
+  if (t0 < t1) {
+    fetch(tl);
+    fetch(t2);
+  }
   frag kf[NS], vf[NS];
   {
     const T* kr = (const T*)a.K + b * a.ks[0] + (int64_t)j * a.ks[1] + hk * a.ks[2];
@@ -423,34 +461,23 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       vf[s] = reg_frag<T>(vr, mine, s, a.dv, a.vvec, lane);
     }
   }
+  if (a.mask && mine) mine = a.mask[b * a.mask_s + j] != 0;
+  if (!mine) {                               // whatever the key holds
+#pragma unroll
+    for (int s = 0; s < NS; ++s) kf[s] = vf[s] = frag{};
+  }
   constexpr float kLift = PLift<T>::value;
   float cs = ds_scale<T>(g, lane), unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
-
-  Stage<T, DP, BQ, VEC> sq, sd;
-  float lo = 0.f, delta = 0.f, hi = 0.f;     // of row `lane` of the tile
-  int h = hk * a.G + (tiles ? t0 / tiles : 0), i0 = tiles ? t0 % tiles * BQ : 0;   // head and first row of the turn's tile
-  int fh = h, fi = i0;                       // and of the tile to fetch next
-  auto fetch = [&]() {
-    int rows = fh < (hk + 1) * a.G ? qn - fi : 0;
-    sq.load((const T*)a.Q + b * a.qs[0] + (int64_t)fi * a.qs[1] + fh * a.qs[2], a.qs[1], rows, a.d, tid);
-    sd.load((const T*)g.dO + b * g.dos[0] + (int64_t)fi * g.dos[1] + fh * g.dos[2], g.dos[1], rows, a.dv, tid);
-    size_t row = ((size_t)b * a.H + fh) * a.nq + fi + lane;
-    lo = __builtin_inff();
-    delta = hi = 0.f;
-    if (lane < BQ && lane < rows) lo = g.lo[row], delta = g.delta[row], hi = g.hi[row];
-    fi += BQ;
-    if (fi >= qn) fi = 0, ++fh;
-  };
-  auto put = [&](int at) {
-    uint64_t keep = __ballot(lo != __builtin_inff()) & (NB == 2 ? ~0ull : 0xffffffffull);
-    sq.store(tile[at][0], keep, tid);
-    sd.store(tile[at][1], keep, tid);
+  auto put = [&](const Loads& x, int at) {
+    uint64_t keep = __ballot(x.lo != __builtin_inff()) & (NB == 2 ? ~0ull : 0xffffffffull);
+    x.q.store(tile[at][0], keep, tid);
+    x.d.store(tile[at][1], keep, tid);
     if (tid < BQ) {
-      stat[at][0][tid] = lo;                 // infinite where nothing is left in the row: weights zero
-      stat[at][1][tid] = delta * ck;
-      stat[at][2][tid] = hi;
+      stat[at][0][tid] = x.lo;                 // infinite where nothing is left in the row: weights zero
+      stat[at][1][tid] = x.delta * ck;
+      stat[at][2][tid] = x.hi;
     }
-    return __any(hi != 0.f);
+    return __any(x.hi != 0.f);
   };
   f32x16 dk[ND], dv[ND], sc[2], pc[2];       // of a turn's two blocks: scores, dP
   sc[0] = pc[0] = f32x16{};
@@ -460,10 +487,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   int rel = rest_above((int64_t)k0 - start_of(a, b));
   bool c0 = false, c1 = false;               // rows with a `hi` in this tile and the next
   if (t0 < t1) {
-    fetch();
-    c0 = put(0);
-    fetch();
-    c1 = put(1);
+    c0 = put(tl, 0);
+    c1 = put(t2, 1);
   }
   settle();
   __syncthreads();
@@ -539,7 +564,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       right = uniform(ln[2 * far + kPad]);
     }
     int nxt = now == 2 ? 0 : now + 1, last = nxt == 2 ? 0 : nxt + 1;
-    fetch();
+    fetch(tl);
     if constexpr (NB == 2) {
       block(Const<0>{}, rel - i0, now, now, c0);
       block(Const<1>{}, rel - i0 - 32, now, nxt, c0);
@@ -549,7 +574,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       pc[0] = pc[1];
     }
     c0 = c1;
-    c1 = put(last);
+    c1 = put(tl, last);
     now = nxt;
     i0 += BQ;
     if (i0 >= qn) i0 = 0, ++h;
