@@ -229,10 +229,9 @@ __device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* d
 // Adds the 32 x 32 block s (keys in the registers, queries in the lanes) along its diagonals: line[j - i] += sum, `line` (the wave's own)
 // pointing at the difference of the first key and the first query.  Halves first exchange registers so that each
 // has 16 keys in a row; a sum then moves one lane per key, towards higher lanes for keys ahead (what leaves a row of 16 lanes
-// lies behind), towards lower ones for keys behind.  Few LDS additions instead of sixteen of all lanes (dQ pass of 8 x 12 x 512 x 640 in bf16,
-// d = 64, when this was changed: 106 us to 44, with two additions and a line per half).  The halves share the wave's line, one adding after the
-// other and its lanes at places of their own, so that the order is fixed: a line per half left no room in LDS for d = 128 with an edge
-// past about 830, and the training step is no slower so (104.1 us, 105.3 with a line per half).
+// lies behind), towards lower ones for keys behind.  That leaves two pieces of a diagonal in each row of 16 lanes, which rows exchange until every lane
+// owns a diagonal of the block: one read and one write of LDS in a fixed order, no atomics.  (dQ pass of 8 x 12 x 512 x 640 in bf16, d = 64:
+// 31 us; with two atomic additions per half 38, with sixteen of all lanes 106 before other steps.)
 __device__ __forceinline__ float from_lane_below(float x) {   // of the row of 16, zero into the first
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x111, 0xf, 0xf, true));
 }
@@ -255,14 +254,32 @@ __device__ __forceinline__ void add_diagonals(const f32x16& s, float* line, int 
     ahead = from_lane_below(ahead) + k[i];
     behind = from_lane_above(behind) + k[15 - i];
   }
-  int q = lane & 15, base = 16 * (lane >> 5) - (lane & 16);
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    if ((lane >> 5) == half) {
-      __hip_atomic_fetch_add(line + base + 15 - q, ahead, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-      if (q) __hip_atomic_fetch_add(line + base - q, behind, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    }
-  }
+  behind = from_lane_above(behind);
+  // Rows of 16 lanes X0 .. X3 of `ahead` and Y0 .. Y3 of `behind`; with 15 - lane % 16 added, X stand at 0, -16, 16, 0 and Y at -16, -32, 0, -16.
+  typedef float pair __attribute__((ext_vector_type(2)));
+  auto swap16 = [](float x, float y) {      // odd rows of x against even rows of y
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(y), false, false);
+    return pair{__int_as_float(r[0]), __int_as_float(r[1])};
+  };
+  auto swap32 = [](float x, float y) {      // rows 2, 3 of x against rows 0, 1 of y
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(y), false, false);
+    return pair{__int_as_float(r[0]), __int_as_float(r[1])};
+  };
+  pair t = swap16(ahead, behind);           // X0 Y0 X2 Y2,  X1 Y1 X3 Y3
+  t = swap32(t[0], t[1]);                   // X0 Y0 X1 Y1,  X2 Y2 X3 Y3
+  float c = t[0];
+  pair d = swap16(t[1], t[1]);              // X2 X2 X3 X3,  Y2 Y2 Y3 Y3
+  pair e = swap16(c, c);                    // X0 X0 X1 X1,  Y0 Y0 Y1 Y1
+  pair f = swap32(d[0], e[1]);              // X2 X2 Y0 Y0,  X3 X3 Y1 Y1
+  bool odd = lane & 16, up = lane & 32;
+  float z = c + d[1] + (up ? f[0] : f[1]);  // rows 0: X0 + Y2 + X3,  2: X1 + Y3 + Y0
+  if (odd) z = up ? c : f[0];               // rows 1: X2,  3: Y1
+  float* mine = line + 15 - (lane & 15) + (odd ? (up ? -32 : 16) : up ? -16 : 0);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // another lane's write of the block before
+  __builtin_amdgcn_wave_barrier();
+  *mine += z;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // A table entry in units of the base-2 exponent.  Finite entries stay finite: one below -2.3e38 counts as that (the same
