@@ -2231,7 +2231,7 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_
     w.bytes += step256(n);
     return at;
   };
-  w.norms = take(64 * BBMM_ATT_NORM_SLOTS);
+  w.norms = take(two_bytes ? 2 * sizeof(float) * BBMM_ATT_NORM_SLOTS : 0);
   w.delta = take(rows * sizeof(float));
   w.lo = take(rows * sizeof(float));
   w.hi = take(rows * sizeof(float));
@@ -2314,12 +2314,12 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   }
   g.ovec = wide_rows(O, nullptr, a.dv, e, 16), g.dovec = wide_rows(dO, g.dos, a.dv, e, 16);
   g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
-  g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (unsigned*)((char*)work + w.norms);
+  g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (float*)((char*)work + w.norms);
   g.pq = (float*)((char*)work + w.pq), g.pk = (float*)((char*)work + w.pk), g.pv = (float*)((char*)work + w.pv);
   GradPlan p = gradient_plan(c, a, e == 2);
   g.qsplit = p.qsplit, g.ksplit = p.ksplit, g.whole_rows = p.whole_rows;
   hipStream_t s = c->stream;
-  launch_attend_delta(s, in->type, a, g);
+  launch_attend_norms(s, in->type, a, g);
   if (rows) launch_attend_dq(s, in->type, a, g);
   if (keys) launch_attend_dkv(s, in->type, a, g);
   launch_attend_sums(s, in->type, a, g);

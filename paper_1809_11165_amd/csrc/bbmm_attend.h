@@ -9,7 +9,7 @@
 #define BBMM_ATT_MAXD 128      // features of Q, K and of V
 #define BBMM_ATT_MAXEDGES 63   // edges of the buckets
 #define BBMM_ATT_FAR 1024      // largest edge
-#define BBMM_ATT_NORM_SLOTS 64
+#define BBMM_ATT_NORM_SLOTS 512
 
 // The buckets of a difference r = j - i - start (edges ascending; further than the last one, everything on a side shares a bucket).
 struct AttBuckets {
@@ -48,10 +48,10 @@ struct AttGrad {
   int ovec, dovec, dqvec, dkvec, dvvec;
   const float* lse;
   void *dQ, *dK, *dV;            // dense
-  // B x H x nq, left by launch_attend_delta: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
+  // B x H x nq, left by the dQ pass for the next: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
   float *delta, *lo, *hi;
   float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets
-  unsigned* norms;               // fp16: bits of the largest |do_i| and |v_j|, 64 bytes per slot
+  float* norms;                  // fp16: largest |do_i| and |v_j|, a pair per slot
   int whole_rows;                // few keys: the dQ pass forms delta from the row itself
   int qsplit, ksplit;            // parts that the keys of the dQ pass, and the queries of the dK, dV pass, are split into
   float *pq, *pk, *pv;           // their results: parts x the size of dQ, dK, dV
@@ -61,7 +61,7 @@ struct AttGrad {
 void launch_attend(hipStream_t s, int type, const AttArgs& a, const AttOut& o);        // 128 queries of one head per workgroup
 void launch_attend_few(hipStream_t s, int type, const AttArgs& a, const AttOut& o);    // rows (i, g) of a shared head packed
 void launch_attend_join(hipStream_t s, int type, const AttArgs& a, const AttOut& o);   // joins the parts
-void launch_attend_delta(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
+void launch_attend_norms(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_dq(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_dkv(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_sums(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);   // adds up what the two passes left in parts

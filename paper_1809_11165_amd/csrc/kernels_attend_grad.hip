@@ -7,7 +7,7 @@
 // k_attend_dkv (owns 128 keys of a shared head and runs over the queries of all its heads; scores with a key in a lane).  Seven matrix products
 // where five would do with dQ added atomically.
 //
-// fp16: p and dS are scaled by powers of two before they are rounded, dS by the largest |do_i| |v_j| (launch_attend_delta): weights of
+// fp16: p and dS are scaled by powers of two before they are rounded, dS by the largest |do_i| |v_j| (k_attend_norms): weights of
 // long rows and small gradients would fall among that type's subnormal numbers.
 #include "attend_dev.h"
 
@@ -18,14 +18,22 @@ namespace {
 template <typename T> struct PLift { static constexpr float value = 0.f; };
 template <> struct PLift<_Float16> { static constexpr float value = 12.f; };
 
-// Largest |do_i| and |v_j| of a call, in kNormSlots slots of 64 bytes (all rows in one place made 64 000 rows of fp16 wait 200 us for each other).
+// Largest |do_i| and |v_j| of a call, in kNormSlots slots, one per workgroup of k_attend_norms (a place that all rows maximise made 64 000 rows of
+// fp16 wait 200 us for each other).
 constexpr int kNormSlots = BBMM_ATT_NORM_SLOTS;
+static_assert(kNormSlots % 64 == 0, "slots per lane");
 
 // Power of two that keeps |dS| <= 2 |do| |v| below 2^15.  All lanes of a wave take part.
 template <typename T>
 __device__ __forceinline__ float ds_scale(const AttGrad& g, int lane) {
   if constexpr (__is_same(T, _Float16)) {
-    float x = __uint_as_float(g.norms[16 * lane]), y = __uint_as_float(g.norms[16 * lane + 1]);
+    float x = 0.f, y = 0.f;
+#pragma unroll
+    for (int k = 0; k < kNormSlots; k += 64) {
+      float2 z = *(const float2*)(g.norms + 2 * (k + lane));
+      x = fmaxf(x, z.x);
+      y = fmaxf(y, z.y);
+    }
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) {
       x = fmaxf(x, __shfl_xor(x, k, 64));
@@ -36,110 +44,52 @@ __device__ __forceinline__ float ds_scale(const AttGrad& g, int lane) {
   }
   return 1.f;
 }
-static_assert(kNormSlots == 64, "a slot per lane");
 
-__global__ void k_zero_norms(unsigned* n) { n[16 * threadIdx.x] = n[16 * threadIdx.x + 1] = 0; }
-
-// Four rows of a wave, 16 lanes each: one maximum (any order) into the workgroup's slot.  Rows without a finite norm are left out.
-__device__ __forceinline__ void put_norm(unsigned* norms, int which, float square, int lane) {
-  float x = square < __builtin_inff() ? sqrtf(square) : 0.f;
-  x = fmaxf(x, __shfl_xor(x, 16, 64));
-  x = fmaxf(x, __shfl_xor(x, 32, 64));
-  if (lane == 0 && x > 0.f) atomicMax(&norms[16 * (blockIdx.x % kNormSlots) + which], __float_as_uint(x));
+// fp16: the norms of the rows that take part, 16 lanes per row; those without a finite norm are left out.
+__global__ __launch_bounds__(256) void k_attend_norms(AttArgs a, AttGrad g) {
+  typedef _Float16 T;
+  __shared__ float part[2][4];
+  int tid = threadIdx.x, lane = tid & 15;
+  int64_t rows = (int64_t)a.B * a.nq * a.H, keys = (int64_t)a.B * a.nk * a.HK;
+  auto square = [&](const T* row, int vec) {
+    u32x4 x = load16<T>(row, 8 * lane, a.dv, vec);
+    float q = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q = fmaf((float)reinterpret_cast<T*>(&x)[e], (float)reinterpret_cast<T*>(&x)[e], q);
+#pragma unroll
+    for (int k = 1; k < 16; k *= 2) q += __shfl_xor(q, k, 16);
+    return q < __builtin_inff() ? q : 0.f;
+  };
+  float x = 0.f, y = 0.f;
+  int64_t first = (int64_t)blockIdx.x * 16 + (tid >> 4), step = (int64_t)kNormSlots * 16;
+#pragma unroll 2
+  for (int64_t n = first; n < rows; n += step) {
+    int h = (int)(n % a.H), i = (int)(n / a.H % a.nq), b = (int)(n / a.H / a.nq);
+    if ((a.q_len && i >= a.q_len[b]) || g.lse[((size_t)b * a.H + h) * a.nq + i] == -__builtin_inff()) continue;
+    x = fmaxf(x, square((const T*)g.dO + b * g.dos[0] + (int64_t)i * g.dos[1] + h * g.dos[2], g.dovec));
+  }
+#pragma unroll 2
+  for (int64_t n = first; n < keys; n += step) {
+    int h = (int)(n % a.HK), j = (int)(n / a.HK % a.nk), b = (int)(n / a.HK / a.nk);
+    if ((a.k_len && j >= a.k_len[b]) || (a.mask && !a.mask[b * a.mask_s + j])) continue;
+    y = fmaxf(y, square((const T*)a.V + b * a.vs[0] + (int64_t)j * a.vs[1] + h * a.vs[2], a.vvec));
+  }
+#pragma unroll
+  for (int k = 16; k < 64; k *= 2) {
+    x = fmaxf(x, __shfl_xor(x, k, 64));
+    y = fmaxf(y, __shfl_xor(y, k, 64));
+  }
+  if ((tid & 63) == 0) {
+    part[0][tid >> 6] = x;
+    part[1][tid >> 6] = y;
+  }
+  __syncthreads();
+  if (tid < 2) g.norms[2 * blockIdx.x + tid] = sqrtf(fmaxf(fmaxf(part[tid][0], part[tid][1]), fmaxf(part[tid][2], part[tid][3])));
 }
 
-// Beyond this, fp32 holds lse too coarsely to recover weights from it (a row of nothing but masks of -1e9 or of the type's lowest value).
+// Beyond this, fp32 holds lse too coarsely to recover weights from it (a row of nothing but masks of -1e9 or of the type's lowest value):
+// the row's largest score and log2 of its sum are formed again and kept apart.
 constexpr float kCoarse = 65536.f;
-
-// Largest score and log2 of the sum relative to it, from the row itself: 16 lanes, a key at a time.  Only for rows beyond kCoarse.
-template <typename T>
-__device__ void row_sums(const AttArgs& a, int b, int h, int i, int lane, float& hi, float& lo) {
-  const T* q = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
-  const T* K = (const T*)a.K + b * a.ks[0] + h / a.G * a.ks[2];
-  int kn = a.k_len ? min(max(a.k_len[b], 0), a.nk) : a.nk;
-  const int64_t lim = (int64_t)1 << 40;
-  int64_t start = a.q_start ? min(max(a.q_start[b], -lim), lim) : 0;
-  float m = -__builtin_inff(), l = 0.f;
-  for (int j = 0; j < kn; ++j) {
-    if (a.mask && !a.mask[b * a.mask_s + j]) continue;
-    float s = 0.f;
-    for (int c = lane; c < a.d; c += 16) s = fmaf((float)q[c], (float)K[(int64_t)j * a.ks[1] + c], s);
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) s += __shfl_xor(s, x, 16);
-    float bias = a.table ? bias2<T>(((const T*)a.table)[(size_t)h * a.bk.buckets + bucket_of(a.bk, clamp_rel((int64_t)j - i - start))]) : 0.f;
-    s = fmaf(s, a.c2, bias);
-    if (s > m) {
-      l = l * __builtin_amdgcn_exp2f(m - s) + 1.f;
-      m = s;
-    } else if (s != -__builtin_inff()) {
-      l += __builtin_amdgcn_exp2f(s - m);
-    }
-  }
-  hi = m;
-  lo = __builtin_amdgcn_logf(l);
-}
-
-// 16 lanes per row (b, i, h): delta, hi and lo, and the largest |do_i| (finite ones) for fp16.
-template <typename T>
-__global__ __launch_bounds__(256) void k_attend_delta(AttArgs a, AttGrad g) {
-  constexpr int E = 16 / (int)sizeof(T);
-  int lane = threadIdx.x & 15;
-  int64_t n = (int64_t)a.B * a.nq * a.H, row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  bool have = row < n;                       // whole groups of 16 lanes
-  if (!have) row = n - 1;
-  int h = (int)(row % a.H), i = (int)(row / a.H % a.nq), b = (int)(row / a.H / a.nq);
-  int qn = a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq;
-  size_t at = ((size_t)b * a.H + h) * a.nq + i;
-  float s = 0.f, q = 0.f, hi = 0.f, lo = __builtin_inff();
-  float lse = i < qn && have ? g.lse[at] : -__builtin_inff();
-  if (lse != -__builtin_inff()) {
-    const T* o = (const T*)g.O + row * a.dv;
-    const T* d = (const T*)g.dO + b * g.dos[0] + (int64_t)i * g.dos[1] + h * g.dos[2];
-    for (int c = lane * E; c < a.dv; c += 16 * E) {
-      u32x4 x = load16<T>(o, c, a.dv, g.ovec), y = load16<T>(d, c, a.dv, g.dovec);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float u = (float)reinterpret_cast<T*>(&x)[e], v = (float)reinterpret_cast<T*>(&y)[e];
-        s = fmaf(u, v, s);
-        q = fmaf(v, v, q);
-      }
-    }
-    lo = lse * kLog2e;
-    if (fabsf(lse) > kCoarse && fabsf(lse) < __builtin_inff()) row_sums<T>(a, b, h, i, lane, hi, lo);
-  }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) {
-    s += __shfl_xor(s, x, 16);
-    q += __shfl_xor(q, x, 16);
-  }
-  if (lane == 0 && have) {
-    g.delta[at] = s;
-    g.lo[at] = lo;
-    g.hi[at] = hi;
-  }
-  if (__is_same(T, _Float16)) put_norm(g.norms, 0, q, threadIdx.x & 63);
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void k_attend_vnorm(AttArgs a, AttGrad g) {
-  constexpr int E = 16 / (int)sizeof(T);
-  int lane = threadIdx.x & 15;
-  int64_t n = (int64_t)a.B * a.nk * a.HK, row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  bool have = row < n;
-  if (!have) row = n - 1;
-  int h = (int)(row % a.HK), j = (int)(row / a.HK % a.nk), b = (int)(row / a.HK / a.nk);
-  if ((a.k_len && j >= a.k_len[b]) || (a.mask && !a.mask[b * a.mask_s + j])) have = false;
-  const T* v = (const T*)a.V + b * a.vs[0] + (int64_t)j * a.vs[1] + h * a.vs[2];
-  float q = 0.f;
-  for (int c = lane * E; c < a.dv && have; c += 16 * E) {
-    u32x4 x = load16<T>(v, c, a.dv, a.vvec);
-#pragma unroll
-    for (int e = 0; e < E; ++e) q = fmaf((float)reinterpret_cast<T*>(&x)[e], (float)reinterpret_cast<T*>(&x)[e], q);
-  }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) q += __shfl_xor(q, x, 64);
-  put_norm(g.norms, 1, q, threadIdx.x & 63);
-}
 
 // 64 keys a turn, as two blocks of 32 (fp32: one block a turn).  While the matrix unit forms the scores and dP of the next block, the vector unit turns this one's into dS; then
 // dQ takes it up.
@@ -196,10 +146,9 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       fetch(t2, t0 + 1);
     }
   };
-  if (!g.whole_rows) first_tiles();
+  first_tiles();
   size_t row = ((size_t)b * a.H + h) * a.nq + i;
-  float lo = __builtin_inff(), hi = 0.f, delta = 0.f;        // nothing left in the row: weights zero
-  if (i < qn) lo = g.lo[row], hi = g.hi[row], delta = g.delta[row];
+  float lse = i < qn ? g.lse[row] : -__builtin_inff(), delta = 0.f;
   frag q[NS], dof[NS];
   {
     const T* qr = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + h * a.qs[2];
@@ -209,12 +158,24 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       q[s] = reg_frag<T>(qr, i < qn, s, a.d, a.qvec, lane);
       dof[s] = reg_frag<T>(dr, i < qn, s, a.dv, g.dovec, lane);
     }
+    const T* orow = (const T*)g.O + (((int64_t)b * a.nq + i) * a.H + h) * a.dv;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      frag o = reg_frag<T>(orow, i < qn, s, a.dv, g.ovec, lane);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)o[e], (float)dof[s][e], delta);
+    }
   }
-  bool some = lo != __builtin_inff(), coarse = __any(hi != 0.f);
+  bool some = lse != -__builtin_inff();      // something is left in the row
+  delta = some ? both_sum(delta) : 0.f;
+  float lo = some ? lse * kLog2e : __builtin_inff(), hi = 0.f;   // weights are exp2((s - hi) - lo)
+  bool wide = fabsf(lse) > kCoarse && fabsf(lse) < __builtin_inff();
   if (!some) {                               // whatever the row holds
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[s] = dof[s] = frag{};
   }
+  if (__any(wide) && lane == 0) side[wave] = 1.f;
+  else if (lane == 0) side[wave] = 0.f;
   const float* ln = nullptr;
   if (a.table) {
     fill_line<T>(line, a, h, tid, 256);
@@ -222,8 +183,6 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     ln = line;
   }
   float cs = ds_scale<T>(g, lane);                 // a power of two: dS is formed times it
-  lo -= __builtin_amdgcn_logf(cs);
-
   auto scores_start = [&](int at, int first) {
     f32x16 c;
     const float* x = from[at] + first + 4 * half;
@@ -242,9 +201,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
   float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
   int rel = rest_below(-(int64_t)q0 - start_of(a, b));
-  if (g.whole_rows) {
-    // delta_i = sum_j p_ij dP_ij from the row itself, for this pass and (in g.delta) the next
-    float total = 0.f, sd = 0.f;
+  // The row from all its keys, ahead of the pass: f(scores' products, dP, mul, add) for every block of 32.
+  auto whole_row = [&](auto f) {
     for (int t = 0; t < tiles; ++t) {
       fetch(tl, t);
       uint64_t keep = put(tl, t, 0);
@@ -264,22 +222,52 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
         for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 32 * n, k, lane), dof[k], dp);
         float mul = a.c2, add = 0.f;
         if (ln) add_bias<true>(s, a.c2, ln, far, rel + t * BK + 32 * n, left, right, lane, mul, add);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float x = fmaf(s[r], mul, add) - hi;
-          x = __builtin_amdgcn_exp2f(x - lo);
-          total += x;
-          sd = fmaf(x, dp[r], sd);
-        }
+        f(s, dp, mul, add);
       }
       __syncthreads();
     }
+  };
+  __syncthreads();
+  bool any_wide = uniform(side[0] + side[1] + side[2] + side[3]) != 0.f;
+  if (any_wide) {
+    float top = -__builtin_inff(), sum = 0.f;
+    whole_row([&](const f32x16& s, const f32x16&, float mul, float add) {
+      float x[16], big = top;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = fmaf(s[r], mul, add);
+        big = fmaxf(big, x[r]);
+      }
+      float ref = big == -__builtin_inff() ? 0.f : big;
+      sum *= __builtin_amdgcn_exp2f(top - ref);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(x[r] - ref);
+      top = big;
+    });
+    float both = both_max(top);
+    sum = both_sum(top == -__builtin_inff() ? 0.f : sum * __builtin_amdgcn_exp2f(top - both));
+    if (wide) hi = both, lo = __builtin_amdgcn_logf(sum);
+  }
+  bool coarse = __any(hi != 0.f);
+  if (g.whole_rows) {
+    // delta_i = sum_j p_ij dP_ij
+    float total = 0.f, sd = 0.f;
+    whole_row([&](const f32x16& s, const f32x16& dp, float mul, float add) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = fmaf(s[r], mul, add) - hi;
+        x = __builtin_amdgcn_exp2f(x - lo);
+        total += x;
+        sd = fmaf(x, dp[r], sd);
+      }
+    });
     total = both_sum(total);
     sd = both_sum(sd);
     delta = some && total != 0.f ? sd / total : 0.f;
-    if (half == 0 && i < qn) g.delta[row] = delta;
-    first_tiles();
   }
+  if (half == 0 && i < qn && sp == 0) g.delta[row] = delta, g.lo[row] = lo, g.hi[row] = hi;   // for the next pass
+  lo -= __builtin_amdgcn_logf(cs);
+  if (any_wide || g.whole_rows) first_tiles();
   if (t0 < t1) {
     k0 = put(tl, t0, 0);
     k1 = put(t2, t0 + 1, 1);
@@ -634,15 +622,6 @@ __global__ __launch_bounds__(256) void k_attend_sum(Sums z) {
   }
 }
 
-template <typename T>
-void delta_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  int64_t n = (int64_t)a.B * a.nq * a.H, nv = (int64_t)a.B * a.nk * a.HK;
-  if (__is_same(T, _Float16)) {
-    k_zero_norms<<<1, kNormSlots, 0, s>>>(g.norms);
-    if (nv) k_attend_vnorm<T><<<(unsigned)((nv + 15) / 16), 256, 0, s>>>(a, g);
-  }
-  if (n) k_attend_delta<T><<<(unsigned)((n + 15) / 16), 256, 0, s>>>(a, g);
-}
 template <typename T, bool VEC>
 void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int nqt = (a.nq + 127) / 128, grid = (a.B * a.H * nqt * g.qsplit + 7) / 8 * 8;
@@ -689,10 +668,8 @@ void sums_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
 
 }  // namespace
 
-void launch_attend_delta(hipStream_t s, int type, const AttArgs& a, const AttGrad& g) {
-  if (type == 0) delta_t<float>(s, a, g);
-  else if (type == 1) delta_t<_Float16>(s, a, g);
-  else delta_t<__bf16>(s, a, g);
+void launch_attend_norms(hipStream_t s, int type, const AttArgs& a, const AttGrad& g) {
+  if (type == 1) k_attend_norms<<<kNormSlots, 256, 0, s>>>(a, g);
 }
 void launch_attend_dq(hipStream_t s, int type, const AttArgs& a, const AttGrad& g) {
   if (type == 0) dq_t<float>(s, a, g);
