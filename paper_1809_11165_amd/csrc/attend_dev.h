@@ -226,6 +226,16 @@ __device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* d
   }
 }
 
+// One wave: the sums of a head's bucket from all parts (tsum: heads x parts x buckets) in a fixed order, 64 bits.
+template <typename T>
+__device__ __forceinline__ void join_bucket(const float* __restrict__ tsum, int parts, int buckets, int h, int n, int lane, T* __restrict__ out) {
+  double s = 0.0;
+  for (int p = lane; p < parts; p += 64) s += (double)tsum[((size_t)h * parts + p) * buckets + n];
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) s += __shfl_xor(s, x, 64);
+  if (lane == 0) out[(size_t)h * buckets + n] = (T)(float)s;
+}
+
 // Adds the 32 x 32 block s (keys in the registers, queries in the lanes) along its diagonals: line[j - i] += sum, `line` (the wave's own)
 // pointing at the difference of the first key and the first query.  Halves first exchange registers so that each
 // has 16 keys in a row; a sum then moves one lane per key, towards higher lanes for keys ahead (what leaves a row of 16 lanes

@@ -2307,7 +2307,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   OnDevice dev(c->device);
   HIPCHK(c, dev.err);
   AttGrad g{};
-  g.O = O, g.dO = dO, g.lse = lse, g.dQ = dQ, g.dK = dK, g.dV = dV;
+  g.O = O, g.dO = dO, g.lse = lse, g.dQ = dQ, g.dK = dK, g.dV = dV, g.dtable = dtable;
   for (int k = 0; k < 3 && do_stride; ++k) {
     if (do_stride[k] < 0) return fail(c, BBMM_EINVAL, "attention: negative stride");
     g.dos[k] = do_stride[k];
@@ -2323,7 +2323,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   if (rows) launch_attend_dq(s, in->type, a, g);
   if (keys) launch_attend_dkv(s, in->type, a, g);
   launch_attend_sums(s, in->type, a, g);
-  if (a.table) launch_bucket_join(s, in->type, g.tsum, a.B * g.qsplit * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
+  if (a.table && !keys) launch_bucket_join(s, in->type, g.tsum, a.B * g.qsplit * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
   HIPCHK(c, hipGetLastError());
   return BBMM_OK;
 }

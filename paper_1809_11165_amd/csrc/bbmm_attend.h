@@ -47,7 +47,7 @@ struct AttGrad {
   int64_t dos[3];
   int ovec, dovec, dqvec, dkvec, dvvec;
   const float* lse;
-  void *dQ, *dK, *dV;            // dense
+  void *dQ, *dK, *dV, *dtable;   // dense
   // B x H x nq, left by the dQ pass for the next: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
   float *delta, *lo, *hi;
   float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets

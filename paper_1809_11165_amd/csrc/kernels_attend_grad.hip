@@ -395,16 +395,23 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
 }
 
-// 64 queries of one head a turn, the heads of the group one after the other; else like k_attend_dq.
+// 64 queries of one head a turn, the heads of the group one after the other; else like k_attend_dq.  Workgroups from `grid` on add up the table's
+// gradient that the dQ pass left, a wave per entry (a launch of its own takes 4.6 us).
 template <typename T, int DP, bool VEC>
-__global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt) {
+__global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt, int grid) {
   typedef typename Frag<T>::type frag;
   constexpr int NB = sizeof(T) == 2 ? 2 : 1, BQ = 32 * NB, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
   __shared__ __align__(16) char tile[3][2][kTile];    // Q, dO
   __shared__ __align__(16) float stat[3][3][BQ];      // lo, delta (scaled like dS), hi
   extern __shared__ float dyn[];                      // with a table: bias line
-  int id = die_order(blockIdx.x, a.B * a.HK, nkt * g.ksplit);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
+  if ((int)blockIdx.x >= grid) {
+    int n = 4 * ((int)blockIdx.x - grid) + wave;
+    if (n < a.H * a.bk.buckets)
+      join_bucket<T>(g.tsum, a.B * g.qsplit * ((a.nq + 127) / 128), a.bk.buckets, n / a.bk.buckets, n % a.bk.buckets, lane, (T*)g.dtable);
+    return;
+  }
+  int id = die_order(blockIdx.x, a.B * a.HK, nkt * g.ksplit);
   int kt = id % nkt, sp = id / nkt % g.ksplit, bh = id / nkt / g.ksplit, hk = bh % a.HK, b = bh / a.HK;
   if (b >= a.B) return;
   int k0 = kt * 128 + wave * 32, j = k0 + (lane & 31);
@@ -632,9 +639,10 @@ void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
 template <typename T, bool VEC>
 void dkv_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int nkt = (a.nk + 127) / 128, grid = (a.B * a.HK * nkt * g.ksplit + 7) / 8 * 8;
+  int more = a.table ? (a.H * a.bk.buckets + 3) / 4 : 0;
   size_t lds = a.table ? sizeof(float) * (2 * (a.bk.far + kPad) + 1) : 0;
-  if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nkt);
-  else k_attend_dkv<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nkt);
+  if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<grid + more, 256, lds, s>>>(a, g, nkt, grid);
+  else k_attend_dkv<T, 128, VEC><<<grid + more, 256, lds, s>>>(a, g, nkt, grid);
 }
 template <typename T>
 void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {

@@ -118,15 +118,10 @@ __global__ __launch_bounds__(256) void k_bucket_grad(const T* __restrict__ dB, A
   bucket_sums(bk, diag, far - 1, side[0][0] + side[0][1] + side[0][2] + side[0][3], side[1][0] + side[1][1] + side[1][2] + side[1][3], out, tid);
 }
 
-// One wave per (head, bucket): the parts in a fixed order, 64 bits.
+// One wave per (head, bucket).
 template <typename T>
 __global__ __launch_bounds__(64) void k_bucket_join(const float* __restrict__ tsum, int nparts, int buckets, T* __restrict__ out) {
-  int lane = threadIdx.x, n = blockIdx.x, h = blockIdx.y;
-  double s = 0.0;
-  for (int p = lane; p < nparts; p += 64) s += (double)tsum[((size_t)h * nparts + p) * buckets + n];
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) s += __shfl_xor(s, x, 64);
-  if (lane == 0) out[(size_t)h * buckets + n] = (T)(float)s;
+  join_bucket<T>(tsum, nparts, buckets, blockIdx.y, blockIdx.x, threadIdx.x, out);
 }
 
 }  // namespace
