@@ -2187,11 +2187,12 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
 // 256 and 512 forward, 165 with these).
 constexpr int64_t kGradPart = 128;
 // delta_i = do_i.o_i takes o_i as the forward pass rounded it.  Where a row holds few keys that is off by as much as dS is rounded (its error goes
-// with the square root of sum p^2), and more in the table's gradient, whose far buckets are small sums of large weights.  Rows of up to
-// kWholeRows keys (kWholeRowsTable with a table) form delta in fp32 from all their scores instead, two products more.  Against 64 bits, bf16, 500
-// queries, without / with: 8 keys: dQ 2.7e-3 / 2.4e-3, table 1.3e-2 / 1.8e-3; 32: table 4.3e-3 / 1.7e-3; 128: 2.9e-3 / 1.6e-3.  Left to the rounded o:
-// 500 keys 2.4e-3, 2000 3.2e-3 (of which the plain sum in fp32 has 2.6e-3).
-constexpr int64_t kWholeRows = 128, kWholeRowsTable = 256;
+// with the square root of sum p^2).  In the table's gradient it stands against what is left of a row's sum of dS, which is zero but for the buckets'
+// differences: where most of a row lies in one bucket (long rows beyond the last edge) it is far more than what is left.  So in two-byte types rows of up to
+// kWholeRows keys, and all rows with a table, form delta in fp32 from all their scores instead, two products more.  Against 64 bits, bf16, without / with:
+// 500 queries of 8 keys: dQ 2.7e-3 / 2.4e-3, table 1.3e-2 / 1.8e-3; table of 37 x 2171, last edge 12: 1.2e-1 / below 4e-3 (training step of 8 x 12
+// heads, 512 x 640, d = 64: 89 / 104 us).
+constexpr int64_t kWholeRows = 128;
 struct GradPlan {
   int qsplit, ksplit;
   bool whole_rows;
@@ -2202,8 +2203,8 @@ GradPlan gradient_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
     return (int)std::max<int64_t>(1, std::min(want, most));
   };
   GradPlan p;
-  p.whole_rows = two_bytes && a.nk <= (a.table ? kWholeRowsTable : kWholeRows);
-  p.qsplit = p.whole_rows ? 1 : parts((int64_t)a.B * a.H * ((a.nq + 127) / 128), a.nk);
+  p.whole_rows = two_bytes && (a.table || a.nk <= kWholeRows);
+  p.qsplit = parts((int64_t)a.B * a.H * ((a.nq + 127) / 128), a.nk);
   p.ksplit = parts((int64_t)a.B * a.HK * ((a.nk + 127) / 128), (int64_t)a.nq * a.G);
   return p;
 }
@@ -2211,7 +2212,7 @@ GradPlan gradient_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
 // Offsets into the workspace, 256-byte steps.
 size_t step256(size_t n) { return (n + 255) / 256 * 256; }
 struct AttWork {
-  size_t pO, pl, delta, lo, hi, tsum, norms, pq, pk, pv, bytes;
+  size_t pO, pl, delta, lo, hi, tsum, norms, rsum, pq, pk, pv, bytes;
 };
 AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_bytes) {
   AttWork w{};
@@ -2237,6 +2238,7 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_
   w.hi = take(rows * sizeof(float));
   w.tsum = take(a.table ? (size_t)a.H * a.B * p.qsplit * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float) : 0);
   size_t keys = (size_t)a.B * a.HK * a.nk * p.ksplit * sizeof(float);
+  w.rsum = take(p.whole_rows && p.qsplit > 1 ? 2 * rows * p.qsplit * sizeof(float) : 0);
   w.pq = take(p.qsplit > 1 ? rows * p.qsplit * a.d * sizeof(float) : 0);
   w.pk = take(p.ksplit > 1 ? keys * a.d : 0);
   w.pv = take(p.ksplit > 1 ? keys * a.dv : 0);
@@ -2315,6 +2317,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   g.ovec = wide_rows(O, nullptr, a.dv, e, 16), g.dovec = wide_rows(dO, g.dos, a.dv, e, 16);
   g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
   g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (float*)((char*)work + w.norms);
+  g.rsum = (float*)((char*)work + w.rsum);
   g.pq = (float*)((char*)work + w.pq), g.pk = (float*)((char*)work + w.pk), g.pv = (float*)((char*)work + w.pv);
   GradPlan p = gradient_plan(c, a, e == 2);
   g.qsplit = p.qsplit, g.ksplit = p.ksplit, g.whole_rows = p.whole_rows;

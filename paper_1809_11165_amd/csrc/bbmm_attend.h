@@ -52,7 +52,9 @@ struct AttGrad {
   float *delta, *lo, *hi;
   float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets
   float* norms;                  // fp16: largest |do_i| and |v_j|, a pair per slot
-  int whole_rows;                // few keys: the dQ pass forms delta from the row itself
+  int whole_rows;                // the dQ pass forms delta from the row itself
+  int rows_only;                 // a launch of the dQ kernel for just that, where the keys are split: into rsum
+  float* rsum;                   // qsplit x B x H x nq pairs: sum of p, sum of p dP
   int qsplit, ksplit;            // parts that the keys of the dQ pass, and the queries of the dK, dV pass, are split into
   float *pq, *pk, *pv;           // their results: parts x the size of dQ, dK, dV
 };

@@ -204,12 +204,12 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
   float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
   int rel = rest_below(-(int64_t)q0 - start_of(a, b));
-  // The row from all its keys, ahead of the pass: f(scores' products, dP, mul, add) for every block of 32.
-  auto whole_row = [&](auto f) {
-    for (int t = 0; t < tiles; ++t) {
-      fetch(tl, t);
-      uint64_t keep = put(tl, t, 0);
-      settle();
+  // The row from its keys of tiles [from_, to), ahead of the pass: f(scores' products, dP, mul, add) for every block of 32.  The next tile is on its way meanwhile.
+  auto whole_row = [&](int from_, int to, auto f) {
+    if (from_ < to) fetch(tl, from_);
+    for (int t = from_, at = 0; t < to; ++t, at ^= 1) {
+      uint64_t keep = put(tl, t, at);
+      fetch(tl, t + 1);
       __syncthreads();
       if (ln) {
         left = uniform(line[kPad]);
@@ -218,23 +218,23 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         f32x16 s = f32x16{}, dp = f32x16{};
-        if (keep != kAll) s = scores_start(0, 32 * n);
+        if (keep != kAll) s = scores_start(at, 32 * n);
 #pragma unroll
-        for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[0][0], 32 * n, k, lane), q[k], s);
+        for (int k = 0; k < NS; ++k) s = Frag<T>::mma(row_frag<T, DP>(tile[at][0], 32 * n, k, lane), q[k], s);
 #pragma unroll
-        for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 32 * n, k, lane), dof[k], dp);
+        for (int k = 0; k < NS; ++k) dp = Frag<T>::mma(row_frag<T, DP>(tile[at][1], 32 * n, k, lane), dof[k], dp);
         float mul = a.c2, add = 0.f;
         if (ln) add_bias<true>(s, a.c2, ln, far, rel + t * BK + 32 * n, left, right, lane, mul, add);
         f(s, dp, mul, add);
       }
-      __syncthreads();
     }
+    __syncthreads();
   };
   __syncthreads();
   bool any_wide = uniform(side[0] + side[1] + side[2] + side[3]) != 0.f;
   if (any_wide) {
     float top = -__builtin_inff(), sum = 0.f;
-    whole_row([&](const f32x16& s, const f32x16&, float mul, float add) {
+    whole_row(0, tiles, [&](const f32x16& s, const f32x16&, float mul, float add) {
       float x[16], big = top;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -253,19 +253,32 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
   bool coarse = __any(hi != 0.f);
   if (g.whole_rows) {
-    // delta_i = sum_j p_ij dP_ij
+    // delta_i = sum_j p_ij dP_ij / sum_j p_ij; of a split row from the parts that a launch of this kernel with rows_only left
     float total = 0.f, sd = 0.f;
-    whole_row([&](const f32x16& s, const f32x16& dp, float mul, float add) {
+    size_t rows = (size_t)a.B * a.H * a.nq;
+    if (g.qsplit == 1 || g.rows_only) {
+      whole_row(t0, t1, [&](const f32x16& s, const f32x16& dp, float mul, float add) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x = fmaf(s[r], mul, add) - hi;
-        x = __builtin_amdgcn_exp2f(x - lo);
-        total += x;
-        sd = fmaf(x, dp[r], sd);
+        for (int r = 0; r < 16; ++r) {
+          float x = fmaf(s[r], mul, add) - hi;
+          x = __builtin_amdgcn_exp2f(x - lo);
+          total += x;
+          sd = fmaf(x, dp[r], sd);
+        }
+      });
+      total = both_sum(total);
+      sd = both_sum(sd);
+      if (g.rows_only) {
+        if (half == 0 && i < qn) *(float2*)(g.rsum + 2 * (sp * rows + row)) = float2{total, sd};
+        return;
       }
-    });
-    total = both_sum(total);
-    sd = both_sum(sd);
+    } else if (i < qn) {
+      for (int k = 0; k < g.qsplit; ++k) {
+        float2 x = *(const float2*)(g.rsum + 2 * (k * rows + row));
+        total += x.x;
+        sd += x.y;
+      }
+    }
     delta = some && total != 0.f ? sd / total : 0.f;
   }
   if (half == 0 && i < qn && sp == 0) g.delta[row] = delta, g.lo[row] = lo, g.hi[row] = hi;   // for the next pass
@@ -649,8 +662,16 @@ void dkv_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
 }
 template <typename T>
 void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
-  if (a.kvec && a.vvec) dq_v<T, true>(s, a, g);
-  else dq_v<T, false>(s, a, g);
+  auto pass = [&](const AttGrad& x) {
+    if (a.kvec && a.vvec) dq_v<T, true>(s, a, x);
+    else dq_v<T, false>(s, a, x);
+  };
+  if (g.whole_rows && g.qsplit > 1) {
+    AttGrad ahead = g;
+    ahead.rows_only = 1;
+    pass(ahead);
+  }
+  pass(g);
 }
 template <typename T>
 void dkv_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {

@@ -500,3 +500,34 @@ def test_two_contexts_at_work_at_once():
             assert all(torch.equal(x, y) for x, y in zip(pair[k], want[k]))
     for c in ctxs:
         c.close()
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("nq,nk,edges,two_sided,start", [
+    (37, 2171, [1, 3, 12], True, 2134),           # nearly all of a row behind the last edge; keys split over workgroups
+    (741, 1498, [1, 2, 3, 4, 5, 8, 13, 28], False, 0),    # and all of many rows in one bucket
+    (1281, 333, [1, 13, 170], True, 0),
+    (90, 900, [1, 1000], True, 40),               # in one between two edges
+    (5, 9000, EDGES, True, 8990),
+])
+def test_a_table_of_rows_that_lie_in_one_bucket(ctx, kind, nq, nk, edges, two_sided, start):
+    """A row's dS sum to zero, so little is left of a bucket that holds nearly all of it: the rounding of o must not stand there.  Bound:
+    half a step of the result, and 64 u32 of what the sums are formed from, sum p (|dP| + |delta|)."""
+    rng = np.random.default_rng(23)
+    att, dO = _case(rng, kind, 1, 2, 1, nq, nk, 48, 48, edges=edges, two_sided=two_sided, start=[start])
+    Q, K, V, T, D = (_host(x)[0] if x.dim() == 4 else _host(x) for x in (att.Q, att.K, att.V, att.table, dO))
+    want, size = np.zeros_like(T), np.zeros_like(T)
+    b = A.bucket(np.arange(nk)[None, :] - np.arange(nq)[:, None] - start, edges, two_sided)
+    for h in range(2):
+        s = Q[:, h] @ K[:, 0].T * 48 ** -0.5 + T[h][b]
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        dP = D[:, h] @ V[:, 0].T
+        delta = (p * dP).sum(1, keepdims=True)
+        for n in range(T.shape[1]):
+            want[h, n] = (p * (dP - delta))[b == n].sum()
+            size[h, n] = (p * (np.abs(dP) + np.abs(delta)))[b == n].sum()
+    O, lse = ctx.bbmm_attend(att)
+    got = _host(ctx.bbmm_attend_grad(att, O, lse, dO)[3])
+    off, lim = np.abs(got - want), A.UNIT[kind] * np.abs(want) + A.TINY[kind] + 64 * A.U32 * size
+    assert (off <= lim).all(), (off / np.maximum(lim, 1e-300)).max()
