@@ -258,10 +258,17 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     size_t rows = (size_t)a.B * a.H * a.nq;
     if (g.qsplit == 1 || g.rows_only) {
       whole_row(t0, t1, [&](const f32x16& s, const f32x16& dp, float mul, float add) {
+        f32x16 y = s;
+        if (coarse) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) y[r] = fmaf(s[r], mul, add) - hi;
+          mul = 1.f;
+          add = 0.f;
+        }
+        add -= lo;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float x = fmaf(s[r], mul, add) - hi;
-          x = __builtin_amdgcn_exp2f(x - lo);
+          float x = __builtin_amdgcn_exp2f(fmaf(y[r], mul, add));
           total += x;
           sd = fmaf(x, dp[r], sd);
         }
