@@ -2191,7 +2191,8 @@ constexpr int64_t kGradPart = 128;
 // differences: where most of a row lies in one bucket (long rows beyond the last edge) it is far more than what is left.  So in two-byte types rows of up to
 // kWholeRows keys, and all rows with a table, form delta in fp32 from all their scores instead, two products more.  Against 64 bits, bf16, without / with:
 // 500 queries of 8 keys: dQ 2.7e-3 / 2.4e-3, table 1.3e-2 / 1.8e-3; table of 37 x 2171, last edge 12: 1.2e-1 / below 4e-3 (training step of 8 x 12
-// heads, 512 x 640, d = 64: 89 / 104 us).
+// heads, 512 x 640, d = 64: 89 / 103 us).  fp32 keeps the rounded o: over 78 drawn calls the table's error is 1.3 times that of the plain form in the
+// median with it and 1.0 with the scores, at most 3.9e-6 and 3.1e-6 in all, for 142 / 181 us a step of 2 x 8 heads, 500 x 1000.
 constexpr int64_t kWholeRows = 128;
 struct GradPlan {
   int qsplit, ksplit;
