@@ -34,6 +34,30 @@ __device__ __forceinline__ void drop_keys(f32x16& s, unsigned keep, float* limit
   __builtin_amdgcn_wave_barrier();
 }
 
+// Whether a lane's operands hold an infinity or NaN.
+template <typename T, int N>
+__device__ __forceinline__ bool not_finite(const typename Frag<T>::type (&f)[N]) {
+  if constexpr (sizeof(T) == 4) {
+    float z = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z = fmaf(f[k][e], 0.f, z);
+    return z != 0.f;
+  } else {
+    // two elements a word; an exponent of ones carries into the sign's place
+    constexpr unsigned kExp = __is_same(T, _Float16) ? 0x7c007c00u : 0x7f807f80u, kOne = kExp & ~(kExp << 1);
+    unsigned z = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      u32x4 w = __builtin_bit_cast(u32x4, f[k]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z |= (w[e] & kExp) + kOne;
+    }
+    return (z & 0x80008000u) != 0;
+  }
+}
+
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attend(AttArgs a, AttOut o, int nqt) {
   typedef typename Frag<T>::type frag;
@@ -95,6 +119,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
     for (int e = 0; e < 8; ++e) p[u][e] = (T)0.f;
   float m = -__builtin_inff(), l = 0.f;     // reference and sum (this lane's half of the keys)
   float left = 0.f, right = 0.f;
+  bool odd = false;                            // some query of the wave holds an infinity or NaN
   const T* kp = K + (int64_t)t0 * BK * a.ks[1];
   const T* vp = V + (int64_t)t0 * BK * a.vs[1];
   int64_t kstep = BK * a.ks[1], vstep = BK * a.vs[1];
@@ -129,6 +154,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
       ln = line;
     }
     settle();
+    odd = __any(not_finite<T>(q));
     __syncthreads();
     if (ln) {
       left = uniform(line[kPad]);
@@ -141,9 +167,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
   }
   // A turn per tile.  On entry the scores' products of this tile are there, and p holds the weights of the tile before; LDS holds the keys of the
   // tile after and the values of the tile before.  Tiles up to `end` are of one kind: plain ones lie beyond the last edge on one side (or have no
-  // bias); their scores are c2 s + side as they stand.
+  // bias); their scores are c2 s + side as they stand.  A wave with odd queries has none: excluded keys, zeros in LDS, make NaN of an infinity or NaN
+  // in a query, so there their scores are set to -infinity again, whatever came out.
   int end = ln ? t0 : t1;
-  bool plain = !ln;
+  bool plain = !ln && !odd;
   float side = 0.f;
   auto turn = [&](auto par_, int t) {
     constexpr int PAR = decltype(par_)::value;
@@ -153,7 +180,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
       int r = rel + t * BK;
       end = t1;
       side = r < 0 ? left : right;
-      plain = (r + 31 <= -far || r - 31 >= far) && fabsf(side) < kFoldable;
+      plain = (r + 31 <= -far || r - 31 >= far) && fabsf(side) < kFoldable && !odd;
       if (r + 31 <= -far) end = min(end, t + (-far - 31 - r) / BK + 1);
       else if (r - 31 < far) end = min(end, t + (far + 30 - r) / BK + 1);
     }
@@ -163,7 +190,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
     kp += kstep;
     vp += vstep;
     float mul = a.c2, add = side;
-    if (!plain) add_bias<true>(s, a.c2, ln, far, rel + t * BK, left, right, lane, mul, add);
+    if (!plain) {
+      add_bias<true>(s, a.c2, ln, far, rel + t * BK, left, right, lane, mul, add);
+      if (odd && k0 != kAll) {
+        unsigned mine = (unsigned)k0 >> (4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = (mine & (1u << (8 * (r >> 2) + (r & 3)))) ? s[r] : -__builtin_inff();
+      }
+    }
     // Steps kept in this order: each reads the operand of the step after next, queues one product of the tile after (scores) or before (values),
     // and does its share of this tile's softmax meanwhile.
     const char *kt = tk[PAR ^ 1], *vt = tv[PAR ^ 1];

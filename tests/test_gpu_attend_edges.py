@@ -1,0 +1,53 @@
+"""GPU parity of the attention where rows, scales and biases are out of the ordinary: rows that nothing is left for beside infinities and NaN in
+places that count, biases that leave an fp32 lse coarse, gradients of unlike size in fp16, and units of work dealt out over the dies."""
+import numpy as np
+import pytest
+
+from oracle import attend_oracle as A
+from test_gpu_attend import DEV, EDGES, TYPES, _case, _check, _host, _oracle, _rand, _run_and_check
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_1809_11165_amd import binding
+    c = binding.Context(0)
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("edges", [None, EDGES])
+@pytest.mark.parametrize("nq,nk", [(2, 130), (100, 130), (100, 1500)])
+def test_queries_of_nan_and_infinities_whose_keys_are_all_masked(ctx, kind, edges, nq, nk):
+    """Nothing is left for these rows, whatever the query and the gradient hold: o = 0, lse = -infinity, no part in any gradient."""
+    rng = np.random.default_rng(31)
+    att, dO = _case(rng, kind, 2, 2, 1, nq, nk, 64, 64, edges=edges, mask=0.7)
+    att.key_mask[1] = False
+    want = _oracle(kind, att, dO)
+    att.Q[1] = float("nan")
+    att.Q[1, ::2] = float("inf")
+    dO[1] = float("nan")
+    O, lse, dQ, dK, dV, dT = _run_and_check(ctx, kind, att, dO, want)
+    assert torch.all(O[1] == 0) and torch.all(lse[1] == -float("inf"))
+    assert torch.all(dQ[1] == 0) and torch.all(dK[1] == 0) and torch.all(dV[1] == 0)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("edges", [None, EDGES])
+@pytest.mark.parametrize("nq", [3, 100])
+def test_queries_whose_scores_are_all_minus_infinity(ctx, kind, edges, nq):
+    """An infinite feature of the query makes every kept score -infinity; the masked ones, whatever they are, do not count."""
+    rng = np.random.default_rng(32)
+    att, dO = _case(rng, kind, 1, 2, 1, nq, 90, 32, 32, edges=edges, mask=0.7)
+    att.K[..., 0] = att.K[..., 0].abs() + 0.5
+    att.Q[0, 1] = 0
+    dO[0, 1] = 0                                           # a row without a part in the gradients, for the oracle
+    val, err = _oracle(kind, att, dO)
+    for name, x in (("o", 0.0), ("dq", 0.0)):
+        val[name][0, 1], err[name][0, 1] = x, 0.0
+    val["lse"][0, :, 1], err["lse"][0, :, 1] = -np.inf, 0.0
+    att.Q[0, 1, :, 0] = -float("inf")
+    _run_and_check(ctx, kind, att, dO, (val, err))
