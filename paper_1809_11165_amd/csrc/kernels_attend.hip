@@ -270,6 +270,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_at
   float inv = some ? 1.f / l : 0.f;
   float lse2 = some ? (m - Lift<T>::value) + __builtin_amdgcn_logf(l) : -__builtin_inff();
   if (i >= a.nq) return;
+  if (!some) {                               // zero also beside infinite values, which make NaN of weights of zero
+#pragma unroll
+    for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
+  }
   size_t row = ((size_t)b * a.H + h) * a.nq + i;
   if (o.nsplit == 1) {
     if (half == 0) o.lse[row] = lse2 * kLn2;

@@ -51,3 +51,19 @@ def test_queries_whose_scores_are_all_minus_infinity(ctx, kind, edges, nq):
     val["lse"][0, :, 1], err["lse"][0, :, 1] = -np.inf, 0.0
     att.Q[0, 1, :, 0] = -float("inf")
     _run_and_check(ctx, kind, att, dO, (val, err))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("nq,nk", [(2, 130), (100, 130), (100, 1500)])
+def test_rows_without_keys_are_zero_beside_infinite_values(ctx, kind, nq, nk):
+    """Rows behind their length, and rows whose bias excludes every key, where a value that others read is infinite."""
+    rng = np.random.default_rng(33)
+    att, _ = _case(rng, kind, 1, 2, 2, nq, nk, 64, 64, edges=EDGES, start=[-1], q_len=[nq - 1])
+    att.table[:, len(EDGES) + 1:] = -float("inf")          # keys ahead: the first row keeps none
+    att.V[0, ::7] = float("inf")
+    att.V[0, 3::7] = -float("inf")
+    O, lse = ctx.bbmm_attend(att)
+    for i in (0, nq - 1):
+        assert torch.all(O[0, i] == 0) and torch.all(lse[0, :, i] == -float("inf")), i
+    if nq > 2:
+        assert torch.isfinite(lse[0, :, 1:nq - 1]).all()
