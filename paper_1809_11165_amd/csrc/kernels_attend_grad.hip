@@ -171,6 +171,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     }
   }
   bool some = lse != -__builtin_inff();      // something is left in the row
+  bool empty = __any(!some);
   delta = some ? both_sum(delta) : 0.f;
   float lo = some ? lse * kLog2e : __builtin_inff(), hi = 0.f;   // weights are exp2((s - hi) - lo)
   bool wide = fabsf(lse) > kCoarse && fabsf(lse) < __builtin_inff();
@@ -356,6 +357,10 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     }
     __builtin_amdgcn_sched_barrier(0);
     if (ln) {
+      if (empty) {                           // an infinity in a key or value of others makes NaN of these lanes' zeros
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = some ? s[r] : 0.f;
+      }
       if (where == 0) {
         add_diagonals(s, diag + wave * nline + rel0 + span, lane);
       } else {
@@ -393,6 +398,10 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
         for (int r = 0; r < 4; ++r)
           store4(out, 32 * n + 8 * r + 4 * half, a.d, vec, acc[n][4 * r] * f, acc[n][4 * r + 1] * f, acc[n][4 * r + 2] * f, acc[n][4 * r + 3] * f);
     };
+    if (!some) {
+#pragma unroll
+      for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
+    }
     if (g.qsplit == 1) write((T*)g.dQ + at, g.dqvec);
     else write(g.pq + sp * ((int64_t)a.B * a.nq * a.H * a.d) + at, a.d % 4 == 0);
   }

@@ -67,3 +67,17 @@ def test_rows_without_keys_are_zero_beside_infinite_values(ctx, kind, nq, nk):
         assert torch.all(O[0, i] == 0) and torch.all(lse[0, :, i] == -float("inf")), i
     if nq > 2:
         assert torch.isfinite(lse[0, :, 1:nq - 1]).all()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("which", ["K", "V"])
+@pytest.mark.parametrize("nq,nk", [(3, 40), (70, 300), (70, 1500)])
+def test_rows_without_keys_have_no_part_in_gradients_beside_infinities(ctx, kind, which, nq, nk):
+    """One live row, the rest behind its length: their dQ is zero, and so are the table's buckets that only they could reach."""
+    rng = np.random.default_rng(34)
+    att, dO = _case(rng, kind, 1, 2, 2, nq, nk, 64, 64, edges=EDGES, q_len=[1])
+    getattr(att, which)[0, 2::9] = float("inf")
+    O, lse = ctx.bbmm_attend(att)
+    dQ, _, _, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    assert torch.all(dQ[0, 1:] == 0)
+    assert torch.all(dT[:, 1:len(EDGES) + 1] == 0)         # keys behind the query: none for the row at the first key
