@@ -519,6 +519,21 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     c1 = put(t2, 1);
   }
   settle();
+  // Rows that take no part run along with zeros: a key that holds an infinity or NaN would make NaN of them, so there their scores are put back to zero
+  // (their lo is infinite: weights zero).  A product with zero tells such keys.
+  float z = 0.f;
+  if constexpr (sizeof(T) == 2) {
+    f32x16 c = f32x16{};
+#pragma unroll
+    for (int k = 0; k < NS; ++k) c = Frag<T>::mma(frag{}, kf[k], c);
+    z = c[0];
+  } else {
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z = fmaf(kf[k][e], 0.f, z);
+  }
+  bool odd = __any(z != 0.f);
   __syncthreads();
   if (t0 < t1) {
 #pragma unroll
@@ -538,6 +553,10 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int n = 0; n < 4; ++n) {
       l4[n] = *(const f32x4*)(st + 8 * n);
       d4[n] = *(const f32x4*)(st + BQ + 8 * n);
+    }
+    if (odd) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = l4[r >> 2][r & 3] < __builtin_inff() ? s[r] : 0.f;
     }
     if (ln) add_bias<false>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
     if (wide) {

@@ -81,3 +81,21 @@ def test_rows_without_keys_have_no_part_in_gradients_beside_infinities(ctx, kind
     dQ, _, _, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
     assert torch.all(dQ[0, 1:] == 0)
     assert torch.all(dT[:, 1:len(EDGES) + 1] == 0)         # keys behind the query: none for the row at the first key
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("nq", [3, 70, 200])
+def test_rows_without_keys_have_no_part_in_gradients_of_infinite_keys(ctx, kind, nq):
+    """A key whose infinite feature makes every live row's score -infinity weighs nothing: its dK and dV are zero, whatever rows behind the
+    length make of it, and the other keys' are as if it were masked."""
+    rng = np.random.default_rng(39)
+    att, dO = _case(rng, kind, 1, 2, 2, nq, 90, 64, 64, edges=EDGES, q_len=[nq - 1], mask=1.1)
+    att.Q[..., 0] = -att.Q[..., 0].abs() - 0.5
+    att.K[0, 5], att.key_mask[0, 5] = 0, False
+    val, err = _oracle(kind, att, dO)
+    att.K[0, 5, :, 0], att.key_mask = float("inf"), None
+    O, lse = ctx.bbmm_attend(att)
+    _, dK, dV, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    for name, x in (("o", O), ("lse", lse), ("dk", dK), ("dv", dV), ("dtable", dT)):
+        _check(x, val, err, name)
+    assert torch.all(dK[0, 5] == 0) and torch.all(dV[0, 5] == 0)
