@@ -91,9 +91,13 @@ __global__ __launch_bounds__(256) void k_attend_norms(AttArgs a, AttGrad g) {
   if (tid < 2) g.norms[2 * blockIdx.x + tid] = sqrtf(fmaxf(fmaxf(part[tid][0], part[tid][1]), fmaxf(part[tid][2], part[tid][3])));
 }
 
-// Beyond this, fp32 holds lse too coarsely to recover weights from it (a row of nothing but masks of -1e9 or of the type's lowest value):
-// the row's largest score and log2 of its sum are formed again and kept apart.
-constexpr float kCoarse = 65536.f;
+// Beyond this, fp32 holds lse too coarsely to recover weights from it: rounded as a logarithm to base 2, to base e and to base 2 again, it
+// leaves all weights of a row off by a common factor of up to 3.3 2^-24 |lse|, which a softmax that divides by its own sum does not have.  The row's
+// largest score and log2 of its sum are formed again there and kept apart.  At these bounds the factor is an eighth of half a step of
+// the type (fp32: 2^-16; scores of that size are rounded by a third of it themselves).
+template <typename T> struct Coarse { static constexpr float value = 64.f; };
+template <> struct Coarse<_Float16> { static constexpr float value = 256.f; };
+template <> struct Coarse<__bf16> { static constexpr float value = 2048.f; };
 
 // 64 keys a turn, as two blocks of 32 (fp32: one block a turn).  While the matrix unit forms the scores and dP of the next block, the vector unit turns this one's into dS; then
 // dQ takes it up.
@@ -174,7 +178,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   bool empty = __any(!some);
   delta = some ? both_sum(delta) : 0.f;
   float lo = some ? lse * kLog2e : __builtin_inff(), hi = 0.f;   // weights are exp2((s - hi) - lo)
-  bool wide = fabsf(lse) > kCoarse && fabsf(lse) < __builtin_inff();
+  bool wide = fabsf(lse) > Coarse<T>::value && fabsf(lse) < __builtin_inff();
   if (!some) {                               // whatever the row holds
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[s] = dof[s] = frag{};

@@ -99,3 +99,33 @@ def test_rows_without_keys_have_no_part_in_gradients_of_infinite_keys(ctx, kind,
     for name, x in (("o", O), ("lse", lse), ("dk", dK), ("dv", dV), ("dtable", dT)):
         _check(x, val, err, name)
     assert torch.all(dK[0, 5] == 0) and torch.all(dV[0, 5] == 0)
+
+
+@pytest.mark.parametrize("kind,value", [(k, v) for k in ("f32", "f16", "bf16") for v in (-300.0, -1000.0, -4000.0, -10000.0, -30000.0, -60000.0, -65504.0, 5000.0)])
+@pytest.mark.parametrize("nq,nk,dv", [(4, 128, 128), (70, 256, 64), (70, 2048, 128)])
+@pytest.mark.parametrize("table", [False, True])
+def test_gradients_of_rows_that_a_large_bias_flattens(ctx, kind, value, nq, nk, dv, table):
+    """The same bias on every key, from a table beside scores too small to be seen (scale 2^-60) or from a feature that is 1 in Q and the bias in
+    K, the others zero: every weight is 1 / nk, a power of two, which all types hold.  Weights recovered from an fp32 lse of that size, rounded on its
+    way, are off by a factor common to the row, and so is dV, all of one sign here.  Single elements may be off by a rounding of the result, the
+    factor (an eighth of half a step of the type, in fp32 2^-16) and fp32 sums; in their total the roundings, 4 dv different ones of at most u, add up like
+    the square root of their number (four deviations)."""
+    rng = np.random.default_rng(36)
+    att, dO = _case(rng, kind, 4, 2, 1, nq, nk, 32, dv, edges=[1] if table else None)
+    dO.abs_()
+    if table:
+        att.table[:] = value
+        att.scale = 2.0 ** -60
+        bias = float(att.table[0, 0])
+    else:
+        att.Q[..., :-1], att.K[..., :-1] = 0, 0
+        att.Q[..., -1], att.K[..., -1], att.scale = 1, value, 1.0
+        bias = float(att.K[0, 0, 0, -1])
+    O, lse = ctx.bbmm_attend(att)
+    assert np.allclose(_host(lse), bias + np.log(nk), rtol=6 * A.U32, atol=0)
+    got = _host(ctx.bbmm_attend_grad(att, O, lse, dO)[2])
+    want = np.repeat(_host(dO).sum((1, 2))[:, None, None], nk, 1) / nk
+    u = A.UNIT[kind]
+    factor = max(u / 8, 2.0 ** -16) + 2 * nq * A.U32
+    assert np.all(np.abs(got - want) <= (u + factor) * want + A.TINY[kind])
+    assert abs(got[:, 0].sum() / want[:, 0].sum() - 1) <= factor + 4 * u / np.sqrt(3 * 4 * dv)
