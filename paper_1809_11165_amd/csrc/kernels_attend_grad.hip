@@ -500,31 +500,9 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
   constexpr float kLift = PLift<T>::value;
   float cs = ds_scale<T>(g, lane), unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
-  auto put = [&](const Loads& x, int at) {
-    uint64_t keep = __ballot(x.lo != __builtin_inff()) & (NB == 2 ? ~0ull : 0xffffffffull);
-    x.q.store(tile[at][0], keep, tid);
-    x.d.store(tile[at][1], keep, tid);
-    if (tid < BQ) {
-      stat[at][0][tid] = x.lo;                 // infinite where nothing is left in the row: weights zero
-      stat[at][1][tid] = x.delta * ck;
-      stat[at][2][tid] = x.hi;
-    }
-    return __any(x.hi != 0.f);
-  };
-  f32x16 dk[ND], dv[ND], sc[2], pc[2];       // of a turn's two blocks: scores, dP
-  sc[0] = pc[0] = f32x16{};
-#pragma unroll
-  for (int n = 0; n < ND; ++n) dk[n] = dv[n] = f32x16{};
-  float left = 0.f, right = 0.f;
-  int rel = rest_above((int64_t)k0 - start_of(a, b));
-  bool c0 = false, c1 = false;               // rows with a `hi` in this tile and the next
-  if (t0 < t1) {
-    c0 = put(tl, 0);
-    c1 = put(t2, 1);
-  }
-  settle();
-  // Rows that take no part run along with zeros: a key that holds an infinity or NaN would make NaN of them, so there their scores are put back to zero
-  // (their lo is infinite: weights zero).  A product with zero tells such keys.
+  // Rows that take no part run along with zeros, of which a key that holds an infinity or NaN makes NaN.  Where it does (a product with zero tells such
+  // keys) their blocks go the way of rows with a `hi`, where the minimum with a number makes a number of NaN; their lo is infinite, so the weight is
+  // zero.  (Rows that count have a lo of NaN beside a score of NaN.)
   float z = 0.f;
   if constexpr (sizeof(T) == 2) {
     f32x16 c = f32x16{};
@@ -538,6 +516,29 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       for (int e = 0; e < 8; ++e) z = fmaf(kf[k][e], 0.f, z);
   }
   bool odd = __any(z != 0.f);
+  auto put = [&](const Loads& x, int at) {
+    uint64_t keep = __ballot(x.lo != __builtin_inff()) & (NB == 2 ? ~0ull : 0xffffffffull);
+    x.q.store(tile[at][0], keep, tid);
+    x.d.store(tile[at][1], keep, tid);
+    if (tid < BQ) {
+      stat[at][0][tid] = x.lo;                 // infinite where nothing is left in the row: weights zero
+      stat[at][1][tid] = x.delta * ck;
+      stat[at][2][tid] = x.hi;
+    }
+    return __any(x.hi != 0.f || (odd && x.lo == __builtin_inff()));
+  };
+  f32x16 dk[ND], dv[ND], sc[2], pc[2];       // of a turn's two blocks: scores, dP
+  sc[0] = pc[0] = f32x16{};
+#pragma unroll
+  for (int n = 0; n < ND; ++n) dk[n] = dv[n] = f32x16{};
+  float left = 0.f, right = 0.f;
+  int rel = rest_above((int64_t)k0 - start_of(a, b));
+  bool c0 = false, c1 = false;               // whether this tile and the next have rows with a `hi`, or zeros beside odd keys
+  if (t0 < t1) {
+    c0 = put(tl, 0);
+    c1 = put(t2, 1);
+  }
+  settle();
   __syncthreads();
   if (t0 < t1) {
 #pragma unroll
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int k = 0; k < NS; ++k) pc[0] = Frag<T>::mma(row_frag<T, DP>(tile[0][1], 0, k, lane), vf[k], pc[0]);
   }
   int now = 0;
-  // Block of the turn at buffer `at` (rel0: its differences, wide: whether it has a `hi`); the next block: rows 32 (block ^ 1) on of buffer `on`.
+  // Block of the turn at buffer `at` (rel0: its differences, wide: see c0); the next block: rows 32 (block ^ 1) on of buffer `on`.
   auto block = [&](auto block_, int rel0, int at, int on, bool wide) {
     constexpr int B = decltype(block_)::value, here = NB == 2 ? 32 * B : 0, there = NB == 2 ? 32 * (B ^ 1) : 0;   // rows in their tiles
     f32x16 &s = sc[B], &dp = pc[B], &s2 = sc[B ^ 1], &dp2 = pc[B ^ 1];
@@ -558,17 +559,13 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       l4[n] = *(const f32x4*)(st + 8 * n);
       d4[n] = *(const f32x4*)(st + BQ + 8 * n);
     }
-    if (odd) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = l4[r >> 2][r & 3] < __builtin_inff() ? s[r] : 0.f;
-    }
     if (ln) add_bias<false>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
     if (wide) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         f32x4 h4 = *(const f32x4*)(st + 2 * BQ + 8 * n);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * n + e] = fmaf(s[4 * n + e], mul, add) - h4[e];
+        for (int e = 0; e < 4; ++e) s[4 * n + e] = fminf(fmaf(s[4 * n + e], mul, add) - h4[e], 3e38f);
       }
       mul = 1.f;
       add = 0.f;
