@@ -406,8 +406,8 @@ int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns
  *                 (strides in elements, none negative; 0 shares an input, its gradient is then returned for every use)
  *   q_len, k_len  device, batch entries (taken as within [0, nq] and [0, nk]), or NULL: all rows
  *   key_mask      device, batch x nk bytes, or NULL
- *   table         device, heads x buckets, or NULL (no bias).  Entries may be -infinity (pairs excluded); finite entries below
- *                 -2.3e38 count as that
+ *   table         device, heads x buckets, or NULL (no bias).  Entries may be -infinity (pairs excluded); finite entries beyond
+ *                 2.3e38 in magnitude count as that
  *   edges         host, n_edges entries, 1 <= e_1 < .. <= 1024; 0 <= n_edges <= 63; only read during the call
  *   q_start       device, batch entries: position of query 0 on the keys' axis, or NULL (0)
  * Limits: batch, heads and kv_heads <= 65535, nq and nk <= 2^30; zero sizes are allowed for batch, nq and nk.

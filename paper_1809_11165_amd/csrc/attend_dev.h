@@ -292,13 +292,14 @@ __device__ __forceinline__ void add_diagonals(const f32x16& s, float* line, int 
   __builtin_amdgcn_wave_barrier();
 }
 
-// A table entry in units of the base-2 exponent.  Finite entries stay finite: one below -2.3e38 counts as that (the same
-// weight zero beside any other score, and weights of its own where a row holds nothing else).
+// A table entry in units of the base-2 exponent.  Finite entries stay finite: one beyond 2.3e38 in magnitude counts as that (below, the same
+// weight zero beside any other score, and weights of its own where a row holds nothing else; above, all of the row's weight).
 template <typename T>
 __device__ __forceinline__ float bias2(T t) {
+  constexpr float kMost = 3.40282347e38f;
   float x = (float)t;
   float y = x * kLog2e;
-  return (x > -__builtin_inff()) ? fmaxf(y, -3.40282347e38f) : y;
+  return fabsf(x) < __builtin_inff() ? fminf(fmaxf(y, -kMost), kMost) : y;
 }
 
 // line[r + far + kPad] = bias of difference r, |r| <= far + kPad, for one head.

@@ -129,3 +129,32 @@ def test_gradients_of_rows_that_a_large_bias_flattens(ctx, kind, value, nq, nk, 
     factor = max(u / 8, 2.0 ** -16) + 2 * nq * A.U32
     assert np.all(np.abs(got - want) <= (u + factor) * want + A.TINY[kind])
     assert abs(got[:, 0].sum() / want[:, 0].sum() - 1) <= factor + 4 * u / np.sqrt(3 * 4 * dv)
+
+
+@pytest.mark.parametrize("kind,value", [("f32", 3e38), ("f32", 3.4028234663852886e38), ("bf16", 3e38), ("bf16", 3.3895313892515355e38), ("f16", 65504.0)])
+@pytest.mark.parametrize("nq", [4, 70])
+def test_tables_of_the_highest_value(ctx, kind, value, nq):
+    """One bucket at the type's end: its keys share the row, the rest weigh nothing.  What a weight 1 / n and a mean of n values take: a
+    rounding of the weight, one of the result, and fp32 sums.  (fp16's largest leaves steps of 2^-7 of a score: scores are kept below.)"""
+    rng = np.random.default_rng(35)
+    att, dO = _case(rng, kind, 1, 2, 1, nq, 90, 32, 32, edges=EDGES)
+    att.scale = 2.0 ** -20
+    att.table[:] = 0
+    att.table[:, -1] = value                                # keys at least the last edge ahead
+    u = A.UNIT[kind]
+    O, lse = ctx.bbmm_attend(att)
+    dQ, dK, dV, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    assert torch.isfinite(lse).all() and (lse[:, :, :min(nq, 69)] > min(value, 2.2e38) / 2).all()
+    V, D, want_dv, size_dv = _host(att.V)[0, :, 0], _host(dO)[0], np.zeros((90, 32)), np.zeros((90, 32))
+    for i in range(nq):
+        at = np.arange(90) >= i + EDGES[-1]
+        if not at.any():                                    # no key that far ahead
+            break
+        mean, size = V[at].mean(0), np.abs(V[at]).mean(0)
+        assert np.all(np.abs(_host(O)[0, i] - mean) <= (2 * u + 128 * A.U32) * size + A.TINY[kind]), i
+        want_dv[at] += D[i].sum(0) / at.sum()
+        size_dv[at] += np.abs(D[i]).sum(0) / at.sum()
+    if nq == 4:                                             # every row has such keys: dV is theirs alone
+        assert np.all(np.abs(_host(dV)[0, :, 0] - want_dv) <= (2 * u + 128 * A.U32) * size_dv + A.TINY[kind])
+    for x in (dQ, dK, dT):
+        assert torch.isfinite(x).all()
