@@ -11,8 +11,8 @@
 // 2 x 8 heads, 500 x 1000, d = 64: 50 and 58 us; there one wave per SIMD fits (registers), and the matrix unit is busy 59 % of the dK, dV pass: the
 // wave's own vector instructions and waits stand between its products.
 //
-// fp16: p and dS are scaled by powers of two before they are rounded, dS by the largest |do_i| |v_j| (k_attend_norms): weights of
-// long rows and small gradients would fall among that type's subnormal numbers.
+// fp16: p and dS are scaled by powers of two before they are rounded, dS by |do_i| times the largest |v_j| (dQ) or the largest |do_i| |v_j| (dK;
+// k_attend_norms): weights of long rows and small gradients would fall among that type's subnormal numbers.
 #include "attend_dev.h"
 
 using namespace att;
@@ -27,26 +27,26 @@ template <> struct PLift<_Float16> { static constexpr float value = 12.f; };
 constexpr int kNormSlots = BBMM_ATT_NORM_SLOTS;
 static_assert(kNormSlots % 64 == 0, "slots per lane");
 
-// Power of two that keeps |dS| <= 2 |do| |v| below 2^15.  All lanes of a wave take part.
-template <typename T>
-__device__ __forceinline__ float ds_scale(const AttGrad& g, int lane) {
-  if constexpr (__is_same(T, _Float16)) {
-    float x = 0.f, y = 0.f;
+// fp16: the largest |do_i| and |v_j|.  All lanes of a wave take part.
+__device__ __forceinline__ float2 norms_of(const AttGrad& g, int lane) {
+  float x = 0.f, y = 0.f;
 #pragma unroll
-    for (int k = 0; k < kNormSlots; k += 64) {
-      float2 z = *(const float2*)(g.norms + 2 * (k + lane));
-      x = fmaxf(x, z.x);
-      y = fmaxf(y, z.y);
-    }
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) {
-      x = fmaxf(x, __shfl_xor(x, k, 64));
-      y = fmaxf(y, __shfl_xor(y, k, 64));
-    }
-    float e = (x > 0.f && y > 0.f) ? 14.f - ceilf(__builtin_amdgcn_logf(x) + __builtin_amdgcn_logf(y)) : 0.f;
-    return uniform(__builtin_amdgcn_exp2f(fminf(fmaxf(e, -100.f), 100.f)));
+  for (int k = 0; k < kNormSlots; k += 64) {
+    float2 z = *(const float2*)(g.norms + 2 * (k + lane));
+    x = fmaxf(x, z.x);
+    y = fmaxf(y, z.y);
   }
-  return 1.f;
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) {
+    x = fmaxf(x, __shfl_xor(x, k, 64));
+    y = fmaxf(y, __shfl_xor(y, k, 64));
+  }
+  return float2{x, y};
+}
+// Power of two that keeps |dS| <= 2 |do| |v| below 2^15.
+__device__ __forceinline__ float ds_scale(float x, float y) {
+  float e = (x > 0.f && y > 0.f) ? 14.f - ceilf(__builtin_amdgcn_logf(x) + __builtin_amdgcn_logf(y)) : 0.f;
+  return __builtin_amdgcn_exp2f(fminf(fmaxf(e, -100.f), 100.f));
 }
 
 // fp16: the norms of the rows that take part, 16 lanes per row; those without a finite norm are left out.
@@ -191,7 +191,18 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int n = tid; n < 4 * nline; n += 256) diag[n] = 0.f;
     ln = line;
   }
-  float cs = ds_scale<T>(g, lane);                 // a power of two: dS is formed times it
+  // a power of two: dS is formed times it.  fp16: a row's own, from its |do_i|, so that a row of small gradients keeps its bits beside others of large ones
+  // (|do| 2^-20 of the largest, weights of 1 / 2000: dQ off by 3e-2 of itself with one for all, 4e-4 so).
+  float cs = 1.f, uncs = 1.f;
+  if constexpr (__is_same(T, _Float16)) {
+    float z = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z = fmaf((float)dof[s][e], (float)dof[s][e], z);
+    cs = ds_scale(sqrtf(both_sum(z)), norms_of(g, lane).y);
+    uncs = 1.f / cs;
+  }
   auto scores_start = [&](int at, int first) {
     f32x16 c;
     const float* x = from[at] + first + 4 * half;
@@ -365,6 +376,10 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = some ? s[r] : 0.f;
       }
+      if constexpr (__is_same(T, _Float16)) {  // rows of unlike scales meet in the table
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= uncs;
+      }
       if (where == 0) {
         add_diagonals(s, diag + wave * nline + rel0 + span, lane);
       } else {
@@ -393,7 +408,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     __syncthreads();
   }
   if (i < a.nq) {
-    float f = a.scale / cs;
+    float f = a.scale * uncs;
     int64_t at = (((int64_t)b * a.nq + i) * a.H + h) * a.d;
     auto write = [&](auto* out, int vec) {
 #pragma unroll
@@ -410,7 +425,6 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     else write(g.pq + sp * ((int64_t)a.B * a.nq * a.H * a.d) + at, a.d % 4 == 0);
   }
   if (ln) {                                  // the loop's last barrier stands before this
-    float f = 1.f / cs;
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
       sl += __shfl_xor(sl, x, 64);
@@ -424,11 +438,11 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       float x = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) x += diag[k * nline + n];
-      line[n] = x * f;
+      line[n] = x;
     }
     __syncthreads();
     float* out = g.tsum + ((((size_t)h * a.B + b) * g.qsplit + sp) * nqt + qt) * a.bk.buckets;
-    bucket_sums(a.bk, line, span, f * (side[0] + side[1] + side[2] + side[3]), f * (side[4] + side[5] + side[6] + side[7]), out, tid);
+    bucket_sums(a.bk, line, span, side[0] + side[1] + side[2] + side[3], side[4] + side[5] + side[6] + side[7], out, tid);
   }
 }
 
@@ -499,7 +513,12 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int s = 0; s < NS; ++s) kf[s] = vf[s] = frag{};
   }
   constexpr float kLift = PLift<T>::value;
-  float cs = ds_scale<T>(g, lane), unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
+  float cs = 1.f;                            // fp16: one power of two for all rows, which add up
+  if constexpr (__is_same(T, _Float16)) {
+    float2 z = norms_of(g, lane);
+    cs = uniform(ds_scale(z.x, z.y));
+  }
+  float unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
   // Rows that take no part run along with zeros, of which a key that holds an infinity or NaN makes NaN.  Where it does (a product with zero tells such
   // keys) their blocks go the way of rows with a `hi`, where the minimum with a number makes a number of NaN; their lo is infinite, so the weight is
   // zero.  (Rows that count have a lo of NaN beside a score of NaN.)

@@ -158,3 +158,28 @@ def test_tables_of_the_highest_value(ctx, kind, value, nq):
         assert np.all(np.abs(_host(dV)[0, :, 0] - want_dv) <= (2 * u + 128 * A.U32) * size_dv + A.TINY[kind])
     for x in (dQ, dK, dT):
         assert torch.isfinite(x).all()
+
+
+@pytest.mark.parametrize("edges", [None, EDGES])
+@pytest.mark.parametrize("nq,nk", [(40, 2000), (300, 2000)])
+def test_small_rows_of_dO_beside_large_ones_in_fp16(ctx, edges, nq, nk):
+    """Rows of dO at 2^10 and at 2^-10 by turns: the small ones' dS, at weights of 1 / 2000, stay out of fp16's subnormal numbers, so that their dQ is off by
+    a rounding of dS, of delta's o and of the result, in the 2-norm of a row one u each."""
+    rng = np.random.default_rng(37)
+    att, dO = _case(rng, "f16", 1, 2, 1, nq, nk, 64, 64, edges=edges)
+    att.scale = 64.0
+    att.Q.mul_(2.0 ** -9)
+    dO[:, ::2].mul_(2.0 ** 10)
+    dO[:, 1::2].mul_(2.0 ** -10)
+    val, err = _oracle("f16", att, dO)
+    O, lse = ctx.bbmm_attend(att)
+    dQ, dK, dV, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    for name, x in (("o", O), ("lse", lse), ("dk", dK), ("dv", dV), ("dtable", dT)):
+        if x is not None:
+            _check(x, val, err, name)
+    got, want = _host(dQ), val["dq"]
+    fits = np.abs(want).max(3) < 65504                     # some large rows go beyond fp16's largest number
+    assert fits[:, 1::2].all()
+    off, size = (np.linalg.norm(x, axis=3) for x in (np.where(fits[..., None], got - want, 0), want))
+    assert size[:, 1::2].min() > 2.0 ** -10                # eight normal features of 2^-14 and more: no steps of subnormal results
+    assert np.all(off <= 3 * A.UNIT["f16"] * size)
