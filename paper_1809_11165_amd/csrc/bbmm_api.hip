@@ -2210,6 +2210,9 @@ GradPlan gradient_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
   return p;
 }
 
+// Workgroups per (batch, shared head) that look for its norms (fp16).
+int norm_slots(const AttArgs& a) { return std::max<int>(1, BBMM_ATT_NORM_SLOTS / std::max<int64_t>(1, (int64_t)a.B * a.HK)); }
+
 // Offsets into the workspace, 256-byte steps.
 size_t step256(size_t n) { return (n + 255) / 256 * 256; }
 struct AttWork {
@@ -2233,7 +2236,7 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_
     w.bytes += step256(n);
     return at;
   };
-  w.norms = take(two_bytes ? 2 * sizeof(float) * BBMM_ATT_NORM_SLOTS : 0);
+  w.norms = take(two_bytes ? 2 * sizeof(float) * a.B * a.HK * norm_slots(a) : 0);
   w.delta = take(rows * sizeof(float));
   w.lo = take(rows * sizeof(float));
   w.hi = take(rows * sizeof(float));
@@ -2323,7 +2326,8 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   GradPlan p = gradient_plan(c, a, e == 2);
   g.qsplit = p.qsplit, g.ksplit = p.ksplit, g.whole_rows = p.whole_rows;
   hipStream_t s = c->stream;
-  launch_attend_norms(s, in->type, a, g);
+  g.norm_slots = norm_slots(a);
+  if (rows || keys) launch_attend_norms(s, in->type, a, g);
   if (rows) launch_attend_dq(s, in->type, a, g);
   if (keys) launch_attend_dkv(s, in->type, a, g);
   launch_attend_sums(s, in->type, a, g);

@@ -9,7 +9,7 @@
 #define BBMM_ATT_MAXD 128      // features of Q, K and of V
 #define BBMM_ATT_MAXEDGES 63   // edges of the buckets
 #define BBMM_ATT_FAR 1024      // largest edge
-#define BBMM_ATT_NORM_SLOTS 512
+#define BBMM_ATT_NORM_SLOTS 512   // workgroups that look for the norms of a call, or one per (batch, shared head)
 
 // The buckets of a difference r = j - i - start (edges ascending; further than the last one, everything on a side shares a bucket).
 struct AttBuckets {
@@ -51,7 +51,8 @@ struct AttGrad {
   // B x H x nq, left by the dQ pass for the next: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
   float *delta, *lo, *hi;
   float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets
-  float* norms;                  // fp16: largest |do_i| and |v_j|, a pair per slot
+  float* norms;                  // fp16: largest |do_i| and |v_j| of each (batch, shared head), a pair per slot: B x HK x norm_slots
+  int norm_slots;
   int whole_rows;                // the dQ pass forms delta from the row itself
   int rows_only;                 // a launch of the dQ kernel for just that, where the keys are split: into rsum
   float* rsum;                   // qsplit x B x H x nq pairs: sum of p, sum of p dP

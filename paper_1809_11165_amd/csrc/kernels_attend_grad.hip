@@ -11,8 +11,8 @@
 // 2 x 8 heads, 500 x 1000, d = 64: 50 and 58 us; there one wave per SIMD fits (registers), and the matrix unit is busy 59 % of the dK, dV pass: the
 // wave's own vector instructions and waits stand between its products.
 //
-// fp16: p and dS are scaled by powers of two before they are rounded, dS by |do_i| times the largest |v_j| (dQ) or the largest |do_i| |v_j| (dK;
-// k_attend_norms): weights of long rows and small gradients would fall among that type's subnormal numbers.
+// fp16: p and dS are scaled by powers of two before they are rounded, dS by |do_i| times the largest |v_j| (dQ) or the largest |do_i| |v_j| (dK) of
+// the shared head (k_attend_norms): weights of long rows and small gradients would fall among that type's subnormal numbers.
 #include "attend_dev.h"
 
 using namespace att;
@@ -22,17 +22,11 @@ namespace {
 template <typename T> struct PLift { static constexpr float value = 0.f; };
 template <> struct PLift<_Float16> { static constexpr float value = 12.f; };
 
-// Largest |do_i| and |v_j| of a call, in kNormSlots slots, one per workgroup of k_attend_norms (a place that all rows maximise made 64 000 rows of
-// fp16 wait 200 us for each other).
-constexpr int kNormSlots = BBMM_ATT_NORM_SLOTS;
-static_assert(kNormSlots % 64 == 0, "slots per lane");
-
-// fp16: the largest |do_i| and |v_j|.  All lanes of a wave take part.
-__device__ __forceinline__ float2 norms_of(const AttGrad& g, int lane) {
+// fp16: largest |do_i| and |v_j| of a shared head (the slots of unit b HK + hk).  All lanes of a wave take part.
+__device__ __forceinline__ float2 norms_of(const AttGrad& g, int unit, int lane) {
   float x = 0.f, y = 0.f;
-#pragma unroll
-  for (int k = 0; k < kNormSlots; k += 64) {
-    float2 z = *(const float2*)(g.norms + 2 * (k + lane));
+  for (int k = lane; k < g.norm_slots; k += 64) {
+    float2 z = *(const float2*)(g.norms + 2 * ((size_t)unit * g.norm_slots + k));
     x = fmaxf(x, z.x);
     y = fmaxf(y, z.y);
   }
@@ -49,12 +43,15 @@ __device__ __forceinline__ float ds_scale(float x, float y) {
   return __builtin_amdgcn_exp2f(fminf(fmaxf(e, -100.f), 100.f));
 }
 
-// fp16: the norms of the rows that take part, 16 lanes per row; those without a finite norm are left out.
+// fp16: the norms of the rows that take part, 16 lanes per row; those without a finite norm are left out.  A workgroup fills one slot of a (batch,
+// shared head), whose gradients so do not depend on the others in the call (a place that all rows maximise made 64 000 rows wait 200 us for each other).
 __global__ __launch_bounds__(256) void k_attend_norms(AttArgs a, AttGrad g) {
   typedef _Float16 T;
   __shared__ float part[2][4];
   int tid = threadIdx.x, lane = tid & 15;
-  int64_t rows = (int64_t)a.B * a.nq * a.H, keys = (int64_t)a.B * a.nk * a.HK;
+  int slot = blockIdx.x % g.norm_slots, unit = blockIdx.x / g.norm_slots, hk = unit % a.HK, b = unit / a.HK;
+  int64_t rows = (int64_t)queries_of(a, b) * a.G;
+  int keys = keys_of(a, b);
   auto square = [&](const T* row, int vec) {
     u32x4 x = load16<T>(row, 8 * lane, a.dv, vec);
     float q = 0.f;
@@ -65,18 +62,17 @@ __global__ __launch_bounds__(256) void k_attend_norms(AttArgs a, AttGrad g) {
     return q < __builtin_inff() ? q : 0.f;
   };
   float x = 0.f, y = 0.f;
-  int64_t first = (int64_t)blockIdx.x * 16 + (tid >> 4), step = (int64_t)kNormSlots * 16;
+  int first = slot * 16 + (tid >> 4), step = g.norm_slots * 16;
 #pragma unroll 2
   for (int64_t n = first; n < rows; n += step) {
-    int h = (int)(n % a.H), i = (int)(n / a.H % a.nq), b = (int)(n / a.H / a.nq);
-    if ((a.q_len && i >= a.q_len[b]) || g.lse[((size_t)b * a.H + h) * a.nq + i] == -__builtin_inff()) continue;
+    int h = hk * a.G + (int)(n % a.G), i = (int)(n / a.G);
+    if (g.lse[((size_t)b * a.H + h) * a.nq + i] == -__builtin_inff()) continue;
     x = fmaxf(x, square((const T*)g.dO + b * g.dos[0] + (int64_t)i * g.dos[1] + h * g.dos[2], g.dovec));
   }
 #pragma unroll 2
-  for (int64_t n = first; n < keys; n += step) {
-    int h = (int)(n % a.HK), j = (int)(n / a.HK % a.nk), b = (int)(n / a.HK / a.nk);
-    if ((a.k_len && j >= a.k_len[b]) || (a.mask && !a.mask[b * a.mask_s + j])) continue;
-    y = fmaxf(y, square((const T*)a.V + b * a.vs[0] + (int64_t)j * a.vs[1] + h * a.vs[2], a.vvec));
+  for (int j = first; j < keys; j += step) {
+    if (a.mask && !a.mask[b * a.mask_s + j]) continue;
+    y = fmaxf(y, square((const T*)a.V + b * a.vs[0] + (int64_t)j * a.vs[1] + hk * a.vs[2], a.vvec));
   }
 #pragma unroll
   for (int k = 16; k < 64; k *= 2) {
@@ -88,7 +84,7 @@ __global__ __launch_bounds__(256) void k_attend_norms(AttArgs a, AttGrad g) {
     part[1][tid >> 6] = y;
   }
   __syncthreads();
-  if (tid < 2) g.norms[2 * blockIdx.x + tid] = sqrtf(fmaxf(fmaxf(part[tid][0], part[tid][1]), fmaxf(part[tid][2], part[tid][3])));
+  if (tid < 2) g.norms[2 * (size_t)blockIdx.x + tid] = sqrtf(fmaxf(fmaxf(part[tid][0], part[tid][1]), fmaxf(part[tid][2], part[tid][3])));
 }
 
 // Beyond this, fp32 holds lse too coarsely to recover weights from it: rounded as a logarithm to base 2, to base e and to base 2 again, it
@@ -200,7 +196,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int e = 0; e < 8; ++e) z = fmaf((float)dof[s][e], (float)dof[s][e], z);
-    cs = ds_scale(sqrtf(both_sum(z)), norms_of(g, lane).y);
+    cs = ds_scale(sqrtf(both_sum(z)), norms_of(g, b * a.HK + hk, lane).y);
     uncs = 1.f / cs;
   }
   auto scores_start = [&](int at, int first) {
@@ -513,9 +509,9 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     for (int s = 0; s < NS; ++s) kf[s] = vf[s] = frag{};
   }
   constexpr float kLift = PLift<T>::value;
-  float cs = 1.f;                            // fp16: one power of two for all rows, which add up
+  float cs = 1.f;                            // fp16: one power of two for all rows of the shared head, which add up
   if constexpr (__is_same(T, _Float16)) {
-    float2 z = norms_of(g, lane);
+    float2 z = norms_of(g, b * a.HK + hk, lane);
     cs = uniform(ds_scale(z.x, z.y));
   }
   float unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
@@ -757,7 +753,7 @@ void sums_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
 }  // namespace
 
 void launch_attend_norms(hipStream_t s, int type, const AttArgs& a, const AttGrad& g) {
-  if (type == 1) k_attend_norms<<<kNormSlots, 256, 0, s>>>(a, g);
+  if (type == 1) k_attend_norms<<<(unsigned)(a.B * a.HK * g.norm_slots), 256, 0, s>>>(a, g);
 }
 void launch_attend_dq(hipStream_t s, int type, const AttArgs& a, const AttGrad& g) {
   if (type == 0) dq_t<float>(s, a, g);

@@ -183,3 +183,31 @@ def test_small_rows_of_dO_beside_large_ones_in_fp16(ctx, edges, nq, nk):
     off, size = (np.linalg.norm(x, axis=3) for x in (np.where(fits[..., None], got - want, 0), want))
     assert size[:, 1::2].min() > 2.0 ** -10                # eight normal features of 2^-14 and more: no steps of subnormal results
     assert np.all(off <= 3 * A.UNIT["f16"] * size)
+
+
+@pytest.mark.parametrize("edges", [None, EDGES])
+@pytest.mark.parametrize("what", ["batch", "heads"])
+@pytest.mark.parametrize("name", ["dq", "dk"])
+def test_small_gradients_of_a_batch_beside_large_ones_in_fp16(ctx, edges, what, name):
+    """dO and V at 2^5 in one half of the batch (or of the shared heads) and at 2^-5 in the other: they meet in no sum of dQ and dK, so each half is as
+    precise as alone.  In the 2-norm one u each for a rounding of dS, of delta's o and of the result.  (The scale of 64 that lifts a result
+    out of the subnormal numbers is taken back in the other operand.)"""
+    rng = np.random.default_rng(40)
+    att, dO = _case(rng, "f16", 2, 4, 2, 120, 2000, 64, 64, edges=edges)
+    att.scale = 64.0
+    (att.Q if name == "dq" else att.K).mul_(2.0 ** -9)
+    size = torch.tensor([2.0 ** 5, 2.0 ** -5], device=DEV, dtype=torch.float16)
+    if what == "batch":
+        att.V.mul_(size[:, None, None, None])
+        dO.mul_(size[:, None, None, None])
+    else:
+        att.V.mul_(size[:, None])
+        dO.mul_(size.repeat_interleave(2)[:, None])
+    val, _ = _oracle("f16", att, dO)
+    O, lse = ctx.bbmm_attend(att)
+    grads = ctx.bbmm_attend_grad(att, O, lse, dO)
+    got, want = _host(grads[0 if name == "dq" else 1]), val[name]
+    half = want.shape[2] // 2
+    got, want = (x[1] if what == "batch" else x[:, :, half:] for x in (got, want))
+    assert np.linalg.norm(want) > 2.0 ** -12 * np.sqrt(want.size)      # normal numbers
+    assert np.linalg.norm(got - want) <= 3 * A.UNIT["f16"] * np.linalg.norm(want)
