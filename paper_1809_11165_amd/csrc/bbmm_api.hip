@@ -2176,9 +2176,10 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
   int64_t wgs = (int64_t)a.B * a.HK * (p.few ? blocks : tiles);
   int64_t want = 2 * c->num_cus / std::max<int64_t>(wgs, 1), most = std::max<int64_t>(1, (a.nk + kAttPart - 1) / kAttPart);
   p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
-  // Lengths of the caller's: smaller parts even them out (8 requests of 32773 .. 18437 keys, 8 heads of 128: 170 us in 8 parts each, 155 in 32;
-  // equal lengths of 30000 in fp32 lose: 106 and 177).
-  if (p.few && a.k_len) p.nsplit = (int)std::max<int64_t>(p.nsplit, std::min(8 * c->num_cus / std::max<int64_t>(wgs, 1), a.nk / kAttEvenPart));
+  // Lengths of the caller's: smaller parts even them out.  8 requests, 32 heads on 8 of 128, 32773 keys, in 8 parts each / in 32: bf16 at lengths of
+  // 32773 .. 18437 170 / 156 us, one long beside seven of a sixteenth 58 / 48, all whole 205 / 197 (fp16 the same); fp32, whose products are
+  // slow, 299 / 369, 168 / 138 and 372 / 439: there the parts stay as they are.
+  if (p.few && two_bytes && a.k_len) p.nsplit = (int)std::max<int64_t>(p.nsplit, std::min(8 * c->num_cus / std::max<int64_t>(wgs, 1), a.nk / kAttEvenPart));
   return p;
 }
 

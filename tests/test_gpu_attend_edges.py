@@ -211,3 +211,13 @@ def test_small_gradients_of_a_batch_beside_large_ones_in_fp16(ctx, edges, what, 
     got, want = (x[1] if what == "batch" else x[:, :, half:] for x in (got, want))
     assert np.linalg.norm(want) > 2.0 ** -12 * np.sqrt(want.size)      # normal numbers
     assert np.linalg.norm(got - want) <= 3 * A.UNIT["f16"] * np.linalg.norm(want)
+
+
+def test_lengths_do_not_change_the_parts_of_fp32(ctx):
+    """Finer parts of a split key axis even out unequal lengths, but cost fp32 more than that: a batch with lengths is split as one without."""
+    from paper_1809_11165_amd import binding
+    q = torch.zeros(8, 1, 32, 128, device=DEV)
+    kv = torch.zeros(1, 1, 8, 128, device=DEV).expand(8, 32773, 8, 128)
+    k_len = torch.full((8,), 32773, dtype=torch.int32, device=DEV)
+    plain, full = binding.Attention(q, kv, kv), binding.Attention(q, kv, kv, k_len=k_len)
+    assert ctx.bbmm_attend_workspace(plain) == ctx.bbmm_attend_workspace(full) > 0
