@@ -595,10 +595,16 @@ class Context:
 
     # ---- attention --------------------------------------------------------------------------
     def _ordered(self, tensors, call):
-        """Runs `call` (which allocates its outputs and queues work) with the context's stream current.  Where that is not
+        """Runs `call` (which allocates its outputs and queues work) with the context's stream current; refuses inputs whose gradients
+        torch is to record, which a result without a graph would lose.  Where the context's stream is not
         the caller's stream, the work waits for what the caller has queued, the caller's stream waits for the work, and
         no tensor's memory is reused before both are done."""
         torch = self.torch
+        if torch.is_grad_enabled():
+            for t in tensors:
+                if t.requires_grad:
+                    raise ValueError("an input requires grad, but the call records no graph of gradients: make it under torch.no_grad(), "
+                                     "or in the forward and backward of a torch.autograd.Function (bbmm_attend_grad, bbmm_bucket_bias_grad)")
         if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
             return call()
         here = torch.cuda.current_stream(self.device)

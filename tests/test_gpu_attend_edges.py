@@ -221,3 +221,54 @@ def test_lengths_do_not_change_the_parts_of_fp32(ctx):
     k_len = torch.full((8,), 32773, dtype=torch.int32, device=DEV)
     plain, full = binding.Attention(q, kv, kv), binding.Attention(q, kv, kv, k_len=k_len)
     assert ctx.bbmm_attend_workspace(plain) == ctx.bbmm_attend_workspace(full) > 0
+
+
+def test_inputs_that_require_grad_are_refused(ctx):
+    """No call is part of a recorded graph of gradients: inputs that such a graph is to follow are refused rather than left out of it."""
+    att, dO = _case(np.random.default_rng(41), "f32", 1, 2, 2, 5, 9, 16, 16, edges=EDGES)
+    O, lse = ctx.bbmm_attend(att)
+    want = ctx.bbmm_attend_grad(att, O, lse, dO)
+    for name in ("Q", "K", "V", "table"):
+        leaf = getattr(att, name).requires_grad_()
+        for call in (lambda: ctx.bbmm_attend(att), lambda: ctx.bbmm_attend_grad(att, O, lse, dO)):
+            with pytest.raises(ValueError, match="requires? grad"):
+                call()
+        with torch.no_grad():
+            assert torch.equal(ctx.bbmm_attend(att)[0], O)
+            assert all(torch.equal(x, y) for x, y in zip(ctx.bbmm_attend_grad(att, O, lse, dO), want))
+        leaf.requires_grad_(False)
+    table = att.table.requires_grad_()
+    with pytest.raises(ValueError):
+        ctx.bbmm_bucket_bias(table, EDGES, 4, 4)
+    dB = torch.zeros(1, 2, 4, 4, device=DEV, requires_grad=True)
+    with pytest.raises(ValueError):
+        ctx.bbmm_bucket_bias_grad(dB, EDGES)
+    with torch.no_grad():
+        assert ctx.bbmm_bucket_bias(table, EDGES, 4, 4).shape == (2, 4, 4)
+
+
+def test_the_calls_inside_a_function_of_torch(ctx):
+    """As a model uses them: the calls as forward and backward of an autograd function, whose gradients are those of the call."""
+    from paper_1809_11165_amd import binding
+
+    class Read(torch.autograd.Function):
+        @staticmethod
+        def forward(save, Q, K, V, table):
+            att = binding.Attention(Q, K, V, table=table, edges=EDGES)
+            O, lse = ctx.bbmm_attend(att)
+            save.att = att
+            save.save_for_backward(O, lse)
+            return O
+
+        @staticmethod
+        def backward(save, dO):
+            return ctx.bbmm_attend_grad(save.att, *save.saved_tensors, dO)
+
+    att, dO = _case(np.random.default_rng(42), "f32", 2, 4, 2, 40, 70, 32, 32, edges=EDGES)
+    O, lse = ctx.bbmm_attend(att)
+    want = ctx.bbmm_attend_grad(att, O, lse, dO)
+    leaves = [x.clone().requires_grad_() for x in (att.Q, att.K, att.V, att.table)]
+    (Read.apply(*leaves) * dO).sum().backward()
+    torch.cuda.synchronize()
+    for leaf, x in zip(leaves, want):
+        assert torch.equal(leaf.grad, x)
