@@ -142,15 +142,17 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     if (keep != kAll && tid < BK) from[at][tid] = ((keep >> tid) & 1) ? 0.f : -__builtin_inff();
     return keep;
   };
-  // All that the loop needs first is asked for before anything is waited for (one latency instead of four).
+  // All that the next loop needs first is asked for before anything is waited for (one latency instead of four): a pass over the row ahead of the
+  // main one needs one tile.
   Loads t2;
-  auto first_tiles = [&]() {
+  bool row_pass = g.whole_rows && (g.qsplit == 1 || g.rows_only);
+  auto first_tiles = [&](bool both) {
     if (t0 < t1) {
       fetch(tl, t0);
-      fetch(t2, t0 + 1);
+      if (both) fetch(t2, t0 + 1);
     }
   };
-  first_tiles();
+  first_tiles(!row_pass);
   size_t row = ((size_t)b * a.H + h) * a.nq + i;
   float lse = i < qn ? g.lse[row] : -__builtin_inff(), delta = 0.f;
   frag q[NS], dof[NS];
@@ -217,9 +219,10 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
   float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
   int rel = rest_below(-(int64_t)q0 - start_of(a, b));
-  // The row from its keys of tiles [from_, to), ahead of the pass: f(scores' products, dP, mul, add) for every block of 32.  The next tile is on its way meanwhile.
-  auto whole_row = [&](int from_, int to, auto f) {
-    if (from_ < to) fetch(tl, from_);
+  // The row from its keys of tiles [from_, to), ahead of the pass: f(scores' products, dP, mul, add) for every block of 32.  The next tile is on its way meanwhile,
+  // and the first one already where `asked`.
+  auto whole_row = [&](int from_, int to, bool asked, auto f) {
+    if (from_ < to && !asked) fetch(tl, from_);
     for (int t = from_, at = 0; t < to; ++t, at ^= 1) {
       uint64_t keep = put(tl, t, at);
       fetch(tl, t + 1);
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   bool any_wide = uniform(side[0] + side[1] + side[2] + side[3]) != 0.f;
   if (any_wide) {
     float top = -__builtin_inff(), sum = 0.f;
-    whole_row(0, tiles, [&](const f32x16& s, const f32x16&, float mul, float add) {
+    whole_row(0, tiles, false, [&](const f32x16& s, const f32x16&, float mul, float add) {
       float x[16], big = top;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -269,8 +272,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     // delta_i = sum_j p_ij dP_ij / sum_j p_ij; of a split row from the parts that a launch of this kernel with rows_only left
     float total = 0.f, sd = 0.f;
     size_t rows = (size_t)a.B * a.H * a.nq;
-    if (g.qsplit == 1 || g.rows_only) {
-      whole_row(t0, t1, [&](const f32x16& s, const f32x16& dp, float mul, float add) {
+    if (row_pass) {
+      whole_row(t0, t1, !any_wide, [&](const f32x16& s, const f32x16& dp, float mul, float add) {
         f32x16 y = s;
         if (coarse) {
 #pragma unroll
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
   if (half == 0 && i < qn && sp == 0) g.delta[row] = delta, g.lo[row] = lo, g.hi[row] = hi;   // for the next pass
   lo -= __builtin_amdgcn_logf(cs);
-  if (any_wide || g.whole_rows) first_tiles();
+  if (any_wide || row_pass) first_tiles(true);
   if (t0 < t1) {
     k0 = put(tl, t0, 0);
     k1 = put(t2, t0 + 1, 1);
