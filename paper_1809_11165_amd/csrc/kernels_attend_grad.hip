@@ -535,7 +535,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
   bool odd = __any(z != 0.f);
   auto put = [&](const Loads& x, int at) {
-    uint64_t keep = __ballot(x.lo != __builtin_inff()) & (NB == 2 ? ~0ull : 0xffffffffull);
+    constexpr uint64_t kAll = NB == 2 ? ~0ull : 0xffffffffull;
+    uint64_t keep = __ballot(x.lo != __builtin_inff()) & kAll;
     x.q.store(tile[at][0], keep, tid);
     x.d.store(tile[at][1], keep, tid);
     if (tid < BQ) {
@@ -543,7 +544,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       stat[at][1][tid] = x.delta * ck;
       stat[at][2][tid] = x.hi;
     }
-    return __any(x.hi != 0.f || (odd && x.lo == __builtin_inff()));
+    return __any(x.hi != 0.f) || (odd && keep != kAll);
   };
   f32x16 dk[ND], dv[ND], sc[2], pc[2];       // of a turn's two blocks: scores, dP
   sc[0] = pc[0] = f32x16{};
