@@ -272,3 +272,40 @@ def test_the_calls_inside_a_function_of_torch(ctx):
     torch.cuda.synchronize()
     for leaf, x in zip(leaves, want):
         assert torch.equal(leaf.grad, x)
+
+
+# batch times kv_heads a multiple of eight: units of several workgroups dealt out to the dies one by one, in all three kernels
+DEALT = {
+    "units_8": (4, 4, 2, 150, 200, 64, 64, dict(edges=EDGES)),
+    "units_16_ragged": (8, 4, 2, 300, 333, 40, 40, dict(edges=EDGES, k_len=[333, 0, 1, 200, 150, 333, 64, 129], q_len=[300, 300, 5, 0, 128, 129, 300, 1])),
+    "units_8_split": (2, 4, 4, 140, 1500, 64, 64, dict(edges=EDGES, start=[1300, -20], mask=0.8)),
+    "units_8_wide": (1, 16, 8, 260, 300, 128, 128, {}),
+}
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("name", list(DEALT))
+def test_units_dealt_out_over_the_dies(ctx, name, kind):
+    *shape, opt = DEALT[name]
+    att, dO = _case(np.random.default_rng(sum(map(ord, name))), kind, *shape, **opt)
+    _run_and_check(ctx, kind, att, dO)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("nq", [4, 70])
+def test_a_causal_table_beside_a_head_of_the_lowest_value(ctx, kind, nq):
+    """The head of the causal table, element by element, in every type; the other head's bias flattens its rows."""
+    rng = np.random.default_rng(38)
+    att, dO = _case(rng, kind, 1, 2, 2, nq, 40, 32, 32, edges=EDGES, start=[-3])
+    n = len(EDGES) + 1
+    att.table[0, n:] = -float("inf")
+    att.table[0, 0] = -float("inf")
+    att.table[1, :] = torch.finfo(TYPES[kind]).min
+    val, err = _oracle(kind, att, dO)
+    O, lse = ctx.bbmm_attend(att)
+    dQ, dK, dV, dT = ctx.bbmm_attend_grad(att, O, lse, dO)
+    assert all(torch.isfinite(x).all() for x in (O, dQ, dK, dV, dT))
+    _check(lse[:, :1], {"lse": val["lse"][:, :1]}, {"lse": err["lse"][:, :1]}, "lse")
+    for name, x in (("o", O), ("dq", dQ), ("dk", dK), ("dv", dV)):
+        _check(x[:, :, :1], {name: val[name][:, :, :1]}, {name: err[name][:, :, :1]}, name)
+    _check(dT[:1], {"dtable": val["dtable"][:1]}, {"dtable": err["dtable"][:1]}, "dtable")
