@@ -207,7 +207,8 @@ __device__ __forceinline__ int bucket_of(const AttBuckets& bk, int r) {
 
 // Sums by bucket of a workgroup of 256: diag[r + span] holds the sum of difference r, |r| <= span; `left` and `right` are sums of differences
 // -far and below, far and above.  A bucket is an interval of differences on one side; eight lanes take one.
-__device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* diag, int span, float left, float right, float* out, int tid) {
+template <typename S>
+__device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* diag, int span, S left, S right, S* out, int tid) {
   int E = bk.n_edges, part = tid & 7;
   for (int n = tid >> 3; n < bk.buckets; n += 32) {
     bool ahead = n > E;                                   // two-sided, r > 0
@@ -216,7 +217,7 @@ __device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* d
     beyond = min(beyond, span);
     int lo = ahead ? max(near, 1) : -beyond, hi = ahead ? beyond : -near;
     if (!bk.two_sided && n == 0) hi = span;
-    float s = 0.f;
+    S s = 0;
     for (int r = lo + part; r <= hi; r += 8) s += diag[r + span];
 #pragma unroll
     for (int x = 1; x < 8; x *= 2) s += __shfl_xor(s, x, 64);
@@ -227,8 +228,8 @@ __device__ __forceinline__ void bucket_sums(const AttBuckets& bk, const float* d
 }
 
 // One wave: the sums of a head's bucket from all parts (tsum: heads x parts x buckets) in a fixed order, 64 bits.
-template <typename T>
-__device__ __forceinline__ void join_bucket(const float* __restrict__ tsum, int parts, int buckets, int h, int n, int lane, T* __restrict__ out) {
+template <typename T, typename S>
+__device__ __forceinline__ void join_bucket(const S* __restrict__ tsum, int parts, int buckets, int h, int n, int lane, T* __restrict__ out) {
   double s = 0.0;
   for (int p = lane; p < parts; p += 64) s += (double)tsum[((size_t)h * parts + p) * buckets + n];
 #pragma unroll

@@ -2192,8 +2192,7 @@ constexpr int64_t kGradPart = 128;
 // differences: where most of a row lies in one bucket (long rows beyond the last edge) it is far more than what is left.  So in two-byte types rows of up to
 // kWholeRows keys, and all rows with a table, form delta in fp32 from all their scores instead, two products more.  Against 64 bits, bf16, without / with:
 // 500 queries of 8 keys: dQ 2.7e-3 / 2.4e-3, table 1.3e-2 / 1.8e-3; table of 37 x 2171, last edge 12: 1.2e-1 / below 4e-3 (training step of 8 x 12
-// heads, 512 x 640, d = 64: 89 / 103 us).  fp32 keeps the rounded o: over 78 drawn calls the table's error is 1.3 times that of the plain form in the
-// median with it and 1.0 with the scores, at most 3.9e-6 and 3.1e-6 in all, for 142 / 181 us a step of 2 x 8 heads, 500 x 1000.
+// heads, 512 x 640, d = 64: 89 / 103 us).  In fp32, whose table is summed by the dK, dV pass, the dQ pass hands on what its rows' dS leave instead.
 constexpr int64_t kWholeRows = 128;
 struct GradPlan {
   int qsplit, ksplit;
@@ -2217,7 +2216,7 @@ int norm_slots(const AttArgs& a) { return std::max<int>(1, BBMM_ATT_NORM_SLOTS /
 // Offsets into the workspace, 256-byte steps.
 size_t step256(size_t n) { return (n + 255) / 256 * 256; }
 struct AttWork {
-  size_t pO, pl, delta, lo, hi, tsum, norms, rsum, pq, pk, pv, bytes;
+  size_t pO, pl, delta, lo, hi, w, tsum, norms, rsum, pq, pk, pv, bytes;
 };
 AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_bytes) {
   AttWork w{};
@@ -2241,9 +2240,11 @@ AttWork attention_work(const bbmm_ctx* c, const AttArgs& a, bool grad, bool two_
   w.delta = take(rows * sizeof(float));
   w.lo = take(rows * sizeof(float));
   w.hi = take(rows * sizeof(float));
-  w.tsum = take(a.table ? (size_t)a.H * a.B * p.qsplit * ((a.nq + 127) / 128) * a.bk.buckets * sizeof(float) : 0);
+  w.w = take(two_bytes ? 0 : rows * sizeof(float));
+  size_t parts = two_bytes ? (size_t)p.qsplit * ((a.nq + 127) / 128) : (size_t)p.ksplit * ((a.nk + 127) / 128);
+  w.tsum = take(a.table ? (size_t)a.H * a.B * parts * a.bk.buckets * (two_bytes ? sizeof(float) : sizeof(double)) : 0);
   size_t keys = (size_t)a.B * a.HK * a.nk * p.ksplit * sizeof(float);
-  w.rsum = take(p.whole_rows && p.qsplit > 1 ? 2 * rows * p.qsplit * sizeof(float) : 0);
+  w.rsum = take((p.whole_rows || !two_bytes) && p.qsplit > 1 ? 2 * rows * p.qsplit * (two_bytes ? sizeof(float) : sizeof(double)) : 0);
   w.pq = take(p.qsplit > 1 ? rows * p.qsplit * a.d * sizeof(float) : 0);
   w.pk = take(p.ksplit > 1 ? keys * a.d : 0);
   w.pv = take(p.ksplit > 1 ? keys * a.dv : 0);
@@ -2321,7 +2322,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   }
   g.ovec = wide_rows(O, nullptr, a.dv, e, 16), g.dovec = wide_rows(dO, g.dos, a.dv, e, 16);
   g.dqvec = wide_rows(dQ, nullptr, a.d, e, 4 * e), g.dkvec = wide_rows(dK, nullptr, a.d, e, 4 * e), g.dvvec = wide_rows(dV, nullptr, a.dv, e, 4 * e);
-  g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.tsum = (float*)((char*)work + w.tsum), g.norms = (float*)((char*)work + w.norms);
+  g.delta = (float*)((char*)work + w.delta), g.lo = (float*)((char*)work + w.lo), g.hi = (float*)((char*)work + w.hi), g.w = (float*)((char*)work + w.w), g.tsum = (float*)((char*)work + w.tsum), g.norms = (float*)((char*)work + w.norms);
   g.rsum = (float*)((char*)work + w.rsum);
   g.pq = (float*)((char*)work + w.pq), g.pk = (float*)((char*)work + w.pk), g.pv = (float*)((char*)work + w.pv);
   GradPlan p = gradient_plan(c, a, e == 2);
@@ -2332,7 +2333,7 @@ int attend_grad(bbmm_ctx* c, const bbmm_attention* in, const void* O, const floa
   if (rows) launch_attend_dq(s, in->type, a, g);
   if (keys) launch_attend_dkv(s, in->type, a, g);
   launch_attend_sums(s, in->type, a, g);
-  if (a.table && !keys) launch_bucket_join(s, in->type, g.tsum, a.B * g.qsplit * ((a.nq + 127) / 128), a.H, a.bk.buckets, dtable);
+  if (a.table && !keys) launch_bucket_join(s, in->type, g.tsum, e == 2 ? a.B * g.qsplit * ((a.nq + 127) / 128) : 0, a.H, a.bk.buckets, dtable);
   HIPCHK(c, hipGetLastError());
   return BBMM_OK;
 }

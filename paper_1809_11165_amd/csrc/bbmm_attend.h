@@ -49,13 +49,14 @@ struct AttGrad {
   const float* lse;
   void *dQ, *dK, *dV, *dtable;   // dense
   // B x H x nq, left by the dQ pass for the next: do_i.o_i, and the row's log2 of the sum as hi + lo (p = exp2((s - hi) - lo); nothing left: lo infinite)
-  float *delta, *lo, *hi;
-  float* tsum;                   // sums of dS by bucket per workgroup of the dQ pass: H x (B qsplit ceil(nq / 128)) x buckets
+  // fp32: w = 1 / sum of these p, and delta with the row's rest of dS, sum p (do_i.v_j - do_i.o_i) w
+  float *delta, *lo, *hi, *w;
+  float* tsum;                   // sums of dS by bucket per workgroup: H x (B qsplit ceil(nq / 128)) x buckets; fp32 H x (B ksplit ceil(nk / 128)) x buckets doubles
   float* norms;                  // fp16: largest |do_i| and |v_j| of each (batch, shared head), a pair per slot: B x HK x norm_slots
   int norm_slots;
   int whole_rows;                // the dQ pass forms delta from the row itself
   int rows_only;                 // a launch of the dQ kernel for just that, where the keys are split: into rsum
-  float* rsum;                   // qsplit x B x H x nq pairs: sum of p, sum of p dP
+  float* rsum;                   // qsplit x B x H x nq pairs: sum of p, sum of p dP (fp32: sum of dS, both doubles)
   int qsplit, ksplit;            // parts that the keys of the dQ pass, and the queries of the dK, dV pass, are split into
   float *pq, *pk, *pv;           // their results: parts x the size of dQ, dK, dV
 };
@@ -67,7 +68,7 @@ void launch_attend_join(hipStream_t s, int type, const AttArgs& a, const AttOut&
 void launch_attend_norms(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_dq(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
 void launch_attend_dkv(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);
-void launch_attend_sums(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);   // adds up what the two passes left in parts
+void launch_attend_sums(hipStream_t s, int type, const AttArgs& a, const AttGrad& g);   // adds up what the two passes left in parts (fp32: and the table's gradient)
 
 // The bias as a matrix (heads x nq x nk, `rows` rows per workgroup), and the sums of a matrix's gradient (batch x heads x nq x nk) by bucket:
 // tsum holds heads x (batch ceil(nq / rows)) x buckets floats, which launch_bucket_join adds up.

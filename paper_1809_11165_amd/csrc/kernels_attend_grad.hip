@@ -104,8 +104,9 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   __shared__ __align__(16) char tile[3][2][kTile];   // K, V
   __shared__ __align__(16) float from[3][BK];        // what a key's scores start from: 0, or -infinity where it takes no part
   __shared__ float side[8];
+  constexpr bool kSums = sizeof(T) == 2;             // the table's gradient is formed here
   static_assert(sizeof tile + sizeof from + sizeof side + 5 * kLine * sizeof(float) <= 160 * 1024, "the longest line fits beside the tiles");
-  extern __shared__ float dyn[];                     // with a table: bias line, then a line of diagonal sums per wave
+  extern __shared__ float dyn[];                     // with a table: bias line, then (kSums) a line of diagonal sums per wave
   int id = die_order(blockIdx.x, a.B * a.HK, a.G * nqt * g.qsplit);
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   int qt = id % nqt, sp = id / nqt % g.qsplit, bh = id / nqt / g.qsplit, h = bh % a.H, b = bh / a.H, hk = h / a.G;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   const float* ln = nullptr;
   if (a.table) {
     fill_line<T>(line, a, h, tid, 256);
-    for (int n = tid; n < 4 * nline; n += 256) diag[n] = 0.f;
+    for (int n = tid; kSums && n < 4 * nline; n += 256) diag[n] = 0.f;
     ln = line;
   }
   // a power of two: dS is formed times it.  fp16: a row's own, from its |do_i|, so that a row of small gradients keeps its bits beside others of large ones
@@ -218,6 +219,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
 #pragma unroll
   for (int n = 0; n < ND; ++n) acc[n] = f32x16{};
   float sl = 0.f, sr = 0.f, left = 0.f, right = 0.f;
+  double psum = 0.0, rest = 0.0;             // fp32: sums of the row's p and dS
   int rel = rest_below(-(int64_t)q0 - start_of(a, b));
   // The row from its keys of tiles [from_, to), ahead of the pass: f(scores' products, dP, mul, add) for every block of 32.  The next tile is on its way meanwhile,
   // and the first one already where `asked`.
@@ -341,6 +343,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     add -= lo;
     const char *kt = tile[on][0], *vt = tile[on][1], *ko = tile[at][0];
     constexpr int A = 2 * NS, M = A + 2 * ND;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f}, left_over[4] = {0.f, 0.f, 0.f, 0.f};
     auto operand = [&](int z) {
       return z < NS ? row_frag<T, DP>(kt, there, z, lane)
              : z < A ? row_frag<T, DP>(vt, there, z - NS, lane)
@@ -363,14 +366,21 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       if (z < A) {
 #pragma unroll
         for (int r = z * 16 / A; r < (z + 1) * 16 / A; ++r) {
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (dp[r] - delta);
+          float x = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add));
+          // fp32: dP - delta would be rounded on dP's grid, the same way for all keys whose dP has an exponent: a delta off by that much for the row
+          s[r] = kSums ? x * (dp[r] - delta) : fmaf(x, dp[r], -(x * delta));
+          if constexpr (!kSums) sum[r & 3] += x, left_over[r & 3] += s[r];
           if (r == 7) ds[0] = pack8<T>(s, 0);
           if (r == 15) ds[1] = pack8<T>(s, 1);
         }
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (ln) {
+    if constexpr (!kSums) {
+      psum += (double)((sum[0] + sum[1]) + (sum[2] + sum[3]));
+      rest += (double)((left_over[0] + left_over[1]) + (left_over[2] + left_over[3]));
+    }
+    if (kSums && ln) {
       if (empty) {                           // an infinity in a key or value of others makes NaN of these lanes' zeros
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = some ? s[r] : 0.f;
@@ -406,6 +416,18 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     now = nxt;
     __syncthreads();
   }
+  if constexpr (!kSums) {
+    psum += __shfl_xor(psum, 32, 64);
+    rest += __shfl_xor(rest, 32, 64);
+    if (!some) psum = rest = 0.0;
+    if (g.qsplit == 1) {
+      double w = psum != 0.0 ? 1.0 / psum : 0.0;
+      uncs = (float)w;
+      if (half == 0 && i < qn) g.w[row] = uncs, g.delta[row] = (float)((double)delta + rest * w);
+    } else if (half == 0 && i < a.nq) {
+      *(double2*)((double*)g.rsum + 2 * ((size_t)sp * a.B * a.H * a.nq + row)) = double2{psum, rest};
+    }
+  }
   if (i < a.nq) {
     float f = a.scale * uncs;
     int64_t at = (((int64_t)b * a.nq + i) * a.H + h) * a.d;
@@ -423,7 +445,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     if (g.qsplit == 1) write((T*)g.dQ + at, g.dqvec);
     else write(g.pq + sp * ((int64_t)a.B * a.nq * a.H * a.d) + at, a.d % 4 == 0);
   }
-  if (ln) {                                  // the loop's last barrier stands before this
+  if (kSums && ln) {                         // the loop's last barrier stands before this
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
       sl += __shfl_xor(sl, x, 64);
@@ -445,15 +467,57 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   }
 }
 
+// fp32: the dQ pass's sums of a row's p and dS in parts, and its dQ, joined: four features per thread.
+__global__ __launch_bounds__(256) void k_attend_rows(AttArgs a, AttGrad g) {
+  int64_t rows = (int64_t)a.B * a.H * a.nq, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int nc = (a.d + 3) / 4, c = 4 * (int)(t % nc);
+  int64_t n = t / nc;
+  if (n >= rows) return;
+  int64_t at = (n / a.H / a.nq * a.H + n % a.H) * a.nq + n / a.H % a.nq;
+  double psum = 0.0, rest = 0.0;
+  float y[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < g.qsplit; ++k) {
+    double2 x = *(const double2*)((const double*)g.rsum + 2 * (k * rows + at));
+    psum += x.x;
+    rest += x.y;
+    const float* part = g.pq + (k * rows + n) * a.d + c;
+    if (a.d % 4 == 0) {
+      f32x4 v = *(const f32x4*)part;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < a.d) y[e] += part[e];
+    }
+  }
+  double inv = psum != 0.0 ? 1.0 / psum : 0.0;
+  float w = (float)inv;
+  store4((float*)g.dQ + n * a.d, c, a.d, g.dqvec, y[0] * w, y[1] * w, y[2] * w, y[3] * w);
+  if (c == 0) {
+    g.w[at] = w;
+    g.delta[at] = (float)((double)g.delta[at] + rest * inv);
+  }
+}
+
 // 64 queries of one head a turn, the heads of the group one after the other; else like k_attend_dq.  Workgroups from `grid` on add up the table's
 // gradient that the dQ pass left, a wave per entry (a launch of its own takes 4.6 us).
+//
+// fp32 takes p times 1 over its row's sum, and delta with the row's rest of dS, from the dQ pass, and so sums the table's gradient here, head by head.
+// Weights recovered from an fp32 lse are off by up to 1e-6 a row, and a delta from the rounded o leaves a rest where dS should sum to zero, which
+// stands against what is left of a bucket.  Over 30 drawn calls the errors of dQ, dK, dV and the table, in units of the formula's own steps in fp32, were
+// 1.25, 1.3, 1.3 and 1.2 in the median without this and are 1.0, 1.0, 1.0 and 0.6 (training step of 2 x 8 heads, 500 x 1000: 142 / 150 us; the same
+// from a pass over the row ahead of the dQ pass, as in two-byte types: 181).
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttArgs a, AttGrad g, int nkt, int grid) {
   typedef typename Frag<T>::type frag;
   constexpr int NB = sizeof(T) == 2 ? 2 : 1, BQ = 32 * NB, ND = DP / 32, NS = DP / 16, kTile = BQ * DP * (int)sizeof(T);
+  constexpr bool kSums = sizeof(T) == 4;              // the table's gradient is formed here
   __shared__ __align__(16) char tile[3][2][kTile];    // Q, dO
-  __shared__ __align__(16) float stat[3][3][BQ];      // lo, delta (scaled like dS), hi
-  extern __shared__ float dyn[];                      // with a table: bias line
+  __shared__ __align__(16) float stat[3][kSums ? 4 : 3][BQ];   // lo, delta (scaled like dS), hi, 1 / sum of p
+  __shared__ double side[8];
+  static_assert(sizeof tile + sizeof stat + sizeof side + (kSums ? 5 : 1) * kLine * sizeof(float) <= 160 * 1024, "the longest line fits beside the tiles");
+  extern __shared__ float dyn[];                      // with a table: bias line, then (kSums) a line of diagonal sums per wave, turned over
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   if ((int)blockIdx.x >= grid) {
     int n = 4 * ((int)blockIdx.x - grid) + wave;
@@ -470,12 +534,23 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   if (kt * 128 >= kn) qn = 0;
   int tiles = (qn + BQ - 1) / BQ, steps = tiles * a.G, per = (steps + g.ksplit - 1) / g.ksplit;   // a part: some tiles of some heads
   int t0 = min(sp * per, steps), t1 = min(t0 + per, steps);
-  int far = a.bk.far;
+  int far = a.bk.far, span = far + kPad, nline = 2 * span + 1;
   const float* ln = a.table ? dyn : nullptr;
+  float* diag = dyn + nline;
+  auto sums_of = [&](int head) { return (double*)g.tsum + ((((size_t)head * a.B + b) * g.ksplit + sp) * nkt + kt) * a.bk.buckets; };
+  if (kSums && ln) {
+    for (int n = tid; n < 4 * nline; n += 256) diag[n] = 0.f;
+    // heads that this part has no tile of
+    int first = t0 < t1 ? t0 / tiles : a.G, last = t0 < t1 ? (t1 - 1) / tiles : -1;
+    for (int n = tid; n < a.G * a.bk.buckets; n += 256) {
+      int x = n / a.bk.buckets;
+      if (x < first || x > last) sums_of(hk * a.G + x)[n % a.bk.buckets] = 0.0;
+    }
+  }
   bool mine = j < kn;
   struct Loads {
     Stage<T, DP, BQ, VEC> q, d;
-    float lo, delta, hi;                     // of row `lane` of the tile
+    float lo, delta, hi, w;                  // of row `lane` of the tile
   };
   Loads tl, t2;
   int h = hk * a.G + (tiles ? t0 / tiles : 0), i0 = tiles ? t0 % tiles * BQ : 0;   // head and first row of the turn's tile
@@ -486,8 +561,11 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     x.d.load((const T*)g.dO + b * g.dos[0] + (int64_t)fi * g.dos[1] + fh * g.dos[2], g.dos[1], rows, a.dv, tid);
     size_t row = ((size_t)b * a.H + fh) * a.nq + fi + lane;
     x.lo = __builtin_inff();
-    x.delta = x.hi = 0.f;
-    if (lane < BQ && lane < rows) x.lo = g.lo[row], x.delta = g.delta[row], x.hi = g.hi[row];
+    x.delta = x.hi = x.w = 0.f;
+    if (lane < BQ && lane < rows) {
+      x.lo = g.lo[row], x.delta = g.delta[row], x.hi = g.hi[row];
+      if constexpr (kSums) x.w = g.w[row];
+    }
     fi += BQ;
     if (fi >= qn) fi = 0, ++fh;
   };
@@ -520,7 +598,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   float unlift = 1.f / (float)(1 << (int)kLift), ck = cs * unlift;
   // Rows that take no part run along with zeros, of which a key that holds an infinity or NaN makes NaN.  Where it does (a product with zero tells such
   // keys) their blocks go the way of rows with a `hi`, where the minimum with a number makes a number of NaN; their lo is infinite, so the weight is
-  // zero.  (Rows that count have a lo of NaN beside a score of NaN.)
+  // zero.  (Rows that count have a lo of NaN beside a score of NaN.  fp32: an infinite value makes NaN of their dS for the table.)
   float z = 0.f;
   if constexpr (sizeof(T) == 2) {
     f32x16 c = f32x16{};
@@ -531,7 +609,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
 #pragma unroll
     for (int k = 0; k < NS; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z = fmaf(kf[k][e], 0.f, z);
+      for (int e = 0; e < 8; ++e) z = fmaf(kf[k][e], 0.f, fmaf(vf[k][e], 0.f, z));
   }
   bool odd = __any(z != 0.f);
   auto put = [&](const Loads& x, int at) {
@@ -543,6 +621,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       stat[at][0][tid] = x.lo;                 // infinite where nothing is left in the row: weights zero
       stat[at][1][tid] = x.delta * ck;
       stat[at][2][tid] = x.hi;
+      if constexpr (kSums) stat[at][3][tid] = x.w;
     }
     return __any(x.hi != 0.f) || (odd && keep != kAll);
   };
@@ -551,6 +630,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
 #pragma unroll
   for (int n = 0; n < ND; ++n) dk[n] = dv[n] = f32x16{};
   float left = 0.f, right = 0.f;
+  double sl = 0.0, sr = 0.0;                 // of rows beyond the last edges, whose dS sum to zero only across all keys: nothing may be lost on the way
+  bool bare = __any(!mine);                  // keys that take no part
   int rel = rest_above((int64_t)k0 - start_of(a, b));
   bool c0 = false, c1 = false;               // whether this tile and the next have rows with a `hi`, or zeros beside odd keys
   if (t0 < t1) {
@@ -572,13 +653,16 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     f32x16 &s = sc[B], &dp = pc[B], &s2 = sc[B ^ 1], &dp2 = pc[B ^ 1];
     float mul = a.c2, add = 0.f;
     const float* st = stat[at][0] + here + 4 * half;
-    f32x4 l4[4], d4[4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    f32x4 l4[4], d4[4], w4[4];
+    auto stats = [&](int n) {
       l4[n] = *(const f32x4*)(st + 8 * n);
       d4[n] = *(const f32x4*)(st + BQ + 8 * n);
-    }
-    if (ln) add_bias<false>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
+      if constexpr (kSums) w4[n] = *(const f32x4*)(st + 3 * BQ + 8 * n);
+    };
+#pragma unroll
+    for (int n = 0; n < (kSums ? 1 : 4); ++n) stats(n);   // fp32: the others as they are wanted, its products leave time and its registers no room
+    int where = 1;
+    if (ln) where = add_bias<false>(s, a.c2, ln, far, rel0, left, right, lane, mul, add);
     if (wide) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
@@ -614,17 +698,66 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       if (z < A) {
 #pragma unroll
         for (int r = z * 16 / A; r < (z + 1) * 16 / A; ++r) {
+          if (kSums && r % 4 == 0 && r < 12) stats(r / 4 + 1);
           s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add - l4[r >> 2][r & 3]));
-          dp[r] = s[r] * fmaf(dp[r], ck, -d4[r >> 2][r & 3]);
+          if constexpr (kSums) s[r] *= w4[r >> 2][r & 3];
+          dp[r] = kSums ? fmaf(s[r], dp[r], -(s[r] * d4[r >> 2][r & 3])) : s[r] * fmaf(dp[r], ck, -d4[r >> 2][r & 3]);
           if (r == 7) p[0] = pack8<T>(s, 0), ds[0] = pack8<T>(dp, 0);
           if (r == 15) p[1] = pack8<T>(s, 1), ds[1] = pack8<T>(dp, 1);
         }
       }
     }
     __builtin_amdgcn_sched_barrier(0);
+    if (kSums && ln) {
+      if (bare) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] = mine ? dp[r] : 0.f;
+      }
+      if (wide) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] = st[8 * (r >> 2) + (r & 3)] < __builtin_inff() ? dp[r] : 0.f;
+      }
+      if (where == 0) {
+        add_diagonals(dp, diag + wave * nline + span - rel0, lane);   // queries in the registers: the line runs the other way
+      } else {
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r & 3] += dp[r];
+        (where < 0 ? sl : sr) += (double)((x[0] + x[1]) + (x[2] + x[3]));
+      }
+    }
+  };
+  // The sums of a head by bucket; a barrier stands before it and before what writes the lines next.
+  auto flush = [&](int head) {
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+      sl += __shfl_xor(sl, x, 64);
+      sr += __shfl_xor(sr, x, 64);
+    }
+    if (lane == 0) {
+      side[wave] = sl;
+      side[4 + wave] = sr;
+    }
+    sl = sr = 0.0;
+    for (int n = tid; n < nline; n += 256) {
+      float x = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float* from = diag + k * nline + nline - 1 - n;
+        x += *from;
+        *from = 0.f;
+      }
+      dyn[n] = x;
+    }
+    __syncthreads();
+    bucket_sums(a.bk, dyn, span, side[0] + side[1] + side[2] + side[3], side[4] + side[5] + side[6] + side[7], sums_of(head), tid);
   };
   for (int t = t0; t < t1; ++t) {
     if (ln && (i0 == 0 || t == t0)) {        // another head: its bias line (nobody reads the old one any more)
+      if (kSums && t > t0) {
+        flush(h - 1);
+        __syncthreads();
+      }
       fill_line<T>(dyn, a, h, tid, 256);
       __syncthreads();
       left = uniform(ln[kPad]);
@@ -647,6 +780,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     if (i0 >= qn) i0 = 0, ++h;
     __syncthreads();
   }
+  if (kSums && ln && t0 < t1) flush(hk * a.G + (t1 - 1) / tiles);
   if (j >= a.nk) return;
   float fk = a.scale / cs;
   int64_t at = ((int64_t)b * a.nk + j) * a.HK + hk, all = (int64_t)a.B * a.nk * a.HK;
@@ -677,10 +811,18 @@ struct Sums {
   void* out[3];
   int64_t n[3];
   int parts[3];
-  unsigned first[4];   // workgroups of each: [first[k], first[k + 1])
+  unsigned first[4];   // workgroups of each: [first[k], first[k + 1]); from first[3] on those that add up the table's gradient, a wave per entry
+  const float* tsum;
+  int tparts, heads, buckets;
+  void* dtable;
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_sum(Sums z) {
+  if (blockIdx.x >= z.first[3]) {
+    int n = 4 * (int)(blockIdx.x - z.first[3]) + (int)(threadIdx.x >> 6);
+    if (n < z.heads * z.buckets) join_bucket<T>((const double*)z.tsum, z.tparts, z.buckets, n / z.buckets, n % z.buckets, threadIdx.x & 63, (T*)z.dtable);
+    return;
+  }
   int k = blockIdx.x >= z.first[2] ? 2 : blockIdx.x >= z.first[1] ? 1 : 0;
   const float* part = z.part[k];
   T* out = (T*)z.out[k];
@@ -704,15 +846,15 @@ __global__ __launch_bounds__(256) void k_attend_sum(Sums z) {
 template <typename T, bool VEC>
 void dq_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int nqt = (a.nq + 127) / 128, grid = (a.B * a.H * nqt * g.qsplit + 7) / 8 * 8;
-  size_t lds = a.table ? sizeof(float) * 5 * (2 * (a.bk.far + kPad) + 1) : 0;
+  size_t lds = a.table ? sizeof(float) * (sizeof(T) == 2 ? 5 : 1) * (2 * (a.bk.far + kPad) + 1) : 0;
   if (a.d <= 64 && a.dv <= 64) k_attend_dq<T, 64, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
   else k_attend_dq<T, 128, VEC><<<grid, 256, lds, s>>>(a, g, nqt);
 }
 template <typename T, bool VEC>
 void dkv_v(hipStream_t s, const AttArgs& a, const AttGrad& g) {
   int nkt = (a.nk + 127) / 128, grid = (a.B * a.HK * nkt * g.ksplit + 7) / 8 * 8;
-  int more = a.table ? (a.H * a.bk.buckets + 3) / 4 : 0;
-  size_t lds = a.table ? sizeof(float) * (2 * (a.bk.far + kPad) + 1) : 0;
+  int more = a.table && sizeof(T) == 2 ? (a.H * a.bk.buckets + 3) / 4 : 0;
+  size_t lds = a.table ? sizeof(float) * (sizeof(T) == 2 ? 1 : 5) * (2 * (a.bk.far + kPad) + 1) : 0;
   if (a.d <= 64 && a.dv <= 64) k_attend_dkv<T, 64, VEC><<<grid + more, 256, lds, s>>>(a, g, nkt, grid);
   else k_attend_dkv<T, 128, VEC><<<grid + more, 256, lds, s>>>(a, g, nkt, grid);
 }
@@ -728,6 +870,10 @@ void dq_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
     pass(ahead);
   }
   pass(g);
+  if (sizeof(T) == 4 && g.qsplit > 1) {
+    int64_t threads = (int64_t)a.B * a.H * a.nq * ((a.d + 3) / 4);
+    k_attend_rows<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a, g);
+  }
 }
 template <typename T>
 void dkv_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
@@ -745,13 +891,16 @@ void sums_t(hipStream_t s, const AttArgs& a, const AttGrad& g) {
     ++k;
   };
   int64_t rows = (int64_t)a.B * a.nq * a.H, keys = (int64_t)a.B * a.nk * a.HK;
-  take(g.pq, g.qsplit, rows * a.d, g.dQ);
+  if (sizeof(T) == 2) take(g.pq, g.qsplit, rows * a.d, g.dQ);      // fp32: k_attend_rows
   take(g.pk, g.ksplit, keys * a.d, g.dK);
   take(g.pv, g.ksplit, keys * a.dv, g.dV);
-  if (k == 0) return;
   unsigned all = z.first[k];
   for (; k < 3; ++k) z.first[k + 1] = all;
-  k_attend_sum<T><<<all, 256, 0, s>>>(z);
+  if (sizeof(T) == 4 && a.table && keys) {
+    z.tsum = g.tsum, z.tparts = a.B * g.ksplit * ((a.nk + 127) / 128), z.heads = a.H, z.buckets = a.bk.buckets, z.dtable = g.dtable;
+    all += (a.H * a.bk.buckets + 3) / 4;
+  }
+  if (all) k_attend_sum<T><<<all, 256, 0, s>>>(z);
 }
 
 }  // namespace

@@ -309,3 +309,55 @@ def test_a_causal_table_beside_a_head_of_the_lowest_value(ctx, kind, nq):
     for name, x in (("o", O), ("dq", dQ), ("dk", dK), ("dv", dV)):
         _check(x[:, :, :1], {name: val[name][:, :, :1]}, {name: err[name][:, :, :1]}, name)
     _check(dT[:1], {"dtable": val["dtable"][:1]}, {"dtable": err["dtable"][:1]}, "dtable")
+
+
+def _f32_gradients(att, dO, dtype):
+    """The formula by elementary products in `dtype`, on the GPU: dq, dk, dv and dtable."""
+    B, nq, H, d = att.Q.shape
+    nk, HK = att.K.shape[1:3]
+    G, edges = H // HK, att.edges
+    q, do = (x.to(dtype).transpose(1, 2).contiguous() for x in (att.Q, dO))
+    k, v = (x.to(dtype).transpose(1, 2).repeat_interleave(G, 1).contiguous() for x in (att.K, att.V))
+    s = torch.matmul(q, k.transpose(2, 3).contiguous()) * d ** -0.5
+    n = None
+    if att.table is not None:
+        r = torch.arange(nk, device=DEV)[None, :] - torch.arange(nq, device=DEV)[:, None]
+        n = torch.from_numpy(A.bucket(r.cpu().numpy(), edges, att.two_sided)).to(DEV)
+        s = s + att.table.to(dtype)[:, n]
+    p = torch.exp(s - s.amax(3, keepdim=True))
+    p = p / p.sum(3, keepdim=True)
+    o = torch.matmul(p, v)
+    ds = p * (torch.matmul(do, v.transpose(2, 3).contiguous()) - (do * o).sum(3, keepdim=True))
+    out = {"dq": (torch.matmul(ds, k) * d ** -0.5).transpose(1, 2)}
+    for name, x, y in (("dk", ds * d ** -0.5, q), ("dv", p, do)):
+        z = torch.matmul(x.transpose(2, 3).contiguous(), y)
+        out[name] = z.view(B, HK, G, nk, -1).sum(2).transpose(1, 2)
+    if n is not None:
+        rows = ds.double().sum(0).reshape(H, -1)
+        out["dtable"] = torch.zeros(H, att.table.shape[1], device=DEV, dtype=torch.float64).index_add_(1, n.reshape(-1), rows).to(dtype)
+    return out
+
+
+@pytest.mark.parametrize("B,H,HK,nq,nk,d,dv,edges,two_sided", [
+    (2, 1, 1, 2627, 484, 96, 16, [1, 2, 3, 4, 5, 7, 10, 14, 20, 30, 42], True),
+    (3, 1, 1, 2249, 998, 80, 80, list(range(1, 17)) + [20, 26, 33, 43, 55], False),
+    (4, 1, 1, 407, 5859, 16, 64, [1, 2, 5, 12, 20], True),
+    (4, 2, 2, 1509, 2854, 32, 16, None, True),
+    (3, 2, 2, 2612, 86, 32, 32, [1, 2, 40], True),          # nearly all rows beyond the last edge
+    (2, 6, 3, 300, 300, 128, 128, [1, 1000], True),         # and all of them between two
+    (1, 8, 1, 150, 3000, 40, 40, EDGES, True),              # parts of both axes, many heads a workgroup
+])
+def test_fp32_gradients_are_as_precise_as_the_formula_in_fp32(ctx, B, H, HK, nq, nk, d, dv, edges, two_sided):
+    """Against 64 bits the 2-norm of a gradient's error is at most one and a half times that of the formula's own steps in fp32, or 4 u32: root mean
+    squares over four inputs, as a bucket that holds most of all rows is one number, in which either side's rounding may happen to cancel."""
+    off, of_plain = {}, {}
+    for seed in range(4):
+        att, dO = _case(np.random.default_rng(seed), "f32", B, H, HK, nq, nk, d, dv, edges=edges, two_sided=two_sided)
+        exact, plain = (_f32_gradients(att, dO, t) for t in (torch.float64, torch.float32))
+        O, lse = ctx.bbmm_attend(att)
+        for name, x in zip(("dq", "dk", "dv", "dtable"), ctx.bbmm_attend_grad(att, O, lse, dO)):
+            for sums, y in (off, x), (of_plain, plain.get(name)):
+                if x is not None:
+                    sums[name] = sums.get(name, 0.0) + float((y.double() - exact[name]).norm() / exact[name].norm()) ** 2 / 4
+    for name in off:
+        assert off[name] ** 0.5 <= max(1.5 * of_plain[name] ** 0.5, 4 * A.U32), (name, off[name] ** 0.5, of_plain[name] ** 0.5)
