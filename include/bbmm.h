@@ -389,8 +389,8 @@ int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns
  *   s_ij = scale q_i.k_j + T[h][bucket(j - i - start_b)]   over the keys j < k_len_b with key_mask_bj != 0,
  *   o_i  = sum_j exp(s_ij - lse_i) v_j,     lse_i = log sum_j exp(s_ij).
  * A row that nothing is left for (no keys, all masked, all scores -infinity) has o_i = 0, lse_i = -infinity and no part in any
- * gradient.  Masked keys, and queries and keys behind their lengths, may hold anything, infinities and NaN
- * included; rows of O at or behind q_len_b are zero (lse -infinity), and so are rows of the gradients behind the lengths and
+ * gradient, whatever its query holds and others' keys and values hold.  Masked keys, and queries and keys behind their lengths, may hold
+ * anything, infinities and NaN included; rows of O at or behind q_len_b are zero (lse -infinity), and so are rows of the gradients behind the lengths and
  * of masked keys.
  *
  *   bucket(r), with edges e_1 < .. < e_E and c(x) the number of edges that are at most x:
@@ -398,7 +398,11 @@ int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns
  *       otherwise:  c(max(-r, 0))                        E + 1 buckets
  *
  *   type          BBMM_TYPE_F32, _F16 or _BF16: of Q, K, V, O, the table and all gradients.  lse is fp32.  Scores, softmax statistics
- *                 and sums are fp32; weights (and dS) are rounded to `type` once as operands of the second products.
+ *                 and sums are fp32; weights (and dS) are rounded to `type` once as operands of the second products.  In fp16 powers of
+ *                 two lift them out of the subnormal numbers first: for dQ by the row's own dO, for dK by the largest dO among the
+ *                 rows of its batch entry and shared head, beside which rows of 2^-20 of that lose bits of their part.
+ *                 In fp32 the gradients are as precise as the formula's steps in fp32; the gradient forms rows of |lse| beyond 64
+ *                 (fp16 256, bf16 2048) once more, because an fp32 lse holds their weights too coarsely
  *   heads         query heads; kv_heads divides it, head h reads keys and values of head h / (heads / kv_heads)
  *   d, dv         features of queries and keys, and of values: 1 .. 128
  *   scale         > 0, scale / log 2 finite in fp32
@@ -410,7 +414,8 @@ int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns
  *                 2.3e38 in magnitude count as that
  *   edges         host, n_edges entries, 1 <= e_1 < .. <= 1024; 0 <= n_edges <= 63; only read during the call
  *   q_start       device, batch entries: position of query 0 on the keys' axis, or NULL (0)
- * Limits: batch, heads and kv_heads <= 65535, nq and nk <= 2^30; zero sizes are allowed for batch, nq and nk.
+ * Limits: batch, heads and kv_heads <= 65535, nq and nk <= 2^30, batch heads nq and batch kv_heads nk <= 2^27, batch heads ceil(nq / 128)
+ * and batch kv_heads ceil(nk / 128) <= 2^23; zero sizes are allowed for batch, nq and nk.
  * Outputs are dense, [batch][row][head][feature]; lse [batch][heads][nq].  Outputs must not overlap inputs or each other.
  * The calls only queue work on the context's stream, allocate nothing and keep nothing: their workspace is the
  * caller's, so they may be recorded in a graph, and two graphs (or streams) may run together if their
@@ -451,7 +456,8 @@ int bbmm_attend(bbmm_ctx* ctx, const bbmm_attention* in, void* O, float* lse, vo
 int bbmm_attend_grad(bbmm_ctx* ctx, const bbmm_attention* in, const void* O, const float* lse, const void* dO,
                      const int64_t* do_stride, void* dQ, void* dK, void* dV, void* dtable, void* work, int64_t work_bytes);
 
-/* The bias as a matrix: B[h][i][j] = table[h][bucket(j - i - start)], device, heads x nq x nk, dense. */
+/* The bias as a matrix: B[h][i][j] = table[h][bucket(j - i - start)], device, heads x nq x nk, dense.  Limits of this call and the next: nq <=
+ * 2^24, batch heads ceil(nq / 4) <= 2^23, nk <= 2^30, start within +-2^40. */
 int bbmm_bucket_bias(bbmm_ctx* ctx, int32_t type, const void* table, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges,
                      const int32_t* edges, int32_t two_sided, int64_t start, void* B);
 

@@ -256,9 +256,11 @@ def _check_same(tensor, shape, dtype, device, name, dense=True):
 
 
 def bucket_edges(num_buckets: int, max_distance: int, two_sided: bool = True):
-    """Edges of the usual buckets: unit steps up to half of a side's buckets, then equal steps of the logarithm up to
-    max_distance, which opens the last one.  An edge is the first whole distance at or beyond its step, found in whole
-    numbers (x^n against powers), so nothing is rounded at a border.  Steps that fall on the same distance move up by one."""
+    """Edges of the usual buckets: unit steps up to half of a side's buckets, then equal steps of the logarithm of which the one behind
+    the last edge would stand at max_distance (32 two-sided buckets and 128: the last edge is 91).  An edge is the first
+    whole distance at or beyond its step, found in whole numbers (x^n against powers), so nothing is rounded at a border.  Edges
+    ascend: of steps that fall on the same distance (32 one-sided buckets with 32 or 33, 64 with 64 to 70) the later ones move up by
+    one, where the usual buckets leave one empty; such a table has no edges here that give its buckets."""
     side = num_buckets // 2 if two_sided else num_buckets
     if side < 1 or (two_sided and num_buckets % 2) or max_distance < 1:
         raise ValueError("num_buckets must be positive (even when two_sided) and max_distance at least 1")
@@ -295,7 +297,8 @@ class Attention:
     """One attention call (see include/bbmm.h, "Attention").  Q (batch, nq, heads, d), K (batch, nk, kv_heads, d), V (batch,
     nk, kv_heads, dv): device tensors of one type, any strides with the last dimension contiguous.  scale: default
     d^-1/2.  q_len, k_len: int32 (batch,); key_mask: bool or uint8 (batch, nk), true takes part; table: (heads, buckets)
-    of Q's type with edges (see bucket_edges); q_start: int64 (batch,)."""
+    of Q's type with edges (see bucket_edges); q_start: int64 (batch,).  The calls record no graph of gradients: inputs that require
+    grad are refused outside torch.no_grad() (a torch.autograd.Function with bbmm_attend_grad as its backward runs so)."""
     Q: "object"
     K: "object"
     V: "object"
@@ -595,10 +598,9 @@ class Context:
 
     # ---- attention --------------------------------------------------------------------------
     def _ordered(self, tensors, call):
-        """Runs `call` (which allocates its outputs and queues work) with the context's stream current; refuses inputs whose gradients
-        torch is to record, which a result without a graph would lose.  Where the context's stream is not
+        """Runs `call` (which allocates its outputs and queues work) with the context's stream current.  Where that is not
         the caller's stream, the work waits for what the caller has queued, the caller's stream waits for the work, and
-        no tensor's memory is reused before both are done."""
+        no tensor's memory is reused before both are done.  Refuses inputs whose gradients torch is to record: the result has no graph."""
         torch = self.torch
         if torch.is_grad_enabled():
             for t in tensors:

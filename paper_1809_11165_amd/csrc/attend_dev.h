@@ -241,8 +241,8 @@ __device__ __forceinline__ void join_bucket(const S* __restrict__ tsum, int part
 // pointing at the difference of the first key and the first query.  Halves first exchange registers so that each
 // has 16 keys in a row; a sum then moves one lane per key, towards higher lanes for keys ahead (what leaves a row of 16 lanes
 // lies behind), towards lower ones for keys behind.  That leaves two pieces of a diagonal in each row of 16 lanes, which rows exchange until every lane
-// owns a diagonal of the block: one read and one write of LDS in a fixed order, no atomics.  (dQ pass of 8 x 12 x 512 x 640 in bf16, d = 64:
-// 31 us; with two atomic additions per half 38, with sixteen of all lanes 106 before other steps.)
+// owns a diagonal of the block: one read and one write of LDS in a fixed order, no atomics.  (dQ pass of 8 x 12 x 512 x 640 in bf16, d = 64,
+// with delta from O: 31 us; with two atomic additions per half 38, with sixteen of all lanes 106 before other steps.)
 __device__ __forceinline__ float from_lane_below(float x) {   // of the row of 16, zero into the first
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x111, 0xf, 0xf, true));
 }

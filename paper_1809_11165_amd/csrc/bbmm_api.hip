@@ -2185,14 +2185,14 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
 
 // The gradient's two passes likewise: the keys of the dQ pass and the queries (of all heads of a group) of the dK, dV pass are split while the
 // workgroups do not fill the device and a part keeps at least kGradPart rows (fp32, 2 x 8 heads, 500 x 1000, training step: 239 us with parts of
-// 256 and 512 forward, 165 with these).
+// 256 and 512 forward, 165 with these, before other steps).
 constexpr int64_t kGradPart = 128;
 // delta_i = do_i.o_i takes o_i as the forward pass rounded it.  Where a row holds few keys that is off by as much as dS is rounded (its error goes
 // with the square root of sum p^2).  In the table's gradient it stands against what is left of a row's sum of dS, which is zero but for the buckets'
 // differences: where most of a row lies in one bucket (long rows beyond the last edge) it is far more than what is left.  So in two-byte types rows of up to
 // kWholeRows keys, and all rows with a table, form delta in fp32 from all their scores instead, two products more.  Against 64 bits, bf16, without / with:
 // 500 queries of 8 keys: dQ 2.7e-3 / 2.4e-3, table 1.3e-2 / 1.8e-3; table of 37 x 2171, last edge 12: 1.2e-1 / below 4e-3 (training step of 8 x 12
-// heads, 512 x 640, d = 64: 89 / 103 us).  In fp32, whose table is summed by the dK, dV pass, the dQ pass hands on what its rows' dS leave instead.
+// heads, 512 x 640, d = 64, when it came in: 89 / 103 us; now 98).  In fp32, whose table is summed by the dK, dV pass, the dQ pass hands on what its rows' dS leave instead.
 constexpr int64_t kWholeRows = 128;
 struct GradPlan {
   int qsplit, ksplit;

@@ -5,12 +5,12 @@
 // a lane, so that maximum, sum, bias offset and rescaling are per-lane scalars and the weights are, as they stand, the
 // second operand of O^T += V^T P^T (see attend_dev.h).  K and V tiles of 32 keys go through LDS, two buffers each.  In the turn of a tile its
 // softmax runs on the vector unit while the matrix unit forms the scores of the tile after and adds up the values of the tile before.
-// Bound by products and vector work together: 2 x 16 heads, 4096 x 10000, d = 128, bf16 with a table 720 us, 930 TFLOP/s (a large matrix
-// product 1200; MFMA with eight vector instructions and an exponential beside each 1370); at d = 64 a score costs the same exponential for half the
-// products: 4 x 16 heads, 1000 x 1537, fp16 with a table, a mask and lengths 49 us, 410 TFLOP/s.
+// Bound by products and vector work together: 2 x 16 heads, 4096 x 10000, d = 128, bf16 with a table 707 us, 949 TFLOP/s (693 to 746 over several
+// devices; a large matrix product 1200; MFMA with eight vector instructions and an exponential beside each 1370); at d = 64 a score costs the same
+// exponential for half the products: 4 x 16 heads, 1000 x 1537, fp16 with a table, a mask and lengths 50 us, 410 TFLOP/s.
 // k_attend_few: up to 32 rows (query, head of the group) of one shared head; the waves split the keys instead, read K straight
 // into registers and V through LDS of their own, and join at the end.  Bound by reading K and V once: one query per request, 8 x 32 heads on 8,
-// keys up to 32773 of 128 features, bf16 155 us with the join, 5.4 TB/s (a large copy moves 4.9, read and written); short calls by their launch (7.8 us).
+// keys up to 32773 of 128 features, bf16 155 us with the join, 5.4 TB/s (a large copy moves 4.9, read and written); short calls by their launch (7.5 us).
 // Both may split the key axis over workgroups; k_attend_join then weighs the parts.
 #include "attend_dev.h"
 

@@ -4,11 +4,12 @@
 //     dT[h, n] = sum of dS_ij over the pairs of bucket n.
 // Two passes, each owning what it writes, so that every sum has a fixed order and nothing is added atomically in memory: k_attend_dq (a
 // workgroup owns 128 queries of a head and runs over the keys; transposed scores, like the forward pass) and
-// k_attend_dkv (owns 128 keys of a shared head and runs over the queries of all its heads; scores with a key in a lane).  Seven matrix products
-// where five would do with dQ added atomically.  Measured, bf16: 2 x 16 heads on 4, 2048 x 8192, d = 128: dQ 525 us and dK, dV 668 us, 785 and 823
-// TFLOP/s of their own products (a large matrix product: 1200); 8 x 12 heads, 512 x 640 with lengths and a table, d = 64: 48 (33 without
-// forming delta from the scores) and 34 us.  fp32,
-// 2 x 8 heads, 500 x 1000, d = 64: 50 and 58 us; there one wave per SIMD fits (registers), and the matrix unit is busy 59 % of the dK, dV pass: the
+// k_attend_dkv (owns 128 keys of a shared head and runs over the queries of all its heads; scores with a key in a lane).  The table's sums are
+// formed by the first in two-byte types, by the second in fp32 (see there).  Seven matrix products
+// where five would do with dQ added atomically.  Measured, bf16: 2 x 16 heads on 4, 2048 x 8192, d = 128: dQ 523 us and dK, dV 661 us, 788 and 832
+// TFLOP/s of their own products (a large matrix product: 1200); 8 x 12 heads, 512 x 640 with lengths and a table, d = 64: 49 (33 without
+// forming delta from the scores) and 35 us.  fp32, 2 x 8 heads, 500 x 1000, d = 64 with a table: 48 and 64 us; there one wave per SIMD fits
+// (registers; the dK, dV pass at d = 128 keeps 168 bytes a lane in scratch), and the matrix unit is busy 54 % of either pass: the
 // wave's own vector instructions and waits stand between its products.
 //
 // fp16: p and dS are scaled by powers of two before they are rounded, dS by |do_i| times the largest |v_j| (dQ) or the largest |do_i| |v_j| (dK) of

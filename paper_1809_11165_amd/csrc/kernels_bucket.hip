@@ -2,7 +2,7 @@
 // its table, dT[h][n] = sum of dB[b][h][i][j] over bucket(j - i - start) = n.  Both are bound by the matrix's bytes.  The matrix
 // is constant beyond the last edge on either side and constant along diagonals between.  16 x 4096 x 8192 in bf16 is written in 183 us, 5.9 TB/s (a
 // plain fill: 6.9; rows dealt out in other orders, one row per workgroup, 4 to 256 rows and non-temporal stores were none faster);
-// the gradient of 4 x 16 x 1024 x 2048 in bf16 is read in 52 us, 5.2 TB/s, and its parts are joined in 6.
+// the gradient of 4 x 16 x 1024 x 2048 in bf16 is read in 50 us, 5.4 TB/s, and its parts are joined in 5.
 #include "attend_dev.h"
 
 using namespace att;
