@@ -2185,8 +2185,10 @@ AttPlan attention_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
 
 // The gradient's two passes likewise: the keys of the dQ pass and the queries (of all heads of a group) of the dK, dV pass are split while the
 // workgroups do not fill the device and a part keeps at least kGradPart rows (fp32, 2 x 8 heads, 500 x 1000, training step: 239 us with parts of
-// 256 and 512 forward, 165 with these, before other steps).
-constexpr int64_t kGradPart = 128;
+// 256 and 512 forward, 165 with these, before other steps).  A head counts as a tile of queries at least, as much work as one (training steps, heads counted
+// by their rows / so: 2 x 100 heads on 1, 1 x 400, with a table bf16 304 / 71 us, fp32 883 / 151; 2 x 64 on 2, 4 x 4000, fp16 143 / 103; 32 on 1, 2 x 30000, fp32
+// 622 / 641).
+constexpr int64_t kGradPart = 128, kGradTile = 32;
 // delta_i = do_i.o_i takes o_i as the forward pass rounded it.  Where a row holds few keys that is off by as much as dS is rounded (its error goes
 // with the square root of sum p^2).  In the table's gradient it stands against what is left of a row's sum of dS, which is zero but for the buckets'
 // differences: where most of a row lies in one bucket (long rows beyond the last edge) it is far more than what is left.  So in two-byte types rows of up to
@@ -2206,7 +2208,7 @@ GradPlan gradient_plan(const bbmm_ctx* c, const AttArgs& a, bool two_bytes) {
   GradPlan p;
   p.whole_rows = two_bytes && (a.table || a.nk <= kWholeRows);
   p.qsplit = parts((int64_t)a.B * a.H * ((a.nq + 127) / 128), a.nk);
-  p.ksplit = parts((int64_t)a.B * a.HK * ((a.nk + 127) / 128), (int64_t)a.nq * a.G);
+  p.ksplit = parts((int64_t)a.B * a.HK * ((a.nk + 127) / 128), std::max<int64_t>(a.nq, kGradTile) * a.G);
   return p;
 }
 

@@ -9,7 +9,7 @@
 // where five would do with dQ added atomically.  Measured, bf16: 2 x 16 heads on 4, 2048 x 8192, d = 128: dQ 523 us and dK, dV 661 us, 788 and 832
 // TFLOP/s of their own products (a large matrix product: 1200); 8 x 12 heads, 512 x 640 with lengths and a table, d = 64: 49 (33 without
 // forming delta from the scores) and 35 us.  fp32, 2 x 8 heads, 500 x 1000, d = 64 with a table: 48 and 64 us; there one wave per SIMD fits
-// (registers; the dK, dV pass at d = 128 keeps 168 bytes a lane in scratch), and the matrix unit is busy 54 % of either pass: the
+// (registers; the dK, dV pass at d = 128 keeps 180 bytes a lane in scratch), and the matrix unit is busy 54 % of either pass: the
 // wave's own vector instructions and waits stand between its products.
 //
 // fp16: p and dS are scaled by powers of two before they are rounded, dS by |do_i| times the largest |v_j| (dQ) or the largest |do_i| |v_j| (dK) of
@@ -517,7 +517,8 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   __shared__ __align__(16) char tile[3][2][kTile];    // Q, dO
   __shared__ __align__(16) float stat[3][kSums ? 4 : 3][BQ];   // lo, delta (scaled like dS), hi, 1 / sum of p
   __shared__ double side[8];
-  static_assert(sizeof tile + sizeof stat + sizeof side + (kSums ? 5 : 1) * kLine * sizeof(float) <= 160 * 1024, "the longest line fits beside the tiles");
+  __shared__ int touched[4];                          // whether a wave's line holds anything
+  static_assert(sizeof tile + sizeof stat + sizeof side + sizeof touched + (kSums ? 5 : 1) * kLine * sizeof(float) <= 160 * 1024, "the longest line fits beside the tiles");
   extern __shared__ float dyn[];                      // with a table: bias line, then (kSums) a line of diagonal sums per wave, turned over
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
   if ((int)blockIdx.x >= grid) {
@@ -633,6 +634,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
   float left = 0.f, right = 0.f;
   double sl = 0.0, sr = 0.0;                 // of rows beyond the last edges, whose dS sum to zero only across all keys: nothing may be lost on the way
   bool bare = __any(!mine);                  // keys that take no part
+  bool near = false;                         // the wave has added to its line
   int rel = rest_above((int64_t)k0 - start_of(a, b));
   bool c0 = false, c1 = false;               // whether this tile and the next have rows with a `hi`, or zeros beside odd keys
   if (t0 < t1) {
@@ -720,6 +722,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       }
       if (where == 0) {
         add_diagonals(dp, diag + wave * nline + span - rel0, lane);   // queries in the registers: the line runs the other way
+        near = true;
       } else {
         float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -738,8 +741,17 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
     if (lane == 0) {
       side[wave] = sl;
       side[4 + wave] = sr;
+      touched[wave] = near;
     }
     sl = sr = 0.0;
+    near = false;
+    __syncthreads();
+    double all_left = side[0] + side[1] + side[2] + side[3], all_right = side[4] + side[5] + side[6] + side[7], *out = sums_of(head);
+    if (!uniform(touched[0] | touched[1] | touched[2] | touched[3])) {   // all beyond the last edges: the lines are zero
+      int E = a.bk.n_edges;
+      for (int n = tid; n < a.bk.buckets; n += 256) out[n] = (n == E ? all_left : 0.0) + (n == (a.bk.two_sided ? 2 * E + 1 : 0) ? all_right : 0.0);
+      return;
+    }
     for (int n = tid; n < nline; n += 256) {
       float x = 0.f;
 #pragma unroll
@@ -751,7 +763,7 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void k_att
       dyn[n] = x;
     }
     __syncthreads();
-    bucket_sums(a.bk, dyn, span, side[0] + side[1] + side[2] + side[3], side[4] + side[5] + side[6] + side[7], sums_of(head), tid);
+    bucket_sums(a.bk, dyn, span, all_left, all_right, out, tid);
   };
   for (int t = t0; t < t1; ++t) {
     if (ln && (i0 == 0 || t == t0)) {        // another head: its bias line (nobody reads the old one any more)
