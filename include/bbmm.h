@@ -401,8 +401,8 @@ int bbmm_predict_var(bbmm_ctx* ctx, int32_t mode, const float* Xstar, int64_t ns
  *                 and sums are fp32; weights (and dS) are rounded to `type` once as operands of the second products.  In fp16 powers of
  *                 two lift them out of the subnormal numbers first: for dQ by the row's own dO, for dK by the largest dO among the
  *                 rows of its batch entry and shared head, beside which rows of 2^-20 of that lose bits of their part.
- *                 In fp32 the gradients are as precise as the formula's steps in fp32; the gradient forms rows of |lse| beyond 64
- *                 (fp16 256, bf16 2048) once more, because an fp32 lse holds their weights too coarsely
+ *                 In fp32 the gradients are as precise as the formula's steps in fp32.  Rows of |lse| beyond 256 (fp16), 2048 (bf16) and
+ *                 65536 (fp32) are formed once more by the gradient, because an fp32 lse holds their weights too coarsely
  *   heads         query heads; kv_heads divides it, head h reads keys and values of head h / (heads / kv_heads)
  *   d, dv         features of queries and keys, and of values: 1 .. 128
  *   scale         > 0, scale / log 2 finite in fp32

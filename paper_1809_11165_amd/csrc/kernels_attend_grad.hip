@@ -90,9 +90,9 @@ __global__ __launch_bounds__(256) void k_attend_norms(AttArgs a, AttGrad g) {
 
 // Beyond this, fp32 holds lse too coarsely to recover weights from it: rounded as a logarithm to base 2, to base e and to base 2 again, it
 // leaves all weights of a row off by a common factor of up to 3.3 2^-24 |lse|, which a softmax that divides by its own sum does not have.  The row's
-// largest score and log2 of its sum are formed again there and kept apart.  At these bounds the factor is an eighth of half a step of
-// the type (fp32: 2^-16; scores of that size are rounded by a third of it themselves).
-template <typename T> struct Coarse { static constexpr float value = 64.f; };
+// largest score and log2 of its sum are formed again there and kept apart.  At the bounds of two-byte types the factor is an eighth of half a step of
+// the type.  fp32 divides by the sum of these weights in any case, and only keeps them from running off (rows of nothing but masks of -1e9, say).
+template <typename T> struct Coarse { static constexpr float value = 65536.f; };
 template <> struct Coarse<_Float16> { static constexpr float value = 256.f; };
 template <> struct Coarse<__bf16> { static constexpr float value = 2048.f; };
 
