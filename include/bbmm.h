@@ -470,6 +470,137 @@ int bbmm_bucket_bias_grad(bbmm_ctx* ctx, int32_t type, const void* dB, int64_t b
                           int64_t n_edges, const int32_t* edges, int32_t two_sided, int64_t start, void* dtable, void* work,
                           int64_t work_bytes);
 
+/* ------------------------------------------------------------------------
+ * Rotation: queries and keys on their way into an attention (bbmm_attend, bbmm_attend_cache), normed for each head and turned by
+ * their positions, in one pass; and its gradient.  For a row x of d features at position pos:
+ *
+ *   z = w x r,  r = (mean_c x_c^2 + eps)^-1/2       (no norm: z = x)
+ *   y_a = z_a cos t - z_b sin t,  y_b = z_b cos t + z_a sin t      for every pair p < rot / 2,  t = pos[axis[p]] freq[p]
+ *   y_c = z_c                                                      behind the first rot features
+ * with (a, b) = (p, p + rot / 2), or (2p, 2p + 1) with `neighbours`.  Norms, angles' functions and sums are fp32, angles are formed and
+ * taken modulo a turn in fp64; outputs are rounded once.
+ *
+ *   type          BBMM_TYPE_F32, _F16 or _BF16: of Q, K, the weights, the outputs and all gradients
+ *   norm, eps     norm != 0: each head's row is normed, eps >= 0 (a row of zeros with eps = 0 becomes NaN); norm = 0: no weights
+ *   batch, rows   of Q and K; rows at or behind len_b are zero in the outputs and the gradients, take no part and may hold anything
+ *   q_heads, k_heads   either may be 0 (that input is then not read and may be NULL)
+ *   d, rot        d in 1 .. 128; rot even, 0 .. d
+ *   Q, K          device; element [b][row][head][feature] at b stride[0] + row stride[1] + head stride[2] + feature (elements)
+ *   q_weight, k_weight   device, d entries, or NULL (ones)
+ *   pos           device, [n_axes][batch][rows] int64, 1 <= n_axes <= 4 (time, height, width, ..); exact to 2^53, an angle is off by 2^-51 of itself
+ *   axis          host, rot / 2 entries below n_axes, or NULL (axis 0); only read during the call
+ *   freq          device, rot / 2 doubles, radians per position; pos and freq may be NULL where rot = 0
+ *   len           device, batch entries (taken as within [0, rows]), or NULL: all rows
+ * Limits: batch, heads <= 65535, rows <= 2^30, batch rows (q_heads + k_heads) <= 2^27.
+ * Outputs are dense, [batch][row][head][feature], and must not overlap inputs or each other.  The calls only queue work on the context's
+ * stream, allocate nothing and keep nothing; results are the same from call to call.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t type;
+  int32_t neighbours;
+  int32_t norm;
+  int32_t n_axes;
+  double eps;
+  int64_t batch, rows, q_heads, k_heads, d, rot;
+  const void* Q;
+  const void* K;
+  int64_t q_stride[3];
+  int64_t k_stride[3];
+  const void* q_weight;
+  const void* k_weight;
+  const int64_t* pos;
+  const uint8_t* axis;
+  const double* freq;
+  const int32_t* len;
+} bbmm_rotation;
+
+/* Qr, Kr: device, batch x rows x q_heads (k_heads) x d. */
+int bbmm_rotate(bbmm_ctx* ctx, const bbmm_rotation* in, void* Qr, void* Kr);
+
+/* Bytes of device workspace (16-byte aligned) of bbmm_rotate_grad; may be 0.  What `in` points to is not read, only which weights are there. */
+int bbmm_rotate_workspace(bbmm_ctx* ctx, const bbmm_rotation* in, int64_t* bytes);
+
+/* Gradients of sum(dQr . Qr) + sum(dKr . Kr): dQ, dK (device, dense) and, for weights that are there, dq_weight, dk_weight (device, d
+ * entries, summed over batch, rows and heads; NULL without the weight).  dQr, dKr: device, strides like Q's and K's. */
+int bbmm_rotate_grad(bbmm_ctx* ctx, const bbmm_rotation* in, const void* dQr, const int64_t* dqr_stride, const void* dKr,
+                     const int64_t* dkr_stride, void* dQ, void* dK, void* dq_weight, void* dk_weight, void* work, int64_t work_bytes);
+
+/* ------------------------------------------------------------------------
+ * Cache: keys and values of growing sequences in pages, written as rows arrive, read back, and read in place by the attention of
+ * new rows.  The memory is the caller's; a page holds page_rows rows of all shared heads.  Row j of sequence b is
+ * row j % page_rows of page table[b][j / page_rows].  A table entry outside [0, pages) is a page that is not there (not yet, or not any
+ * more): nothing is written to it, its rows read as zeros and take no part in an attention.  Sequences may share pages that they only read.
+ *
+ *   type          BBMM_TYPE_F32, _F16, _BF16, or BBMM_TYPE_E4M3: 8-bit floats (4 exponent and 3 mantissa bits, largest 448) with a
+ *                 power of two for every 32 features of a row (the last block may be shorter): the smallest 2^e, e >= -117, by which
+ *                 the block's largest finite magnitude becomes at most 448.  Stored is x / 2^e rounded to nearest even (but not
+ *                 beyond the type that x came in: 240 2^e is the last value then), infinities and NaN as NaN.  A value
+ *                 read back is exact in fp32 and bf16, and rounded to fp16 where that type's range is left
+ *   pages, page_rows   pages in 0 .. 2^31 - 1, page_rows in 1 .. 2^30, max_pages page_rows <= 2^30
+ *   d, dv         features of keys and of values: 1 .. 128
+ *   K, V          device; element [page][row][head][feature] at page stride[0] + row stride[1] + head stride[2] + feature (elements).
+ *                 Rows start at multiples of 16 bytes and own memory up to the next multiple (written as zeros): pointers and
+ *                 strides in bytes are multiples of 16, strides[1] below 2^21 elements
+ *   K_exp, V_exp  device, E4M3 only: [pages][kv_heads][page_rows][4] bytes, e + 127 of a row's blocks
+ *   table         device, batch x max_pages
+ * Limits: batch and kv_heads <= 65535.  Rows that a call writes must be distinct places; no call writes to other rows.
+ * ---------------------------------------------------------------------- */
+enum { BBMM_TYPE_E4M3 = 3 };
+
+typedef struct {
+  int32_t type;
+  int32_t reserved;                      /* 0 */
+  int64_t pages, page_rows, kv_heads, d, dv, batch, max_pages;
+  void* K;
+  void* V;
+  int64_t k_stride[3];
+  int64_t v_stride[3];
+  uint8_t* K_exp;
+  uint8_t* V_exp;
+  const int32_t* table;
+} bbmm_cache;
+
+/* Writes row r < n_new_b of K and V (device, batch x rows x kv_heads x d and dv, of `type`, which is the cache's own unless that is E4M3;
+ * strides as of bbmm_attention) as row start_b + r of sequence b.  start, n_new: device, batch entries, or NULL (0; all rows).
+ * Rows that fall outside [0, max_pages page_rows) are not written.  batch rows kv_heads <= 2^27. */
+int bbmm_cache_write(bbmm_ctx* ctx, const bbmm_cache* cache, int32_t type, int64_t rows, const void* K, const int64_t* k_stride,
+                     const void* V, const int64_t* v_stride, const int32_t* start, const int32_t* n_new);
+
+/* Reads rows start_b + r, r < rows, of every sequence into K and V (device, dense, batch x rows x kv_heads x d and dv, of `type`, as
+ * above); rows at or behind length_b (a row number of the sequence, NULL: none) and rows outside the table are zeros. */
+int bbmm_cache_read(bbmm_ctx* ctx, const bbmm_cache* cache, int32_t type, int64_t rows, const int32_t* start, const int32_t* length,
+                    void* K, void* V);
+
+/* Attention of nq new rows of every sequence over its cached rows, their own among them (written before):
+ *
+ *   s_ij = scale q_i.k_j, or cap tanh(scale q_i.k_j / cap) with cap > 0,   o_i = sum_j exp(s_ij - lse_i) v_j
+ *   over rows j < k_len_b of pages that are there; with `causal` j <= p_i, with window > 0 j > p_i - window, where
+ *   p_i = k_len_b - q_len_b + i is the row's own place (the new rows are the sequence's last).
+ * Rows that nothing is left for, and rows at or behind q_len_b, have o_i = 0 and lse_i = -infinity; what takes no part may hold
+ * anything.  Scores, statistics and sums are fp32; weights are rounded to `type` once as operands.
+ *
+ *   type          of Q and O; the cache's own unless that is E4M3.  heads: a multiple of the cache's kv_heads, head h reads
+ *                 shared head h / (heads / kv_heads)
+ *   q_len, k_len  device, batch entries (taken as within [0, nq] and [0, max_pages page_rows]); q_len may be NULL: nq
+ *   cap           0 (none) or > 0; scale > 0, both (and scale / cap) finite and not zero in fp32, also in units of log 2
+ *   window        0 (none) or > 0
+ * Limits: heads <= 65535, nq <= 2^20, batch heads nq <= 2^27, batch kv_heads ceil(nq heads / kv_heads / 16) <= 2^23.
+ * O (device, dense, batch x nq x heads x dv), lse (device, batch x heads x nq float), workspace, streams and graphs as of bbmm_attend. */
+typedef struct {
+  int32_t type;
+  int32_t causal;
+  int64_t heads, nq, window;
+  double scale, cap;
+  const void* Q;
+  int64_t q_stride[3];
+  const int32_t* q_len;
+  const int32_t* k_len;
+} bbmm_cached_attention;
+
+int bbmm_attend_cache_workspace(bbmm_ctx* ctx, const bbmm_cache* cache, const bbmm_cached_attention* in, int64_t* bytes);
+int bbmm_attend_cache(bbmm_ctx* ctx, const bbmm_cache* cache, const bbmm_cached_attention* in, void* O, float* lse, void* work,
+                      int64_t work_bytes);
+
 #ifdef __cplusplus
 }
 #endif

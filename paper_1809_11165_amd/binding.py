@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libbbmm.so")
 
 KERNEL_RBF, KERNEL_MATERN52 = 0, 1
 MODE_MATERIALISED, MODE_ONTHEFLY, MODE_SGPR = 0, 1, 2
-TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
+TYPE_F32, TYPE_F16, TYPE_BF16, TYPE_E4M3 = 0, 1, 2, 3
 OK, EINVAL, ENOMEM, ENOTPD, ENONFINITE, EHIP, ENOCONV = 0, 1, 2, 3, 4, 5, 6
 MAX_ITERS = 256
 
@@ -34,6 +34,8 @@ EXPORTS = [
     "bbmm_predict_mean", "bbmm_predict_var",
     "bbmm_attend_workspace", "bbmm_attend", "bbmm_attend_grad",
     "bbmm_bucket_bias", "bbmm_bucket_bias_workspace", "bbmm_bucket_bias_grad",
+    "bbmm_rotate", "bbmm_rotate_workspace", "bbmm_rotate_grad",
+    "bbmm_cache_write", "bbmm_cache_read", "bbmm_attend_cache_workspace", "bbmm_attend_cache",
 ]
 
 
@@ -74,6 +76,27 @@ class _Attention(C.Structure):
                 ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
                 ("q_len", C.c_void_p), ("k_len", C.c_void_p), ("key_mask", C.c_void_p), ("table", C.c_void_p),
                 ("n_edges", C.c_int64), ("edges", C.POINTER(C.c_int32)), ("q_start", C.c_void_p)]
+
+
+class _Rotation(C.Structure):
+    _fields_ = [("type", C.c_int32), ("neighbours", C.c_int32), ("norm", C.c_int32), ("n_axes", C.c_int32), ("eps", C.c_double),
+                ("batch", C.c_int64), ("rows", C.c_int64), ("q_heads", C.c_int64), ("k_heads", C.c_int64), ("d", C.c_int64),
+                ("rot", C.c_int64), ("Q", C.c_void_p), ("K", C.c_void_p), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("pos", C.c_void_p), ("axis", C.c_char_p), ("freq", C.c_void_p),
+                ("len", C.c_void_p)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("type", C.c_int32), ("reserved", C.c_int32), ("pages", C.c_int64), ("page_rows", C.c_int64), ("kv_heads", C.c_int64),
+                ("d", C.c_int64), ("dv", C.c_int64), ("batch", C.c_int64), ("max_pages", C.c_int64), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p),
+                ("table", C.c_void_p)]
+
+
+class _CachedAttention(C.Structure):
+    _fields_ = [("type", C.c_int32), ("causal", C.c_int32), ("heads", C.c_int64), ("nq", C.c_int64), ("window", C.c_int64),
+                ("scale", C.c_double), ("cap", C.c_double), ("Q", C.c_void_p), ("q_stride", C.c_int64 * 3), ("q_len", C.c_void_p),
+                ("k_len", C.c_void_p)]
 
 
 _lib = None
@@ -138,6 +161,16 @@ def load_library() -> C.CDLL:
     lib.bbmm_bucket_bias_grad.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
                                           C.c_int64, C.POINTER(C.c_int32), C.c_int32, C.c_int64, C.c_void_p, C.c_void_p,
                                           C.c_int64]
+    lib.bbmm_rotate.argtypes = [C.c_void_p, C.POINTER(_Rotation), C.c_void_p, C.c_void_p]
+    lib.bbmm_rotate_workspace.argtypes = [C.c_void_p, C.POINTER(_Rotation), C.POINTER(C.c_int64)]
+    lib.bbmm_rotate_grad.argtypes = [C.c_void_p, C.POINTER(_Rotation), C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.POINTER(C.c_int64),
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]
+    lib.bbmm_cache_write.argtypes = [C.c_void_p, C.POINTER(_Cache), C.c_int32, C.c_int64, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p,
+                                     C.POINTER(C.c_int64), C.c_void_p, C.c_void_p]
+    lib.bbmm_cache_read.argtypes = [C.c_void_p, C.POINTER(_Cache), C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.bbmm_attend_cache_workspace.argtypes = [C.c_void_p, C.POINTER(_Cache), C.POINTER(_CachedAttention), C.POINTER(C.c_int64)]
+    lib.bbmm_attend_cache.argtypes = [C.c_void_p, C.POINTER(_Cache), C.POINTER(_CachedAttention), C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_int64]
     _lib = lib
     return lib
 
@@ -356,6 +389,188 @@ class Attention:
                 _check_same(self.q_start, (b,), torch.int64, device, "q_start")
                 a.q_start = self.q_start.data_ptr()
         return a
+
+
+@dataclass
+class Rotation:
+    """One rotation of queries and keys (see include/bbmm.h, "Rotation").  Q (batch, rows, heads, d) and K (batch, rows, k_heads, d):
+    device tensors of one type, any strides with the last dimension contiguous; either may be None.  pos: int64 (batch, rows) or
+    (axes, batch, rows); freq: float64 (rot / 2,), radians per position; axis: the axis of every pair (default 0).  Pairs are halves of
+    the first rot features, or neighbours.  eps: each head's row is normed (None: no norm); q_weight, k_weight: (d,) of Q's type.
+    row_len: int32 (batch,), rows that are there.  The calls record no graph of gradients (see Attention)."""
+    Q: "object"
+    K: "object"
+    pos: "object"
+    freq: "object"
+    axis: "object" = None
+    neighbours: bool = False
+    eps: Optional[float] = None
+    q_weight: "object" = None
+    k_weight: "object" = None
+    row_len: "object" = None
+
+    def tensors(self):
+        return [t for t in (self.Q, self.K, self.pos, self.freq, self.q_weight, self.k_weight, self.row_len) if t is not None]
+
+    def to_c(self, device) -> _Rotation:
+        Q, K, pos, freq = self.Q, self.K, self.pos, self.freq
+        one = Q if Q is not None else K
+        if one is None:
+            raise ValueError("Q or K is required")
+        code, t = _type_of(one, "Q" if Q is not None else "K"), one.dtype
+        if one.dim() != 4:
+            raise ValueError("Q and K must have four dimensions (batch, row, head, feature)")
+        b, rows, _, d = one.shape
+        r = _Rotation(code, bool(self.neighbours), self.eps is not None, 1, self.eps or 0.0, b, rows, 0, 0, d, 0)
+        for x, name in ((Q, "Q"), (K, "K")):
+            if x is None:
+                continue
+            if getattr(x, "ndim", 4) != 4:
+                raise ValueError("%s must have four dimensions (batch, row, head, feature)" % name)
+            _check_same(x, (b, rows, x.shape[2], d) if hasattr(x, "shape") else (), t, device, name, dense=False)
+        if Q is not None:
+            r.Q, r.q_heads, r.q_stride = Q.data_ptr(), Q.shape[2], Q.stride()[:3]
+        if K is not None:
+            r.K, r.k_heads, r.k_stride = K.data_ptr(), K.shape[2], K.stride()[:3]
+        double, int64, int32 = _rotation_types()
+        half = 0
+        if freq is not None:
+            half = freq.shape[0] if getattr(freq, "ndim", 0) == 1 else 0
+            _check_same(freq, (half,), double, device, "freq")
+            if half:
+                r.rot, r.freq = 2 * half, freq.data_ptr()
+        if pos is not None:
+            r.n_axes = pos.shape[0] if getattr(pos, "ndim", 0) == 3 else 1
+            _check_same(pos, (r.n_axes, b, rows) if getattr(pos, "ndim", 0) == 3 else (b, rows), int64, device, "pos")
+            r.pos = pos.data_ptr()
+        if self.axis is not None:
+            try:
+                r.axis = bytes(self.axis)
+            except (ValueError, TypeError):
+                raise ValueError("axis must hold whole numbers of axes") from None
+            if len(self.axis) != half:
+                raise ValueError("axis has %d entries, expected %d" % (len(self.axis), half))
+        if self.q_weight is not None:
+            _check_same(self.q_weight, (d,), t, device, "q_weight")
+            r.q_weight = self.q_weight.data_ptr()
+        if self.k_weight is not None:
+            _check_same(self.k_weight, (d,), t, device, "k_weight")
+            r.k_weight = self.k_weight.data_ptr()
+        if self.row_len is not None:
+            _check_same(self.row_len, (b,), int32, device, "row_len")
+            r.len = self.row_len.data_ptr()
+        return r
+
+
+def _rotation_types():
+    import torch
+    return torch.float64, torch.int64, torch.int32
+
+
+@dataclass
+class Cache:
+    """Pages of keys and values (see include/bbmm.h, "Cache").  K (pages, page_rows, kv_heads, d), V (pages, page_rows, kv_heads, dv):
+    device tensors of one type, float32, float16, bfloat16 or float8_e4m3fn, rows starting at multiples of 16 bytes (`Cache.empty`
+    makes such pages); table: int32 (batch, max_pages), entries outside [0, pages) are pages that are not there; k_exp, v_exp: uint8
+    (pages, kv_heads, page_rows, 4), with float8 pages."""
+    K: "object"
+    V: "object"
+    table: "object"
+    k_exp: "object" = None
+    v_exp: "object" = None
+
+    @classmethod
+    def empty(cls, pages: int, page_rows: int, kv_heads: int, d: int, dv: Optional[int] = None, dtype=None, table=None, device="cuda:0"):
+        """Pages without values, heads outside rows in memory (a head's rows of a page lie side by side).  dtype: default bfloat16."""
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        size = torch.empty(0, dtype=dtype).element_size()
+        step = 16 // size
+
+        def side(width):
+            held = torch.empty(pages, kv_heads, page_rows, (width + step - 1) // step * step, dtype=dtype, device=device)
+            return held[..., :width].transpose(1, 2)
+
+        exps = [None, None]
+        if dtype == torch.float8_e4m3fn:
+            exps = [torch.empty(pages, kv_heads, page_rows, 4, dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(side(d), side(d if dv is None else dv), table, *exps)
+
+    def tensors(self):
+        return [t for t in (self.K, self.V, self.table, self.k_exp, self.v_exp) if t is not None]
+
+    def to_c(self, device) -> _Cache:
+        K, V, table = self.K, self.V, self.table
+        t = getattr(K, "dtype", None)
+        e4m3 = t is not None and t is _float8()
+        code = TYPE_E4M3 if e4m3 else _type_of(K, "K")
+        try:
+            pages, page_rows, hk, d = K.shape
+            _, _, _, dv = V.shape
+        except (ValueError, AttributeError):
+            raise ValueError("K and V must have four dimensions (page, row, head, feature)") from None
+        _check_same(K, (pages, page_rows, hk, d), t, device, "K", dense=False)
+        _check_same(V, (pages, page_rows, hk, dv), t, device, "V", dense=False)
+        if getattr(table, "ndim", 0) != 2:
+            raise ValueError("table must have two dimensions (batch, page)")
+        b, most = table.shape
+        _check_same(table, (b, most), _rotation_types()[2], device, "table")
+        c = _Cache(code, 0, pages, page_rows, hk, d, dv, b, most, K.data_ptr(), V.data_ptr(), K.stride()[:3], V.stride()[:3])
+        c.table = table.data_ptr()
+        if e4m3:
+            import torch
+            for x, name in ((self.k_exp, "k_exp"), (self.v_exp, "v_exp")):
+                if x is None:
+                    raise ValueError("float8 pages need %s" % name)
+                _check_same(x, (pages, hk, page_rows, 4), torch.uint8, device, name)
+            c.K_exp, c.V_exp = self.k_exp.data_ptr(), self.v_exp.data_ptr()
+        elif self.k_exp is not None or self.v_exp is not None:
+            raise ValueError("exponents without float8 pages")
+        return c
+
+
+def _float8():
+    import torch
+    return torch.float8_e4m3fn
+
+
+@dataclass
+class CachedAttention:
+    """Attention of new rows over a cache (see include/bbmm.h, "Cache").  Q (batch, nq, heads, d): any strides with the last dimension
+    contiguous, of the cache's type unless that is float8.  k_len: int32 (batch,), rows of each sequence, the new ones among them;
+    q_len: int32 (batch,).  scale: default d^-1/2.  causal: row i of a sequence's last q_len rows takes keys up to its own place; window:
+    no more than that many of them, 0 all; cap: scores become cap tanh(s / cap), 0 none."""
+    cache: Cache
+    Q: "object"
+    k_len: "object"
+    q_len: "object" = None
+    scale: Optional[float] = None
+    causal: bool = True
+    window: int = 0
+    cap: float = 0.0
+
+    def tensors(self):
+        return self.cache.tensors() + [t for t in (self.Q, self.k_len, self.q_len) if t is not None]
+
+    def to_c(self, device):
+        c = self.cache.to_c(device)
+        Q = self.Q
+        code, t = _type_of(Q, "Q"), Q.dtype
+        if Q.dim() != 4:
+            raise ValueError("Q must have four dimensions (batch, row, head, feature)")
+        b, nq, h, d = Q.shape
+        _check_same(Q, (c.batch, nq, h, c.d), t, device, "Q", dense=False)
+        if c.type != TYPE_E4M3 and c.type != code:
+            raise TypeError("Q must be of the cache's type")
+        a = _CachedAttention(code, bool(self.causal), h, nq, _int64(self.window), max(d, 1) ** -0.5 if self.scale is None else self.scale,
+                             self.cap, Q.data_ptr(), Q.stride()[:3])
+        int32 = _rotation_types()[2]
+        _check_same(self.k_len, (b,), int32, device, "k_len")
+        a.k_len = self.k_len.data_ptr()
+        if self.q_len is not None:
+            _check_same(self.q_len, (b,), int32, device, "q_len")
+            a.q_len = self.q_len.data_ptr()
+        return c, a
 
 
 @dataclass
@@ -708,6 +923,120 @@ class Context:
             return dtable
 
         return self._ordered([dB], call)
+
+    # ---- rotation and cache -----------------------------------------------------------------
+    def bbmm_rotate(self, rot: Rotation):
+        """(Qr, Kr), dense, of the shapes of Q and K; None for an input that is None."""
+        r = rot.to_c(self.device)
+
+        def call():
+            out = [None if x is None else self.torch.empty(x.shape, dtype=x.dtype, device=self.device) for x in (rot.Q, rot.K)]
+            self._ck(self.lib.bbmm_rotate(self.h, C.byref(r), *[None if y is None else y.data_ptr() for y in out]))
+            return tuple(out)
+
+        return self._ordered(rot.tensors(), call)
+
+    def _rotate_bytes(self, r: _Rotation) -> int:
+        n = C.c_int64(0)
+        self._ck(self.lib.bbmm_rotate_workspace(self.h, C.byref(r), C.byref(n)))
+        return n.value
+
+    def bbmm_rotate_workspace(self, rot: Rotation) -> int:
+        """Bytes that bbmm_rotate_grad takes from torch's allocator besides its outputs."""
+        return self._rotate_bytes(rot.to_c(self.device))
+
+    def bbmm_rotate_grad(self, rot: Rotation, dQr, dKr):
+        """(dQ, dK, dq_weight, dk_weight) of sum(dQr * Qr) + sum(dKr * Kr); None for what is None in the rotation."""
+        r = rot.to_c(self.device)
+        given, ptr, stride = [], [], []
+        for x, g, name in ((rot.Q, dQr, "dQr"), (rot.K, dKr, "dKr")):
+            if x is None:
+                if g is not None:
+                    raise ValueError("%s without its input" % name)
+                ptr.append(None)
+                stride.append(None)
+                continue
+            _check_same(g, x.shape, x.dtype, self.device, name, dense=False)
+            given.append(g)
+            ptr.append(g.data_ptr())
+            stride.append((C.c_int64 * 3)(*g.stride()[:3]))
+
+        def call():
+            out = [None if x is None else self.torch.empty(x.shape, dtype=x.dtype, device=self.device)
+                   for x in (rot.Q, rot.K, rot.q_weight, rot.k_weight)]
+            w, wp, n = self._work(self._rotate_bytes(r))
+            self._ck(self.lib.bbmm_rotate_grad(self.h, C.byref(r), ptr[0], stride[0], ptr[1], stride[1],
+                                               *[None if y is None else y.data_ptr() for y in out], wp, n))
+            return tuple(out)
+
+        return self._ordered(rot.tensors() + given, call)
+
+    def _lengths(self, x, batch, name):
+        if x is None:
+            return None
+        _check_same(x, (batch,), self.torch.int32, self.device, name)
+        return x.data_ptr()
+
+    def bbmm_cache_write(self, cache: Cache, K, V, start=None, n_new=None):
+        """Writes rows of K (batch, rows, kv_heads, d) and V (.., dv) as rows start, start + 1, .. of every sequence.  start, n_new:
+        int32 (batch,); default 0 and all rows."""
+        c = cache.to_c(self.device)
+        code = _type_of(K, "K")
+        if K.dim() != 4:
+            raise ValueError("K must have four dimensions (batch, row, head, feature)")
+        rows = K.shape[1]
+        _check_same(K, (c.batch, rows, c.kv_heads, c.d), K.dtype, self.device, "K", dense=False)
+        _check_same(V, (c.batch, rows, c.kv_heads, c.dv), K.dtype, self.device, "V", dense=False)
+        s, n = self._lengths(start, c.batch, "start"), self._lengths(n_new, c.batch, "n_new")
+
+        def call():
+            self._ck(self.lib.bbmm_cache_write(self.h, C.byref(c), code, rows, K.data_ptr(), (C.c_int64 * 3)(*K.stride()[:3]),
+                                               V.data_ptr(), (C.c_int64 * 3)(*V.stride()[:3]), s, n))
+
+        return self._ordered(cache.tensors() + [t for t in (K, V, start, n_new) if t is not None], call)
+
+    def bbmm_cache_read(self, cache: Cache, rows: int, start=None, length=None, dtype=None):
+        """(K, V), dense (batch, rows, kv_heads, d and dv): rows start, start + 1, .. of every sequence, zeros from row number `length` on.
+        dtype: the cache's own; of float8 pages float32, float16 or bfloat16 (default)."""
+        c = cache.to_c(self.device)
+        torch = self.torch
+        if dtype is None:
+            dtype = torch.bfloat16 if c.type == TYPE_E4M3 else cache.K.dtype
+        code = _type_of(torch.empty(0, dtype=dtype), "dtype")
+        s, n = self._lengths(start, c.batch, "start"), self._lengths(length, c.batch, "length")
+        rows = int(rows)
+        if rows < 0:
+            raise ValueError("rows must be >= 0")
+
+        def call():
+            K = torch.empty(c.batch, rows, c.kv_heads, c.d, dtype=dtype, device=self.device)
+            V = torch.empty(c.batch, rows, c.kv_heads, c.dv, dtype=dtype, device=self.device)
+            self._ck(self.lib.bbmm_cache_read(self.h, C.byref(c), code, rows, s, n, K.data_ptr(), V.data_ptr()))
+            return K, V
+
+        return self._ordered(cache.tensors() + [t for t in (start, length) if t is not None], call)
+
+    def _cached_bytes(self, c: _Cache, a: _CachedAttention) -> int:
+        n = C.c_int64(0)
+        self._ck(self.lib.bbmm_attend_cache_workspace(self.h, C.byref(c), C.byref(a), C.byref(n)))
+        return n.value
+
+    def bbmm_attend_cache_workspace(self, att: CachedAttention) -> int:
+        """Bytes that bbmm_attend_cache takes from torch's allocator besides its outputs."""
+        return self._cached_bytes(*att.to_c(self.device))
+
+    def bbmm_attend_cache(self, att: CachedAttention):
+        """(O, lse): (batch, nq, heads, dv) of Q's type and (batch, heads, nq) float32."""
+        c, a = att.to_c(self.device)
+
+        def call():
+            O = self.torch.empty((c.batch, a.nq, a.heads, c.dv), dtype=att.Q.dtype, device=self.device)
+            lse = self.torch.empty((c.batch, a.heads, a.nq), dtype=self.torch.float32, device=self.device)
+            w, wp, n = self._work(self._cached_bytes(c, a))
+            self._ck(self.lib.bbmm_attend_cache(self.h, C.byref(c), C.byref(a), O.data_ptr(), lse.data_ptr(), wp, n))
+            return O, lse
+
+        return self._ordered(att.tensors(), call)
 
 
 def problem_from_workload(w, mode: int, device="cuda:0") -> Problem:

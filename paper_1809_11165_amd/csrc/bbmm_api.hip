@@ -4,6 +4,7 @@
 // copies the scalar results back with a single stream synchronisation.
 #include "bbmm.h"
 #include "bbmm_attend.h"
+#include "bbmm_cache.h"
 #include "bbmm_dev.h"
 #include "bbmm_plan.h"
 
@@ -2387,6 +2388,283 @@ int bucket_bias_grad(bbmm_ctx* c, int32_t type, const void* dB, int64_t batch, i
   return BBMM_OK;
 }
 
+// ------------------------------------------------------------------ rotation and cache
+size_t elem_size(int32_t type) { return type == BBMM_TYPE_E4M3 ? 1 : type == BBMM_TYPE_F32 ? 4 : 2; }
+
+// Whether rows of `width` elements at p may be moved 16 bytes at a time (strides null: dense rows).
+bool whole_pieces(const void* p, const int64_t* stride, int64_t width, size_t elem) {
+  bool ok = (uintptr_t)p % 16 == 0 && width * elem % 16 == 0;
+  for (int k = 0; k < 3 && stride; ++k) ok = ok && stride[k] * elem % 16 == 0;
+  return ok;
+}
+
+bool negative(const int64_t* stride) { return stride[0] < 0 || stride[1] < 0 || stride[2] < 0; }
+
+constexpr int64_t kMaxRows = (int64_t)1 << 27;             // (batch, row, head) in a call
+
+// Sizes and, where `pointers` is set, all inputs.
+int rotation_args(bbmm_ctx* c, const bbmm_rotation* in, bool pointers, RotArgs* a) {
+  if (!in) return fail(c, BBMM_EINVAL, "rotation: no description");
+  if (in->type < BBMM_TYPE_F32 || in->type > BBMM_TYPE_BF16) return fail(c, BBMM_EINVAL, "rotation: unknown type");
+  if (in->batch < 0 || in->batch > kAttMaxHeads || in->q_heads < 0 || in->q_heads > kAttMaxHeads || in->k_heads < 0 || in->k_heads > kAttMaxHeads ||
+      in->rows < 0 || in->rows > kAttMaxLen)
+    return fail(c, BBMM_EINVAL, "rotation: batch and heads up to 65535, rows up to 2^30");
+  if (in->d < 1 || in->d > BBMM_ATT_MAXD || in->rot < 0 || in->rot > in->d || in->rot % 2) return fail(c, BBMM_EINVAL, "rotation: d from 1 to 128, rot even, up to d");
+  if (in->n_axes < 1 || in->n_axes > BBMM_ROT_AXES) return fail(c, BBMM_EINVAL, "rotation: 1 to 4 axes");
+  if (in->norm && !(in->eps >= 0.0 && isfinite((float)in->eps))) return fail(c, BBMM_EINVAL, "rotation: eps must be >= 0 and finite in fp32");
+  if (!in->norm && (in->q_weight || in->k_weight)) return fail(c, BBMM_EINVAL, "rotation: weights without a norm");
+  if (in->batch * in->rows * (in->q_heads + in->k_heads) > kMaxRows) return fail(c, BBMM_EINVAL, "rotation: more than 2^27 rows in one call");
+  memset(a, 0, sizeof *a);
+  a->heads[0] = (int)in->q_heads, a->heads[1] = (int)in->k_heads;
+  a->tokens = in->q_heads + in->k_heads ? in->batch * in->rows : 0;
+  a->rows = (int)in->rows, a->d = (int)in->d, a->rot = (int)in->rot, a->norm = in->norm != 0, a->neighbours = in->neighbours != 0, a->eps = in->eps;
+  a->w[0] = in->q_weight, a->w[1] = in->k_weight;
+  if (!pointers) return BBMM_OK;
+  size_t e = elem_size(in->type);
+  bool some = a->tokens > 0, q = some && a->heads[0], k = some && a->heads[1];
+  if ((q && !in->Q) || (k && !in->K)) return fail(c, BBMM_EINVAL, "rotation: Q and K are required");
+  if (some && a->rot && (!in->pos || !in->freq)) return fail(c, BBMM_EINVAL, "rotation: pos and freq are required");
+  if (((uintptr_t)in->Q | (uintptr_t)in->K | (uintptr_t)in->q_weight | (uintptr_t)in->k_weight) % e) return fail(c, BBMM_EINVAL, "rotation: pointer not aligned to its type");
+  if (((uintptr_t)in->pos | (uintptr_t)in->freq) % 8 || (uintptr_t)in->len % 4) return fail(c, BBMM_EINVAL, "rotation: positions, frequencies or lengths not aligned to their type");
+  if ((q && negative(in->q_stride)) || (k && negative(in->k_stride))) return fail(c, BBMM_EINVAL, "rotation: negative stride");
+  for (int p = 0; in->axis && p < a->rot / 2; ++p) {
+    if (in->axis[p] >= in->n_axes) return fail(c, BBMM_EINVAL, "rotation: a pair's axis must be below n_axes");
+    a->axis[p] = in->axis[p];
+  }
+  a->x[0] = in->Q, a->x[1] = in->K;
+  memcpy(a->xs[0], in->q_stride, sizeof a->xs[0]);
+  memcpy(a->xs[1], in->k_stride, sizeof a->xs[1]);
+  a->pos = in->pos, a->freq = in->freq, a->len = in->len;
+  a->by_rows = div_by((uint32_t)std::max<int64_t>(in->rows, 1));
+  for (int w = 0; w < 2; ++w) a->by_heads[w] = div_by((uint32_t)std::max(a->heads[w], 1));
+  bool whole = a->neighbours || a->rot / 2 * e % 16 == 0;  // a piece holds whole pairs, or the pairs of another one
+  a->vec = whole && (!q || whole_pieces(a->x[0], a->xs[0], a->d, e)) && (!k || whole_pieces(a->x[1], a->xs[1], a->d, e));
+  return BBMM_OK;
+}
+
+// Tokens of a workgroup: as many as its lanes hold rows of at a time (up to 8, whose angles are kept), fewer where the device has room left.  The
+// gradient's workgroups go on to further tokens, so that sums of the weights' gradients are few.
+constexpr int64_t kRotBlocks = (int64_t)1 << 20;
+int64_t rotate_most(const bbmm_ctx* c, bool grad) { return grad ? 4 * c->num_cus : kRotBlocks; }
+void rotate_plan(const bbmm_ctx* c, int type, bool grad, RotArgs* a) {
+  int hand = rotate_rows(type, grad, a->d, a->vec);
+  for (int w = 0; w < 2; ++w) {
+    int64_t t = a->heads[w] ? std::min<int64_t>(hand / a->heads[w], BBMM_ROT_TOKENS) : 1;
+    t = std::max<int64_t>(1, std::min<int64_t>(t, a->tokens / (2 * c->num_cus)));
+    a->tokens_per[w] = (int)t;
+    a->blocks[w] = a->heads[w] ? (int)std::min<int64_t>((a->tokens + t - 1) / t, rotate_most(c, grad)) : 0;
+  }
+}
+size_t rotate_work(const bbmm_ctx* c, const RotArgs& a) {
+  if (!a.w[0] && !a.w[1]) return 0;
+  return step256(2 * (size_t)std::min<int64_t>(a.tokens, rotate_most(c, true)) * a.d * sizeof(float));
+}
+
+int rotate(bbmm_ctx* c, const bbmm_rotation* in, void* Qr, void* Kr) {
+  RotArgs a;
+  int rc = rotation_args(c, in, true, &a);
+  if (rc) return rc;
+  if (a.tokens == 0) return BBMM_OK;
+  size_t e = elem_size(in->type);
+  if ((a.heads[0] && !Qr) || (a.heads[1] && !Kr) || ((uintptr_t)Qr | (uintptr_t)Kr) % e) return fail(c, BBMM_EINVAL, "rotation: outputs are required, aligned to their type");
+  a.y[0] = Qr, a.y[1] = Kr;
+  for (int w = 0; w < 2; ++w) a.vec = a.vec && (!a.heads[w] || whole_pieces(a.y[w], nullptr, a.d, e));
+  rotate_plan(c, in->type, false, &a);
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  launch_rotate(c->stream, in->type, a);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+int rotate_grad(bbmm_ctx* c, const bbmm_rotation* in, const void* dQr, const int64_t* dqr_stride, const void* dKr, const int64_t* dkr_stride, void* dQ,
+                void* dK, void* dq_weight, void* dk_weight, void* work, int64_t work_bytes) {
+  RotArgs a;
+  int rc = rotation_args(c, in, true, &a);
+  if (rc) return rc;
+  size_t e = elem_size(in->type);
+  bool q = a.tokens && a.heads[0], k = a.tokens && a.heads[1];
+  if ((q && (!dQr || !dqr_stride || !dQ)) || (k && (!dKr || !dkr_stride || !dK))) return fail(c, BBMM_EINVAL, "rotation: gradients of the outputs and of the inputs are required");
+  if ((a.w[0] != nullptr) != (dq_weight != nullptr) || (a.w[1] != nullptr) != (dk_weight != nullptr))
+    return fail(c, BBMM_EINVAL, "rotation: a weight and its gradient go together");
+  if (((uintptr_t)dQr | (uintptr_t)dKr | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dq_weight | (uintptr_t)dk_weight) % e)
+    return fail(c, BBMM_EINVAL, "rotation: pointer not aligned to its type");
+  if ((q && negative(dqr_stride)) || (k && negative(dkr_stride))) return fail(c, BBMM_EINVAL, "rotation: negative stride");
+  rc = check_work(c, work, work_bytes, rotate_work(c, a));
+  if (rc) return rc;
+  a.g[0] = dQr, a.g[1] = dKr, a.y[0] = dQ, a.y[1] = dK, a.w_part = work;
+  if (q) memcpy(a.gs[0], dqr_stride, sizeof a.gs[0]);
+  if (k) memcpy(a.gs[1], dkr_stride, sizeof a.gs[1]);
+  for (int w = 0; w < 2; ++w)
+    a.vec = a.vec && (!(w ? k : q) || (whole_pieces(a.g[w], a.gs[w], a.d, e) && whole_pieces(a.y[w], nullptr, a.d, e)));
+  rotate_plan(c, in->type, true, &a);
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  if (a.tokens) launch_rotate_grad(c->stream, in->type, a);
+  if (dq_weight || dk_weight) launch_rotate_join(c->stream, in->type, a, dq_weight, dk_weight);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+// Sizes and, where `pointers` is set, the pages, the exponents and the table.
+int cache_args(bbmm_ctx* c, const bbmm_cache* in, bool pointers, CacheArgs* a) {
+  if (!in) return fail(c, BBMM_EINVAL, "cache: no description");
+  if (in->type < BBMM_TYPE_F32 || in->type > BBMM_TYPE_E4M3) return fail(c, BBMM_EINVAL, "cache: unknown type");
+  if (in->reserved) return fail(c, BBMM_EINVAL, "cache: reserved must be 0");
+  if (in->batch < 0 || in->batch > kAttMaxHeads || in->kv_heads < 1 || in->kv_heads > kAttMaxHeads) return fail(c, BBMM_EINVAL, "cache: batch and kv_heads up to 65535");
+  if (in->pages < 0 || in->pages > INT32_MAX || in->page_rows < 1 || in->page_rows > kAttMaxLen || in->max_pages < 0 || in->max_pages > kAttMaxLen ||
+      in->max_pages * in->page_rows > kAttMaxLen)
+    return fail(c, BBMM_EINVAL, "cache: pages below 2^31, page_rows from 1 to 2^30, max_pages page_rows up to 2^30");
+  if (in->d < 1 || in->d > BBMM_ATT_MAXD || in->dv < 1 || in->dv > BBMM_ATT_MAXD) return fail(c, BBMM_EINVAL, "cache: d and dv from 1 to 128");
+  memset(a, 0, sizeof *a);
+  a->pages = (int)in->pages, a->max_pages = (int)in->max_pages, a->B = (int)in->batch, a->HK = (int)in->kv_heads, a->d = (int)in->d, a->dv = (int)in->dv;
+  a->page = div_by((uint32_t)in->page_rows);
+  a->rows_most = in->max_pages * in->page_rows;
+  if (!pointers) return BBMM_OK;
+  size_t e = elem_size(in->type);
+  bool e4m3 = in->type == BBMM_TYPE_E4M3;
+  if (in->pages && (!in->K || !in->V || (e4m3 && (!in->K_exp || !in->V_exp)))) return fail(c, BBMM_EINVAL, "cache: K and V (and, for E4M3, K_exp and V_exp) are required");
+  if (in->batch && in->max_pages && !in->table) return fail(c, BBMM_EINVAL, "cache: table is required");
+  if (((uintptr_t)in->K | (uintptr_t)in->V | (uintptr_t)in->K_exp | (uintptr_t)in->V_exp) % 16 || (uintptr_t)in->table % 4)
+    return fail(c, BBMM_EINVAL, "cache: K, V and exponents must be 16-byte aligned, the table 4-byte aligned");
+  if (negative(in->k_stride) || negative(in->v_stride)) return fail(c, BBMM_EINVAL, "cache: negative stride");
+  for (int k = 0; k < 3; ++k)
+    if (in->k_stride[k] * e % 16 || in->v_stride[k] * e % 16) return fail(c, BBMM_EINVAL, "cache: rows must start at multiples of 16 bytes");
+  if (in->k_stride[1] >= (int64_t)1 << 21 || in->v_stride[1] >= (int64_t)1 << 21) return fail(c, BBMM_EINVAL, "cache: rows of a page must be less than 2^21 elements apart");
+  a->K = in->K, a->V = in->V, a->ke = in->K_exp, a->ve = in->V_exp, a->table = in->table;
+  memcpy(a->ks, in->k_stride, sizeof a->ks);
+  memcpy(a->vs, in->v_stride, sizeof a->vs);
+  return BBMM_OK;
+}
+
+// The type of rows outside the cache.
+int outside_type(bbmm_ctx* c, const bbmm_cache* cache, int32_t type) {
+  if (type < BBMM_TYPE_F32 || type > BBMM_TYPE_BF16) return fail(c, BBMM_EINVAL, "cache: unknown type of the rows outside");
+  if (cache->type != BBMM_TYPE_E4M3 && cache->type != type) return fail(c, BBMM_EINVAL, "cache: rows outside must be of its own type, unless that is E4M3");
+  return BBMM_OK;
+}
+
+int move_args(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows, const void* K, const void* V, const int32_t* start, const int32_t* n,
+              CacheArgs* a, CacheMove* m) {
+  int rc = cache_args(c, cache, true, a);
+  if (!rc) rc = outside_type(c, cache, type);
+  if (rc) return rc;
+  if (rows < 0 || rows > kAttMaxLen || cache->batch * rows * cache->kv_heads > kMaxRows) return fail(c, BBMM_EINVAL, "cache: more than 2^27 rows in one call");
+  if (cache->batch && rows && (!K || !V)) return fail(c, BBMM_EINVAL, "cache: K and V outside are required");
+  if (((uintptr_t)K | (uintptr_t)V) % elem_size(type) || ((uintptr_t)start | (uintptr_t)n) % 4) return fail(c, BBMM_EINVAL, "cache: pointer not aligned to its type");
+  memset(m, 0, sizeof *m);
+  m->K = K, m->V = V, m->start = start, m->n = n, m->rows = (int)rows;
+  m->by_rows = div_by((uint32_t)std::max<int64_t>(rows, 1)), m->by_heads = div_by((uint32_t)a->HK);
+  return BBMM_OK;
+}
+
+int cache_write(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows, const void* K, const int64_t* k_stride, const void* V,
+                const int64_t* v_stride, const int32_t* start, const int32_t* n_new) {
+  CacheArgs a;
+  CacheMove m;
+  int rc = move_args(c, cache, type, rows, K, V, start, n_new, &a, &m);
+  if (rc) return rc;
+  if (!a.B || !rows || !a.pages) return BBMM_OK;
+  if (!k_stride || !v_stride || negative(k_stride) || negative(v_stride)) return fail(c, BBMM_EINVAL, "cache: strides are required, none negative");
+  memcpy(m.ks, k_stride, sizeof m.ks);
+  memcpy(m.vs, v_stride, sizeof m.vs);
+  m.kvec = whole_pieces(K, m.ks, a.d, elem_size(type)), m.vvec = whole_pieces(V, m.vs, a.dv, elem_size(type));
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  launch_cache_write(c->stream, type, cache->type == BBMM_TYPE_E4M3, a, m);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows, const int32_t* start, const int32_t* length, void* K, void* V) {
+  CacheArgs a;
+  CacheMove m;
+  int rc = move_args(c, cache, type, rows, K, V, start, length, &a, &m);
+  if (rc) return rc;
+  if (!a.B || !rows) return BBMM_OK;
+  m.kvec = whole_pieces(K, nullptr, a.d, elem_size(type)), m.vvec = whole_pieces(V, nullptr, a.dv, elem_size(type));
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  launch_cache_read(c->stream, type, cache->type == BBMM_TYPE_E4M3, a, m);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
+// The keys are split over workgroups while those fill the device less than four times over and parts keep kCachePart keys.
+constexpr int64_t kCachePart = 256;
+// Sizes, the split of the keys, and, where `pointers` is set, everything else.
+int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attention* in, bool pointers, CacheArgs* a, CacheAtt* t) {
+  int rc = cache_args(c, cache, pointers, a);
+  if (rc) return rc;
+  if (!in) return fail(c, BBMM_EINVAL, "cached attention: no description");
+  rc = outside_type(c, cache, in->type);
+  if (rc) return rc;
+  if (in->heads < 1 || in->heads > kAttMaxHeads || in->heads % cache->kv_heads) return fail(c, BBMM_EINVAL, "cached attention: heads up to 65535, kv_heads must divide them");
+  if (in->nq < 0 || in->nq > (int64_t)1 << 20) return fail(c, BBMM_EINVAL, "cached attention: nq up to 2^20");
+  if (in->window < 0) return fail(c, BBMM_EINVAL, "cached attention: window must be >= 0");
+  constexpr double kLog2e = 1.4426950408889634;
+  auto usable = [&](double x) { return x > 0.0 && isfinite((float)(x * kLog2e)) && (float)x > 0.f; };
+  if (!usable(in->scale)) return fail(c, BBMM_EINVAL, "cached attention: scale must be > 0, and finite in units of log 2");
+  if (in->cap != 0.0 && (!usable(in->cap) || !usable(in->scale / in->cap))) return fail(c, BBMM_EINVAL, "cached attention: cap must be 0 or > 0, it and scale / cap finite in units of log 2");
+  memset(t, 0, sizeof *t);
+  t->H = (int)in->heads, t->G = t->H / a->HK, t->nq = (int)in->nq, t->causal = in->causal != 0, t->window = (int)std::min(in->window, kAttMaxLen);
+  t->c2 = (float)(in->scale * kLog2e);
+  if (in->cap != 0.0) t->cap2 = (float)(in->cap * kLog2e), t->cap_in = (float)(in->scale / in->cap);
+  int64_t rows = in->nq * t->G, tile = cache_rows(in->type, rows);
+  t->blocks = (int)((rows + tile - 1) / tile);
+  int64_t wgs = cache->batch * cache->kv_heads * ((rows + 15) / 16);
+  if (cache->batch * in->heads * in->nq > kMaxRows || wgs > kAttMaxGrid) return fail(c, BBMM_EINVAL, "cached attention: more than 2^27 rows in one call");
+  wgs = (int64_t)a->B * a->HK * t->blocks;
+  int64_t reach = t->window ? std::min<int64_t>(a->rows_most, (int64_t)t->window + t->nq) : a->rows_most;
+  int64_t want = 4 * c->num_cus / std::max<int64_t>(wgs, 1), most = (reach + kCachePart - 1) / kCachePart;
+  t->nsplit = (int)std::max<int64_t>(1, std::min(want, most));
+  t->dv4 = (a->dv + 3) / 4 * 4;
+  if (!pointers) return BBMM_OK;
+  size_t e = elem_size(in->type);
+  bool some = a->B && t->nq;
+  if (some && (!in->Q || !in->k_len)) return fail(c, BBMM_EINVAL, "cached attention: Q and k_len are required");
+  if ((uintptr_t)in->Q % e || ((uintptr_t)in->q_len | (uintptr_t)in->k_len) % 4) return fail(c, BBMM_EINVAL, "cached attention: pointer not aligned to its type");
+  if (negative(in->q_stride)) return fail(c, BBMM_EINVAL, "cached attention: negative stride");
+  t->Q = in->Q, t->q_len = in->q_len, t->k_len = in->k_len;
+  memcpy(t->qs, in->q_stride, sizeof t->qs);
+  t->qvec = whole_pieces(t->Q, t->qs, a->d, e);
+  return BBMM_OK;
+}
+
+struct CachedWork {
+  size_t pl, bytes;
+};
+CachedWork cached_work(const CacheArgs& a, const CacheAtt& t) {
+  CachedWork w{};
+  if (t.nsplit > 1) {
+    size_t rows = (size_t)a.B * t.H * t.nq * t.nsplit;
+    w.pl = step256(rows * t.dv4 * sizeof(float));
+    w.bytes = w.pl + step256(rows * sizeof(float));
+  }
+  return w;
+}
+
+int attend_cache(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attention* in, void* O, float* lse, void* work, int64_t work_bytes) {
+  CacheArgs a;
+  CacheAtt t;
+  int rc = cached_args(c, cache, in, true, &a, &t);
+  if (rc) return rc;
+  if (!a.B || !t.nq) return BBMM_OK;
+  size_t e = elem_size(in->type);
+  if (!O || !lse || (uintptr_t)O % e || (uintptr_t)lse % 4) return fail(c, BBMM_EINVAL, "cached attention: O and lse are required, aligned to their type");
+  CachedWork w = cached_work(a, t);
+  rc = check_work(c, work, work_bytes, w.bytes);
+  if (rc) return rc;
+  t.O = O, t.lse = lse, t.pO = (float*)work, t.pl = (float*)((char*)work + w.pl);
+  t.ovec = wide_rows(O, nullptr, a.dv, e, 4 * e);
+  OnDevice dev(c->device);
+  HIPCHK(c, dev.err);
+  launch_attend_cache(c->stream, in->type, cache->type == BBMM_TYPE_E4M3, a, t);
+  if (t.nsplit > 1) launch_attend_cache_join(c->stream, in->type, a, t);
+  HIPCHK(c, hipGetLastError());
+  return BBMM_OK;
+}
+
 // A C entry lets no exception out (the only one is a failed allocation of a message).
 template <typename F>
 int guarded(bbmm_ctx* c, F f) {
@@ -2443,6 +2721,51 @@ int bbmm_bucket_bias_workspace(bbmm_ctx* c, int64_t batch, int64_t heads, int64_
 int bbmm_bucket_bias_grad(bbmm_ctx* c, int32_t type, const void* dB, int64_t batch, int64_t heads, int64_t nq, int64_t nk, int64_t n_edges,
                           const int32_t* edges, int32_t two_sided, int64_t start, void* dtable, void* work, int64_t work_bytes) {
   return guarded(c, [&] { return bucket_bias_grad(c, type, dB, batch, heads, nq, nk, n_edges, edges, two_sided, start, dtable, work, work_bytes); });
+}
+
+int bbmm_rotate(bbmm_ctx* c, const bbmm_rotation* in, void* Qr, void* Kr) {
+  return guarded(c, [&] { return rotate(c, in, Qr, Kr); });
+}
+
+int bbmm_rotate_workspace(bbmm_ctx* c, const bbmm_rotation* in, int64_t* bytes) {
+  return guarded(c, [&] {
+    RotArgs a;
+    int rc = rotation_args(c, in, false, &a);
+    if (rc) return rc;
+    if (!bytes) return fail(c, BBMM_EINVAL, "rotation: bytes is required");
+    *bytes = (int64_t)rotate_work(c, a);
+    return (int)BBMM_OK;
+  });
+}
+
+int bbmm_rotate_grad(bbmm_ctx* c, const bbmm_rotation* in, const void* dQr, const int64_t* dqr_stride, const void* dKr, const int64_t* dkr_stride,
+                     void* dQ, void* dK, void* dq_weight, void* dk_weight, void* work, int64_t work_bytes) {
+  return guarded(c, [&] { return rotate_grad(c, in, dQr, dqr_stride, dKr, dkr_stride, dQ, dK, dq_weight, dk_weight, work, work_bytes); });
+}
+
+int bbmm_cache_write(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows, const void* K, const int64_t* k_stride, const void* V,
+                     const int64_t* v_stride, const int32_t* start, const int32_t* n_new) {
+  return guarded(c, [&] { return cache_write(c, cache, type, rows, K, k_stride, V, v_stride, start, n_new); });
+}
+
+int bbmm_cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows, const int32_t* start, const int32_t* length, void* K, void* V) {
+  return guarded(c, [&] { return cache_read(c, cache, type, rows, start, length, K, V); });
+}
+
+int bbmm_attend_cache_workspace(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attention* in, int64_t* bytes) {
+  return guarded(c, [&] {
+    CacheArgs a;
+    CacheAtt t;
+    int rc = cached_args(c, cache, in, false, &a, &t);
+    if (rc) return rc;
+    if (!bytes) return fail(c, BBMM_EINVAL, "cached attention: bytes is required");
+    *bytes = (int64_t)cached_work(a, t).bytes;
+    return (int)BBMM_OK;
+  });
+}
+
+int bbmm_attend_cache(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attention* in, void* O, float* lse, void* work, int64_t work_bytes) {
+  return guarded(c, [&] { return attend_cache(c, cache, in, O, lse, work, work_bytes); });
 }
 
 }  // extern "C"

@@ -1,0 +1,639 @@
+// Attention of a sequence's new rows over its cached ones (see include/bbmm.h, "Cache"): one pass over the keys with the running reference and
+// sum of the softmax, keys and values read once, straight from their pages into the registers in which the matrix instructions want them.
+//
+// A workgroup takes 16 (or 32) rows (query, head of the group) of one shared head and a part of the keys; its four waves take blocks of 32
+// keys in turn, without barriers, and join at the end.  All products are 16 x 16 blocks: S^T = K Q^T puts a row in a lane and four keys
+// 16 kb + 4 (lane / 16) + r in its registers, which are the second operand of O^T += V^T P^T as they stand.
+//   keys: a lane reads 16 bytes of key 16 kb + lane % 16 at piece 4 s + lane / 16; any order of the features serves that is the queries' too.
+//   values: a lane reads, of the eight keys whose weights it will meet, DP / 16 neighbouring features, 16 lanes a row.  Two-byte values then
+//           change places in pairs (one byte permutation per two values); fp32 values are operands as they stand.  No LDS before the join.
+// 8-bit rows become T on the way, by the instruction that applies their block's power of two.
+#include "cache_dev.h"
+
+using namespace att;
+
+namespace {
+
+template <typename T> struct Mma;
+template <> struct Mma<__bf16> {
+  typedef bf16x8 frag;
+  static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<_Float16> {
+  typedef f16x8 frag;
+  static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<float> {
+  typedef f32x8 frag;
+  static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// Four quarters of a wave.
+__device__ __forceinline__ float quarters_max(float x) {
+  x = both_max(x);
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
+  return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+}
+__device__ __forceinline__ float quarters_sum(float x) {
+  x = both_sum(x);
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
+  return __int_as_float(r[0]) + __int_as_float(r[1]);
+}
+
+// c + a b where a, values, holds infinities or NaN that rows of weight zero must not meet: finite values are multiplied as ever; a column gets
+// an infinity or NaN where its weight for one is not zero.
+template <typename T>
+__device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, typename Mma<T>::frag b, f32x4 c) {
+  const float odd[3] = {__builtin_inff(), -__builtin_inff(), __builtin_nanf("")};
+  typename Mma<T>::frag x = a;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = fabsf((float)a[e]) < __builtin_inff() ? a[e] : (T)0.f;
+  c = Mma<T>::mma(x, b, c);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float y = (float)a[e];
+      x[e] = (k == 2 ? y != y : y == odd[k]) ? (T)1.f : (T)0.f;
+    }
+    f32x4 z = Mma<T>::mma(x, b, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (z[r] != 0.f) c[r] += odd[k];
+  }
+  return c;
+}
+
+constexpr int kBlock = 32;                                 // keys of a wave's turn
+
+// One side (keys or values) of a block on its way: raw registers and the rows' exponents.
+//   T held as such: a piece is 16 bytes (values of up to 64 features in two bytes: 8); E4M3: the same features in a half or a quarter of that.
+template <typename T, bool E4M3, int DP, int NT, bool EVEN>
+__global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a) {
+  typedef Mma<T> M;
+  typedef typename M::frag frag;
+  constexpr int SB = E4M3 ? 1 : (int)sizeof(T);            // bytes of a held element
+  constexpr int ROWS = 16 * NT;
+  constexpr int NS = DP / 32;                              // steps of eight features a lane
+  constexpr int KP = DP * SB / 64;                         // 16-byte pieces of a key per lane
+  constexpr int FV = DP / 16;                              // features of a value per lane
+  constexpr int VW = FV * SB / 4;                          // words of a value per lane
+  constexpr int kPart = ROWS * (DP + 4);
+  __shared__ __align__(16) float buf[2 * kPart];
+  __shared__ float wm[4][ROWS], wl[4][ROWS];
+  int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, q4 = lane >> 4;
+  int x = blockIdx.x, sp = x % a.nsplit, rb = (x / a.nsplit) % a.blocks, bh = x / a.nsplit / a.blocks, hk = bh % c.HK, b = bh / c.HK;
+  int qn = a.q_len ? uniform(min(max(a.q_len[b], 0), a.nq)) : a.nq;
+  int kn = uniform((int)min((int64_t)max(a.k_len[b], 0), c.rows_most));
+  int rows = a.nq * a.G, first = rb * ROWS, i0 = first / a.G, i1 = min(min(first + ROWS, rows) - 1, qn * a.G - 1) / a.G;
+  // keys that some row of these takes: [lo, hi)
+  int64_t p0 = (int64_t)kn - qn + i0, p1 = (int64_t)kn - qn + i1;
+  int lo = a.window ? (int)min(max(p0 - a.window + 1, (int64_t)0), (int64_t)kn) : 0;
+  int hi = a.causal ? (int)max(min(p1 + 1, (int64_t)kn), (int64_t)0) : kn;
+  if (first >= qn * (int64_t)a.G) hi = lo;
+  int b0 = lo / kBlock, b1 = hi > lo ? (hi + kBlock - 1) / kBlock : b0;
+  int per = max((b1 - b0 + a.nsplit - 1) / a.nsplit, 4);
+  int t0 = min(b0 + sp * per, b1), t1 = min(t0 + per, b1);
+
+  const char* K = (const char*)c.K + (int64_t)hk * c.ks[2] * SB;
+  const char* V = (const char*)c.V + (int64_t)hk * c.vs[2] * SB;
+  int64_t kpage = c.ks[0] * SB, vpage = c.vs[0] * SB, epage = (int64_t)c.HK * c.page.d * 4;
+  unsigned kpitch = (unsigned)(c.ks[1] * SB), vpitch = (unsigned)(c.vs[1] * SB);
+  const uint8_t *ke = E4M3 ? c.ke + (int64_t)hk * c.page.d * 4 : nullptr, *ve = E4M3 ? c.ve + (int64_t)hk * c.page.d * 4 : nullptr;
+  const int32_t* __restrict__ table = c.table + (int64_t)b * c.max_pages;
+
+  // ---- pages of a block: EVEN (page rows a multiple of 16): two of them, in scalar registers; else one key a lane
+  struct Pages { int page[2], row[2]; };
+  auto find = [&](int t) {
+    Pages p;
+    if constexpr (EVEN) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t at = (uint32_t)(t * kBlock + 16 * k), n = over(at, c.page);
+        p.row[k] = uniform((int)(at - n * c.page.d));
+        p.page[k] = -1;
+        if (at < (uint32_t)hi) p.page[k] = uniform(table[uniform((int)n)]);
+      }
+    } else {
+      uint32_t at = (uint32_t)(t * kBlock + (lane & 31)), n = over(at, c.page);
+      p.row[0] = (int)(at - n * c.page.d);
+      p.page[0] = at < (uint32_t)hi ? table[n] : -1;
+    }
+    return p;
+  };
+  // keys of a block that take part, before the rows' own bounds
+  auto kept = [&](int t, const Pages& p) {
+    int j0 = t * kBlock;
+    unsigned m = hi - j0 >= kBlock ? ~0u : (1u << (hi - j0)) - 1;
+    if (lo > j0) m &= ~0u << (lo - j0);                    // lo < j0 + 32: blocks begin at lo / 32
+    if constexpr (EVEN) {
+      if ((unsigned)p.page[0] >= (unsigned)c.pages) m &= 0xffff0000u;
+      if ((unsigned)p.page[1] >= (unsigned)c.pages) m &= 0x0000ffffu;
+    } else {
+      m &= (unsigned)__ballot((unsigned)p.page[0] < (unsigned)c.pages);
+    }
+    return m;
+  };
+
+  u32x4 kr[2][KP];
+  unsigned vr[8][VW];
+  unsigned kx[2];                                          // E4M3: exponents of the lane's keys,
+  u32x4 vx[2];                                             // and of its values' rows
+  unsigned koff = (unsigned)col * kpitch, voff = (unsigned)(4 * q4) * vpitch;
+  auto fetch_k = [&](const Pages& p, unsigned keep) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      bool ok = (keep >> (16 * k + col)) & 1;
+      if constexpr (EVEN) {
+        bool there = (keep >> (16 * k)) & 0xffffu;
+        int pg = there ? p.page[k] : 0, row = there ? p.row[k] : 0;
+        __amdgpu_buffer_rsrc_t mem = bounded(K + pg * kpage + (int64_t)row * kpitch, there ? 15 * kpitch + (unsigned)(c.d * SB + 15) / 16 * 16 : 0u);
+#pragma unroll
+        for (int s = 0; s < KP; ++s) {
+          unsigned at = 16u * (4 * s + q4);
+          kr[k][s] = __builtin_amdgcn_raw_buffer_load_b128(mem, ok && at < (unsigned)(c.d * SB) ? koff + at : kNowhere, 0, 0);
+        }
+        if constexpr (E4M3) {
+          __amdgpu_buffer_rsrc_t ex = bounded(ke + pg * epage + (int64_t)row * 4, there ? 64u : 0u);
+          kx[k] = __builtin_amdgcn_raw_buffer_load_b32(ex, 4 * col, 0, 0);
+        }
+      } else {
+        int pg = __shfl(p.page[0], 16 * k + col, 64), row = __shfl(p.row[0], 16 * k + col, 64);
+        const char* at = K + pg * kpage + (int64_t)row * kpitch;
+#pragma unroll
+        for (int s = 0; s < KP; ++s) {
+          int o = 16 * (4 * s + q4);
+          kr[k][s] = u32x4{0u, 0u, 0u, 0u};
+          if (ok && o < c.d * SB) kr[k][s] = *(const u32x4*)(at + o);
+        }
+        if constexpr (E4M3) kx[k] = ok ? *(const unsigned*)(ke + pg * epage + (int64_t)row * 4) : 0u;
+      }
+    }
+  };
+  auto fetch_v = [&](const Pages& p, unsigned keep) {
+    unsigned o = (unsigned)(col * FV * SB);
+    bool mine = o < (unsigned)(c.dv * SB);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if constexpr (EVEN) {
+        bool there = (keep >> (16 * k)) & 0xffffu;
+        int pg = there ? p.page[k] : 0, row = there ? p.row[k] : 0;
+        __amdgpu_buffer_rsrc_t mem = bounded(V + pg * vpage + (int64_t)row * vpitch, there ? 15 * vpitch + (unsigned)(c.dv * SB + 15) / 16 * 16 : 0u);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          unsigned at = mine && ((keep >> (16 * k + 4 * q4 + r)) & 1) ? voff + r * vpitch + o : kNowhere;
+          unsigned* v = vr[4 * k + r];
+          if constexpr (VW == 1) {
+            v[0] = __builtin_amdgcn_raw_buffer_load_b32(mem, at, 0, 0);
+          } else if constexpr (VW == 2) {
+            auto w = __builtin_amdgcn_raw_buffer_load_b64(mem, at, 0, 0);
+            v[0] = w[0], v[1] = w[1];
+          } else if constexpr (VW == 4) {
+            u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, at, 0, 0);
+            v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3];
+          } else {                                         // fp32, 128 features: 4 of each half
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              unsigned f = 256u * z + 16u * col;
+              u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, ((keep >> (16 * k + 4 * q4 + r)) & 1) && f < 4u * c.dv ? voff + r * vpitch + f : kNowhere, 0, 0);
+              v[4 * z] = w[0], v[4 * z + 1] = w[1], v[4 * z + 2] = w[2], v[4 * z + 3] = w[3];
+            }
+          }
+        }
+        if constexpr (E4M3) {                              // (of excluded keys: see add_values)
+          __amdgpu_buffer_rsrc_t ex = bounded(ve + pg * epage + (int64_t)row * 4, there ? 64u : 0u);
+          vx[k] = __builtin_amdgcn_raw_buffer_load_b128(ex, 16 * q4, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          int key = 16 * k + 4 * q4 + r;
+          bool ok = (keep >> key) & 1;
+          int pg = __shfl(p.page[0], key, 64), row = __shfl(p.row[0], key, 64);
+          const char* at = V + pg * vpage + (int64_t)row * vpitch;
+          unsigned* v = vr[4 * k + r];
+#pragma unroll
+          for (int w = 0; w < VW; ++w) v[w] = 0u;
+          if constexpr (VW <= 4) {
+            if (ok && mine) {
+              if constexpr (VW == 1) v[0] = *(const unsigned*)(at + o);
+              else if constexpr (VW == 2) { uint2 w = *(const uint2*)(at + o); v[0] = w.x, v[1] = w.y; }
+              else { u32x4 w = *(const u32x4*)(at + o); v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3]; }
+            }
+          } else {
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+              if (ok && 64 * z + 4 * col < c.dv) {
+                u32x4 w = *(const u32x4*)(at + 256 * z + 16 * col);
+                v[4 * z] = w[0], v[4 * z + 1] = w[1], v[4 * z + 2] = w[2], v[4 * z + 3] = w[3];
+              }
+          }
+          if constexpr (E4M3) vx[k][r] = ok ? *(const unsigned*)(ve + pg * epage + (int64_t)row * 4) : 0u;
+        }
+      }
+    }
+  };
+
+  // Features of a lane's step s of the scores: eight from `feature(s)` on (fp32: four, twice).
+  auto step_at = [&](int s) { return E4M3 ? 16 * (4 * (s >> 1) + q4) + 8 * (s & 1) : 8 * (4 * s + q4); };
+  // fp32 pieces hold four features: step s has pieces 2s, 2s + 1
+  frag qf[NT][NS];
+  int rho[NT], qi[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    rho[n] = first + 16 * n + col;
+    qi[n] = rho[n] / a.G;
+    bool have = rho[n] < rows && qi[n] < qn;
+    const T* row = (const T*)a.Q + b * a.qs[0] + (int64_t)qi[n] * a.qs[1] + (int64_t)(hk * a.G + rho[n] % a.G) * a.qs[2];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      if constexpr (sizeof(T) == 2) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (have) v = load16<T>(row, step_at(s), c.d, a.qvec);
+        qf[n][s] = __builtin_bit_cast(frag, v);
+      } else {
+        int f0 = E4M3 ? step_at(s) : 4 * (8 * s + q4), f1 = E4M3 ? f0 + 4 : 4 * (8 * s + 4 + q4);
+        u32x4 v0 = {0u, 0u, 0u, 0u}, v1 = v0;
+        if (have) {
+          v0 = load16<T>(row, f0, c.d, a.qvec);
+          v1 = load16<T>(row, f1, c.d, a.qvec);
+        }
+        qf[n][s] = __builtin_shufflevector(__builtin_bit_cast(f32x4, v0), __builtin_bit_cast(f32x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    }
+  }
+  // Behind the last feature a piece holds whatever the row's memory does.
+  bool ragged = (c.d * SB) % 16 != 0;
+  unsigned blocks_there = c.d > 96 ? ~0u : (1u << (8 * ((c.d + 31) / 32))) - 1;
+  auto trim = [&] {
+    if constexpr (E4M3) {                                  // nothing times an exponent that nobody wrote
+#pragma unroll
+      for (int k = 0; k < 2; ++k) kx[k] = (kx[k] & blocks_there) | (0x7f7f7f7fu & ~blocks_there);
+    }
+    if (!ragged) return;
+    int last = c.d * SB / 16, left = c.d * SB - 16 * last;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int s = 0; s < KP; ++s)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          int n = min(max(left - 4 * w, 0), 4);
+          if (4 * s + q4 == last) kr[k][s][w] &= n == 4 ? ~0u : (1u << (8 * n)) - 1;
+        }
+  };
+  auto key_frag = [&](int k, int s) {
+    if constexpr (!E4M3) {
+      if constexpr (sizeof(T) == 2) return __builtin_bit_cast(frag, kr[k][s]);
+      else return __builtin_shufflevector(__builtin_bit_cast(f32x4, kr[k][2 * s]), __builtin_bit_cast(f32x4, kr[k][2 * s + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      frag f;
+      float scale = __uint_as_float(((kx[k] >> (8 * (2 * (s >> 1) + (q4 >> 1)))) & 0xffu) << 23);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        unsigned q = kr[k][s >> 1][2 * (s & 1) + w];
+        auto x0 = Wide<T>::template get<false>(q, scale);
+        auto x1 = Wide<T>::template get<true>(q, scale);
+        f[4 * w] = x0[0], f[4 * w + 1] = x0[1], f[4 * w + 2] = x1[0], f[4 * w + 3] = x1[1];
+      }
+      return f;
+    }
+  };
+
+  f32x4 acc[NT][FV];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int f = 0; f < FV; ++f) acc[n][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m[NT], l[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
+
+  // O^T += V^T P^T; s[n][k][r]: weight of row n, key 16 k + 4 q4 + r.  fp32: eight single products make a step, of four keys each.
+  auto add_values = [&](const f32x4 (*p)[2], unsigned keep, bool odd) {
+    frag pf[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[n][e] = (T)p[n][e >> 2][e & 3];
+    auto product = [&](frag v, int f) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if (__builtin_expect(odd, 0)) acc[n][f] = mma_odd<T>(v, pf[n], acc[n][f]);
+        else acc[n][f] = M::mma(v, pf[n], acc[n][f]);
+      }
+    };
+    if constexpr (E4M3) {
+      int shift = 8 * (col * FV / 32);
+      float scale[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) scale[e] = __uint_as_float(((vx[e >> 2][e & 3] >> shift) & 0xffu) << 23);
+      if (keep != ~0u) {                                   // excluded rows are zeros, whatever their exponents hold
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!((keep >> (16 * (e >> 2) + 4 * q4 + (e & 3))) & 1)) scale[e] = 1.f;
+      }
+#pragma unroll
+      for (int w = 0; w < 2 * VW; ++w) {                   // features 2 w, 2 w + 1
+        typename Wide<T>::two x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          x[e] = w & 1 ? Wide<T>::template get<true>(vr[e][w >> 1], scale[e]) : Wide<T>::template get<false>(vr[e][w >> 1], scale[e]);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          frag v;
+          if constexpr (sizeof(T) == 2) {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[e] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, x[2 * e + 1]), __builtin_bit_cast(unsigned, x[2 * e]), f ? 0x07060302u : 0x05040100u);
+            v = __builtin_bit_cast(frag, y);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x[e][f];
+          }
+          product(v, 2 * w + f);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < FV; ++f) {
+        frag v;
+        if constexpr (sizeof(T) == 2) {
+          u32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_perm(vr[2 * e + 1][f >> 1], vr[2 * e][f >> 1], f & 1 ? 0x07060302u : 0x05040100u);
+          v = __builtin_bit_cast(frag, y);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(vr[e][f]);
+        }
+        product(v, f);
+      }
+    }
+  };
+  // Whether the lane's values hold an infinity or NaN.
+  auto odd_values = [&] {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int w = 0; w < VW; ++w) {
+        unsigned y = vr[e][w];
+        if constexpr (E4M3) odd |= (((y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+        else if constexpr (sizeof(T) == 4) odd |= (y & 0x7f800000u) == 0x7f800000u;
+        else {
+          constexpr unsigned m = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+          odd |= (y & m) == m || (y & (m << 16)) == (m << 16);
+        }
+      }
+    return odd;
+  };
+
+  settle();
+  int t = t0 + wave;
+  Pages here{}, next{};
+  unsigned keep = 0;
+  if (t < t1) {
+    here = find(t);
+    next = t + 4 < t1 ? find(t + 4) : here;
+    keep = kept(t, here);
+    fetch_k(here, keep);
+    fetch_v(here, keep);
+  }
+    for (; t < t1; t += 4) {
+    int j0 = t * kBlock;
+    f32x4 s[NT][2];
+    trim();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int z = 0; z < NS; ++z) {
+        frag f = key_frag(k, z);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][k] = M::mma(f, qf[n][z], s[n][k]);
+      }
+    unsigned keep_next = 0;
+    Pages after = next;
+    if (t + 4 < t1) {
+      if (t + 8 < t1) after = find(t + 8);
+      keep_next = kept(t + 4, next);
+      fetch_k(next, keep_next);
+    }
+    // scores in units of the base-2 exponent
+    if (a.cap2 != 0.f) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float y = s[n][e >> 2][e & 3] * a.cap_in;
+          if constexpr (sizeof(T) == 4) {
+            s[n][e >> 2][e & 3] = a.cap2 * tanhf(y);
+          } else {                                         // 1 - 2 / (exp 2y + 1): off by 2^-23 of the cap, nothing beside a weight's rounding to T
+            float z = __builtin_amdgcn_exp2f(y * (2.f * kLog2e));
+            s[n][e >> 2][e & 3] = a.cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(z + 1.f));
+          }
+        }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[n][e >> 2][e & 3] *= a.c2;
+    }
+    // queries that differ in what they take of this block
+    bool edge = i0 != i1 && ((a.causal && j0 + kBlock - 1 > p0) || (a.window && j0 <= p1 - a.window));
+    unsigned mine[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) mine[n] = keep;
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        int64_t p = (int64_t)kn - qn + qi[n] - j0;         // the row's place in the block
+        if (a.causal) mine[n] &= p < 0 ? 0u : p >= 31 ? ~0u : (2u << (int)p) - 1;
+        if (a.window) {
+          int64_t w = p - a.window + 1;                    // the first key
+          mine[n] &= w <= 0 ? ~0u : w >= 32 ? 0u : ~0u << (int)w;
+        }
+      }
+    }
+    if (edge || keep != ~0u) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!((mine[n] >> (16 * (e >> 2) + 4 * q4 + (e & 3))) & 1)) s[n][e >> 2][e & 3] = -__builtin_inff();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float top = s[n][0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, s[n][e >> 2][e & 3]);
+      if (__any(top > m[n] + kSlack)) {
+        top = quarters_max(top);
+        bool move = top > m[n] + kSlack;
+        float up = move ? __builtin_amdgcn_exp2f(m[n] - top) : 1.f;
+        m[n] = move ? top : m[n];
+        l[n] *= up;
+#pragma unroll
+        for (int f = 0; f < FV; ++f) acc[n][f] *= up;
+      }
+      float ref = (m[n] == -__builtin_inff() ? 0.f : m[n]) - Lift<T>::value;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float y = __builtin_amdgcn_exp2f(s[n][e >> 2][e & 3] - ref);
+        s[n][e >> 2][e & 3] = y;
+        l[n] += y;
+      }
+    }
+    // infinities and NaN among the values of keys that only some of the rows take (an 8-bit value may become infinite in fp16 as well)
+    add_values(s, keep, edge && (__any(odd_values()) || (E4M3 && __is_same(T, _Float16))));
+    if (t + 4 < t1) fetch_v(next, keep_next);
+    here = next;
+    next = after;
+    keep = keep_next;
+  }
+
+  // the waves' sums: each scales its own to the largest reference; two leave theirs in LDS, the other two add them, all write
+  float top[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    l[n] = quarters_sum(l[n]);
+    if (q4 == 0) {
+      wm[wave][16 * n + col] = m[n];
+      wl[wave][16 * n + col] = l[n];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    int r = 16 * n + col;
+    top[n] = fmaxf(fmaxf(wm[0][r], wm[1][r]), fmaxf(wm[2][r], wm[3][r]));
+    float w = m[n] == -__builtin_inff() && l[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[n] - top[n]);
+#pragma unroll
+    for (int f = 0; f < FV; ++f) acc[n][f] *= w;
+  }
+  // feature of acc[.][f][r]: two bytes: FV (4 q4 + r) + f;  fp32: 64 (f / 4) + 4 (4 q4 + r) + f % 4
+  auto spot = [&](int n, int f, int r) {
+    int at = sizeof(T) == 2 || E4M3 ? FV * (4 * q4 + r) + f : 64 * (f >> 2) + 4 * (4 * q4 + r);
+    return buf + (wave & 1) * kPart + (16 * n + col) * (DP + 4) + at;
+  };
+  auto each = [&](auto act) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int f = 0; f < FV; f += 4)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) act((f32x4*)spot(n, f, r), f32x4{acc[n][f][r], acc[n][f + 1][r], acc[n][f + 2][r], acc[n][f + 3][r]});
+  };
+  if (wave >= 2) each([](f32x4* p, f32x4 v) { *p = v; });
+  __syncthreads();
+  if (wave < 2) each([](f32x4* p, f32x4 v) { *p += v; });
+  __syncthreads();
+  constexpr int TR = 256 / ROWS;                           // threads of a row
+  int row = tid / TR, rr = first + row, i = rr / a.G, h = hk * a.G + rr % a.G;
+  if (rr >= rows) return;
+  float best = fmaxf(fmaxf(wm[0][row], wm[1][row]), fmaxf(wm[2][row], wm[3][row])), sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum += wm[k][row] == -__builtin_inff() && wl[k][row] == 0.f ? 0.f : __builtin_amdgcn_exp2f(wm[k][row] - best) * wl[k][row];
+  bool some = sum != 0.f && i < qn;                        // NaN counts as something
+  float inv = some ? 1.f / sum : 0.f;
+  float lse2 = some ? (best - Lift<T>::value) + __builtin_amdgcn_logf(sum) : -__builtin_inff();
+  size_t at = ((size_t)b * a.H + h) * a.nq + i, n = (size_t)c.B * a.H * a.nq;
+  if (tid % TR == 0) {
+    if (a.nsplit == 1) a.lse[at] = lse2 * kLn2;
+    else a.pl[sp * n + at] = lse2;
+  }
+  if (a.nsplit > 1 && !some) return;                       // parts without weight are not read
+  const float* src = buf + row * (DP + 4);
+  T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
+  for (int f = tid % TR * 4; f < DP; f += 4 * TR) {
+    f32x4 y = (*(const f32x4*)(src + f) + *(const f32x4*)(src + kPart + f)) * inv;
+    if (!some) y = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (a.nsplit == 1) store4<T>(out, f, c.dv, a.ovec, y[0], y[1], y[2], y[3]);
+    else if (f < a.dv4) *(f32x4*)(a.pO + (sp * n + at) * a.dv4 + f) = y;
+  }
+}
+
+// Parts of a row joined by their log sums: 32 lanes a row, four features a lane; parts without weight are not read.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt a) {
+  int64_t n = (int64_t)c.B * a.H * a.nq, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  int lane = threadIdx.x & 31, f = 4 * lane;
+  if (row >= n) return;
+  float top = -__builtin_inff();
+  for (int s = lane; s < a.nsplit; s += 32) top = fmaxf(top, a.pl[s * n + row]);
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 32));
+  float sum = 0.f;
+  f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
+    float p[8];
+    f32x4 v[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) p[s] = s0 + s < a.nsplit ? a.pl[(s0 + s) * n + row] : -__builtin_inff();
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      v[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (p[s] != -__builtin_inff() && f < a.dv4) v[s] = *(const f32x4*)(a.pO + ((s0 + s) * n + row) * a.dv4 + f);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      float w = p[s] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(p[s] - top);
+      sum += w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(w, v[s][e], y[e]);
+    }
+  }
+  bool some = sum != 0.f;
+  float inv = some ? 1.f / sum : 0.f;
+  if (lane == 0) a.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+  int i = (int)(row % a.nq), h = (int)(row / a.nq % a.H), b = (int)(row / a.nq / a.H);
+  T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
+  store4<T>(out, f, c.dv, a.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+}
+
+template <typename T, bool E4M3, int DP, int NT>
+void attend_n(hipStream_t s, const CacheArgs& c, const CacheAtt& a) {
+  unsigned grid = (unsigned)((int64_t)c.B * c.HK * a.blocks * a.nsplit);
+  if (c.page.d % 16 == 0) k_attend_cache<T, E4M3, DP, NT, true><<<grid, 256, 0, s>>>(c, a);
+  else k_attend_cache<T, E4M3, DP, NT, false><<<grid, 256, 0, s>>>(c, a);
+}
+template <typename T, bool E4M3, int DP>
+void attend_d(hipStream_t s, int type, const CacheArgs& c, const CacheAtt& a) {
+  if constexpr (sizeof(T) == 2) {
+    if (cache_rows(type, (int64_t)a.nq * a.G) == 32) return attend_n<T, E4M3, DP, 2>(s, c, a);
+  }
+  attend_n<T, E4M3, DP, 1>(s, c, a);
+}
+template <typename T, bool E4M3>
+void attend_e(hipStream_t s, int type, const CacheArgs& c, const CacheAtt& a) {
+  if (c.d <= 64 && c.dv <= 64) attend_d<T, E4M3, 64>(s, type, c, a);
+  else attend_d<T, E4M3, 128>(s, type, c, a);
+}
+template <typename T>
+void attend_t(hipStream_t s, int type, int e4m3, const CacheArgs& c, const CacheAtt& a) {
+  if (e4m3) attend_e<T, true>(s, type, c, a);
+  else attend_e<T, false>(s, type, c, a);
+}
+
+}  // namespace
+
+int cache_rows(int type, int64_t rows) { return type != 0 && rows > 16 ? 32 : 16; }
+
+void launch_attend_cache(hipStream_t s, int type, int e4m3, const CacheArgs& c, const CacheAtt& a) {
+  if (type == 0) attend_t<float>(s, type, e4m3, c, a);
+  else if (type == 1) attend_t<_Float16>(s, type, e4m3, c, a);
+  else attend_t<__bf16>(s, type, e4m3, c, a);
+}
+void launch_attend_cache_join(hipStream_t s, int type, const CacheArgs& c, const CacheAtt& a) {
+  unsigned grid = (unsigned)(((int64_t)c.B * a.H * a.nq + 7) / 8);
+  if (type == 0) k_attend_cache_join<float><<<grid, 256, 0, s>>>(c, a);
+  else if (type == 1) k_attend_cache_join<_Float16><<<grid, 256, 0, s>>>(c, a);
+  else k_attend_cache_join<__bf16><<<grid, 256, 0, s>>>(c, a);
+}

@@ -1,0 +1,415 @@
+// Norm and rotation of queries and keys, and its gradient (see include/bbmm.h, "Rotation").
+//
+//   z = w n,  n = r x,  r = (mean x^2 + eps)^-1/2;   y = R z, R a turn of every pair by its angle
+//   dz = R^T dy;  dw = sum dz n;  dx = r (w dz - n mean(w dz n))
+// A few lanes take a row: each holds two pieces of it whose pairs are complete, so a turn stays in the lane and the row's sums cross
+// the few lanes only.  Cosines and sines are formed once per (token, pair) of a workgroup and serve all heads.  Workgroups work on one of Q and K.
+// Bound by memory: rows are read and written once.
+#include "cache_dev.h"
+
+using namespace att;
+
+namespace {
+
+// cos and sin of pos freq.  The angle is formed and taken modulo a turn in 64 bits: fp32 holds positions of 10^5 to 10^-2.
+__device__ __forceinline__ float2 turn_of(int64_t pos, double freq) {
+  constexpr double kTurns = 0.15915494309189533577;       // 1 / (2 pi)
+  double t = (double)pos * freq * kTurns;
+  t -= rint(t);
+  float s, c;
+  sincospif((float)(t + t), &s, &c);
+  return make_float2(c, s);
+}
+
+// Sum (or maximum) over the LPR lanes of a row, LPR a power of two up to 16: neighbours, pairs of them, and mirrors, which meet the other half's
+// result in any lane.
+template <int C> __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), C, 0xf, 0xf, true)); }
+template <int LPR, typename F>
+__device__ __forceinline__ float across(float x, F f) {
+  if constexpr (LPR >= 2) x = f(x, dpp<0xb1>(x));          // quad_perm 1 0 3 2
+  if constexpr (LPR >= 4) x = f(x, dpp<0x4e>(x));          // quad_perm 2 3 0 1
+  if constexpr (LPR >= 8) x = f(x, dpp<0x141>(x));         // mirror of eight
+  if constexpr (LPR >= 16) x = f(x, dpp<0x140>(x));        // mirror of sixteen
+  return x;
+}
+template <int LPR> __device__ __forceinline__ float row_sum(float x) { return across<LPR>(x, [](float a, float b) { return a + b; }); }
+template <int LPR> __device__ __forceinline__ float row_max(float x) { return across<LPR>(x, [](float a, float b) { return fmaxf(a, b); }); }
+
+// How a row is dealt out: E elements a piece (16 bytes, or 1), slot j = lane + LPR k holds two pieces.
+//   halves: j < rot / 2E holds pieces j and j + rot / 2E (turned); behind, 2j and 2j + 1;  neighbours: 2j and 2j + 1 (turned below rot).
+template <typename T, int E, int LPR, int KS>
+struct Row {
+  static constexpr int N = 2 * E;
+  typedef unsigned word;
+  struct Raw { u32x4 v[E > 1 ? 2 * KS : 1]; T e[E > 1 ? 1 : 2 * KS]; };
+  int p0[KS], p1[KS];                                       // first elements of the two pieces
+  int pair0[KS];                                            // the slot's first pair
+  int d, half;
+  bool nb;
+  __device__ __forceinline__ Row(const RotArgs& a, int lane) {
+    d = a.d, half = a.rot >> 1, nb = a.neighbours;
+    int h = half / E;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      int j = lane + LPR * k;
+      bool split = !nb && j < h;
+      p0[k] = split ? j * E : 2 * j * E;
+      p1[k] = split ? (j + h) * E : (2 * j + 1) * E;
+      pair0[k] = j * E;
+    }
+  }
+  __device__ __forceinline__ void load(Raw& r, const T* row, bool have) const {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      if constexpr (E > 1) {
+        r.v[2 * k] = r.v[2 * k + 1] = u32x4{0u, 0u, 0u, 0u};
+        if (have && p0[k] < d) r.v[2 * k] = *(const u32x4*)(row + p0[k]);
+        if (have && p1[k] < d) r.v[2 * k + 1] = *(const u32x4*)(row + p1[k]);
+      } else {
+        r.e[2 * k] = r.e[2 * k + 1] = (T)0.f;
+        if (have && p0[k] < d) r.e[2 * k] = row[p0[k]];
+        if (have && p1[k] < d) r.e[2 * k + 1] = row[p1[k]];
+      }
+    }
+  }
+  // element i < 2E of slot k
+  __device__ __forceinline__ static float at(const Raw& r, int k, int i) {
+    if constexpr (E > 1) return (float)reinterpret_cast<const T*>(&r.v[2 * k + i / E])[i % E];
+    else return (float)r.e[2 * k + i];
+  }
+  __device__ __forceinline__ void weights(float* w, const T* p) const {      // ones without weights
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        int c = (i < E ? p0[k] : p1[k]) + i % E;
+        w[k * N + i] = !p ? 1.f : c < d ? (float)p[c] : 0.f;
+      }
+  }
+  __device__ __forceinline__ void store(T* row, const float* y) const {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        int c = x ? p1[k] : p0[k];
+        if (c >= d) continue;
+        if constexpr (E > 1) {
+          u32x4 v;
+          T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+          for (int i = 0; i < E; ++i) e[i] = (T)y[k * N + x * E + i];
+          *(u32x4*)(row + c) = v;
+        } else {
+          row[c] = (T)y[k * N + x];
+        }
+      }
+  }
+  // The slot's pairs turned by trig (back: the other way round).
+  __device__ __forceinline__ void turn(float* y, const float2* trig, bool back) const {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      float* v = y + k * N;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        int p = pair0[k] + i;
+        if (p >= half) continue;
+        float2 t = trig[p];
+        if (back) t.y = -t.y;
+        if (E > 1 && nb) {
+          float u = v[2 * i], w = v[2 * i + 1];
+          v[2 * i] = u * t.x - w * t.y;
+          v[2 * i + 1] = w * t.x + u * t.y;
+        } else {
+          float u = v[i], w = v[E + i];
+          v[i] = u * t.x - w * t.y;
+          v[E + i] = w * t.x + u * t.y;
+        }
+      }
+    }
+  }
+};
+
+// n = r x of a row in place, and r.  Squares that leave fp32 (or lose bits near its smallest numbers) are formed of scaled values instead.
+template <int LPR, int M>
+__device__ __forceinline__ float norm_row(float* x, int d, double eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < M; ++i) s = fmaf(x[i], x[i], s);
+  s = row_sum<LPR>(s);
+  float mean = fmaf(s, 1.f / (float)d, (float)eps), r = rsqrtf(mean), scale = 1.f;
+  bool lost = !(s < 1e37f) || mean < 1e-27f;
+  if (__any(lost)) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < M; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = row_max<LPR>(top);
+    int e = top > 0.f && top < __builtin_inff() ? ilogbf(top) : 0;
+    if (eps > 0.0) e = max(e, ilogb(eps) / 2);               // beside eps smaller squares are nothing
+    e = min(max(e, -126), 126);
+    float down = ldexpf(1.f, -e), q = 0.f;
+#pragma unroll
+    for (int i = 0; i < M; ++i) q = fmaf(x[i] * down, x[i] * down, q);
+    q = row_sum<LPR>(q);
+    if (lost) {
+      scale = down;
+      r = 1.f / sqrtf(fmaf(q, 1.f / (float)d, (float)(eps * down * down)));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < M; ++i) x[i] = x[i] * scale * r;
+  return scale * r;
+}
+
+template <typename T>
+__device__ __forceinline__ void token_row(const RotArgs& a, uint32_t tok, int h, const T* x, const int64_t* s, const T** row, bool* live) {
+  uint32_t b = over(tok, a.by_rows);
+  int i = (int)(tok - b * (uint32_t)a.rows);
+  *live = !a.len || i < a.len[b];
+  *row = x + (int64_t)b * s[0] + (int64_t)i * s[1] + (int64_t)h * s[2];
+}
+
+__device__ __forceinline__ void fill_trig(const RotArgs& a, float2* trig, int64_t tok0, int n, int tid) {
+  int half = a.rot >> 1;
+  for (int i = tid; i < n * half; i += 256) {
+    int t = i / half, p = i - t * half;
+    if (tok0 + t < a.tokens) trig[t * (BBMM_ATT_MAXD / 2) + p] = turn_of(a.pos[(int64_t)a.axis[p] * a.tokens + tok0 + t], a.freq[p]);
+  }
+}
+
+// Rows of the workgroup's tokens, groups of LPR lanes a row, U rows of a group in hand at a time.
+template <typename T, int E, int LPR, int KS, int U>
+__global__ __launch_bounds__(256) void k_rotate(RotArgs a) {
+  typedef Row<T, E, LPR, KS> Rows;
+  constexpr int GP = 256 / LPR, M = Rows::N * KS;
+  __shared__ float2 trig[BBMM_ROT_TOKENS * (BBMM_ATT_MAXD / 2)];
+  int tid = threadIdx.x, which = blockIdx.x >= (unsigned)a.blocks[0];
+  int blk = blockIdx.x - (which ? a.blocks[0] : 0), per = a.tokens_per[which];
+  Rows rows(a, tid % LPR);
+  const T* x = (const T*)a.x[which];
+  T* y = (T*)a.y[which];
+  float w[M];
+  if (a.norm) rows.weights(w, (const T*)a.w[which]);
+  for (int64_t tok0 = (int64_t)blk * per; tok0 < a.tokens; tok0 += (int64_t)a.blocks[which] * per) {
+    int n = (int)min((int64_t)per, a.tokens - tok0) * a.heads[which];
+    typename Rows::Raw raw[U];
+    bool live[U];
+    auto load = [&](int r0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        int r = r0 + u * GP;
+        live[u] = false;
+        if (r < n) {
+          uint32_t t = over(r, a.by_heads[which]);
+          const T* row;
+          token_row(a, (uint32_t)tok0 + t, r - (int)t * a.heads[which], x, a.xs[which], &row, &live[u]);
+          rows.load(raw[u], row, live[u]);
+        }
+      }
+    };
+    int r0 = tid / LPR;
+    load(r0);                                              // on their way while the angles are formed
+    fill_trig(a, trig, tok0, per, tid);
+    __syncthreads();
+    for (;;) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        int r = r0 + u * GP;
+        if (r >= n) break;
+        float v[M];
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = live[u] ? Rows::at(raw[u], k, i) : 0.f;
+        if (live[u]) {
+          if (a.norm) {
+            norm_row<LPR, M>(v, a.d, a.eps);
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] *= w[i];
+          }
+          rows.turn(v, trig + over(r, a.by_heads[which]) * (BBMM_ATT_MAXD / 2), false);
+        }
+        rows.store(y + ((tok0 * a.heads[which]) + r) * a.d, v);
+      }
+      r0 += U * GP;
+      if (r0 - tid / LPR >= n) break;
+      load(r0);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, int E, int LPR, int KS, int U>
+__global__ __launch_bounds__(256) void k_rotate_grad(RotArgs a) {
+  typedef Row<T, E, LPR, KS> Rows;
+  constexpr int GP = 256 / LPR, M = Rows::N * KS;
+  __shared__ float2 trig[BBMM_ROT_TOKENS * (BBMM_ATT_MAXD / 2)];
+  __shared__ float sums[4][BBMM_ATT_MAXD];
+  int tid = threadIdx.x, which = blockIdx.x >= (unsigned)a.blocks[0];
+  int blk = blockIdx.x - (which ? a.blocks[0] : 0), per = a.tokens_per[which];
+  Rows rows(a, tid % LPR);
+  const T *x = (const T*)a.x[which], *g = (const T*)a.g[which];
+  T* dx = (T*)a.y[which];
+  float w[M], dw[M];
+  if (a.norm) rows.weights(w, (const T*)a.w[which]);
+#pragma unroll
+  for (int i = 0; i < M; ++i) dw[i] = 0.f;
+  for (int64_t tok0 = (int64_t)blk * per; tok0 < a.tokens; tok0 += (int64_t)a.blocks[which] * per) {
+    int n = (int)min((int64_t)per, a.tokens - tok0) * a.heads[which];
+    typename Rows::Raw rx[U], rg[U];
+    bool live[U];
+    auto load = [&](int r0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        int r = r0 + u * GP;
+        live[u] = false;
+        if (r < n) {
+          uint32_t t = over(r, a.by_heads[which]);
+          const T* row;
+          token_row(a, (uint32_t)tok0 + t, r - (int)t * a.heads[which], g, a.gs[which], &row, &live[u]);
+          rows.load(rg[u], row, live[u]);
+          if (a.norm) {
+            token_row(a, (uint32_t)tok0 + t, r - (int)t * a.heads[which], x, a.xs[which], &row, &live[u]);
+            rows.load(rx[u], row, live[u]);
+          }
+        }
+      }
+    };
+    int r0 = tid / LPR;
+    load(r0);
+    fill_trig(a, trig, tok0, per, tid);
+    __syncthreads();
+    for (;;) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        int r = r0 + u * GP;
+        if (r >= n) break;
+        float v[M];
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = live[u] ? Rows::at(rg[u], k, i) : 0.f;
+        if (live[u]) {
+          rows.turn(v, trig + over(r, a.by_heads[which]) * (BBMM_ATT_MAXD / 2), true);
+          if (a.norm) {
+            float nx[M];
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+              for (int i = 0; i < Rows::N; ++i) nx[k * Rows::N + i] = Rows::at(rx[u], k, i);
+            float rr = norm_row<LPR, M>(nx, a.d, a.eps), dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+              dw[i] = fmaf(v[i], nx[i], dw[i]);
+              v[i] *= w[i];
+              dot = fmaf(v[i], nx[i], dot);
+            }
+            dot = row_sum<LPR>(dot) * (1.f / (float)a.d);
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] = rr * fmaf(-nx[i], dot, v[i]);
+          }
+        }
+        rows.store(dx + ((tok0 * a.heads[which]) + r) * a.d, v);
+      }
+      r0 += U * GP;
+      if (r0 - tid / LPR >= n) break;
+      load(r0);
+    }
+    __syncthreads();
+  }
+  if (!a.w[which]) return;
+  // the workgroup's sums: over the rows of a wave, then over the waves
+  for (int i = tid; i < 4 * BBMM_ATT_MAXD; i += 256) (&sums[0][0])[i] = 0.f;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+#pragma unroll
+    for (int s = LPR; s < 64; s *= 2) dw[i] += __shfl_xor(dw[i], s, 64);
+  if ((tid & 63) < LPR) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < Rows::N; ++i) {
+        int c = (i < E ? rows.p0[k] : rows.p1[k]) + i % E;
+        if (c < a.d) sums[tid >> 6][c] = dw[k * Rows::N + i];
+      }
+  }
+  __syncthreads();
+  for (int c = tid; c < a.d; c += 256) ((float*)a.w_part)[(size_t)blockIdx.x * a.d + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+}
+
+// The weights' gradients from the workgroups' sums: 16 features a workgroup, 16 threads a feature's parts, in 64 bits and a fixed order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_rotate_join(RotArgs a, T* dq, T* dk, int tiles) {
+  __shared__ double part[16][17];
+  int which = blockIdx.x >= (unsigned)tiles, c = (blockIdx.x - (which ? tiles : 0)) * 16 + (threadIdx.x & 15), p0 = threadIdx.x >> 4;
+  const float* src = (const float*)a.w_part + (which ? (size_t)a.blocks[0] * a.d : 0);
+  T* out = which ? dk : dq;
+  if (!out) return;
+  double s = 0.0;
+  if (c < a.d) {
+#pragma unroll 8
+    for (int p = p0; p < a.blocks[which]; p += 16) s += (double)src[(size_t)p * a.d + c];
+  }
+  part[p0][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (threadIdx.x < 16 && c < a.d) {
+    for (int p = 1; p < 16; ++p) s += part[p][threadIdx.x];
+    out[c] = (T)(float)s;
+  }
+}
+
+// 16-byte pieces: lanes of a row for features up to 32, 64, 128; else single elements, 16 lanes and four slots each.
+template <typename T, int U, typename F>
+void rotate_shape(const RotArgs& a, F f) {
+  constexpr int E = 16 / (int)sizeof(T);
+  if (!a.vec) f(Const<1>{}, Const<16>{}, Const<4>{}, Const<(U > 2 ? 2 : 1)>{});
+  else if (a.d <= 32) f(Const<E>{}, Const<16 / E>{}, Const<1>{}, Const<U>{});
+  else if (a.d <= 64) f(Const<E>{}, Const<32 / E>{}, Const<1>{}, Const<U>{});
+  else f(Const<E>{}, Const<64 / E>{}, Const<1>{}, Const<U>{});
+}
+constexpr int kFwd = 4, kBwd = 2;            // rows of a group in hand
+
+template <typename T>
+void rotate_t(hipStream_t s, const RotArgs& a) {
+  rotate_shape<T, kFwd>(a, [&](auto e, auto l, auto k, auto u) {
+    k_rotate<T, decltype(e)::value, decltype(l)::value, decltype(k)::value, decltype(u)::value><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+  });
+}
+template <typename T>
+void rotate_grad_t(hipStream_t s, const RotArgs& a) {
+  rotate_shape<T, kBwd>(a, [&](auto e, auto l, auto k, auto u) {
+    k_rotate_grad<T, decltype(e)::value, decltype(l)::value, decltype(k)::value, decltype(u)::value><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+  });
+}
+template <typename T>
+void rotate_join_t(hipStream_t s, const RotArgs& a, void* dq, void* dk) {
+  int tiles = (a.d + 15) / 16;
+  k_rotate_join<T><<<2 * tiles, 256, 0, s>>>(a, (T*)dq, (T*)dk, tiles);
+}
+
+}  // namespace
+
+int rotate_rows(int type, bool grad, int d, int vec) {
+  int n = 0;
+  RotArgs a{};
+  a.d = d, a.vec = vec;
+  auto f = [&](auto, auto l, auto, auto u) { n = 256 / decltype(l)::value * decltype(u)::value; };
+  if (type == 0) grad ? rotate_shape<float, kBwd>(a, f) : rotate_shape<float, kFwd>(a, f);
+  else grad ? rotate_shape<__bf16, kBwd>(a, f) : rotate_shape<__bf16, kFwd>(a, f);
+  return n;
+}
+void launch_rotate(hipStream_t s, int type, const RotArgs& a) {
+  if (type == 0) rotate_t<float>(s, a);
+  else if (type == 1) rotate_t<_Float16>(s, a);
+  else rotate_t<__bf16>(s, a);
+}
+void launch_rotate_grad(hipStream_t s, int type, const RotArgs& a) {
+  if (type == 0) rotate_grad_t<float>(s, a);
+  else if (type == 1) rotate_grad_t<_Float16>(s, a);
+  else rotate_grad_t<__bf16>(s, a);
+}
+void launch_rotate_join(hipStream_t s, int type, const RotArgs& a, void* dq_weight, void* dk_weight) {
+  if (type == 0) rotate_join_t<float>(s, a, dq_weight, dk_weight);
+  else if (type == 1) rotate_join_t<_Float16>(s, a, dq_weight, dk_weight);
+  else rotate_join_t<__bf16>(s, a, dq_weight, dk_weight);
+}
