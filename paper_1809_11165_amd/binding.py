@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from array import array
 from dataclasses import dataclass, field
 from typing import Optional
@@ -84,6 +85,7 @@ class _Rotation(C.Structure):
                 ("rot", C.c_int64), ("Q", C.c_void_p), ("K", C.c_void_p), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
                 ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("pos", C.c_void_p), ("axis", C.c_char_p), ("freq", C.c_void_p),
                 ("len", C.c_void_p)]
+    pack = struct.Struct("4id6q2P6q6P").pack      # a filled one by from_buffer_copy: a tenth of the constructor's time
 
 
 class _Cache(C.Structure):
@@ -91,12 +93,14 @@ class _Cache(C.Structure):
                 ("d", C.c_int64), ("dv", C.c_int64), ("batch", C.c_int64), ("max_pages", C.c_int64), ("K", C.c_void_p), ("V", C.c_void_p),
                 ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p),
                 ("table", C.c_void_p)]
+    pack = struct.Struct("2i7q2P6q3P").pack
 
 
 class _CachedAttention(C.Structure):
     _fields_ = [("type", C.c_int32), ("causal", C.c_int32), ("heads", C.c_int64), ("nq", C.c_int64), ("window", C.c_int64),
                 ("scale", C.c_double), ("cap", C.c_double), ("Q", C.c_void_p), ("q_stride", C.c_int64 * 3), ("q_len", C.c_void_p),
                 ("k_len", C.c_void_p)]
+    pack = struct.Struct("2i3q2dP3q2P").pack
 
 
 _lib = None
@@ -414,57 +418,78 @@ class Rotation:
 
     def to_c(self, device) -> _Rotation:
         Q, K, pos, freq = self.Q, self.K, self.pos, self.freq
-        one = Q if Q is not None else K
+        one, name = (Q, "Q") if Q is not None else (K, "K")
         if one is None:
             raise ValueError("Q or K is required")
-        code, t = _type_of(one, "Q" if Q is not None else "K"), one.dtype
-        if one.dim() != 4:
-            raise ValueError("Q and K must have four dimensions (batch, row, head, feature)")
-        b, rows, _, d = one.shape
-        r = _Rotation(code, bool(self.neighbours), self.eps is not None, 1, self.eps or 0.0, b, rows, 0, 0, d, 0)
-        for x, name in ((Q, "Q"), (K, "K")):
-            if x is None:
-                continue
-            if getattr(x, "ndim", 4) != 4:
-                raise ValueError("%s must have four dimensions (batch, row, head, feature)" % name)
-            _check_same(x, (b, rows, x.shape[2], d) if hasattr(x, "shape") else (), t, device, name, dense=False)
-        if Q is not None:
-            r.Q, r.q_heads, r.q_stride = Q.data_ptr(), Q.shape[2], Q.stride()[:3]
-        if K is not None:
-            r.K, r.k_heads, r.k_stride = K.data_ptr(), K.shape[2], K.stride()[:3]
-        double, int64, int32 = _rotation_types()
-        half = 0
+        code, t = _type_of(one, name), one.dtype
+        try:
+            b, rows, qh, d = one.shape
+            qp = kp = kh = 0
+            qs = ks = _NO_STRIDE
+            if K is not None:
+                _, _, kh, _ = K.shape
+                _check_same(K, (b, rows, kh, d), t, device, "K", dense=False)
+                kp, ks = K.data_ptr(), K.stride()
+            if Q is None:
+                qh = 0
+            else:
+                _check_same(Q, (b, rows, qh, d), t, device, "Q", dense=False)
+                qp, qs = Q.data_ptr(), Q.stride()
+        except ValueError as e:
+            if "unpack" in str(e):
+                raise ValueError("Q and K must have four dimensions (batch, row, head, feature)") from None
+            raise
+        except AttributeError:
+            raise TypeError("Q and K must be tensors") from None
+        float64, int64, int32, _, _ = _others()
+        half = fp = pp = qw = kw = lp = ap = 0
+        axes, axis = 1, None
         if freq is not None:
-            half = freq.shape[0] if getattr(freq, "ndim", 0) == 1 else 0
-            _check_same(freq, (half,), double, device, "freq")
-            if half:
-                r.rot, r.freq = 2 * half, freq.data_ptr()
+            half = len(freq)
+            _check_same(freq, (half,), float64, device, "freq")
+            fp = freq.data_ptr()
         if pos is not None:
-            r.n_axes = pos.shape[0] if getattr(pos, "ndim", 0) == 3 else 1
-            _check_same(pos, (r.n_axes, b, rows) if getattr(pos, "ndim", 0) == 3 else (b, rows), int64, device, "pos")
-            r.pos = pos.data_ptr()
+            if pos.ndim == 3:
+                axes = pos.shape[0]
+                _check_same(pos, (axes, b, rows), int64, device, "pos")
+            else:
+                _check_same(pos, (b, rows), int64, device, "pos")
+            pp = pos.data_ptr()
         if self.axis is not None:
             try:
-                r.axis = bytes(self.axis)
+                axis = array("B", bytes(self.axis))
             except (ValueError, TypeError):
                 raise ValueError("axis must hold whole numbers of axes") from None
-            if len(self.axis) != half:
-                raise ValueError("axis has %d entries, expected %d" % (len(self.axis), half))
+            if len(axis) != half:
+                raise ValueError("axis has %d entries, expected %d" % (len(axis), half))
+            ap = axis.buffer_info()[0]
         if self.q_weight is not None:
             _check_same(self.q_weight, (d,), t, device, "q_weight")
-            r.q_weight = self.q_weight.data_ptr()
+            qw = self.q_weight.data_ptr()
         if self.k_weight is not None:
             _check_same(self.k_weight, (d,), t, device, "k_weight")
-            r.k_weight = self.k_weight.data_ptr()
+            kw = self.k_weight.data_ptr()
         if self.row_len is not None:
             _check_same(self.row_len, (b,), int32, device, "row_len")
-            r.len = self.row_len.data_ptr()
+            lp = self.row_len.data_ptr()
+        norm = self.eps is not None
+        r = _Rotation.from_buffer_copy(_Rotation.pack(code, bool(self.neighbours), norm, axes, self.eps if norm else 0.0, b, rows, qh, kh, d, 2 * half,
+                                                      qp, kp, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], qw, kw, pp, ap, fp, lp))
+        r.keep = axis
         return r
 
 
-def _rotation_types():
-    import torch
-    return torch.float64, torch.int64, torch.int32
+_NO_STRIDE = (0, 0, 0, 0)
+_other_types = ()
+
+
+def _others():
+    """float64, int64, int32, uint8 and the 8-bit float of torch."""
+    global _other_types
+    if not _other_types:
+        import torch
+        _other_types = (torch.float64, torch.int64, torch.int32, torch.uint8, torch.float8_e4m3fn)
+    return _other_types
 
 
 @dataclass
@@ -501,8 +526,9 @@ class Cache:
 
     def to_c(self, device) -> _Cache:
         K, V, table = self.K, self.V, self.table
+        _, _, int32, uint8, float8 = _others()
         t = getattr(K, "dtype", None)
-        e4m3 = t is not None and t is _float8()
+        e4m3 = t is float8
         code = TYPE_E4M3 if e4m3 else _type_of(K, "K")
         try:
             pages, page_rows, hk, d = K.shape
@@ -511,27 +537,23 @@ class Cache:
             raise ValueError("K and V must have four dimensions (page, row, head, feature)") from None
         _check_same(K, (pages, page_rows, hk, d), t, device, "K", dense=False)
         _check_same(V, (pages, page_rows, hk, dv), t, device, "V", dense=False)
-        if getattr(table, "ndim", 0) != 2:
-            raise ValueError("table must have two dimensions (batch, page)")
-        b, most = table.shape
-        _check_same(table, (b, most), _rotation_types()[2], device, "table")
-        c = _Cache(code, 0, pages, page_rows, hk, d, dv, b, most, K.data_ptr(), V.data_ptr(), K.stride()[:3], V.stride()[:3])
-        c.table = table.data_ptr()
+        try:
+            b, most = table.shape
+        except (ValueError, AttributeError):
+            raise ValueError("table must have two dimensions (batch, page)") from None
+        _check_same(table, (b, most), int32, device, "table")
+        ke = ve = 0
         if e4m3:
-            import torch
             for x, name in ((self.k_exp, "k_exp"), (self.v_exp, "v_exp")):
                 if x is None:
                     raise ValueError("float8 pages need %s" % name)
-                _check_same(x, (pages, hk, page_rows, 4), torch.uint8, device, name)
-            c.K_exp, c.V_exp = self.k_exp.data_ptr(), self.v_exp.data_ptr()
+                _check_same(x, (pages, hk, page_rows, 4), uint8, device, name)
+            ke, ve = self.k_exp.data_ptr(), self.v_exp.data_ptr()
         elif self.k_exp is not None or self.v_exp is not None:
             raise ValueError("exponents without float8 pages")
-        return c
-
-
-def _float8():
-    import torch
-    return torch.float8_e4m3fn
+        ks, vs = K.stride(), V.stride()
+        return _Cache.from_buffer_copy(_Cache.pack(code, 0, pages, page_rows, hk, d, dv, b, most, K.data_ptr(), V.data_ptr(), ks[0], ks[1], ks[2],
+                                                   vs[0], vs[1], vs[2], ke, ve, table.data_ptr()))
 
 
 @dataclass
@@ -555,22 +577,23 @@ class CachedAttention:
     def to_c(self, device):
         c = self.cache.to_c(device)
         Q = self.Q
-        code, t = _type_of(Q, "Q"), Q.dtype
-        if Q.dim() != 4:
-            raise ValueError("Q must have four dimensions (batch, row, head, feature)")
-        b, nq, h, d = Q.shape
-        _check_same(Q, (c.batch, nq, h, c.d), t, device, "Q", dense=False)
+        code = _type_of(Q, "Q")
+        try:
+            b, nq, h, d = Q.shape
+        except ValueError:
+            raise ValueError("Q must have four dimensions (batch, row, head, feature)") from None
+        _check_same(Q, (c.batch, nq, h, c.d), Q.dtype, device, "Q", dense=False)
         if c.type != TYPE_E4M3 and c.type != code:
             raise TypeError("Q must be of the cache's type")
-        a = _CachedAttention(code, bool(self.causal), h, nq, _int64(self.window), max(d, 1) ** -0.5 if self.scale is None else self.scale,
-                             self.cap, Q.data_ptr(), Q.stride()[:3])
-        int32 = _rotation_types()[2]
+        int32, ql = _others()[2], 0
         _check_same(self.k_len, (b,), int32, device, "k_len")
-        a.k_len = self.k_len.data_ptr()
         if self.q_len is not None:
             _check_same(self.q_len, (b,), int32, device, "q_len")
-            a.q_len = self.q_len.data_ptr()
-        return c, a
+            ql = self.q_len.data_ptr()
+        qs = Q.stride()
+        return c, _CachedAttention.from_buffer_copy(_CachedAttention.pack(
+            code, bool(self.causal), h, nq, _int64(self.window), max(d, 1) ** -0.5 if self.scale is None else self.scale, self.cap, Q.data_ptr(),
+            qs[0], qs[1], qs[2], ql, self.k_len.data_ptr()))
 
 
 @dataclass
@@ -930,9 +953,10 @@ class Context:
         r = rot.to_c(self.device)
 
         def call():
-            out = [None if x is None else self.torch.empty(x.shape, dtype=x.dtype, device=self.device) for x in (rot.Q, rot.K)]
-            self._ck(self.lib.bbmm_rotate(self.h, C.byref(r), *[None if y is None else y.data_ptr() for y in out]))
-            return tuple(out)
+            q = None if rot.Q is None else rot.Q.new_empty((r.batch, r.rows, r.q_heads, r.d))
+            k = None if rot.K is None else rot.K.new_empty((r.batch, r.rows, r.k_heads, r.d))
+            self._ck(self.lib.bbmm_rotate(self.h, C.byref(r), None if q is None else q.data_ptr(), None if k is None else k.data_ptr()))
+            return q, k
 
         return self._ordered(rot.tensors(), call)
 
@@ -962,12 +986,13 @@ class Context:
             stride.append((C.c_int64 * 3)(*g.stride()[:3]))
 
         def call():
-            out = [None if x is None else self.torch.empty(x.shape, dtype=x.dtype, device=self.device)
-                   for x in (rot.Q, rot.K, rot.q_weight, rot.k_weight)]
-            w, wp, n = self._work(self._rotate_bytes(r))
+            b, rows, d = r.batch, r.rows, r.d
+            out = (None if rot.Q is None else rot.Q.new_empty((b, rows, r.q_heads, d)), None if rot.K is None else rot.K.new_empty((b, rows, r.k_heads, d)),
+                   None if rot.q_weight is None else rot.q_weight.new_empty((d,)), None if rot.k_weight is None else rot.k_weight.new_empty((d,)))
+            w, wp, n = self._work(self._rotate_bytes(r)) if r.q_weight or r.k_weight else (None, None, 0)
             self._ck(self.lib.bbmm_rotate_grad(self.h, C.byref(r), ptr[0], stride[0], ptr[1], stride[1],
                                                *[None if y is None else y.data_ptr() for y in out], wp, n))
-            return tuple(out)
+            return out
 
         return self._ordered(rot.tensors() + given, call)
 
@@ -1030,8 +1055,9 @@ class Context:
         c, a = att.to_c(self.device)
 
         def call():
-            O = self.torch.empty((c.batch, a.nq, a.heads, c.dv), dtype=att.Q.dtype, device=self.device)
-            lse = self.torch.empty((c.batch, a.heads, a.nq), dtype=self.torch.float32, device=self.device)
+            b, h, nq = c.batch, a.heads, a.nq
+            O = att.Q.new_empty((b, nq, h, c.dv))
+            lse = self.torch.empty((b, h, nq), dtype=self.torch.float32, device=self.device)
             w, wp, n = self._work(self._cached_bytes(c, a))
             self._ck(self.lib.bbmm_attend_cache(self.h, C.byref(c), C.byref(a), O.data_ptr(), lse.data_ptr(), wp, n))
             return O, lse

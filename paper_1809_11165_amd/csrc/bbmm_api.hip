@@ -2417,7 +2417,7 @@ int rotation_args(bbmm_ctx* c, const bbmm_rotation* in, bool pointers, RotArgs* 
   memset(a, 0, sizeof *a);
   a->heads[0] = (int)in->q_heads, a->heads[1] = (int)in->k_heads;
   a->tokens = in->q_heads + in->k_heads ? in->batch * in->rows : 0;
-  a->rows = (int)in->rows, a->d = (int)in->d, a->rot = (int)in->rot, a->norm = in->norm != 0, a->neighbours = in->neighbours != 0, a->eps = in->eps;
+  a->rows = (int)in->rows, a->d = (int)in->d, a->rot = (int)in->rot, a->norm = in->norm != 0, a->neighbours = in->neighbours != 0, a->eps = in->eps, a->eps32 = (float)in->eps, a->inv_d = 1.f / (float)in->d;
   a->w[0] = in->q_weight, a->w[1] = in->k_weight;
   if (!pointers) return BBMM_OK;
   size_t e = elem_size(in->type);
@@ -2443,21 +2443,24 @@ int rotation_args(bbmm_ctx* c, const bbmm_rotation* in, bool pointers, RotArgs* 
 }
 
 // Tokens of a workgroup: as many as its lanes hold rows of at a time (up to 8, whose angles are kept), fewer where the device has room left.  The
-// gradient's workgroups go on to further tokens, so that sums of the weights' gradients are few.
+// gradient's workgroups go on to further tokens, so that sums of the weights' gradients are few: three to a compute unit (what the registers
+// admit), dealt out to Q and K by their heads.
 constexpr int64_t kRotBlocks = (int64_t)1 << 20;
-int64_t rotate_most(const bbmm_ctx* c, bool grad) { return grad ? 4 * c->num_cus : kRotBlocks; }
+int64_t rotate_most(const bbmm_ctx* c, const RotArgs& a, int w) {
+  return std::max<int64_t>(1, 3 * (int64_t)c->num_cus * a.heads[w] / std::max<int64_t>((int64_t)a.heads[0] + a.heads[1], 1));
+}
 void rotate_plan(const bbmm_ctx* c, int type, bool grad, RotArgs* a) {
   int hand = rotate_rows(type, grad, a->d, a->vec);
   for (int w = 0; w < 2; ++w) {
-    int64_t t = a->heads[w] ? std::min<int64_t>(hand / a->heads[w], BBMM_ROT_TOKENS) : 1;
-    t = std::max<int64_t>(1, std::min<int64_t>(t, a->tokens / (2 * c->num_cus)));
-    a->tokens_per[w] = (int)t;
-    a->blocks[w] = a->heads[w] ? (int)std::min<int64_t>((a->tokens + t - 1) / t, rotate_most(c, grad)) : 0;
+    if (!a->heads[w]) continue;
+    int64_t t = std::min<int64_t>({hand / a->heads[w], BBMM_ROT_TOKENS, (a->tokens + c->num_cus - 1) / c->num_cus});
+    a->tokens_per[w] = (int)std::max<int64_t>(1, t);
+    a->blocks[w] = (int)std::min<int64_t>((a->tokens + a->tokens_per[w] - 1) / a->tokens_per[w], grad ? rotate_most(c, *a, w) : kRotBlocks);
   }
 }
 size_t rotate_work(const bbmm_ctx* c, const RotArgs& a) {
   if (!a.w[0] && !a.w[1]) return 0;
-  return step256(2 * (size_t)std::min<int64_t>(a.tokens, rotate_most(c, true)) * a.d * sizeof(float));
+  return step256((size_t)(std::min(a.tokens, rotate_most(c, a, 0)) + std::min(a.tokens, rotate_most(c, a, 1))) * a.d * sizeof(float));
 }
 
 int rotate(bbmm_ctx* c, const bbmm_rotation* in, void* Qr, void* Kr) {

@@ -22,6 +22,7 @@ struct RotArgs {
   int64_t tokens;                // batch x rows
   int rows, d, rot, norm, neighbours;
   double eps;                    // as the caller has it: beside tiny rows a subnormal one counts
+  float eps32, inv_d;
   int vec;                       // all rows may be read and written 16 bytes at a time, and pairs are pieces or lie within one
   uint8_t axis[BBMM_ATT_MAXD / 2];
 };

@@ -37,54 +37,50 @@ template <int LPR> __device__ __forceinline__ float row_max(float x) { return ac
 
 // How a row is dealt out: E elements a piece (16 bytes, or 1), slot j = lane + LPR k holds two pieces.
 //   halves: j < rot / 2E holds pieces j and j + rot / 2E (turned); behind, 2j and 2j + 1;  neighbours: 2j and 2j + 1 (turned below rot).
-template <typename T, int E, int LPR, int KS>
+template <typename T, int E, int LPR, int KS, bool NB>
 struct Row {
   static constexpr int N = 2 * E;
-  typedef unsigned word;
-  struct Raw { u32x4 v[E > 1 ? 2 * KS : 1]; T e[E > 1 ? 1 : 2 * KS]; };
+  typedef T piece __attribute__((ext_vector_type(E)));
+  struct Raw { piece v[2 * KS]; };
   int p0[KS], p1[KS];                                       // first elements of the two pieces
   int pair0[KS];                                            // the slot's first pair
   int d, half;
-  bool nb;
   __device__ __forceinline__ Row(const RotArgs& a, int lane) {
-    d = a.d, half = a.rot >> 1, nb = a.neighbours;
+    d = a.d, half = a.rot >> 1;
     int h = half / E;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       int j = lane + LPR * k;
-      bool split = !nb && j < h;
+      bool split = !NB && j < h;
       p0[k] = split ? j * E : 2 * j * E;
       p1[k] = split ? (j + h) * E : (2 * j + 1) * E;
       pair0[k] = j * E;
     }
   }
-  __device__ __forceinline__ void load(Raw& r, const T* row, bool have) const {
+  // Pieces behind the row stay as they are: zeros (see clear).
+  __device__ __forceinline__ void load(Raw& r, const T* row) const {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      if constexpr (E > 1) {
-        r.v[2 * k] = r.v[2 * k + 1] = u32x4{0u, 0u, 0u, 0u};
-        if (have && p0[k] < d) r.v[2 * k] = *(const u32x4*)(row + p0[k]);
-        if (have && p1[k] < d) r.v[2 * k + 1] = *(const u32x4*)(row + p1[k]);
-      } else {
-        r.e[2 * k] = r.e[2 * k + 1] = (T)0.f;
-        if (have && p0[k] < d) r.e[2 * k] = row[p0[k]];
-        if (have && p1[k] < d) r.e[2 * k + 1] = row[p1[k]];
-      }
+      if (p0[k] < d) r.v[2 * k] = *(const piece*)(row + p0[k]);
+      if (p1[k] < d) r.v[2 * k + 1] = *(const piece*)(row + p1[k]);
     }
   }
-  // element i < 2E of slot k
-  __device__ __forceinline__ static float at(const Raw& r, int k, int i) {
-    if constexpr (E > 1) return (float)reinterpret_cast<const T*>(&r.v[2 * k + i / E])[i % E];
-    else return (float)r.e[2 * k + i];
+  __device__ __forceinline__ static void clear(Raw& r) {
+#pragma unroll
+    for (int k = 0; k < 2 * KS; ++k) r.v[k] = (piece)(T)0.f;
   }
-  __device__ __forceinline__ void weights(float* w, const T* p) const {      // ones without weights
+  // element i < 2E of slot k
+  __device__ __forceinline__ static float at(const Raw& r, int k, int i) { return (float)r.v[2 * k + i / E][i % E]; }
+  __device__ __forceinline__ void weights(float* w, const T* p) const {      // ones without weights, zeros behind the row
+    typedef piece some __attribute__((aligned(sizeof(T))));
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+    for (int k = 0; k < 2 * KS; ++k) {
+      int c = k & 1 ? p1[k / 2] : p0[k / 2];
+      piece v = (piece)(T)(p ? 0.f : 1.f);
+      if (p && c < d) v = *(const some*)(p + c);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        int c = (i < E ? p0[k] : p1[k]) + i % E;
-        w[k * N + i] = !p ? 1.f : c < d ? (float)p[c] : 0.f;
-      }
+      for (int i = 0; i < E; ++i) w[k * E + i] = (float)v[i];
+    }
   }
   __device__ __forceinline__ void store(T* row, const float* y) const {
 #pragma unroll
@@ -92,38 +88,34 @@ struct Row {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         int c = x ? p1[k] : p0[k];
-        if (c >= d) continue;
-        if constexpr (E > 1) {
-          u32x4 v;
-          T* e = reinterpret_cast<T*>(&v);
+        piece v;
 #pragma unroll
-          for (int i = 0; i < E; ++i) e[i] = (T)y[k * N + x * E + i];
-          *(u32x4*)(row + c) = v;
-        } else {
-          row[c] = (T)y[k * N + x];
-        }
+        for (int i = 0; i < E; ++i) v[i] = (T)y[k * N + x * E + i];
+        if (c < d) *(piece*)(row + c) = v;
       }
   }
-  // The slot's pairs turned by trig (back: the other way round).
-  __device__ __forceinline__ void turn(float* y, const float2* trig, bool back) const {
+  // Cosines and sines of the slots' pairs, from those of their token.
+  __device__ __forceinline__ void angles(float2* t, const float2* trig) const {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < E; ++i) t[k * E + i] = trig[pair0[k] + i];
+  }
+  // The slots' pairs turned (BACK: the other way round).  Halves are a slot's pairs or none of them.
+  template <bool BACK>
+  __device__ __forceinline__ void turn(float* y, const float2* t) const {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      float* v = y + k * N;
+      int there = half - pair0[k];                          // pairs of the slot, if positive
+      constexpr bool kInside = NB && E > 1;                 // pairs within a piece, any number of them; else a slot's pairs or none
+      if (!kInside && there <= 0) continue;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        int p = pair0[k] + i;
-        if (p >= half) continue;
-        float2 t = trig[p];
-        if (back) t.y = -t.y;
-        if (E > 1 && nb) {
-          float u = v[2 * i], w = v[2 * i + 1];
-          v[2 * i] = u * t.x - w * t.y;
-          v[2 * i + 1] = w * t.x + u * t.y;
-        } else {
-          float u = v[i], w = v[E + i];
-          v[i] = u * t.x - w * t.y;
-          v[E + i] = w * t.x + u * t.y;
-        }
+        float &u = y[k * N + (kInside ? 2 * i : i)], &w = y[k * N + (kInside ? 2 * i + 1 : E + i)];
+        float c = t[k * E + i].x, s = BACK ? -t[k * E + i].y : t[k * E + i].y;
+        float p = u * c - w * s, q = w * c + u * s;
+        u = !kInside || i < there ? p : u;
+        w = !kInside || i < there ? q : w;
       }
     }
   }
@@ -131,12 +123,12 @@ struct Row {
 
 // n = r x of a row in place, and r.  Squares that leave fp32 (or lose bits near its smallest numbers) are formed of scaled values instead.
 template <int LPR, int M>
-__device__ __forceinline__ float norm_row(float* x, int d, double eps) {
+__device__ __forceinline__ float norm_row(float* x, float inv_d, float eps32, double eps) {
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < M; ++i) s = fmaf(x[i], x[i], s);
   s = row_sum<LPR>(s);
-  float mean = fmaf(s, 1.f / (float)d, (float)eps), r = rsqrtf(mean), scale = 1.f;
+  float mean = fmaf(s, inv_d, eps32), r = __builtin_amdgcn_rsqf(mean), scale = 1.f;
   bool lost = !(s < 1e37f) || mean < 1e-27f;
   if (__any(lost)) {
     float top = 0.f;
@@ -147,26 +139,38 @@ __device__ __forceinline__ float norm_row(float* x, int d, double eps) {
     if (eps > 0.0) e = max(e, ilogb(eps) / 2);               // beside eps smaller squares are nothing
     e = min(max(e, -126), 126);
     float down = ldexpf(1.f, -e), q = 0.f;
+    if (!lost) down = 1.f;
 #pragma unroll
-    for (int i = 0; i < M; ++i) q = fmaf(x[i] * down, x[i] * down, q);
+    for (int i = 0; i < M; ++i) {
+      x[i] *= down;
+      q = fmaf(x[i], x[i], q);
+    }
     q = row_sum<LPR>(q);
     if (lost) {
       scale = down;
-      r = 1.f / sqrtf(fmaf(q, 1.f / (float)d, (float)(eps * down * down)));
+      r = 1.f / sqrtf(fmaf(q, inv_d, (float)(eps * down * down)));
     }
   }
 #pragma unroll
-  for (int i = 0; i < M; ++i) x[i] = x[i] * scale * r;
+  for (int i = 0; i < M; ++i) x[i] *= r;
   return scale * r;
 }
 
+// A run of rows of a workgroup: row r of its tokens is head r % heads of token r / heads.
 template <typename T>
-__device__ __forceinline__ void token_row(const RotArgs& a, uint32_t tok, int h, const T* x, const int64_t* s, const T** row, bool* live) {
-  uint32_t b = over(tok, a.by_rows);
-  int i = (int)(tok - b * (uint32_t)a.rows);
-  *live = !a.len || i < a.len[b];
-  *row = x + (int64_t)b * s[0] + (int64_t)i * s[1] + (int64_t)h * s[2];
-}
+struct Cursor {
+  const T* row[2];                                          // of up to two inputs
+  int token, head;                                          // token of the workgroup
+  bool live;
+  // s1 null: one input only
+  __device__ __forceinline__ void token_start(const RotArgs& a, uint32_t tok0, const T* x0, const int64_t* s0, const T* x1, const int64_t* s1) {
+    uint32_t tok = tok0 + token, b = over(tok, a.by_rows);
+    int i = (int)(tok - b * (uint32_t)a.rows);
+    live = !a.len || i < a.len[b];
+    row[0] = x0 + (int64_t)b * s0[0] + (int64_t)i * s0[1] + (int64_t)head * s0[2];
+    if (x1) row[1] = x1 + (int64_t)b * s1[0] + (int64_t)i * s1[1] + (int64_t)head * s1[2];
+  }
+};
 
 __device__ __forceinline__ void fill_trig(const RotArgs& a, float2* trig, int64_t tok0, int n, int tid) {
   int half = a.rot >> 1;
@@ -176,45 +180,57 @@ __device__ __forceinline__ void fill_trig(const RotArgs& a, float2* trig, int64_
   }
 }
 
-// Rows of the workgroup's tokens, groups of LPR lanes a row, U rows of a group in hand at a time.
-template <typename T, int E, int LPR, int KS, int U>
+// Rows of the workgroup's tokens: a group of LPR lanes takes U neighbouring rows at a time, of one token mostly, whose angles it then keeps.
+template <typename T, int E, int LPR, int KS, int U, bool NB>
 __global__ __launch_bounds__(256) void k_rotate(RotArgs a) {
-  typedef Row<T, E, LPR, KS> Rows;
+  typedef Row<T, E, LPR, KS, NB> Rows;
   constexpr int GP = 256 / LPR, M = Rows::N * KS;
   __shared__ float2 trig[BBMM_ROT_TOKENS * (BBMM_ATT_MAXD / 2)];
   int tid = threadIdx.x, which = blockIdx.x >= (unsigned)a.blocks[0];
-  int blk = blockIdx.x - (which ? a.blocks[0] : 0), per = a.tokens_per[which];
+  int blk = blockIdx.x - (which ? a.blocks[0] : 0), per = a.tokens_per[which], heads = a.heads[which];
   Rows rows(a, tid % LPR);
   const T* x = (const T*)a.x[which];
   T* y = (T*)a.y[which];
   float w[M];
   if (a.norm) rows.weights(w, (const T*)a.w[which]);
+  typename Rows::Raw raw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) Rows::clear(raw[u]);
   for (int64_t tok0 = (int64_t)blk * per; tok0 < a.tokens; tok0 += (int64_t)a.blocks[which] * per) {
-    int n = (int)min((int64_t)per, a.tokens - tok0) * a.heads[which];
-    typename Rows::Raw raw[U];
+    int n = (int)min((int64_t)per, a.tokens - tok0) * heads;
+    int mine = min(U, (n + GP - 1) / GP);                  // rows of a group at a time
     bool live[U];
+    int token[U];
     auto load = [&](int r0) {
+      Cursor<T> at;
+      at.token = (int)over(r0, a.by_heads[which]);
+      at.head = r0 - at.token * heads;
+      if (r0 < n) at.token_start(a, (uint32_t)tok0, x, a.xs[which], (const T*)nullptr, nullptr);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        int r = r0 + u * GP;
-        live[u] = false;
-        if (r < n) {
-          uint32_t t = over(r, a.by_heads[which]);
-          const T* row;
-          token_row(a, (uint32_t)tok0 + t, r - (int)t * a.heads[which], x, a.xs[which], &row, &live[u]);
-          rows.load(raw[u], row, live[u]);
+        if (u == mine) break;
+        live[u] = r0 + u < n && at.live;
+        token[u] = at.token;
+        if (live[u]) rows.load(raw[u], at.row[0]);
+        at.row[0] += a.xs[which][2];
+        if (u + 1 < U && ++at.head == heads) {
+          at.head = 0;
+          ++at.token;
+          if (r0 + u + 1 < n) at.token_start(a, (uint32_t)tok0, x, a.xs[which], (const T*)nullptr, nullptr);
         }
       }
     };
-    int r0 = tid / LPR;
+    int r0 = tid / LPR * mine;
     load(r0);                                              // on their way while the angles are formed
     fill_trig(a, trig, tok0, per, tid);
     __syncthreads();
     for (;;) {
+      float2 t[KS * E];
+      if (r0 < n) rows.angles(t, trig + token[0] * (BBMM_ATT_MAXD / 2));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        int r = r0 + u * GP;
-        if (r >= n) break;
+        if (u == mine || r0 + u >= n) break;
+        if (u && token[u] != token[u - 1]) rows.angles(t, trig + token[u] * (BBMM_ATT_MAXD / 2));
         float v[M];
 #pragma unroll
         for (int k = 0; k < KS; ++k)
@@ -222,96 +238,111 @@ __global__ __launch_bounds__(256) void k_rotate(RotArgs a) {
           for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = live[u] ? Rows::at(raw[u], k, i) : 0.f;
         if (live[u]) {
           if (a.norm) {
-            norm_row<LPR, M>(v, a.d, a.eps);
+            norm_row<LPR, M>(v, a.inv_d, a.eps32, a.eps);
 #pragma unroll
             for (int i = 0; i < M; ++i) v[i] *= w[i];
           }
-          rows.turn(v, trig + over(r, a.by_heads[which]) * (BBMM_ATT_MAXD / 2), false);
+          rows.template turn<false>(v, t);
         }
-        rows.store(y + ((tok0 * a.heads[which]) + r) * a.d, v);
+        rows.store(y + ((tok0 * heads) + r0 + u) * a.d, v);
       }
-      r0 += U * GP;
-      if (r0 - tid / LPR >= n) break;
+      r0 += mine * GP;
+      if (r0 - tid / LPR * mine >= n) break;
       load(r0);
     }
     __syncthreads();
   }
 }
 
-template <typename T, int E, int LPR, int KS, int U>
+template <typename T, int E, int LPR, int KS, int U, bool NB>
 __global__ __launch_bounds__(256) void k_rotate_grad(RotArgs a) {
-  typedef Row<T, E, LPR, KS> Rows;
+  typedef Row<T, E, LPR, KS, NB> Rows;
   constexpr int GP = 256 / LPR, M = Rows::N * KS;
   __shared__ float2 trig[BBMM_ROT_TOKENS * (BBMM_ATT_MAXD / 2)];
   __shared__ float sums[4][BBMM_ATT_MAXD];
   int tid = threadIdx.x, which = blockIdx.x >= (unsigned)a.blocks[0];
-  int blk = blockIdx.x - (which ? a.blocks[0] : 0), per = a.tokens_per[which];
+  int blk = blockIdx.x - (which ? a.blocks[0] : 0), per = a.tokens_per[which], heads = a.heads[which];
   Rows rows(a, tid % LPR);
-  const T *x = (const T*)a.x[which], *g = (const T*)a.g[which];
+  const T *x = a.norm ? (const T*)a.x[which] : nullptr, *g = (const T*)a.g[which];
   T* dx = (T*)a.y[which];
   float w[M], dw[M];
   if (a.norm) rows.weights(w, (const T*)a.w[which]);
 #pragma unroll
   for (int i = 0; i < M; ++i) dw[i] = 0.f;
+  typename Rows::Raw rx[U], rg[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    Rows::clear(rx[u]);
+    Rows::clear(rg[u]);
+  }
   for (int64_t tok0 = (int64_t)blk * per; tok0 < a.tokens; tok0 += (int64_t)a.blocks[which] * per) {
-    int n = (int)min((int64_t)per, a.tokens - tok0) * a.heads[which];
-    typename Rows::Raw rx[U], rg[U];
+    int n = (int)min((int64_t)per, a.tokens - tok0) * heads;
+    int mine = min(U, (n + GP - 1) / GP);
     bool live[U];
+    int token[U];
     auto load = [&](int r0) {
+      Cursor<T> at;
+      at.token = (int)over(r0, a.by_heads[which]);
+      at.head = r0 - at.token * heads;
+      if (r0 < n) at.token_start(a, (uint32_t)tok0, g, a.gs[which], x, a.xs[which]);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        int r = r0 + u * GP;
-        live[u] = false;
-        if (r < n) {
-          uint32_t t = over(r, a.by_heads[which]);
-          const T* row;
-          token_row(a, (uint32_t)tok0 + t, r - (int)t * a.heads[which], g, a.gs[which], &row, &live[u]);
-          rows.load(rg[u], row, live[u]);
-          if (a.norm) {
-            token_row(a, (uint32_t)tok0 + t, r - (int)t * a.heads[which], x, a.xs[which], &row, &live[u]);
-            rows.load(rx[u], row, live[u]);
-          }
+        if (u == mine) break;
+        live[u] = r0 + u < n && at.live;
+        token[u] = at.token;
+        if (live[u]) {
+          rows.load(rg[u], at.row[0]);
+          if (a.norm) rows.load(rx[u], at.row[1]);
+        }
+        at.row[0] += a.gs[which][2];
+        if (a.norm) at.row[1] += a.xs[which][2];
+        if (u + 1 < U && ++at.head == heads) {
+          at.head = 0;
+          ++at.token;
+          if (r0 + u + 1 < n) at.token_start(a, (uint32_t)tok0, g, a.gs[which], x, a.xs[which]);
         }
       }
     };
-    int r0 = tid / LPR;
+    int r0 = tid / LPR * mine;
     load(r0);
     fill_trig(a, trig, tok0, per, tid);
     __syncthreads();
     for (;;) {
+      float2 t[KS * E];
+      if (r0 < n) rows.angles(t, trig + token[0] * (BBMM_ATT_MAXD / 2));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        int r = r0 + u * GP;
-        if (r >= n) break;
+        if (u == mine || r0 + u >= n) break;
+        if (u && token[u] != token[u - 1]) rows.angles(t, trig + token[u] * (BBMM_ATT_MAXD / 2));
         float v[M];
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
           for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = live[u] ? Rows::at(rg[u], k, i) : 0.f;
         if (live[u]) {
-          rows.turn(v, trig + over(r, a.by_heads[which]) * (BBMM_ATT_MAXD / 2), true);
+          rows.template turn<true>(v, t);
           if (a.norm) {
             float nx[M];
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
               for (int i = 0; i < Rows::N; ++i) nx[k * Rows::N + i] = Rows::at(rx[u], k, i);
-            float rr = norm_row<LPR, M>(nx, a.d, a.eps), dot = 0.f;
+            float rr = norm_row<LPR, M>(nx, a.inv_d, a.eps32, a.eps), dot = 0.f;
 #pragma unroll
             for (int i = 0; i < M; ++i) {
               dw[i] = fmaf(v[i], nx[i], dw[i]);
               v[i] *= w[i];
               dot = fmaf(v[i], nx[i], dot);
             }
-            dot = row_sum<LPR>(dot) * (1.f / (float)a.d);
+            dot = row_sum<LPR>(dot) * a.inv_d;
 #pragma unroll
             for (int i = 0; i < M; ++i) v[i] = rr * fmaf(-nx[i], dot, v[i]);
           }
         }
-        rows.store(dx + ((tok0 * a.heads[which]) + r) * a.d, v);
+        rows.store(dx + ((tok0 * heads) + r0 + u) * a.d, v);
       }
-      r0 += U * GP;
-      if (r0 - tid / LPR >= n) break;
+      r0 += mine * GP;
+      if (r0 - tid / LPR * mine >= n) break;
       load(r0);
     }
     __syncthreads();
@@ -337,23 +368,31 @@ __global__ __launch_bounds__(256) void k_rotate_grad(RotArgs a) {
   for (int c = tid; c < a.d; c += 256) ((float*)a.w_part)[(size_t)blockIdx.x * a.d + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
 }
 
-// The weights' gradients from the workgroups' sums: 16 features a workgroup, 16 threads a feature's parts, in 64 bits and a fixed order.
+// The weights' gradients from the workgroups' sums: 16 features a workgroup, 64 threads a feature's parts, in 64 bits and a fixed order.
 template <typename T>
-__global__ __launch_bounds__(256) void k_rotate_join(RotArgs a, T* dq, T* dk, int tiles) {
+__global__ __launch_bounds__(1024) void k_rotate_join(RotArgs a, T* dq, T* dk, int tiles) {
   __shared__ double part[16][17];
-  int which = blockIdx.x >= (unsigned)tiles, c = (blockIdx.x - (which ? tiles : 0)) * 16 + (threadIdx.x & 15), p0 = threadIdx.x >> 4;
+  int which = blockIdx.x >= (unsigned)tiles, f = threadIdx.x & 15, c = (blockIdx.x - (which ? tiles : 0)) * 16 + f, p0 = threadIdx.x >> 4;
   const float* src = (const float*)a.w_part + (which ? (size_t)a.blocks[0] * a.d : 0);
   T* out = which ? dk : dq;
   if (!out) return;
   double s = 0.0;
   if (c < a.d) {
-#pragma unroll 8
-    for (int p = p0; p < a.blocks[which]; p += 16) s += (double)src[(size_t)p * a.d + c];
+    for (int p = p0; p < a.blocks[which]; p += 512) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = p + 64 * u < a.blocks[which] ? src[(size_t)(p + 64 * u) * a.d + c] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += (double)v[u];
+    }
   }
-  part[p0][threadIdx.x & 15] = s;
+  s += __shfl_xor(s, 16, 64);
+  s += __shfl_xor(s, 32, 64);
+  if ((threadIdx.x & 63) < 16) part[threadIdx.x >> 6][f] = s;
   __syncthreads();
   if (threadIdx.x < 16 && c < a.d) {
-    for (int p = 1; p < 16; ++p) s += part[p][threadIdx.x];
+#pragma unroll
+    for (int p = 1; p < 16; ++p) s += part[p][f];
     out[c] = (T)(float)s;
   }
 }
@@ -372,19 +411,23 @@ constexpr int kFwd = 4, kBwd = 2;            // rows of a group in hand
 template <typename T>
 void rotate_t(hipStream_t s, const RotArgs& a) {
   rotate_shape<T, kFwd>(a, [&](auto e, auto l, auto k, auto u) {
-    k_rotate<T, decltype(e)::value, decltype(l)::value, decltype(k)::value, decltype(u)::value><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+    constexpr int E = decltype(e)::value, L = decltype(l)::value, K = decltype(k)::value, U = decltype(u)::value;
+    if (a.neighbours) k_rotate<T, E, L, K, U, true><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+    else k_rotate<T, E, L, K, U, false><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
   });
 }
 template <typename T>
 void rotate_grad_t(hipStream_t s, const RotArgs& a) {
   rotate_shape<T, kBwd>(a, [&](auto e, auto l, auto k, auto u) {
-    k_rotate_grad<T, decltype(e)::value, decltype(l)::value, decltype(k)::value, decltype(u)::value><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+    constexpr int E = decltype(e)::value, L = decltype(l)::value, K = decltype(k)::value, U = decltype(u)::value;
+    if (a.neighbours) k_rotate_grad<T, E, L, K, U, true><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+    else k_rotate_grad<T, E, L, K, U, false><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
   });
 }
 template <typename T>
 void rotate_join_t(hipStream_t s, const RotArgs& a, void* dq, void* dk) {
   int tiles = (a.d + 15) / 16;
-  k_rotate_join<T><<<2 * tiles, 256, 0, s>>>(a, (T*)dq, (T*)dk, tiles);
+  k_rotate_join<T><<<2 * tiles, 1024, 0, s>>>(a, (T*)dq, (T*)dk, tiles);
 }
 
 }  // namespace
