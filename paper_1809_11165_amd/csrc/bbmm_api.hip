@@ -2593,8 +2593,15 @@ int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows,
   return BBMM_OK;
 }
 
-// The keys are split over workgroups while those fill the device less than four times over and parts keep kCachePart keys.
-constexpr int64_t kCachePart = 256;
+// Parts that the keys are split into, over workgroups: as many as fill the device once (two workgroups a compute unit) while parts keep kCachePart
+// keys, and up to eight a compute unit while they keep kCacheEvenPart, which evens out lengths that only the device knows; none where three a compute
+// unit are there anyway, but for parts of more than kCacheLongPart keys, which one long sequence among short ones must not leave to a few.
+constexpr int64_t kCachePart = 256, kCacheEvenPart = 1024, kCacheLongPart = 16384;
+int cache_parts(int64_t cus, int64_t wgs, int64_t reach) {
+  int64_t n = 1;
+  if (wgs < 3 * cus) n = std::max(std::min(2 * cus / wgs, (reach + kCachePart - 1) / kCachePart), std::min(8 * cus / wgs, reach / kCacheEvenPart));
+  return (int)std::max<int64_t>({n, (reach + kCacheLongPart - 1) / kCacheLongPart, 1});
+}
 // Sizes, the split of the keys, and, where `pointers` is set, everything else.
 int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attention* in, bool pointers, CacheArgs* a, CacheAtt* t) {
   int rc = cache_args(c, cache, pointers, a);
@@ -2619,8 +2626,7 @@ int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attentio
   if (cache->batch * in->heads * in->nq > kMaxRows || wgs > kAttMaxGrid) return fail(c, BBMM_EINVAL, "cached attention: more than 2^27 rows in one call");
   wgs = (int64_t)a->B * a->HK * t->blocks;
   int64_t reach = t->window ? std::min<int64_t>(a->rows_most, (int64_t)t->window + t->nq) : a->rows_most;
-  int64_t want = 4 * c->num_cus / std::max<int64_t>(wgs, 1), most = (reach + kCachePart - 1) / kCachePart;
-  t->nsplit = (int)std::max<int64_t>(1, std::min(want, most));
+  t->nsplit = cache_parts(c->num_cus, std::max<int64_t>(wgs, 1), reach);
   t->dv4 = (a->dv + 3) / 4 * 4;
   if (!pointers) return BBMM_OK;
   size_t e = elem_size(in->type);

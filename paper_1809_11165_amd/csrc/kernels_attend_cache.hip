@@ -73,7 +73,7 @@ constexpr int kBlock = 32;                                 // keys of a wave's t
 // One side (keys or values) of a block on its way: raw registers and the rows' exponents.
 //   T held as such: a piece is 16 bytes (values of up to 64 features in two bytes: 8); E4M3: the same features in a half or a quarter of that.
 template <typename T, bool E4M3, int DP, int NT, bool EVEN>
-__global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a) {
+__global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 3) void k_attend_cache(CacheArgs c, CacheAtt a) {
   typedef Mma<T> M;
   typedef typename M::frag frag;
   constexpr int SB = E4M3 ? 1 : (int)sizeof(T);            // bytes of a held element
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
   int64_t p0 = (int64_t)kn - qn + i0, p1 = (int64_t)kn - qn + i1;
   int lo = a.window ? (int)min(max(p0 - a.window + 1, (int64_t)0), (int64_t)kn) : 0;
   int hi = a.causal ? (int)max(min(p1 + 1, (int64_t)kn), (int64_t)0) : kn;
-  if (first >= qn * (int64_t)a.G) hi = lo;
+  if (first >= qn * (int64_t)a.G || c.pages == 0) hi = lo;
   int b0 = lo / kBlock, b1 = hi > lo ? (hi + kBlock - 1) / kBlock : b0;
   int per = max((b1 - b0 + a.nsplit - 1) / a.nsplit, 4);
   int t0 = min(b0 + sp * per, b1), t1 = min(t0 + per, b1);
@@ -104,7 +104,10 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
   int64_t kpage = c.ks[0] * SB, vpage = c.vs[0] * SB, epage = (int64_t)c.HK * c.page.d * 4;
   unsigned kpitch = (unsigned)(c.ks[1] * SB), vpitch = (unsigned)(c.vs[1] * SB);
   const uint8_t *ke = E4M3 ? c.ke + (int64_t)hk * c.page.d * 4 : nullptr, *ve = E4M3 ? c.ve + (int64_t)hk * c.page.d * 4 : nullptr;
-  const int32_t* __restrict__ table = c.table + (int64_t)b * c.max_pages;
+  // The table is not written while the kernel runs: read at uniform places through the scalar cache, whose loads nothing in the loop waits for (a
+  // vector load there waits for all keys and values on their way: 16 requests of up to 65536 8-bit keys 360 us, so 288, before other steps).
+  typedef const __attribute__((address_space(4))) int32_t* scalar_table;
+  const int32_t* table = c.table + (int64_t)b * c.max_pages;
 
   // ---- pages of a block: EVEN (page rows a multiple of 16): two of them, in scalar registers; else one key a lane
   struct Pages { int page[2], row[2]; };
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
         uint32_t at = (uint32_t)(t * kBlock + 16 * k), n = over(at, c.page);
         p.row[k] = uniform((int)(at - n * c.page.d));
         p.page[k] = -1;
-        if (at < (uint32_t)hi) p.page[k] = uniform(table[uniform((int)n)]);
+        if (at < (uint32_t)hi) p.page[k] = ((scalar_table)table)[uniform((int)n)];
       }
     } else {
       uint32_t at = (uint32_t)(t * kBlock + (lane & 31)), n = over(at, c.page);
@@ -163,14 +166,14 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
         }
       } else {
         int pg = __shfl(p.page[0], 16 * k + col, 64), row = __shfl(p.row[0], 16 * k + col, 64);
+        if (!ok) pg = row = 0;                             // some row: loads without branches are counted, and waited for, one by one
         const char* at = K + pg * kpage + (int64_t)row * kpitch;
 #pragma unroll
         for (int s = 0; s < KP; ++s) {
           int o = 16 * (4 * s + q4);
-          kr[k][s] = u32x4{0u, 0u, 0u, 0u};
-          if (ok && o < c.d * SB) kr[k][s] = *(const u32x4*)(at + o);
+          kr[k][s] = *(const u32x4*)(at + (o < c.d * SB ? o : 0));
         }
-        if constexpr (E4M3) kx[k] = ok ? *(const unsigned*)(ke + pg * epage + (int64_t)row * 4) : 0u;
+        if constexpr (E4M3) kx[k] = *(const unsigned*)(ke + pg * epage + (int64_t)row * 4);
       }
     }
   };
@@ -212,29 +215,35 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           int key = 16 * k + 4 * q4 + r;
-          bool ok = (keep >> key) & 1;
           int pg = __shfl(p.page[0], key, 64), row = __shfl(p.row[0], key, 64);
+          if (!((keep >> key) & 1)) pg = row = 0;
           const char* at = V + pg * vpage + (int64_t)row * vpitch;
           unsigned* v = vr[4 * k + r];
-#pragma unroll
-          for (int w = 0; w < VW; ++w) v[w] = 0u;
           if constexpr (VW <= 4) {
-            if (ok && mine) {
-              if constexpr (VW == 1) v[0] = *(const unsigned*)(at + o);
-              else if constexpr (VW == 2) { uint2 w = *(const uint2*)(at + o); v[0] = w.x, v[1] = w.y; }
-              else { u32x4 w = *(const u32x4*)(at + o); v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3]; }
-            }
+            at += mine ? o : 0u;
+            if constexpr (VW == 1) v[0] = *(const unsigned*)at;
+            else if constexpr (VW == 2) { uint2 w = *(const uint2*)at; v[0] = w.x, v[1] = w.y; }
+            else { u32x4 w = *(const u32x4*)at; v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3]; }
           } else {
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
-              if (ok && 64 * z + 4 * col < c.dv) {
-                u32x4 w = *(const u32x4*)(at + 256 * z + 16 * col);
-                v[4 * z] = w[0], v[4 * z + 1] = w[1], v[4 * z + 2] = w[2], v[4 * z + 3] = w[3];
-              }
+            for (int z = 0; z < 2; ++z) {
+              u32x4 w = *(const u32x4*)(at + (64 * z + 4 * col < c.dv ? 256 * z + 16 * col : 0));
+              v[4 * z] = w[0], v[4 * z + 1] = w[1], v[4 * z + 2] = w[2], v[4 * z + 3] = w[3];
+            }
           }
-          if constexpr (E4M3) vx[k][r] = ok ? *(const unsigned*)(ve + pg * epage + (int64_t)row * 4) : 0u;
+          if constexpr (E4M3) vx[k][r] = *(const unsigned*)(ve + pg * epage + (int64_t)row * 4);
         }
       }
+    }
+  };
+  // EVEN: the bounded reads have left zeros.  Else excluded rows' values are made zeros here.
+  auto clear_values = [&](unsigned keep) {
+    if constexpr (!EVEN) {
+      if (keep == ~0u) return;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int w = 0; w < VW; ++w) vr[e][w] = (keep >> (16 * (e >> 2) + 4 * q4 + (e & 3))) & 1 ? vr[e][w] : 0u;
     }
   };
 
@@ -274,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
 #pragma unroll
       for (int k = 0; k < 2; ++k) kx[k] = (kx[k] & blocks_there) | (0x7f7f7f7fu & ~blocks_there);
     }
-    if (!ragged) return;
+    if (EVEN ? !ragged : c.d == DP) return;
     int last = c.d * SB / 16, left = c.d * SB - 16 * last;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -284,6 +293,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
         for (int w = 0; w < 4; ++w) {
           int n = min(max(left - 4 * w, 0), 4);
           if (4 * s + q4 == last) kr[k][s][w] &= n == 4 ? ~0u : (1u << (8 * n)) - 1;
+          if (!EVEN && 4 * s + q4 > last) kr[k][s][w] = 0u;
         }
   };
   auto key_frag = [&](int k, int s) {
@@ -314,7 +324,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
   for (int n = 0; n < NT; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
 
   // O^T += V^T P^T; s[n][k][r]: weight of row n, key 16 k + 4 q4 + r.  fp32: eight single products make a step, of four keys each.
-  auto add_values = [&](const f32x4 (*p)[2], unsigned keep, bool odd) {
+  auto add_values = [&](const f32x4 (*p)[2], unsigned keep, auto odd) {
     frag pf[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -323,7 +333,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
     auto product = [&](frag v, int f) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        if (__builtin_expect(odd, 0)) acc[n][f] = mma_odd<T>(v, pf[n], acc[n][f]);
+        if constexpr (decltype(odd)::value) acc[n][f] = mma_odd<T>(v, pf[n], acc[n][f]);
         else acc[n][f] = M::mma(v, pf[n], acc[n][f]);
       }
     };
@@ -394,20 +404,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
     return odd;
   };
 
-  settle();
-  int t = t0 + wave;
-  Pages here{}, next{};
-  unsigned keep = 0;
-  if (t < t1) {
-    here = find(t);
-    next = t + 4 < t1 ? find(t + 4) : here;
-    keep = kept(t, here);
-    fetch_k(here, keep);
-    fetch_v(here, keep);
-  }
-    for (; t < t1; t += 4) {
-    int j0 = t * kBlock;
-    f32x4 s[NT][2];
+  // Scores of the block in kr, and the weights that they become: s[n][k][r] of row n, key 16 k + 4 q4 + r.
+  f32x4 s[NT][2];
+  auto scores = [&] {
     trim();
 #pragma unroll
     for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -419,14 +418,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[n][k] = M::mma(f, qf[n][z], s[n][k]);
       }
-    unsigned keep_next = 0;
-    Pages after = next;
-    if (t + 4 < t1) {
-      if (t + 8 < t1) after = find(t + 8);
-      keep_next = kept(t + 4, next);
-      fetch_k(next, keep_next);
-    }
-    // scores in units of the base-2 exponent
+  };
+  auto weights = [&](int j0, unsigned keep, auto edge) {
+    // in units of the base-2 exponent
     if (a.cap2 != 0.f) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -446,28 +440,22 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[n][e >> 2][e & 3] *= a.c2;
     }
-    // queries that differ in what they take of this block
-    bool edge = i0 != i1 && ((a.causal && j0 + kBlock - 1 > p0) || (a.window && j0 <= p1 - a.window));
-    unsigned mine[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) mine[n] = keep;
-    if (edge) {
+    if (decltype(edge)::value || keep != ~0u) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        int64_t p = (int64_t)kn - qn + qi[n] - j0;         // the row's place in the block
-        if (a.causal) mine[n] &= p < 0 ? 0u : p >= 31 ? ~0u : (2u << (int)p) - 1;
-        if (a.window) {
-          int64_t w = p - a.window + 1;                    // the first key
-          mine[n] &= w <= 0 ? ~0u : w >= 32 ? 0u : ~0u << (int)w;
+        unsigned mine = keep;
+        if constexpr (decltype(edge)::value) {
+          int64_t p = (int64_t)kn - qn + qi[n] - j0;       // the row's place in the block
+          if (a.causal) mine &= p < 0 ? 0u : p >= 31 ? ~0u : (2u << (int)p) - 1;
+          if (a.window) {
+            int64_t w = p - a.window + 1;                  // the first key
+            mine &= w <= 0 ? ~0u : w >= 32 ? 0u : ~0u << (int)w;
+          }
         }
-      }
-    }
-    if (edge || keep != ~0u) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (!((mine[n] >> (16 * (e >> 2) + 4 * q4 + (e & 3))) & 1)) s[n][e >> 2][e & 3] = -__builtin_inff();
+          if (!((mine >> (16 * (e >> 2) + 4 * q4 + (e & 3))) & 1)) s[n][e >> 2][e & 3] = -__builtin_inff();
+      }
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -491,12 +479,55 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
         l[n] += y;
       }
     }
-    // infinities and NaN among the values of keys that only some of the rows take (an 8-bit value may become infinite in fp16 as well)
-    add_values(s, keep, edge && (__any(odd_values()) || (E4M3 && __is_same(T, _Float16))));
-    if (t + 4 < t1) fetch_v(next, keep_next);
-    here = next;
+  };
+
+  // Blocks of which all queries take the same keys: [a0, a1).  The next block's keys are on their way from the end of the scores on, its values from
+  // the end of the products with them.
+  int a0 = t0, a1 = t1;
+  if (i0 != i1) {
+    if (a.window) a0 = (int)min(max(p1 - a.window < 0 ? 0 : (p1 - a.window) / kBlock + 1, (int64_t)t0), (int64_t)t1);
+    if (a.causal) a1 = (int)min(max(p0 < kBlock - 1 ? 0 : (p0 - (kBlock - 1)) / kBlock + 1, (int64_t)a0), (int64_t)t1);
+  }
+  settle();
+  int t = a0 + wave;
+  Pages next{};
+  unsigned keep = 0;
+  if (t < a1) {
+    Pages here = find(t);
+    next = t + 4 < a1 ? find(t + 4) : here;
+    keep = kept(t, here);
+    fetch_k(here, keep);
+    fetch_v(here, keep);
+  }
+  for (; t < a1; t += 4) {
+    scores();
+    unsigned keep_next = 0;
+    Pages after = next;
+    if (t + 4 < a1) {
+      if (t + 8 < a1) after = find(t + 8);
+      keep_next = kept(t + 4, next);
+      fetch_k(next, keep_next);
+    }
+    weights(t * kBlock, keep, Const<0>{});
+    clear_values(keep);
+    add_values(s, keep, Const<0>{});
+    if (t + 4 < a1) fetch_v(next, keep_next);
     next = after;
     keep = keep_next;
+  }
+  // and the others, few: [t0, a0) and [a1, t1).  Infinities and NaN among their values are kept from rows that do not take them (an 8-bit value may
+  // become infinite in fp16 as well).
+  for (int u = wave; u < (a0 - t0) + (t1 - a1); u += 4) {
+    int at = u < a0 - t0 ? t0 + u : a1 + u - (a0 - t0);
+    Pages here = find(at);
+    keep = kept(at, here);
+    fetch_k(here, keep);
+    fetch_v(here, keep);
+    scores();
+    weights(at * kBlock, keep, Const<1>{});
+    clear_values(keep);
+    if (__any(odd_values()) || (E4M3 && __is_same(T, _Float16))) add_values(s, keep, Const<1>{});
+    else add_values(s, keep, Const<0>{});
   }
 
   // the waves' sums: each scales its own to the largest reference; two leave theirs in LDS, the other two add them, all write
@@ -560,34 +591,57 @@ __global__ __launch_bounds__(256, 2) void k_attend_cache(CacheArgs c, CacheAtt a
   }
 }
 
-// Parts of a row joined by their log sums: 32 lanes a row, four features a lane; parts without weight are not read.
-template <typename T>
+// Parts of a row joined by their log sums: 32 lanes a row, four features a lane, GROUPS of them that take every GROUPS-th part (and join in LDS).  What
+// parts without weight hold is not used.
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt a) {
-  int64_t n = (int64_t)c.B * a.H * a.nq, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  int lane = threadIdx.x & 31, f = 4 * lane;
-  if (row >= n) return;
-  float top = -__builtin_inff();
-  for (int s = lane; s < a.nsplit; s += 32) top = fmaxf(top, a.pl[s * n + row]);
-#pragma unroll
-  for (int x = 1; x < 32; x *= 2) top = fmaxf(top, __shfl_xor(top, x, 32));
-  float sum = 0.f;
+  __shared__ __align__(16) f32x4 part[8][32];
+  __shared__ float tops[8], sums[8];
+  int64_t n = (int64_t)c.B * a.H * a.nq, row = (int64_t)blockIdx.x * (8 / GROUPS) + (threadIdx.x >> 5) / GROUPS;
+  int lane = threadIdx.x & 31, f = 4 * lane, all = threadIdx.x >> 5, g = all % GROUPS;
+  if (row >= n) return;                                    // GROUPS == 8: no workgroup is behind the last row
+  float top = -__builtin_inff(), sum = 0.f;
   f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
+  for (int s0 = g; s0 < a.nsplit; s0 += 8 * GROUPS) {
     float p[8];
     f32x4 v[8];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) p[s] = s0 + s < a.nsplit ? a.pl[(s0 + s) * n + row] : -__builtin_inff();
-#pragma unroll
     for (int s = 0; s < 8; ++s) {
-      v[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (p[s] != -__builtin_inff() && f < a.dv4) v[s] = *(const f32x4*)(a.pO + ((s0 + s) * n + row) * a.dv4 + f);
+      int at = s0 + GROUPS * s;
+      p[s] = at < a.nsplit ? a.pl[at * n + row] : -__builtin_inff();
+      v[s] = at < a.nsplit && f < a.dv4 ? *(const f32x4*)(a.pO + (at * n + row) * a.dv4 + f) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    float best = top;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) best = fmaxf(best, p[s]);
+    float up = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - best);
+    sum *= up;
+    y *= up;
+    top = best;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      float w = p[s] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(p[s] - top);
+      if (p[s] == -__builtin_inff()) continue;
+      float w = __builtin_amdgcn_exp2f(p[s] - best);
       sum += w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = fmaf(w, v[s][e], y[e]);
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    part[all][lane] = y;
+    if (lane == 0) tops[all] = top, sums[all] = sum;
+    __syncthreads();
+    if (g) return;
+    top = -__builtin_inff(), sum = 0.f;
+    y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, tops[all + k]);
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      if (sums[all + k] == 0.f) continue;
+      float w = __builtin_amdgcn_exp2f(tops[all + k] - top);
+      sum = fmaf(w, sums[all + k], sum);
+      y += w * part[all + k][lane];
     }
   }
   bool some = sum != 0.f;
@@ -622,6 +676,13 @@ void attend_t(hipStream_t s, int type, int e4m3, const CacheArgs& c, const Cache
   else attend_e<T, false>(s, type, c, a);
 }
 
+template <typename T>
+void join_t(hipStream_t s, const CacheArgs& c, const CacheAtt& a) {
+  int64_t n = (int64_t)c.B * a.H * a.nq;
+  if (a.nsplit <= 8) k_attend_cache_join<T, 1><<<(unsigned)((n + 7) / 8), 256, 0, s>>>(c, a);
+  else k_attend_cache_join<T, 8><<<(unsigned)n, 256, 0, s>>>(c, a);
+}
+
 }  // namespace
 
 int cache_rows(int type, int64_t rows) { return type != 0 && rows > 16 ? 32 : 16; }
@@ -632,8 +693,7 @@ void launch_attend_cache(hipStream_t s, int type, int e4m3, const CacheArgs& c, 
   else attend_t<__bf16>(s, type, e4m3, c, a);
 }
 void launch_attend_cache_join(hipStream_t s, int type, const CacheArgs& c, const CacheAtt& a) {
-  unsigned grid = (unsigned)(((int64_t)c.B * a.H * a.nq + 7) / 8);
-  if (type == 0) k_attend_cache_join<float><<<grid, 256, 0, s>>>(c, a);
-  else if (type == 1) k_attend_cache_join<_Float16><<<grid, 256, 0, s>>>(c, a);
-  else k_attend_cache_join<__bf16><<<grid, 256, 0, s>>>(c, a);
+  if (type == 0) join_t<float>(s, c, a);
+  else if (type == 1) join_t<_Float16>(s, c, a);
+  else join_t<__bf16>(s, c, a);
 }
