@@ -13,6 +13,7 @@ struct RotArgs {
   void *y[2], *w_part;           // dense outputs (the gradients of Q and K); w_part: parts x d floats, those of K behind those of Q
   int64_t xs[2][3], gs[2][3];
   const void* w[2];
+  void* dw[2];                   // the weights' gradients, where one workgroup each sums them
   int heads[2];
   int tokens_per[2], blocks[2];  // tokens of a workgroup, workgroups
   Div by_heads[2], by_rows;
