@@ -8,6 +8,8 @@
 //   values: a lane reads, of the eight keys whose weights it will meet, DP / 16 neighbouring features, 16 lanes a row.  Two-byte values then
 //           change places in pairs (one byte permutation per two values); fp32 values are operands as they stand.  No LDS before the join.
 // 8-bit rows become T on the way, by the instruction that applies their block's power of two.
+#include <type_traits>
+
 #include "cache_dev.h"
 
 using namespace att;
@@ -45,14 +47,15 @@ __device__ __forceinline__ float quarters_sum(float x) {
 }
 
 // c + a b where a, values, holds infinities or NaN that rows of weight zero must not meet: finite values are multiplied as ever; a column gets
-// an infinity or NaN where its weight for one is not zero.
-template <typename T>
-__device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, typename Mma<T>::frag b, f32x4 c) {
+// an infinity or NaN where its weight for one is not zero.  b: the weights' parts.
+template <typename T, int PARTS>
+__device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, const typename Mma<T>::frag (&b)[PARTS], f32x4 c) {
   const float odd[3] = {__builtin_inff(), -__builtin_inff(), __builtin_nanf("")};
   typename Mma<T>::frag x = a;
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = fabsf((float)a[e]) < __builtin_inff() ? a[e] : (T)0.f;
-  c = Mma<T>::mma(x, b, c);
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) c = Mma<T>::mma(x, b[p], c);
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
 #pragma unroll
@@ -60,12 +63,27 @@ __device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, typename Mma<T
       float y = (float)a[e];
       x[e] = (k == 2 ? y != y : y == odd[k]) ? (T)1.f : (T)0.f;
     }
-    f32x4 z = Mma<T>::mma(x, b, f32x4{0.f, 0.f, 0.f, 0.f});
+    f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) z = Mma<T>::mma(x, b[p], z);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (z[r] != 0.f) c[r] += odd[k];
   }
   return c;
+}
+
+// fp32 numbers as three of bf16, 8 bits each: what is left is 2^-25 of them.  Products with 8-bit rows, which bf16 holds exactly, then run at a
+// fifth of the fp32 instructions' time.
+__device__ __forceinline__ void in_three(const f32x8& x, bf16x8 (&p)[3]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float first = __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);   // cut off: rounding could leave the range
+    float rest = fabsf(x[e]) < __builtin_inff() ? x[e] - first : 0.f;
+    p[0][e] = (__bf16)first;
+    p[1][e] = (__bf16)rest;
+    p[2][e] = (__bf16)(rest - (float)p[1][e]);
+  }
 }
 
 constexpr int kBlock = 32;                                 // keys of a wave's turn
@@ -74,7 +92,10 @@ constexpr int kBlock = 32;                                 // keys of a wave's t
 //   T held as such: a piece is 16 bytes (values of up to 64 features in two bytes: 8); E4M3: the same features in a half or a quarter of that.
 template <typename T, bool E4M3, int DP, int NT, bool EVEN>
 __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 3) void k_attend_cache(CacheArgs c, CacheAtt a) {
-  typedef Mma<T> M;
+  constexpr bool kThree = sizeof(T) == 4 && E4M3;          // operands in three parts of bf16
+  constexpr int PARTS = kThree ? 3 : 1;
+  typedef std::conditional_t<kThree, __bf16, T> C;         // type of the operands
+  typedef Mma<C> M;
   typedef typename M::frag frag;
   constexpr int SB = E4M3 ? 1 : (int)sizeof(T);            // bytes of a held element
   constexpr int ROWS = 16 * NT;
@@ -250,7 +271,7 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
   // Features of a lane's step s of the scores: eight from `feature(s)` on (fp32: four, twice).
   auto step_at = [&](int s) { return E4M3 ? 16 * (4 * (s >> 1) + q4) + 8 * (s & 1) : 8 * (4 * s + q4); };
   // fp32 pieces hold four features: step s has pieces 2s, 2s + 1
-  frag qf[NT][NS];
+  frag qf[NT][NS][PARTS];
   int rho[NT], qi[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -263,7 +284,7 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
       if constexpr (sizeof(T) == 2) {
         u32x4 v = {0u, 0u, 0u, 0u};
         if (have) v = load16<T>(row, step_at(s), c.d, a.qvec);
-        qf[n][s] = __builtin_bit_cast(frag, v);
+        qf[n][s][0] = __builtin_bit_cast(frag, v);
       } else {
         int f0 = E4M3 ? step_at(s) : 4 * (8 * s + q4), f1 = E4M3 ? f0 + 4 : 4 * (8 * s + 4 + q4);
         u32x4 v0 = {0u, 0u, 0u, 0u}, v1 = v0;
@@ -271,7 +292,9 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
           v0 = load16<T>(row, f0, c.d, a.qvec);
           v1 = load16<T>(row, f1, c.d, a.qvec);
         }
-        qf[n][s] = __builtin_shufflevector(__builtin_bit_cast(f32x4, v0), __builtin_bit_cast(f32x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
+        f32x8 x = __builtin_shufflevector(__builtin_bit_cast(f32x4, v0), __builtin_bit_cast(f32x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
+        if constexpr (kThree) in_three(x, qf[n][s]);
+        else qf[n][s][0] = x;
       }
     }
   }
@@ -306,8 +329,8 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         unsigned q = kr[k][s >> 1][2 * (s & 1) + w];
-        auto x0 = Wide<T>::template get<false>(q, scale);
-        auto x1 = Wide<T>::template get<true>(q, scale);
+        auto x0 = Wide<C>::template get<false>(q, scale);
+        auto x1 = Wide<C>::template get<true>(q, scale);
         f[4 * w] = x0[0], f[4 * w + 1] = x0[1], f[4 * w + 2] = x1[0], f[4 * w + 3] = x1[1];
       }
       return f;
@@ -325,16 +348,25 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
 
   // O^T += V^T P^T; s[n][k][r]: weight of row n, key 16 k + 4 q4 + r.  fp32: eight single products make a step, of four keys each.
   auto add_values = [&](const f32x4 (*p)[2], unsigned keep, auto odd) {
-    frag pf[NT];
+    frag pf[NT][PARTS];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+      if constexpr (kThree) {
+        in_three(__builtin_shufflevector(p[n][0], p[n][1], 0, 1, 2, 3, 4, 5, 6, 7), pf[n]);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) pf[n][e] = (T)p[n][e >> 2][e & 3];
+        for (int e = 0; e < 8; ++e) pf[n][0][e] = (T)p[n][e >> 2][e & 3];
+      }
+    }
     auto product = [&](frag v, int f) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        if constexpr (decltype(odd)::value) acc[n][f] = mma_odd<T>(v, pf[n], acc[n][f]);
-        else acc[n][f] = M::mma(v, pf[n], acc[n][f]);
+        if constexpr (decltype(odd)::value) {
+          acc[n][f] = mma_odd<C, PARTS>(v, pf[n], acc[n][f]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < PARTS; ++x) acc[n][f] = M::mma(v, pf[n][x], acc[n][f]);
+        }
       }
     };
     if constexpr (E4M3) {
@@ -349,23 +381,17 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
       }
 #pragma unroll
       for (int w = 0; w < 2 * VW; ++w) {                   // features 2 w, 2 w + 1
-        typename Wide<T>::two x[8];
+        typename Wide<C>::two x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          x[e] = w & 1 ? Wide<T>::template get<true>(vr[e][w >> 1], scale[e]) : Wide<T>::template get<false>(vr[e][w >> 1], scale[e]);
+          x[e] = w & 1 ? Wide<C>::template get<true>(vr[e][w >> 1], scale[e]) : Wide<C>::template get<false>(vr[e][w >> 1], scale[e]);
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          frag v;
-          if constexpr (sizeof(T) == 2) {
-            u32x4 y;
+          u32x4 y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              y[e] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, x[2 * e + 1]), __builtin_bit_cast(unsigned, x[2 * e]), f ? 0x07060302u : 0x05040100u);
-            v = __builtin_bit_cast(frag, y);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = x[e][f];
-          }
+          for (int e = 0; e < 4; ++e)
+            y[e] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, x[2 * e + 1]), __builtin_bit_cast(unsigned, x[2 * e]), f ? 0x07060302u : 0x05040100u);
+          frag v = __builtin_bit_cast(frag, y);
           product(v, 2 * w + f);
         }
       }
@@ -416,7 +442,9 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
       for (int z = 0; z < NS; ++z) {
         frag f = key_frag(k, z);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][k] = M::mma(f, qf[n][z], s[n][k]);
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) s[n][k] = M::mma(f, qf[n][z][p], s[n][k]);
       }
   };
   auto weights = [&](int j0, unsigned keep, auto edge) {
