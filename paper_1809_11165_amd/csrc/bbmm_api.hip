@@ -2600,13 +2600,17 @@ int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows,
   return BBMM_OK;
 }
 
-// Parts that the keys are split into, over workgroups: as many as fill the device once (two workgroups a compute unit) while parts keep kCachePart
-// keys, and up to eight a compute unit while they keep kCacheEvenPart, which evens out lengths that only the device knows; none where three a compute
-// unit are there anyway, but for parts of more than kCacheLongPart keys, which one long sequence among short ones must not leave to a few.
+// Parts that the keys are split into, over workgroups: as many as the device holds at once (`held` a compute unit) while parts keep kCachePart keys; or,
+// where parts of kCacheEvenPart keys make at least two such rounds, up to eight a compute unit, which evens out lengths that only the device knows
+// (between one round and two, the second is mostly empty); none where three a compute unit are there anyway, but for parts of more than
+// kCacheLongPart keys, which one long sequence among short ones must not leave to a few.
 constexpr int64_t kCachePart = 256, kCacheEvenPart = 1024, kCacheLongPart = 16384;
-int cache_parts(int64_t cus, int64_t wgs, int64_t reach) {
+int cache_parts(int64_t cus, int64_t held, int64_t wgs, int64_t reach) {
   int64_t n = 1;
-  if (wgs < 3 * cus) n = std::max(std::min(2 * cus / wgs, (reach + kCachePart - 1) / kCachePart), std::min(8 * cus / wgs, reach / kCacheEvenPart));
+  if (wgs < 3 * cus) {
+    int64_t round = std::max<int64_t>(held * cus / wgs, 1), many = std::min(8 * cus / wgs, reach / kCacheEvenPart);
+    n = many >= 2 * round ? many : std::min(round, (reach + kCachePart - 1) / kCachePart);
+  }
   return (int)std::max<int64_t>({n, (reach + kCacheLongPart - 1) / kCacheLongPart, 1});
 }
 // Sizes, the split of the keys, and, where `pointers` is set, everything else.
@@ -2633,7 +2637,8 @@ int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attentio
   if (cache->batch * in->heads * in->nq > kMaxRows || wgs > kAttMaxGrid) return fail(c, BBMM_EINVAL, "cached attention: more than 2^27 rows in one call");
   wgs = (int64_t)a->B * a->HK * t->blocks;
   int64_t reach = t->window ? std::min<int64_t>(a->rows_most, (int64_t)t->window + t->nq) : a->rows_most;
-  t->nsplit = cache_parts(c->num_cus, std::max<int64_t>(wgs, 1), reach);
+  int held = cache_held(in->type, cache->type == BBMM_TYPE_E4M3, *a, rows);
+  t->nsplit = cache_parts(c->num_cus, held, std::max<int64_t>(wgs, 1), reach);
   t->dv4 = (a->dv + 3) / 4 * 4;
   if (!pointers) return BBMM_OK;
   size_t e = elem_size(in->type);

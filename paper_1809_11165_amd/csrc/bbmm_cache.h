@@ -67,5 +67,6 @@ struct CacheAtt {
   int nsplit, dv4, ovec, blocks; // blocks of rows per shared head
 };
 int cache_rows(int type, int64_t rows);     // rows (query, head of the group) of a workgroup, where there are so many
+int cache_held(int type, int e4m3, const CacheArgs& c, int64_t rows);   // workgroups that a compute unit holds
 void launch_attend_cache(hipStream_t s, int type, int e4m3, const CacheArgs& c, const CacheAtt& a);
 void launch_attend_cache_join(hipStream_t s, int type, const CacheArgs& c, const CacheAtt& a);

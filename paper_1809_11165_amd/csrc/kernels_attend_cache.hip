@@ -88,10 +88,16 @@ __device__ __forceinline__ void in_three(const f32x8& x, bf16x8 (&p)[3]) {
 
 constexpr int kBlock = 32;                                 // keys of a wave's turn
 
-// One side (keys or values) of a block on its way: raw registers and the rows' exponents.
-//   T held as such: a piece is 16 bytes (values of up to 64 features in two bytes: 8); E4M3: the same features in a half or a quarter of that.
+// Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.
+constexpr int waves_of(int size, bool e4m3, int dp, int nt, bool even) {
+  if (nt == 2) return 2;
+  if (size == 4) return dp == 64 && (even || !e4m3) ? 3 : 2;
+  return dp == 64 ? (even ? 4 : 3) : e4m3 && even ? 3 : 2;
+}
+
+// T held as such: a key's piece is 16 bytes, a value's 16 (two-byte values of up to 64 features: 8); E4M3: the same features in a half or a quarter.
 template <typename T, bool E4M3, int DP, int NT, bool EVEN>
-__global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 3) void k_attend_cache(CacheArgs c, CacheAtt a) {
+__global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void k_attend_cache(CacheArgs c, CacheAtt a) {
   constexpr bool kThree = sizeof(T) == 4 && E4M3;          // operands in three parts of bf16
   constexpr int PARTS = kThree ? 3 : 1;
   typedef std::conditional_t<kThree, __bf16, T> C;         // type of the operands
@@ -135,12 +141,14 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
   auto find = [&](int t) {
     Pages p;
     if constexpr (EVEN) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint32_t at = (uint32_t)(t * kBlock + 16 * k), n = over(at, c.page);
-        p.row[k] = uniform((int)(at - n * c.page.d));
-        p.page[k] = -1;
-        if (at < (uint32_t)hi) p.page[k] = ((scalar_table)table)[uniform((int)n)];
+      uint32_t at = (uint32_t)(t * kBlock), n = over(at, c.page);
+      p.row[0] = uniform((int)(at - n * c.page.d));
+      p.page[0] = ((scalar_table)table)[uniform((int)n)];   // a block's first key lies before hi
+      p.row[1] = p.row[0] + 16;
+      p.page[1] = p.page[0];
+      if (p.row[1] == (int)c.page.d) {
+        p.row[1] = 0;
+        p.page[1] = at + 16 < (uint32_t)hi ? ((scalar_table)table)[uniform((int)n) + 1] : -1;
       }
     } else {
       uint32_t at = (uint32_t)(t * kBlock + (lane & 31)), n = over(at, c.page);
@@ -167,8 +175,9 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
   unsigned vr[8][VW];
   unsigned kx[2];                                          // E4M3: exponents of the lane's keys,
   u32x4 vx[2];                                             // and of its values' rows
-  unsigned koff = (unsigned)col * kpitch, voff = (unsigned)(4 * q4) * vpitch;
+  unsigned koff = (unsigned)col * kpitch + 16u * q4, voff = (unsigned)(4 * q4) * vpitch;
   auto fetch_k = [&](const Pages& p, unsigned keep) {
+    bool all = keep == ~0u;                                // mostly: then nothing is worked out for the lanes
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       bool ok = (keep >> (16 * k + col)) & 1;
@@ -176,11 +185,10 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
         bool there = (keep >> (16 * k)) & 0xffffu;
         int pg = there ? p.page[k] : 0, row = there ? p.row[k] : 0;
         __amdgpu_buffer_rsrc_t mem = bounded(K + pg * kpage + (int64_t)row * kpitch, there ? 15 * kpitch + (unsigned)(c.d * SB + 15) / 16 * 16 : 0u);
+        unsigned mine = all || ok ? koff : kNowhere;
 #pragma unroll
-        for (int s = 0; s < KP; ++s) {
-          unsigned at = 16u * (4 * s + q4);
-          kr[k][s] = __builtin_amdgcn_raw_buffer_load_b128(mem, ok && at < (unsigned)(c.d * SB) ? koff + at : kNowhere, 0, 0);
-        }
+        for (int s = 0; s < KP; ++s)
+          kr[k][s] = __builtin_amdgcn_raw_buffer_load_b128(mem, 16u * (4 * s + q4) < (unsigned)(c.d * SB) ? mine : kNowhere, 64 * s, 0);
         if constexpr (E4M3) {
           __amdgpu_buffer_rsrc_t ex = bounded(ke + pg * epage + (int64_t)row * 4, there ? 64u : 0u);
           kx[k] = __builtin_amdgcn_raw_buffer_load_b32(ex, 4 * col, 0, 0);
@@ -200,7 +208,8 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
   };
   auto fetch_v = [&](const Pages& p, unsigned keep) {
     unsigned o = (unsigned)(col * FV * SB);
-    bool mine = o < (unsigned)(c.dv * SB);
+    bool mine = o < (unsigned)(c.dv * SB), all = keep == ~0u;
+    unsigned vlane = mine ? voff + o : kNowhere;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       if constexpr (EVEN) {
@@ -209,21 +218,23 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
         __amdgpu_buffer_rsrc_t mem = bounded(V + pg * vpage + (int64_t)row * vpitch, there ? 15 * vpitch + (unsigned)(c.dv * SB + 15) / 16 * 16 : 0u);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          unsigned at = mine && ((keep >> (16 * k + 4 * q4 + r)) & 1) ? voff + r * vpitch + o : kNowhere;
+          bool ok = all || (keep >> (16 * k + 4 * q4 + r)) & 1;
+          unsigned at = ok ? vlane : kNowhere;
+          int step = (int)(r * vpitch);
           unsigned* v = vr[4 * k + r];
           if constexpr (VW == 1) {
-            v[0] = __builtin_amdgcn_raw_buffer_load_b32(mem, at, 0, 0);
+            v[0] = __builtin_amdgcn_raw_buffer_load_b32(mem, at, step, 0);
           } else if constexpr (VW == 2) {
-            auto w = __builtin_amdgcn_raw_buffer_load_b64(mem, at, 0, 0);
+            auto w = __builtin_amdgcn_raw_buffer_load_b64(mem, at, step, 0);
             v[0] = w[0], v[1] = w[1];
           } else if constexpr (VW == 4) {
-            u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, at, 0, 0);
+            u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, at, step, 0);
             v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3];
           } else {                                         // fp32, 128 features: 4 of each half
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
               unsigned f = 256u * z + 16u * col;
-              u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, ((keep >> (16 * k + 4 * q4 + r)) & 1) && f < 4u * c.dv ? voff + r * vpitch + f : kNowhere, 0, 0);
+              u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, ok && f < 4u * c.dv ? voff + 16u * col : kNowhere, step + 256 * z, 0);
               v[4 * z] = w[0], v[4 * z + 1] = w[1], v[4 * z + 2] = w[2], v[4 * z + 3] = w[3];
             }
           }
@@ -394,6 +405,7 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
           frag v = __builtin_bit_cast(frag, y);
           product(v, 2 * w + f);
         }
+        if (w & 1) __builtin_amdgcn_sched_barrier(0);
       }
     } else {
 #pragma unroll
@@ -409,6 +421,7 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
           for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(vr[e][f]);
         }
         product(v, f);
+        if (f & 1) __builtin_amdgcn_sched_barrier(0);      // else operands of all products are made ahead, and registers run out
       }
     }
   };
@@ -462,12 +475,8 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
             s[n][e >> 2][e & 3] = a.cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(z + 1.f));
           }
         }
-    } else {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[n][e >> 2][e & 3] *= a.c2;
     }
+    float mul = a.cap2 != 0.f ? 1.f : a.c2;
     if (decltype(edge)::value || keep != ~0u) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -490,6 +499,7 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
       float top = s[n][0][0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, s[n][e >> 2][e & 3]);
+      top *= mul;
       if (__any(top > m[n] + kSlack)) {
         top = quarters_max(top);
         bool move = top > m[n] + kSlack;
@@ -502,7 +512,7 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
       float ref = (m[n] == -__builtin_inff() ? 0.f : m[n]) - Lift<T>::value;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float y = __builtin_amdgcn_exp2f(s[n][e >> 2][e & 3] - ref);
+        float y = __builtin_amdgcn_exp2f(fmaf(s[n][e >> 2][e & 3], mul, -ref));
         s[n][e >> 2][e & 3] = y;
         l[n] += y;
       }
@@ -525,7 +535,9 @@ __global__ __launch_bounds__(256, NT == 2 ? 2 : sizeof(T) == 4 ? (DP == 64 ? 3 :
     next = t + 4 < a1 ? find(t + 4) : here;
     keep = kept(t, here);
     fetch_k(here, keep);
+    __builtin_amdgcn_sched_barrier(0);                     // in the loop's order: else its first wait is for all of them
     fetch_v(here, keep);
+    __builtin_amdgcn_sched_barrier(0);
   }
   for (; t < a1; t += 4) {
     scores();
@@ -714,6 +726,9 @@ void join_t(hipStream_t s, const CacheArgs& c, const CacheAtt& a) {
 }  // namespace
 
 int cache_rows(int type, int64_t rows) { return type != 0 && rows > 16 ? 32 : 16; }
+int cache_held(int type, int e4m3, const CacheArgs& c, int64_t rows) {
+  return waves_of(type == 0 ? 4 : 2, e4m3, c.d <= 64 && c.dv <= 64 ? 64 : 128, cache_rows(type, rows) / 16, c.page.d % 16 == 0);
+}
 
 void launch_attend_cache(hipStream_t s, int type, int e4m3, const CacheArgs& c, const CacheAtt& a) {
   if (type == 0) attend_t<float>(s, type, e4m3, c, a);
