@@ -2603,11 +2603,12 @@ int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows,
 // Parts that the keys are split into, over workgroups: as many as the device holds at once (`held` a compute unit) while parts keep kCachePart keys; or,
 // where parts of kCacheEvenPart keys make at least two such rounds, up to eight a compute unit, which evens out lengths that only the device knows
 // (between one round and two, the second is mostly empty); none where three a compute unit are there anyway, but for parts of more than
-// kCacheLongPart keys, which one long sequence among short ones must not leave to a few.
-constexpr int64_t kCachePart = 256, kCacheEvenPart = 1024, kCacheLongPart = 16384;
+// kCacheLongPart keys, which one long sequence among short ones must not leave to a few.  Up to kCacheWhole keys the second launch costs more than the
+// parts save (one request, 8 shared heads of 128, bf16, in parts / whole: 300 keys 9.7 / 8.6 us, 500 10.3 / 9.9, 1000 11.3 / 15.8).
+constexpr int64_t kCacheWhole = 384, kCachePart = 256, kCacheEvenPart = 1024, kCacheLongPart = 16384;
 int cache_parts(int64_t cus, int64_t held, int64_t wgs, int64_t reach) {
   int64_t n = 1;
-  if (wgs < 3 * cus) {
+  if (wgs < 3 * cus && reach > kCacheWhole) {
     int64_t round = std::max<int64_t>(held * cus / wgs, 1), many = std::min(8 * cus / wgs, reach / kCacheEvenPart);
     n = many >= 2 * round ? many : std::min(round, (reach + kCachePart - 1) / kCachePart);
   }
