@@ -2442,19 +2442,20 @@ int rotation_args(bbmm_ctx* c, const bbmm_rotation* in, bool pointers, RotArgs* 
   return BBMM_OK;
 }
 
-// Tokens of a workgroup: as many as its lanes hold rows of at a time (up to 8, whose angles are kept), fewer where the device has room left.  The
-// gradient's workgroups go on to further tokens, so that sums of the weights' gradients are few: three to a compute unit (what the registers
-// admit), dealt out to Q and K by their heads.
+// Tokens of a workgroup, up to 8, whose angles are kept: as many as give all its lanes rows, and more while that leaves four workgroups a compute unit.
+// The gradient's workgroups go on to further tokens, so that sums of the weights' gradients are few: four to a compute unit, dealt out to Q and K by
+// their heads.
 constexpr int64_t kRotBlocks = (int64_t)1 << 20;
 int64_t rotate_most(const bbmm_ctx* c, const RotArgs& a, int w) {
-  return std::max<int64_t>(1, 3 * (int64_t)c->num_cus * a.heads[w] / std::max<int64_t>((int64_t)a.heads[0] + a.heads[1], 1));
+  return std::max<int64_t>(1, 4 * (int64_t)c->num_cus * a.heads[w] / std::max<int64_t>((int64_t)a.heads[0] + a.heads[1], 1));
 }
 void rotate_plan(const bbmm_ctx* c, int type, bool grad, RotArgs* a) {
-  int hand = rotate_rows(type, grad, a->d, a->vec);
+  int64_t hand = rotate_rows(type, a->d, a->vec), cus = c->num_cus;
   bool one = a->tokens && (a->w[0] || a->w[1]) && a->tokens * std::max(a->heads[0], a->heads[1]) <= 2 * hand;
   for (int w = 0; w < 2; ++w) {
     if (!a->heads[w]) continue;
-    int64_t t = std::min<int64_t>({hand / a->heads[w], BBMM_ROT_TOKENS, (a->tokens + c->num_cus - 1) / c->num_cus});
+    int64_t t = std::min((hand + a->heads[w] - 1) / a->heads[w], (a->tokens + cus - 1) / cus);
+    t = std::min<int64_t>(std::max(t, a->tokens / (4 * cus)), BBMM_ROT_TOKENS);
     // few rows: one workgroup goes over them all, and what it sums needs no joining (15 tokens of 4 + 4 heads of 96,
     // bf16, forward and gradient: 13.9 us, so 11.1)
     if (grad && one) t = std::min<int64_t>(a->tokens, BBMM_ROT_TOKENS);

@@ -31,7 +31,7 @@ void launch_rotate(hipStream_t s, int type, const RotArgs& a);
 void launch_rotate_grad(hipStream_t s, int type, const RotArgs& a);                    // and what each workgroup has of the weights' gradients
 void launch_rotate_join(hipStream_t s, int type, const RotArgs& a, void* dq_weight, void* dk_weight);
 // Rows that a workgroup has in hand at a time.
-int rotate_rows(int type, bool grad, int d, int vec);
+int rotate_rows(int type, int d, int vec);
 
 struct CacheArgs {
   void *K, *V;

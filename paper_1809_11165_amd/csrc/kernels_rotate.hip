@@ -156,19 +156,21 @@ __device__ __forceinline__ float norm_row(float* x, float inv_d, float eps32, do
   return scale * r;
 }
 
-// A run of rows of a workgroup: row r of its tokens is head r % heads of token r / heads.
+// Row r of a workgroup's tokens: head r % heads of token r / heads.  Its place in one or two inputs, and whether it is there.
 template <typename T>
-struct Cursor {
-  const T* row[2];                                          // of up to two inputs
-  int token, head;                                          // token of the workgroup
+struct Place {
+  const T* row[2];
+  int token;
   bool live;
-  // s1 null: one input only
-  __device__ __forceinline__ void token_start(const RotArgs& a, uint32_t tok0, const T* x0, const int64_t* s0, const T* x1, const int64_t* s1) {
+  __device__ __forceinline__ Place(const RotArgs& a, int which, uint32_t tok0, int r, int n, const T* x0, const int64_t* s0, const T* x1, const int64_t* s1) {
+    r = min(r, n - 1);
+    token = (int)over(r, a.by_heads[which]);
+    int head = r - token * a.heads[which];
     uint32_t tok = tok0 + token, b = over(tok, a.by_rows);
     int i = (int)(tok - b * (uint32_t)a.rows);
     live = !a.len || i < a.len[b];
     row[0] = x0 + (int64_t)b * s0[0] + (int64_t)i * s0[1] + (int64_t)head * s0[2];
-    if (x1) row[1] = x1 + (int64_t)b * s1[0] + (int64_t)i * s1[1] + (int64_t)head * s1[2];
+    row[1] = x1 ? x1 + (int64_t)b * s1[0] + (int64_t)i * s1[1] + (int64_t)head * s1[2] : nullptr;
   }
 };
 
@@ -176,12 +178,12 @@ __device__ __forceinline__ void fill_trig(const RotArgs& a, float2* trig, int64_
   int half = a.rot >> 1;
   for (int i = tid; i < n * half; i += 256) {
     int t = i / half, p = i - t * half;
-    if (tok0 + t < a.tokens) trig[t * (BBMM_ATT_MAXD / 2) + p] = turn_of(a.pos[(int64_t)a.axis[p] * a.tokens + tok0 + t], a.freq[p]);
+    trig[t * (BBMM_ATT_MAXD / 2) + p] = turn_of(a.pos[(int64_t)a.axis[p] * a.tokens + tok0 + t], a.freq[p]);
   }
 }
 
-// Rows of the workgroup's tokens: a group of LPR lanes takes U neighbouring rows at a time, of one token mostly, whose angles it then keeps.
-template <typename T, int E, int LPR, int KS, int U, bool NB>
+// Rows of the workgroup's tokens, a group of LPR lanes a row at a time; the next one is on its way meanwhile.
+template <typename T, int E, int LPR, int KS, bool NB>
 __global__ __launch_bounds__(256) void k_rotate(RotArgs a) {
   typedef Row<T, E, LPR, KS, NB> Rows;
   constexpr int GP = 256 / LPR, M = Rows::N * KS;
@@ -193,68 +195,58 @@ __global__ __launch_bounds__(256) void k_rotate(RotArgs a) {
   T* y = (T*)a.y[which];
   float w[M];
   if (a.norm) rows.weights(w, (const T*)a.w[which]);
-  typename Rows::Raw raw[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) Rows::clear(raw[u]);
-  for (int64_t tok0 = (int64_t)blk * per; tok0 < a.tokens; tok0 += (int64_t)a.blocks[which] * per) {
-    int n = (int)min((int64_t)per, a.tokens - tok0) * heads;
-    int mine = min(U, (n + GP - 1) / GP);                  // rows of a group at a time
-    bool live[U];
-    int token[U];
-    auto load = [&](int r0) {
-      Cursor<T> at;
-      at.token = (int)over(r0, a.by_heads[which]);
-      at.head = r0 - at.token * heads;
-      if (r0 < n) at.token_start(a, (uint32_t)tok0, x, a.xs[which], (const T*)nullptr, nullptr);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u == mine) break;
-        live[u] = r0 + u < n && at.live;
-        token[u] = at.token;
-        if (live[u]) rows.load(raw[u], at.row[0]);
-        at.row[0] += a.xs[which][2];
-        if (u + 1 < U && ++at.head == heads) {
-          at.head = 0;
-          ++at.token;
-          if (r0 + u + 1 < n) at.token_start(a, (uint32_t)tok0, x, a.xs[which], (const T*)nullptr, nullptr);
-        }
-      }
+  struct Hand {
+    typename Rows::Raw x;
+    int token;
+    bool live;
+  } one, two;
+  Rows::clear(one.x);
+  Rows::clear(two.x);
+  int64_t last = a.tokens * (blk + 1) / a.blocks[which];    // the workgroups' shares differ by a token at most
+  for (int64_t tok0 = a.tokens * blk / a.blocks[which]; tok0 < last; tok0 += per) {
+    int some = (int)min((int64_t)per, last - tok0), n = some * heads;
+    auto load = [&](Hand& h, int r) {
+      Place<T> at(a, which, (uint32_t)tok0, r, n, x, a.xs[which], (const T*)nullptr, nullptr);
+      h.token = at.token;
+      h.live = at.live;
+      if (at.live) rows.load(h.x, at.row[0]);
     };
-    int r0 = tid / LPR * mine;
-    load(r0);                                              // on their way while the angles are formed
-    fill_trig(a, trig, tok0, per, tid);
-    __syncthreads();
-    for (;;) {
-      float2 t[KS * E];
-      if (r0 < n) rows.angles(t, trig + token[0] * (BBMM_ATT_MAXD / 2));
+    auto work = [&](const Hand& h, int r) {
+      if (r >= n) return;
+      float v[M];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u == mine || r0 + u >= n) break;
-        if (u && token[u] != token[u - 1]) rows.angles(t, trig + token[u] * (BBMM_ATT_MAXD / 2));
-        float v[M];
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = h.live ? Rows::at(h.x, k, i) : 0.f;
+      if (h.live) {
+        float2 t[KS * E];
+        rows.angles(t, trig + h.token * (BBMM_ATT_MAXD / 2));
+        if (a.norm) {
+          norm_row<LPR, M>(v, a.inv_d, a.eps32, a.eps);
 #pragma unroll
-          for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = live[u] ? Rows::at(raw[u], k, i) : 0.f;
-        if (live[u]) {
-          if (a.norm) {
-            norm_row<LPR, M>(v, a.inv_d, a.eps32, a.eps);
-#pragma unroll
-            for (int i = 0; i < M; ++i) v[i] *= w[i];
-          }
-          rows.template turn<false>(v, t);
+          for (int i = 0; i < M; ++i) v[i] *= w[i];
         }
-        rows.store(y + ((tok0 * heads) + r0 + u) * a.d, v);
+        rows.template turn<false>(v, t);
       }
-      r0 += mine * GP;
-      if (r0 - tid / LPR * mine >= n) break;
-      load(r0);
+      rows.store(y + ((tok0 * heads) + r) * a.d, v);
+    };
+    int g = tid / LPR;
+    load(one, g);                                          // on its way while the angles are formed
+    fill_trig(a, trig, tok0, some, tid);
+    __syncthreads();
+    for (int r0 = 0;; r0 += 2 * GP) {
+      if (r0 + GP < n) load(two, r0 + GP + g);
+      work(one, r0 + g);
+      if (r0 + GP >= n) break;
+      if (r0 + 2 * GP < n) load(one, r0 + 2 * GP + g);
+      work(two, r0 + GP + g);
+      if (r0 + 2 * GP >= n) break;
     }
     __syncthreads();
   }
 }
 
-template <typename T, int E, int LPR, int KS, int U, bool NB>
+template <typename T, int E, int LPR, int KS, bool NB>
 __global__ __launch_bounds__(256) void k_rotate_grad(RotArgs a) {
   typedef Row<T, E, LPR, KS, NB> Rows;
   constexpr int GP = 256 / LPR, M = Rows::N * KS;
@@ -269,81 +261,65 @@ __global__ __launch_bounds__(256) void k_rotate_grad(RotArgs a) {
   if (a.norm) rows.weights(w, (const T*)a.w[which]);
 #pragma unroll
   for (int i = 0; i < M; ++i) dw[i] = 0.f;
-  typename Rows::Raw rx[U], rg[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    Rows::clear(rx[u]);
-    Rows::clear(rg[u]);
-  }
-  for (int64_t tok0 = (int64_t)blk * per; tok0 < a.tokens; tok0 += (int64_t)a.blocks[which] * per) {
-    int n = (int)min((int64_t)per, a.tokens - tok0) * heads;
-    int mine = min(U, (n + GP - 1) / GP);
-    bool live[U];
-    int token[U];
-    auto load = [&](int r0) {
-      Cursor<T> at;
-      at.token = (int)over(r0, a.by_heads[which]);
-      at.head = r0 - at.token * heads;
-      if (r0 < n) at.token_start(a, (uint32_t)tok0, g, a.gs[which], x, a.xs[which]);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u == mine) break;
-        live[u] = r0 + u < n && at.live;
-        token[u] = at.token;
-        if (live[u]) {
-          rows.load(rg[u], at.row[0]);
-          if (a.norm) rows.load(rx[u], at.row[1]);
-        }
-        at.row[0] += a.gs[which][2];
-        if (a.norm) at.row[1] += a.xs[which][2];
-        if (u + 1 < U && ++at.head == heads) {
-          at.head = 0;
-          ++at.token;
-          if (r0 + u + 1 < n) at.token_start(a, (uint32_t)tok0, g, a.gs[which], x, a.xs[which]);
-        }
+  struct Hand {
+    typename Rows::Raw x, g;
+    int token;
+    bool live;
+  } one;
+  Rows::clear(one.x);
+  Rows::clear(one.g);
+  int64_t last = a.tokens * (blk + 1) / a.blocks[which];    // the workgroups' shares differ by a token at most
+  for (int64_t tok0 = a.tokens * blk / a.blocks[which]; tok0 < last; tok0 += per) {
+    int some = (int)min((int64_t)per, last - tok0), n = some * heads;
+    auto load = [&](Hand& h, int r) {
+      Place<T> at(a, which, (uint32_t)tok0, r, n, g, a.gs[which], x, a.xs[which]);
+      h.token = at.token;
+      h.live = at.live;
+      if (at.live) {
+        rows.load(h.g, at.row[0]);
+        if (a.norm) rows.load(h.x, at.row[1]);
       }
     };
-    int r0 = tid / LPR * mine;
-    load(r0);
-    fill_trig(a, trig, tok0, per, tid);
-    __syncthreads();
-    for (;;) {
-      float2 t[KS * E];
-      if (r0 < n) rows.angles(t, trig + token[0] * (BBMM_ATT_MAXD / 2));
+    auto work = [&](const Hand& h, int r) {
+      if (r >= n) return;
+      float v[M];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u == mine || r0 + u >= n) break;
-        if (u && token[u] != token[u - 1]) rows.angles(t, trig + token[u] * (BBMM_ATT_MAXD / 2));
-        float v[M];
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = h.live ? Rows::at(h.g, k, i) : 0.f;
+      if (h.live) {
+        float2 t[KS * E];
+        rows.angles(t, trig + h.token * (BBMM_ATT_MAXD / 2));
+        rows.template turn<true>(v, t);
+        if (a.norm) {
+          float nx[M];
 #pragma unroll
-          for (int i = 0; i < Rows::N; ++i) v[k * Rows::N + i] = live[u] ? Rows::at(rg[u], k, i) : 0.f;
-        if (live[u]) {
-          rows.template turn<true>(v, t);
-          if (a.norm) {
-            float nx[M];
+          for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+            for (int i = 0; i < Rows::N; ++i) nx[k * Rows::N + i] = Rows::at(h.x, k, i);
+          float rr = norm_row<LPR, M>(nx, a.inv_d, a.eps32, a.eps), dot = 0.f;
 #pragma unroll
-              for (int i = 0; i < Rows::N; ++i) nx[k * Rows::N + i] = Rows::at(rx[u], k, i);
-            float rr = norm_row<LPR, M>(nx, a.inv_d, a.eps32, a.eps), dot = 0.f;
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-              dw[i] = fmaf(v[i], nx[i], dw[i]);
-              v[i] *= w[i];
-              dot = fmaf(v[i], nx[i], dot);
-            }
-            dot = row_sum<LPR>(dot) * a.inv_d;
-#pragma unroll
-            for (int i = 0; i < M; ++i) v[i] = rr * fmaf(-nx[i], dot, v[i]);
+          for (int i = 0; i < M; ++i) {
+            dw[i] = fmaf(v[i], nx[i], dw[i]);
+            v[i] *= w[i];
+            dot = fmaf(v[i], nx[i], dot);
           }
+          dot = row_sum<LPR>(dot) * a.inv_d;
+#pragma unroll
+          for (int i = 0; i < M; ++i) v[i] = rr * fmaf(-nx[i], dot, v[i]);
         }
-        rows.store(dx + ((tok0 * heads) + r0 + u) * a.d, v);
       }
-      r0 += mine * GP;
-      if (r0 - tid / LPR * mine >= n) break;
-      load(r0);
+      rows.store(dx + ((tok0 * heads) + r) * a.d, v);
+    };
+    int gr = tid / LPR;
+    load(one, gr);
+    fill_trig(a, trig, tok0, some, tid);
+    __syncthreads();
+    for (int r0 = 0;;) {
+      work(one, r0 + gr);
+      r0 += GP;
+      if (r0 >= n) break;
+      load(one, r0 + gr);
     }
     __syncthreads();
   }
@@ -403,30 +379,29 @@ __global__ __launch_bounds__(1024) void k_rotate_join(RotArgs a, T* dq, T* dk, i
 }
 
 // 16-byte pieces: lanes of a row for features up to 32, 64, 128; else single elements, 16 lanes and four slots each.
-template <typename T, int U, typename F>
+template <typename T, typename F>
 void rotate_shape(const RotArgs& a, F f) {
   constexpr int E = 16 / (int)sizeof(T);
-  if (!a.vec) f(Const<1>{}, Const<16>{}, Const<4>{}, Const<(U > 2 ? 2 : 1)>{});
-  else if (a.d <= 32) f(Const<E>{}, Const<16 / E>{}, Const<1>{}, Const<U>{});
-  else if (a.d <= 64) f(Const<E>{}, Const<32 / E>{}, Const<1>{}, Const<U>{});
-  else f(Const<E>{}, Const<64 / E>{}, Const<1>{}, Const<U>{});
+  if (!a.vec) f(Const<1>{}, Const<16>{}, Const<4>{});
+  else if (a.d <= 32) f(Const<E>{}, Const<16 / E>{}, Const<1>{});
+  else if (a.d <= 64) f(Const<E>{}, Const<32 / E>{}, Const<1>{});
+  else f(Const<E>{}, Const<64 / E>{}, Const<1>{});
 }
-constexpr int kFwd = 2, kBwd = 1;            // rows of a group in hand (4 and 2: prompt of 8192 x 40 heads of 128, bf16 44.2 us, so 41.8; training step 65.9, 61.5)
 
 template <typename T>
 void rotate_t(hipStream_t s, const RotArgs& a) {
-  rotate_shape<T, kFwd>(a, [&](auto e, auto l, auto k, auto u) {
-    constexpr int E = decltype(e)::value, L = decltype(l)::value, K = decltype(k)::value, U = decltype(u)::value;
-    if (a.neighbours) k_rotate<T, E, L, K, U, true><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
-    else k_rotate<T, E, L, K, U, false><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+  rotate_shape<T>(a, [&](auto e, auto l, auto k) {
+    constexpr int E = decltype(e)::value, L = decltype(l)::value, K = decltype(k)::value;
+    if (a.neighbours) k_rotate<T, E, L, K, true><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+    else k_rotate<T, E, L, K, false><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
   });
 }
 template <typename T>
 void rotate_grad_t(hipStream_t s, const RotArgs& a) {
-  rotate_shape<T, kBwd>(a, [&](auto e, auto l, auto k, auto u) {
-    constexpr int E = decltype(e)::value, L = decltype(l)::value, K = decltype(k)::value, U = decltype(u)::value;
-    if (a.neighbours) k_rotate_grad<T, E, L, K, U, true><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
-    else k_rotate_grad<T, E, L, K, U, false><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+  rotate_shape<T>(a, [&](auto e, auto l, auto k) {
+    constexpr int E = decltype(e)::value, L = decltype(l)::value, K = decltype(k)::value;
+    if (a.neighbours) k_rotate_grad<T, E, L, K, true><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
+    else k_rotate_grad<T, E, L, K, false><<<a.blocks[0] + a.blocks[1], 256, 0, s>>>(a);
   });
 }
 template <typename T>
@@ -437,13 +412,13 @@ void rotate_join_t(hipStream_t s, const RotArgs& a, void* dq, void* dk) {
 
 }  // namespace
 
-int rotate_rows(int type, bool grad, int d, int vec) {
+int rotate_rows(int type, int d, int vec) {
   int n = 0;
   RotArgs a{};
   a.d = d, a.vec = vec;
-  auto f = [&](auto, auto l, auto, auto u) { n = 256 / decltype(l)::value * decltype(u)::value; };
-  if (type == 0) grad ? rotate_shape<float, kBwd>(a, f) : rotate_shape<float, kFwd>(a, f);
-  else grad ? rotate_shape<__bf16, kBwd>(a, f) : rotate_shape<__bf16, kFwd>(a, f);
+  auto f = [&](auto, auto l, auto) { n = 256 / decltype(l)::value; };
+  if (type == 0) rotate_shape<float>(a, f);
+  else rotate_shape<__bf16>(a, f);
   return n;
 }
 void launch_rotate(hipStream_t s, int type, const RotArgs& a) {
