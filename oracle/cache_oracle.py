@@ -6,14 +6,14 @@
     attention  s_ij = scale q_i.k_j or cap tanh(scale q_i.k_j / cap) over the keys that row i takes; o_i = sum softmax(s_i)_j v_j
 
 Beside every value stands an elementwise bound on what rounding may do to it when norms, functions, scores and sums are fp32 (unit u32 = 2^-24;
-sums of n terms n u32) and outputs, and weights as operands, are rounded to the type once (unit u):
+sums of n terms n u32) and outputs are rounded to the type once (unit u), weights as operands twice (what the first rounding leaves is a second operand):
     r          er = (d / 2 + 8) u32 of itself: d squares, the root;   cos, sin   ec = 6 u32 + 2^-51 |angle|, absolutely
     y          (|z_a| + |z_b|) (ec + er + 5 u32) + u |y|
     dz         e_dz = (|dy_a| + |dy_b|) (ec + 3 u32)
     dw         sum |n| (e_dz + |dz| (er + (terms + 2) u32)) + u |dw| + terms 2^-150 (sums of tiny terms)
     dx         r (|w| e_dz + |n| e_m + (2 er + 8 u32) (|w dz| + |n m|)) + u |dx|,   m the mean, e_m = mean |n| (|w| e_dz + |w dz| (er + (d + 4) u32))
     scores     ds = 2 (d + 8) u32 max_j (scale sum |q||k| + |lse|) + 16 u32 cap   (of a weight; tanh is off by less than 8 u32)
-    o          (u + ds + n u32) sum p|v| + u |o|
+    o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|
 fp16 adds half a step of its subnormal numbers (weights are lifted by 2^6 before they meet them).
 """
 from __future__ import annotations
@@ -140,9 +140,9 @@ def taken(n, nq, total, causal=True, window=0):
     return keep
 
 
-def attend(kind, Q, K, V, scale, k_len, q_len=None, causal=True, window=0, cap=0.0, there=None):
-    """Q (batch, nq, heads, d); K, V (batch, rows, kv_heads, .) of every sequence; there (batch, rows): rows whose page is there.
-    Returns (values, bounds): dicts with o and lse."""
+def attend(kind, Q, K, V, scale, k_len, q_len=None, causal=True, window=0, cap=0.0, there=None, once=False):
+    """Q (batch, nq, heads, d); K, V (batch, rows, kv_heads, .) of every sequence; there (batch, rows): rows whose page is there;
+    once: weights are rounded once only, as bbmm_attend does.  Returns (values, bounds): dicts with o and lse."""
     u, tiny = UNIT[kind], TINY[kind]
     B, nq, H, d = Q.shape
     total, HK, dv = K.shape[1], K.shape[2], V.shape[3]
@@ -171,6 +171,6 @@ def attend(kind, Q, K, V, scale, k_len, q_len=None, causal=True, window=0, cap=0
                 ds = 2 * (d + 8) * U32 * (big + abs(lse)) + 16 * U32 * cap
                 o = p @ v
                 val["o"][b, i, h], val["lse"][b, h, i] = o, lse
-                err["o"][b, i, h] = (u + ds + len(at) * U32) * (p @ np.abs(v)) + u * np.abs(o) + tiny * (1 + 2.0 ** -4 * np.abs(v).sum(0))
+                err["o"][b, i, h] = ((u if once else u * u) + ds + (len(at) + 1) * U32) * (p @ np.abs(v)) + u * np.abs(o) + tiny * (1 + 2.0 ** -4 * np.abs(v).sum(0))
                 err["lse"][b, h, i] = ds + (len(at) + 4) * U32 + 4 * U32 * abs(lse)
     return val, err

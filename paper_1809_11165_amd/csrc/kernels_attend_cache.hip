@@ -99,7 +99,8 @@ constexpr int waves_of(int size, bool e4m3, int dp, int nt, bool even) {
 template <typename T, bool E4M3, int DP, int NT, bool EVEN>
 __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void k_attend_cache(CacheArgs c, CacheAtt a) {
   constexpr bool kThree = sizeof(T) == 4 && E4M3;          // operands in three parts of bf16
-  constexpr int PARTS = kThree ? 3 : 1;
+  constexpr int PARTS = kThree ? 3 : 1;                    // of the queries, and of the weights:
+  constexpr int WPARTS = kThree ? 3 : sizeof(T) == 2 ? 2 : 1;   // what rounding to T leaves is a second operand, and costs nothing beside the reads
   typedef std::conditional_t<kThree, __bf16, T> C;         // type of the operands
   typedef Mma<C> M;
   typedef typename M::frag frag;
@@ -359,24 +360,27 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
 
   // O^T += V^T P^T; s[n][k][r]: weight of row n, key 16 k + 4 q4 + r.  fp32: eight single products make a step, of four keys each.
   auto add_values = [&](const f32x4 (*p)[2], unsigned keep, auto odd) {
-    frag pf[NT][PARTS];
+    frag pf[NT][WPARTS];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       if constexpr (kThree) {
         in_three(__builtin_shufflevector(p[n][0], p[n][1], 0, 1, 2, 3, 4, 5, 6, 7), pf[n]);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pf[n][0][e] = (T)p[n][e >> 2][e & 3];
+        for (int e = 0; e < 8; ++e) {
+          pf[n][0][e] = (T)p[n][e >> 2][e & 3];
+          if constexpr (WPARTS == 2) pf[n][1][e] = (T)(p[n][e >> 2][e & 3] - (float)pf[n][0][e]);
+        }
       }
     }
     auto product = [&](frag v, int f) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         if constexpr (decltype(odd)::value) {
-          acc[n][f] = mma_odd<C, PARTS>(v, pf[n], acc[n][f]);
+          acc[n][f] = mma_odd<C, WPARTS>(v, pf[n], acc[n][f]);
         } else {
 #pragma unroll
-          for (int x = 0; x < PARTS; ++x) acc[n][f] = M::mma(v, pf[n][x], acc[n][f]);
+          for (int x = 0; x < WPARTS; ++x) acc[n][f] = M::mma(v, pf[n][x], acc[n][f]);
         }
       }
     };

@@ -498,8 +498,8 @@ def test_a_sequence_decoded_token_by_token(ctx):
         whole = binding.Attention(q, k, v, table=edges, edges=[])
         O, lse = ctx.bbmm_attend(whole)
         got = torch.cat([x for x, _ in rows], 1), torch.cat([x for _, x in rows], 2)
-        val, err = A.attend("bf16", _host(q), _host(k), _host(v), d ** -0.5, [total] * B)
-        for pair in (got, (O, lse)):
+        for pair, once in ((got, False), ((O, lse), True)):
+            val, err = A.attend("bf16", _host(q), _host(k), _host(v), d ** -0.5, [total] * B, once=once)
             _check(pair[0], val, err, "o")
             _check(pair[1], val, err, "lse")
 
