@@ -2601,19 +2601,27 @@ int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows,
   return BBMM_OK;
 }
 
-// Parts that the keys are split into, over workgroups: as many as the device holds at once (`held` a compute unit) while parts keep kCachePart keys; or,
-// where parts of kCacheEvenPart keys make at least two such rounds, up to eight a compute unit, which evens out lengths that only the device knows
-// (between one round and two, the second is mostly empty); none where three a compute unit are there anyway, but for parts of more than
-// kCacheLongPart keys, which one long sequence among short ones must not leave to a few.  Up to kCacheWhole keys the second launch costs more than the
-// parts save (one request, 8 shared heads of 128, bf16, in parts / whole: 300 keys 9.7 / 8.6 us, 500 10.3 / 9.9, 1000 11.3 / 15.8).
-constexpr int64_t kCacheWhole = 384, kCachePart = 256, kCacheEvenPart = 1024, kCacheLongPart = 16384;
-int cache_parts(int64_t cus, int64_t held, int64_t wgs, int64_t reach) {
-  int64_t n = 1;
-  if (wgs < 3 * cus && reach > kCacheWhole) {
-    int64_t round = std::max<int64_t>(held * cus / wgs, 1), many = std::min(8 * cus / wgs, reach / kCacheEvenPart);
-    n = many >= 2 * round ? many : std::min(round, (reach + kCachePart - 1) / kCachePart);
+// Parts that the keys of all sequences are split into, over workgroups.  As many as the device holds at once (`held` a compute unit, `units` workgroups a
+// part) while parts keep kCachePart keys; or, where parts of kCacheEvenPart keys make at least two such rounds, up to eight a compute unit (between one
+// round and two, the second is mostly empty).  Where three workgroups a compute unit are there anyway, one round more, which shortens a long sequence
+// among short ones.  Up to kCacheWhole keys the second launch costs more than the parts save (one request, 8 shared heads of 128, bf16, in parts /
+// whole: 300 keys 9.7 / 8.6 us, 500 10.3 / 9.9, 1000 11.3 / 15.8).  `reach`: what the table (or the window) has room for.  From kCacheDeal keys on
+// (kCacheDealMany, if three workgroups a compute unit are not there) the kernel deals the parts out by the lengths, which only the device knows, where there are several (one sequence of 65536 keys beside 127 of 500, 8
+// shared heads of 128, bf16: the same number of parts for each 235 us, dealt 104; 8 of up to 32773 130 / 126; but 2 of 10000 26.8 / 30.5).
+constexpr int64_t kCacheWhole = 384, kCacheDeal = 4096, kCacheDealMany = 16384, kCachePart = 256, kCacheEvenPart = 1024, kCacheBlock = 32, kCacheShare = 256;
+void cache_parts(int64_t cus, int64_t held, int64_t batch, int64_t units, int64_t reach, CacheAtt* t) {
+  bool filled = batch * units >= 3 * cus, deal = batch > 1 && batch <= kCacheShare && reach > (filled ? kCacheDeal : kCacheDealMany);
+  int64_t round = std::max<int64_t>(held * cus / units, 1), n = batch;
+  if (filled) {
+    if (deal) n = batch + round;
+  } else if (reach > kCacheWhole) {
+    int64_t many = std::min(8 * cus / units, batch * reach / kCacheEvenPart);
+    n = std::max(batch, many >= 2 * round ? many : std::min(round, batch * ((reach + kCachePart - 1) / kCachePart)));
   }
-  return (int)std::max<int64_t>({n, (reach + kCacheLongPart - 1) / kCacheLongPart, 1});
+  t->dealt = deal && n > batch;
+  t->even = t->dealt || !batch ? 1 : (int)(n / batch);
+  t->items = t->dealt ? (int)n : (int)batch * t->even;
+  t->least = (int)(kCachePart / kCacheBlock);
 }
 // Sizes, the split of the keys, and, where `pointers` is set, everything else.
 int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attention* in, bool pointers, CacheArgs* a, CacheAtt* t) {
@@ -2637,12 +2645,12 @@ int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attentio
   t->blocks = (int)((rows + tile - 1) / tile);
   int64_t wgs = cache->batch * cache->kv_heads * ((rows + 15) / 16);
   if (cache->batch * in->heads * in->nq > kMaxRows || wgs > kAttMaxGrid) return fail(c, BBMM_EINVAL, "cached attention: more than 2^27 rows in one call");
-  wgs = (int64_t)a->B * a->HK * t->blocks;
   int64_t reach = t->window ? std::min<int64_t>(a->rows_most, (int64_t)t->window + t->nq) : a->rows_most;
-  int held = cache_held(in->type, cache->type == BBMM_TYPE_E4M3, *a, rows);
-  t->nsplit = cache_parts(c->num_cus, held, std::max<int64_t>(wgs, 1), reach);
+  cache_parts(c->num_cus, cache_held(in->type, cache->type == BBMM_TYPE_E4M3, *a, rows), a->B, std::max<int64_t>((int64_t)a->HK * t->blocks, 1), reach, t);
   t->dv4 = (a->dv + 3) / 4 * 4;
   if (!pointers) return BBMM_OK;
+  t->by_blocks = div_by((uint32_t)std::max(t->blocks, 1)), t->by_hk = div_by((uint32_t)a->HK), t->by_even = div_by((uint32_t)t->even);
+  t->by_nq = div_by((uint32_t)std::max(t->nq, 1)), t->by_heads = div_by((uint32_t)t->H);
   size_t e = elem_size(in->type);
   bool some = a->B && t->nq;
   if (some && (!in->Q || !in->k_len)) return fail(c, BBMM_EINVAL, "cached attention: Q and k_len are required");
@@ -2655,14 +2663,15 @@ int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attentio
 }
 
 struct CachedWork {
-  size_t pl, bytes;
+  size_t pl, first, bytes;
 };
 CachedWork cached_work(const CacheArgs& a, const CacheAtt& t) {
   CachedWork w{};
-  if (t.nsplit > 1) {
-    size_t rows = (size_t)a.B * t.H * t.nq * t.nsplit;
+  if (t.items > a.B && t.nq) {
+    size_t rows = (size_t)t.items * t.H * t.nq;
     w.pl = step256(rows * t.dv4 * sizeof(float));
-    w.bytes = w.pl + step256(rows * sizeof(float));
+    w.first = w.pl + step256(rows * sizeof(float));
+    w.bytes = w.first + step256((a.B + 1) * sizeof(int));
   }
   return w;
 }
@@ -2678,12 +2687,12 @@ int attend_cache(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attenti
   CachedWork w = cached_work(a, t);
   rc = check_work(c, work, work_bytes, w.bytes);
   if (rc) return rc;
-  t.O = O, t.lse = lse, t.pO = (float*)work, t.pl = (float*)((char*)work + w.pl);
+  t.O = O, t.lse = lse, t.pO = (float*)work, t.pl = (float*)((char*)work + w.pl), t.first = (int*)((char*)work + w.first);
   t.ovec = wide_rows(O, nullptr, a.dv, e, 4 * e);
   OnDevice dev(c->device);
   HIPCHK(c, dev.err);
   launch_attend_cache(c->stream, in->type, cache->type == BBMM_TYPE_E4M3, a, t);
-  if (t.nsplit > 1) launch_attend_cache_join(c->stream, in->type, a, t);
+  if (t.items > a.B) launch_attend_cache_join(c->stream, in->type, a, t);
   HIPCHK(c, hipGetLastError());
   return BBMM_OK;
 }

@@ -63,8 +63,12 @@ struct CacheAtt {
   float cap2, cap_in;            // cap log2(e), scale / cap (0: none)
   void* O;                       // dense
   float* lse;
-  float *pO, *pl;                // parts: nsplit x B x H x nq (x dv4), and their log2 sums
-  int nsplit, dv4, ovec, blocks; // blocks of rows per shared head
+  float *pO, *pl;                // parts: items x H x nq (x dv4), and their log2 sums
+  int* first;                    // each sequence's first item, and one behind the last: B + 1
+  int items, even, dealt;        // parts of all sequences; `even` of each, or (dealt) as the lengths want it, `items` in all at most
+  int least;                     // blocks of 32 keys in a part, at least (dealt)
+  int dv4, ovec, blocks;         // blocks of rows per shared head
+  Div by_blocks, by_hk, by_even, by_nq, by_heads;
 };
 int cache_rows(int type, int64_t rows);     // rows (query, head of the group) of a workgroup, where there are so many
 int cache_held(int type, int e4m3, const CacheArgs& c, int64_t rows);   // workgroups that a compute unit holds

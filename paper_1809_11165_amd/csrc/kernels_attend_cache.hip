@@ -88,6 +88,86 @@ __device__ __forceinline__ void in_three(const f32x8& x, bf16x8 (&p)[3]) {
 
 constexpr int kBlock = 32;                                 // keys of a wave's turn
 
+__device__ __forceinline__ int queries_of(const CacheAtt& a, int b) { return a.q_len ? uniform(min(max(a.q_len[b], 0), a.nq)) : a.nq; }
+__device__ __forceinline__ int keys_of(const CacheArgs& c, const CacheAtt& a, int b) { return uniform((int)min((int64_t)max(a.k_len[b], 0), c.rows_most)); }
+
+// Blocks that a sequence's rows take, and the first of them; one where there are none (somebody has to write its rows).
+__device__ __forceinline__ int blocks_of(const CacheAtt& a, int qn, int kn, int* first) {
+  int64_t p = (int64_t)kn - qn;
+  int lo = a.window ? (int)min(max(p - a.window + 1, (int64_t)0), (int64_t)kn) : 0;
+  *first = lo / kBlock;
+  return max((kn + kBlock - 1) / kBlock - *first, 1);
+}
+
+// Sums over a wave without LDS: rows of 16 lanes by neighbours and mirrors, then the four rows.
+template <int C, bool BOUND> __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(0, x, C, 0xf, 0xf, BOUND); }
+__device__ __forceinline__ int wave_sum(int x) {
+  x += dpp<0xb1, true>(x);
+  x += dpp<0x4e, true>(x);
+  x += dpp<0x141, true>(x);
+  x += dpp<0x140, true>(x);
+  return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) + __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
+}
+__device__ __forceinline__ int wave_before(int x, int lane) {       // of the lanes below
+  int y = x;
+  y += dpp<0x111, true>(y);                                // from 1, 2, 4, 8 lanes below in the row, zero before its first
+  y += dpp<0x112, true>(y);
+  y += dpp<0x114, true>(y);
+  y += dpp<0x118, true>(y);
+  int r0 = __builtin_amdgcn_readlane(y, 15), r1 = r0 + __builtin_amdgcn_readlane(y, 31), r2 = r1 + __builtin_amdgcn_readlane(y, 47);
+  return y - x + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2);
+}
+
+// A workgroup's share: a part of a sequence's keys.  The sequences are cut into parts of about `per` blocks, per the least of nine steps that makes
+// no more than `items` of them, so parts differ little however the lengths do, and none is without keys.  Every wave works this out for itself
+// (up to 256 sequences, number 64 k + lane); the first of all leaves the sequences' first items for the join.
+struct Share {
+  int b, part, parts;
+};
+__device__ __forceinline__ Share share_of(const CacheArgs& c, const CacheAtt& a, int item, bool leave, int lane) {
+  int n[4], sum = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    n[k] = 0;
+    int b = 64 * k + lane;
+    if (b >= c.B) continue;
+    int s0;
+    n[k] = blocks_of(a, a.q_len ? min(max(a.q_len[b], 0), a.nq) : a.nq, (int)min((int64_t)max(a.k_len[b], 0), c.rows_most), &s0);
+    sum += n[k] >> 3;                                      // eighths: 256 of 2^25 blocks pass 2^31
+  }
+  float all = 8.f * (float)wave_sum(sum) + 8.f * (float)c.B;
+  // between what would do if nothing were left over and what does in any case
+  float low = fmaxf(all / (float)a.items, (float)a.least), high = fmaxf(all / (float)(a.items - c.B) * 1.0001f, low);
+  int parts[4];
+  for (int step = 0; step <= 8; ++step) {
+    float inv = 1.f / (low + (high - low) * 0.125f * (float)step);
+    sum = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // a part's blocks rounded up a hair: n a multiple of per makes n / per parts (a sequence of 2^25 blocks in one part and less than another's 2^-16)
+      parts[k] = n[k] ? max((int)ceilf((float)n[k] * inv * 0.9999f), 1) : 0;
+      sum += parts[k];
+    }
+    if (wave_sum(sum) <= a.items) break;
+  }
+  Share mine{0, 0, 0};
+  int base = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (64 * k >= c.B) break;
+    int at = base + wave_before(parts[k], lane), b = 64 * k + lane;
+    base += wave_sum(parts[k]);
+    if (leave && b < c.B) a.first[b] = at;
+    uint64_t who = __ballot(item >= at && item < at + parts[k]);
+    if (who) {
+      int l = __ffsll((unsigned long long)who) - 1;
+      mine = Share{64 * k + l, item - __builtin_amdgcn_readlane(at, l), __builtin_amdgcn_readlane(parts[k], l)};
+    }
+  }
+  if (leave && lane == 0) a.first[c.B] = base;
+  return mine;
+}
+
 // Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.
 constexpr int waves_of(int size, bool e4m3, int dp, int nt, bool even) {
   if (nt == 2) return 2;
@@ -114,18 +194,35 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   __shared__ __align__(16) float buf[2 * kPart];
   __shared__ float wm[4][ROWS], wl[4][ROWS];
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, q4 = lane >> 4;
-  int x = blockIdx.x, sp = x % a.nsplit, rb = (x / a.nsplit) % a.blocks, bh = x / a.nsplit / a.blocks, hk = bh % c.HK, b = bh / c.HK;
-  int qn = a.q_len ? uniform(min(max(a.q_len[b], 0), a.nq)) : a.nq;
-  int kn = uniform((int)min((int64_t)max(a.k_len[b], 0), c.rows_most));
+  // blocks of rows that read the same keys stand eight apart: on one die, whose L2 they share
+  int x = blockIdx.x, of = (int)over(x >> 3, a.by_blocks), rb = (x >> 3) - of * a.blocks, unit = of * 8 + (x & 7);
+  // dealt: the shared heads of an item are neighbours; else the parts of a sequence's head
+  int q = (int)over(unit, a.dealt ? a.by_hk : a.by_even), seq = (int)over(q, a.by_hk);
+  int hk = a.dealt ? unit - q * c.HK : q - seq * c.HK, part = a.dealt ? 0 : unit - q * a.even, item = a.dealt ? q : seq * a.even + part;
+  if (item >= a.items) return;
+  Share mine{seq, part, a.even};
+  if (a.dealt) mine = share_of(c, a, item, x == 0 && wave == 0, lane);
+  if (mine.parts == 0) return;                             // more workgroups than parts
+  int b = mine.b;
+  int qn = queries_of(a, b);
+  int kn = keys_of(c, a, b);
   int rows = a.nq * a.G, first = rb * ROWS, i0 = first / a.G, i1 = min(min(first + ROWS, rows) - 1, qn * a.G - 1) / a.G;
   // keys that some row of these takes: [lo, hi)
   int64_t p0 = (int64_t)kn - qn + i0, p1 = (int64_t)kn - qn + i1;
   int lo = a.window ? (int)min(max(p0 - a.window + 1, (int64_t)0), (int64_t)kn) : 0;
   int hi = a.causal ? (int)max(min(p1 + 1, (int64_t)kn), (int64_t)0) : kn;
   if (first >= qn * (int64_t)a.G || c.pages == 0) hi = lo;
-  int b0 = lo / kBlock, b1 = hi > lo ? (hi + kBlock - 1) / kBlock : b0;
-  int per = max((b1 - b0 + a.nsplit - 1) / a.nsplit, 4);
-  int t0 = min(b0 + sp * per, b1), t1 = min(t0 + per, b1);
+  int t0 = lo / kBlock, t1 = hi > lo ? (hi + kBlock - 1) / kBlock : t0;
+  if (mine.parts > 1) {
+    int s0, n = blocks_of(a, qn, kn, &s0);                 // of the whole sequence
+    t0 = max(t0, s0 + (int)((int64_t)mine.part * n / mine.parts));
+    t1 = max(min(t1, s0 + (int)((int64_t)(mine.part + 1) * n / mine.parts)), t0);
+    if (t0 == t1) {                                        // nothing here: the join reads no more than this
+      int r = first + tid;
+      if (tid < ROWS && r < rows) a.pl[((size_t)item * a.H + hk * a.G + r % a.G) * a.nq + r / a.G] = -__builtin_inff();
+      return;
+    }
+  }
 
   const char* K = (const char*)c.K + (int64_t)hk * c.ks[2] * SB;
   const char* V = (const char*)c.V + (int64_t)hk * c.vs[2] * SB;
@@ -178,25 +275,23 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   u32x4 vx[2];                                             // and of its values' rows
   unsigned koff = (unsigned)col * kpitch + 16u * q4, voff = (unsigned)(4 * q4) * vpitch;
   auto fetch_k = [&](const Pages& p, unsigned keep) {
-    bool all = keep == ~0u;                                // mostly: then nothing is worked out for the lanes
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      bool ok = (keep >> (16 * k + col)) & 1;
+      unsigned gone = (~keep >> (16 * k + col)) << 31;
       if constexpr (EVEN) {
         bool there = (keep >> (16 * k)) & 0xffffu;
         int pg = there ? p.page[k] : 0, row = there ? p.row[k] : 0;
         __amdgpu_buffer_rsrc_t mem = bounded(K + pg * kpage + (int64_t)row * kpitch, there ? 15 * kpitch + (unsigned)(c.d * SB + 15) / 16 * 16 : 0u);
-        unsigned mine = all || ok ? koff : kNowhere;
 #pragma unroll
         for (int s = 0; s < KP; ++s)
-          kr[k][s] = __builtin_amdgcn_raw_buffer_load_b128(mem, 16u * (4 * s + q4) < (unsigned)(c.d * SB) ? mine : kNowhere, 64 * s, 0);
+          kr[k][s] = __builtin_amdgcn_raw_buffer_load_b128(mem, (16u * (4 * s + q4) < (unsigned)(c.d * SB) ? koff : kNowhere) | gone, 64 * s, 0);
         if constexpr (E4M3) {
           __amdgpu_buffer_rsrc_t ex = bounded(ke + pg * epage + (int64_t)row * 4, there ? 64u : 0u);
           kx[k] = __builtin_amdgcn_raw_buffer_load_b32(ex, 4 * col, 0, 0);
         }
       } else {
         int pg = __shfl(p.page[0], 16 * k + col, 64), row = __shfl(p.row[0], 16 * k + col, 64);
-        if (!ok) pg = row = 0;                             // some row: loads without branches are counted, and waited for, one by one
+        if (gone) pg = row = 0;                             // some row: loads without branches are counted, and waited for, one by one
         const char* at = K + pg * kpage + (int64_t)row * kpitch;
 #pragma unroll
         for (int s = 0; s < KP; ++s) {
@@ -209,7 +304,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   };
   auto fetch_v = [&](const Pages& p, unsigned keep) {
     unsigned o = (unsigned)(col * FV * SB);
-    bool mine = o < (unsigned)(c.dv * SB), all = keep == ~0u;
+    bool mine = o < (unsigned)(c.dv * SB);
     unsigned vlane = mine ? voff + o : kNowhere;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -219,8 +314,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
         __amdgpu_buffer_rsrc_t mem = bounded(V + pg * vpage + (int64_t)row * vpitch, there ? 15 * vpitch + (unsigned)(c.dv * SB + 15) / 16 * 16 : 0u);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          bool ok = all || (keep >> (16 * k + 4 * q4 + r)) & 1;
-          unsigned at = ok ? vlane : kNowhere;
+          unsigned gone = (~keep >> (16 * k + 4 * q4 + r)) << 31, at = vlane | gone;   // behind every bound; a branch would spoil the counting of loads
           int step = (int)(r * vpitch);
           unsigned* v = vr[4 * k + r];
           if constexpr (VW == 1) {
@@ -235,7 +329,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
               unsigned f = 256u * z + 16u * col;
-              u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, ok && f < 4u * c.dv ? voff + 16u * col : kNowhere, step + 256 * z, 0);
+              u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(mem, (f < 4u * c.dv ? voff + 16u * col : kNowhere) | gone, step + 256 * z, 0);
               v[4 * z] = w[0], v[4 * z + 1] = w[1], v[4 * z + 2] = w[2], v[4 * z + 3] = w[3];
             }
           }
@@ -619,19 +713,20 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   bool some = sum != 0.f && i < qn;                        // NaN counts as something
   float inv = some ? 1.f / sum : 0.f;
   float lse2 = some ? (best - Lift<T>::value) + __builtin_amdgcn_logf(sum) : -__builtin_inff();
-  size_t at = ((size_t)b * a.H + h) * a.nq + i, n = (size_t)c.B * a.H * a.nq;
+  bool whole = mine.parts == 1;
+  size_t at = ((size_t)(whole ? b : item) * a.H + h) * a.nq + i;
   if (tid % TR == 0) {
-    if (a.nsplit == 1) a.lse[at] = lse2 * kLn2;
-    else a.pl[sp * n + at] = lse2;
+    if (whole) a.lse[at] = lse2 * kLn2;
+    else a.pl[at] = lse2;
   }
-  if (a.nsplit > 1 && !some) return;                       // parts without weight are not read
+  if (!whole && !some) return;                             // parts without weight are not read
   const float* src = buf + row * (DP + 4);
   T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
   for (int f = tid % TR * 4; f < DP; f += 4 * TR) {
     f32x4 y = (*(const f32x4*)(src + f) + *(const f32x4*)(src + kPart + f)) * inv;
     if (!some) y = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (a.nsplit == 1) store4<T>(out, f, c.dv, a.ovec, y[0], y[1], y[2], y[3]);
-    else if (f < a.dv4) *(f32x4*)(a.pO + (sp * n + at) * a.dv4 + f) = y;
+    if (whole) store4<T>(out, f, c.dv, a.ovec, y[0], y[1], y[2], y[3]);
+    else if (f < a.dv4) *(f32x4*)(a.pO + at * a.dv4 + f) = y;
   }
 }
 
@@ -641,19 +736,28 @@ template <typename T, int GROUPS>
 __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt a) {
   __shared__ __align__(16) f32x4 part[8][32];
   __shared__ float tops[8], sums[8];
-  int64_t n = (int64_t)c.B * a.H * a.nq, row = (int64_t)blockIdx.x * (8 / GROUPS) + (threadIdx.x >> 5) / GROUPS;
+  int n = c.B * a.H * a.nq, row = blockIdx.x * (8 / GROUPS) + (threadIdx.x >> 5) / GROUPS;
   int lane = threadIdx.x & 31, f = 4 * lane, all = threadIdx.x >> 5, g = all % GROUPS;
   if (row >= n) return;                                    // GROUPS == 8: no workgroup is behind the last row
+  int bh = (int)over(row, a.by_nq), i = row - bh * a.nq, b = (int)over(bh, a.by_heads), h = bh - b * a.H;
+  int64_t first = (int64_t)b * a.even, step = (int64_t)a.H * a.nq;
+  int parts = a.even;
+  if (a.dealt) {
+    first = a.first[b];
+    parts = a.first[b + 1] - (int)first;
+  }
+  int64_t from = first * step + (int64_t)h * a.nq + i;
+  if (parts == 1) return;                                  // written as it was
   float top = -__builtin_inff(), sum = 0.f;
   f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = g; s0 < a.nsplit; s0 += 8 * GROUPS) {
+  for (int s0 = g; s0 < parts; s0 += 8 * GROUPS) {
     float p[8];
     f32x4 v[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       int at = s0 + GROUPS * s;
-      p[s] = at < a.nsplit ? a.pl[at * n + row] : -__builtin_inff();
-      v[s] = at < a.nsplit && f < a.dv4 ? *(const f32x4*)(a.pO + (at * n + row) * a.dv4 + f) : f32x4{0.f, 0.f, 0.f, 0.f};
+      p[s] = at < parts ? a.pl[from + at * step] : -__builtin_inff();
+      v[s] = at < parts && f < a.dv4 ? *(const f32x4*)(a.pO + (from + at * step) * a.dv4 + f) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
     float best = top;
 #pragma unroll
@@ -691,14 +795,13 @@ __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt
   bool some = sum != 0.f;
   float inv = some ? 1.f / sum : 0.f;
   if (lane == 0) a.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
-  int i = (int)(row % a.nq), h = (int)(row / a.nq % a.H), b = (int)(row / a.nq / a.H);
   T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
   store4<T>(out, f, c.dv, a.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
 template <typename T, bool E4M3, int DP, int NT>
 void attend_n(hipStream_t s, const CacheArgs& c, const CacheAtt& a) {
-  unsigned grid = (unsigned)((int64_t)c.B * c.HK * a.blocks * a.nsplit);
+  unsigned grid = (unsigned)(((int64_t)a.items * c.HK + 7) / 8 * 8 * a.blocks);
   if (c.page.d % 16 == 0) k_attend_cache<T, E4M3, DP, NT, true><<<grid, 256, 0, s>>>(c, a);
   else k_attend_cache<T, E4M3, DP, NT, false><<<grid, 256, 0, s>>>(c, a);
 }
@@ -723,7 +826,7 @@ void attend_t(hipStream_t s, int type, int e4m3, const CacheArgs& c, const Cache
 template <typename T>
 void join_t(hipStream_t s, const CacheArgs& c, const CacheAtt& a) {
   int64_t n = (int64_t)c.B * a.H * a.nq;
-  if (a.nsplit <= 8) k_attend_cache_join<T, 1><<<(unsigned)((n + 7) / 8), 256, 0, s>>>(c, a);
+  if (n > 4096) k_attend_cache_join<T, 1><<<(unsigned)((n + 7) / 8), 256, 0, s>>>(c, a);
   else k_attend_cache_join<T, 8><<<(unsigned)n, 256, 0, s>>>(c, a);
 }
 
