@@ -2608,10 +2608,10 @@ int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows,
 // whole: 300 keys 9.7 / 8.6 us, 500 10.3 / 9.9, 1000 11.3 / 15.8).  `reach`: what the table (or the window) has room for.  From kCacheDeal keys on
 // (kCacheDealMany, if three workgroups a compute unit are not there) the kernel deals the parts out by the lengths, which only the device knows, where there are several (one sequence of 65536 keys beside 127 of 500, 8
 // shared heads of 128, bf16: the same number of parts for each 235 us, dealt 104; 8 of up to 32773 130 / 126; but 2 of 10000 26.8 / 30.5).
-constexpr int64_t kCacheWhole = 384, kCacheDeal = 4096, kCacheDealMany = 16384, kCachePart = 256, kCacheEvenPart = 1024, kCacheBlock = 32, kCacheShare = 256;
+constexpr int64_t kCacheWhole = 384, kCacheDeal = 4096, kCacheDealMany = 16384, kCacheDealParts = 4, kCachePart = 256, kCacheEvenPart = 1024, kCacheBlock = 32, kCacheShare = 256;
 void cache_parts(int64_t cus, int64_t held, int64_t batch, int64_t units, int64_t reach, CacheAtt* t) {
-  bool filled = batch * units >= 3 * cus, deal = batch > 1 && batch <= kCacheShare && reach > (filled ? kCacheDeal : kCacheDealMany);
   int64_t round = std::max<int64_t>(held * cus / units, 1), n = batch;
+  bool filled = batch * units >= 3 * cus, deal = batch > 1 && batch <= kCacheShare && round >= kCacheDealParts && reach > (filled ? kCacheDeal : kCacheDealMany);
   if (filled) {
     if (deal) n = batch + round;
   } else if (reach > kCacheWhole) {

@@ -332,6 +332,94 @@ def test_attention_over_pages_matches_the_oracle(ctx, name, kind, held):
     _attend_and_check(ctx, kind, c, _rand(rng, kind, len(k_len), nq, heads, d), k_len, **opt)
 
 
+# Tables wide enough that the keys of several sequences are cut by what their lengths are, not by the table's width.
+def _short(b, most, **long):
+    """b lengths up to `most`, some of them zero, but for {"at<number>": length}."""
+    rng = np.random.default_rng(b)
+    n = [int(x) for x in rng.integers(0, most + 1, b) * (rng.random(b) < 0.9)]
+    for k, x in long.items():
+        n[int(k[2:])] = x
+    return n
+
+
+# k_len, heads, hk, nq, d, dv, page, pages of a table row, options of the call
+DEALT = {
+    "a_long_and_a_short": ([17000, 3], 4, 2, 1, 64, 64, 16, 1100, {}),
+    "a_short_and_a_long": ([3, 17000], 4, 2, 1, 64, 64, 16, 1100, {}),
+    "all_short": ([1, 0, 40, 500, 64], 4, 2, 1, 64, 64, 16, 1100, {}),
+    "all_empty": ([0, 0, 0], 4, 2, 1, 64, 64, 16, 1100, {}),
+    "one_has_all": ([0, 0, 20000, 0], 4, 1, 1, 128, 128, 64, 320, {}),
+    "equal": ([4100] * 4, 4, 1, 1, 64, 64, 16, 1100, {}),
+    "lengths_out_of_range": ([-5, 2 ** 31 - 1, 700], 2, 1, 1, 32, 32, 4096, 5, dict(oracle=[0, 20480, 700])),
+    "sixty_three": (_short(63, 300, at0=4000), 2, 1, 1, 32, 32, 16, 1100, {}),
+    "sixty_four": (_short(64, 300, at63=4000), 2, 1, 1, 32, 32, 16, 1100, {}),
+    "sixty_five": (_short(65, 300, at64=4000, at1=0), 2, 1, 1, 32, 32, 16, 1100, {}),
+    "hundred_and_thirty": (_short(130, 300, at0=0, at129=3000, at64=2000), 2, 1, 1, 32, 32, 16, 1100, {}),
+    "two_hundred_and_fifty_six": (_short(256, 200, at255=2500, at128=2000), 2, 1, 1, 32, 32, 16, 1100, {}),
+    "two_hundred_and_fifty_seven": (_short(257, 200, at256=2500), 2, 1, 1, 32, 32, 16, 1100, {}),
+    "as_many_as_fill_the_device": (_short(128, 200, at5=2500), 6, 6, 1, 16, 16, 16, 300, {}),
+    "many_as_fill_the_device": (_short(256, 150, at0=2000, at255=0), 6, 3, 1, 16, 16, 16, 300, {}),
+    "new_rows": ([17000, 64, 9], 4, 2, 8, 64, 64, 16, 1100, {}),
+    "padded_new_rows": ([17000, 64, 9, 50, 0], 8, 1, 9, 64, 64, 16, 1100, dict(q_len=[9, 3, 0, -2, 9])),
+    "new_rows_all_keys": ([3000, 64, 9], 8, 1, 9, 128, 128, 16, 1100, dict(causal=False)),
+    "window": ([18000, 17100, 5, 0], 4, 1, 2, 64, 64, 32, 600, dict(window=17000)),
+    "page_of_twenty": ([5000, 333, 50], 6, 2, 3, 128, 128, 20, 900, {}),
+    "odd_features_page_of_five": ([2000, 90], 3, 1, 2, 33, 7, 5, 3400, {}),
+    "cap": ([3000, 90], 4, 2, 2, 64, 64, 16, 1100, dict(cap=1.5)),
+    "missing_pages": ([3000, 90, 32, 700], 4, 2, 2, 64, 64, 32, 600, dict(holes=True)),
+    "missing_pages_of_five": ([3000, 90, 5, 700], 4, 2, 2, 64, 64, 5, 3400, dict(holes=True)),
+}
+
+
+@pytest.mark.parametrize("held", ["own", "e4m3"])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("name", list(DEALT))
+def test_keys_cut_by_all_lengths_match_the_oracle(ctx, name, kind, held):
+    from paper_1809_11165_amd import binding
+    k_len, heads, hk, nq, d, dv, page, most, opt = DEALT[name]
+    rng = np.random.default_rng(sum(map(ord, name)))
+    opt = dict(opt)
+    there, holes = opt.pop("oracle", k_len), opt.pop("holes", False)
+    c = _filled(rng, kind, kind if held == "own" else held, there, page, hk, d, dv, most)
+    if holes:
+        c.table[:, ::3] = -1                                 # and the first page of each: one sequence is left without keys
+    Q = _rand(rng, kind, len(k_len), nq, heads, d)
+    want = _oracle(kind, c, Q, there, **opt)
+    first = _attend_and_check(ctx, kind, c, Q, k_len, want=want, **opt)
+    again = _attend_and_check(ctx, kind, c, Q, k_len, want=want, **opt)
+    assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
+@pytest.mark.parametrize("held", ["own", "e4m3"])
+def test_a_recorded_call_cuts_the_keys_by_the_lengths_of_each_replay(held):
+    from paper_1809_11165_amd import binding
+    rng = np.random.default_rng(14)
+    full = [16500, 300, 4000, 1]
+    c = _filled(rng, "bf16", "bf16" if held == "own" else held, full, 16, 2, 64, 64)
+    Q, n = _rand(rng, "bf16", 4, 2, 4, 64), _int([2, 2, 2, 1])
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = binding.Context(0)
+        ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, n))
+        stream.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, n))
+        for now in ([16500, 300, 4000, 1], [0, 0, 0, 0], [5, 300, 0, 1], [16500, 0, 0, 0], [900, 20, 4000, 0]):
+            n.copy_(_int(now))
+            g.replay()
+            stream.synchronize()
+            eager = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, n))
+            stream.synchronize()
+            assert torch.equal(O, eager[0]) and torch.equal(lse, eager[1]), now
+            val, err = _oracle("bf16", c, Q, now)
+            _check(O, val, err, "o")
+            _check(lse, val, err, "lse")
+        del g
+    ctx.close()
+
+
 @pytest.mark.parametrize("held", ["own", "e4m3"])
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("page", [16, 32, 5])
