@@ -191,6 +191,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   constexpr int FV = DP / 16;                              // features of a value per lane
   constexpr int VW = FV * SB / 4;                          // words of a value per lane
   constexpr int kPart = ROWS * (DP + 4);
+  constexpr bool kQueries = sizeof(T) == 2 && NT == 2 && DP == 128;   // queries stay in LDS: in registers, others of the loop's went to scratch
   __shared__ __align__(16) float buf[2 * kPart];
   __shared__ float wm[4][ROWS], wl[4][ROWS];
   int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, q4 = lane >> 4;
@@ -377,7 +378,8 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   // Features of a lane's step s of the scores: eight from `feature(s)` on (fp32: four, twice).
   auto step_at = [&](int s) { return E4M3 ? 16 * (4 * (s >> 1) + q4) + 8 * (s & 1) : 8 * (4 * s + q4); };
   // fp32 pieces hold four features: step s has pieces 2s, 2s + 1
-  frag qf[NT][NS][PARTS];
+  frag qf[kQueries ? 1 : NT][kQueries ? 1 : NS][PARTS];
+  frag* held = (frag*)buf + lane;                          // of row block n, step s: held[64 (NS n + s)]
   int rho[NT], qi[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -389,8 +391,14 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     for (int s = 0; s < NS; ++s) {
       if constexpr (sizeof(T) == 2) {
         u32x4 v = {0u, 0u, 0u, 0u};
-        if (have) v = load16<T>(row, step_at(s), c.d, a.qvec);
-        qf[n][s][0] = __builtin_bit_cast(frag, v);
+        if constexpr (kQueries) {
+          if (s != 0) continue;                            // each wave brings one of the four steps
+          if (have) v = load16<T>(row, step_at(wave), c.d, a.qvec);
+          held[64 * (NS * n + wave)] = __builtin_bit_cast(frag, v);
+        } else {
+          if (have) v = load16<T>(row, step_at(s), c.d, a.qvec);
+          qf[n][s][0] = __builtin_bit_cast(frag, v);
+        }
       } else {
         int f0 = E4M3 ? step_at(s) : 4 * (8 * s + q4), f1 = E4M3 ? f0 + 4 : 4 * (8 * s + 4 + q4);
         u32x4 v0 = {0u, 0u, 0u, 0u}, v1 = v0;
@@ -404,6 +412,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
       }
     }
   }
+  if constexpr (kQueries) __syncthreads();
   // Behind the last feature a piece holds whatever the row's memory does.
   bool ragged = (c.d * SB) % 16 != 0;
   unsigned blocks_there = c.d > 96 ? ~0u : (1u << (8 * ((c.d + 31) / 32))) - 1;
@@ -547,16 +556,33 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     trim();
 #pragma unroll
     for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
+    if constexpr (kQueries) {
+      int here = 0;
+      asm volatile("" : "+v"(here));                       // read anew each time
 #pragma unroll
       for (int z = 0; z < NS; ++z) {
-        frag f = key_frag(k, z);
+        frag q[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) q[n] = held[64 * (NS * n + z) + here];
 #pragma unroll
-          for (int p = 0; p < PARTS; ++p) s[n][k] = M::mma(f, qf[n][z][p], s[n][k]);
+        for (int k = 0; k < 2; ++k) {
+          frag f = key_frag(k, z);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) s[n][k] = M::mma(f, q[n], s[n][k]);
+        }
       }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int z = 0; z < NS; ++z) {
+          frag f = key_frag(k, z);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) s[n][k] = M::mma(f, qf[n][z][p], s[n][k]);
+        }
+    }
   };
   auto weights = [&](int j0, unsigned keep, auto edge) {
     // in units of the base-2 exponent
@@ -626,39 +652,38 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   }
   settle();
   int t = a0 + wave;
-  Pages next{};
-  unsigned keep = 0;
   if (t < a1) {
-    Pages here = find(t);
-    next = t + 4 < a1 ? find(t + 4) : here;
-    keep = kept(t, here);
+    Pages here = find(t), next = t + 4 < a1 ? find(t + 4) : here;
+    unsigned keep = kept(t, here);
     fetch_k(here, keep);
     __builtin_amdgcn_sched_barrier(0);                     // in the loop's order: else its first wait is for all of them
     fetch_v(here, keep);
     __builtin_amdgcn_sched_barrier(0);
-  }
-  for (; t < a1; t += 4) {
-    scores();
-    unsigned keep_next = 0;
-    Pages after = next;
-    if (t + 4 < a1) {
+    // no load under a condition: waits go by the count of the loads behind, the same on every way here
+    for (; t + 4 < a1; t += 4) {
+      scores();
+      unsigned keep_next = kept(t + 4, next);
+      Pages after = next;
       if (t + 8 < a1) after = find(t + 8);
-      keep_next = kept(t + 4, next);
       fetch_k(next, keep_next);
+      weights(t * kBlock, keep, Const<0>{});
+      clear_values(keep);
+      add_values(s, keep, Const<0>{});
+      fetch_v(next, keep_next);
+      next = after;
+      keep = keep_next;
     }
+    scores();
     weights(t * kBlock, keep, Const<0>{});
     clear_values(keep);
     add_values(s, keep, Const<0>{});
-    if (t + 4 < a1) fetch_v(next, keep_next);
-    next = after;
-    keep = keep_next;
   }
   // and the others, few: [t0, a0) and [a1, t1).  Infinities and NaN among their values are kept from rows that do not take them (an 8-bit value may
   // become infinite in fp16 as well).
   for (int u = wave; u < (a0 - t0) + (t1 - a1); u += 4) {
     int at = u < a0 - t0 ? t0 + u : a1 + u - (a0 - t0);
     Pages here = find(at);
-    keep = kept(at, here);
+    unsigned keep = kept(at, here);
     fetch_k(here, keep);
     fetch_v(here, keep);
     scores();
