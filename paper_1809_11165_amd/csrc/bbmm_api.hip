@@ -2603,11 +2603,12 @@ int cache_read(bbmm_ctx* c, const bbmm_cache* cache, int32_t type, int64_t rows,
 
 // Parts that the keys of all sequences are split into, over workgroups.  As many as the device holds at once (`held` a compute unit, `units` workgroups a
 // part) while parts keep kCachePart keys; or, where parts of kCacheEvenPart keys make at least two such rounds, up to eight a compute unit (between one
-// round and two, the second is mostly empty).  Where three workgroups a compute unit are there anyway, one round more, which shortens a long sequence
-// among short ones.  Up to kCacheWhole keys the second launch costs more than the parts save (one request, 8 shared heads of 128, bf16, in parts /
-// whole: 300 keys 9.7 / 8.6 us, 500 10.3 / 9.9, 1000 11.3 / 15.8).  `reach`: what the table (or the window) has room for.  From kCacheDeal keys on
-// (kCacheDealMany, if three workgroups a compute unit are not there) the kernel deals the parts out by the lengths, which only the device knows, where there are several (one sequence of 65536 keys beside 127 of 500, 8
-// shared heads of 128, bf16: the same number of parts for each 235 us, dealt 104; 8 of up to 32773 130 / 126; but 2 of 10000 26.8 / 30.5).
+// round and two, the second is mostly empty).  Up to kCacheWhole keys the second launch costs more than the parts save (one request, 8 shared heads of
+// 128, bf16, in parts / whole: 300 keys 9.7 / 8.6 us, 500 10.3 / 9.9, 1000 11.3 / 15.8).  `reach`: what the table (or the window) has room for.
+// From kCacheDeal keys on (kCacheDealMany, if three workgroups a compute unit are not there) the kernel deals the parts out by the lengths, which only
+// the device knows, where there are several (8 shared heads of 128, bf16, the same number of parts for each / dealt: one sequence of 65536 keys beside
+// 127 of 500 235 / 104 us, 8 of up to 32773 130 / 126; but 2 of 10000 26.8 / 30.5), and where kCacheDealParts are there beside one a sequence (16 of
+// 128 new rows, one of 32768 keys among 1000: four, 458 / 303; of 256 rows: two, 517 / 551).
 constexpr int64_t kCacheWhole = 384, kCacheDeal = 4096, kCacheDealMany = 16384, kCacheDealParts = 4, kCachePart = 256, kCacheEvenPart = 1024, kCacheBlock = 32, kCacheShare = 256;
 void cache_parts(int64_t cus, int64_t held, int64_t batch, int64_t units, int64_t reach, CacheAtt* t) {
   int64_t round = std::max<int64_t>(held * cus / units, 1), n = batch;

@@ -1,6 +1,8 @@
 // Rows into the pages of a cache, and back (see include/bbmm.h, "Cache").  A few lanes take a row, 16 bytes of the wide side each; 8-bit blocks of 32
-// features are four or eight of these lanes.  Bound by memory, single rows by their launch: rows are read and written once, in whole
-// pieces of 128 bytes and more.
+// features are four or eight of these lanes:  e = least with max |x| / 2^e <= 448,  q = round(x / 2^e),  and back  x = q 2^e.
+// Bound by memory, single rows by their launch: rows are read and written once, in whole pieces of 128 bytes and more.  4 x 2048 rows of 8 heads of
+// 128 from bf16 into 8-bit pages, 51 MB: 15.1 us, 3.4 TB/s (a workgroup's rows end together, and the next one's places are looked up anew);
+// 4 x 8192 read back, 204 MB: 35.3 us, 5.8 TB/s; one row of eight requests: 3.2 us, three loads in a chain and the launch.
 #include "cache_dev.h"
 
 using namespace att;

@@ -319,6 +319,9 @@ ATTEND = {
     "cap_window": ([700, 90], 4, 2, 2, 128, 128, 16, dict(cap=30.0, window=100)),
     "scale": ([300, 90], 4, 2, 2, 64, 64, 16, dict(scale=1.7)),
     "prompt": ([260, 200], 4, 1, 200, 64, 64, 64, dict(q_len=[200, 150])),
+    "rows_33_page_of_twenty": ([333, 50], 11, 1, 3, 128, 128, 20, {}),
+    "rows_40_cap": ([700, 130], 8, 1, 5, 100, 120, 32, dict(cap=3.0)),
+    "rows_320_window": ([900, 41, 300], 32, 2, 20, 128, 128, 16, dict(window=70, q_len=[20, 20, 13])),
 }
 
 
