@@ -473,10 +473,15 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
       if constexpr (kThree) {
         in_three(__builtin_shufflevector(p[n][0], p[n][1], 0, 1, 2, 3, 4, 5, 6, 7), pf[n]);
       } else {
+        f32x8 w = __builtin_shufflevector(p[n][0], p[n][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        pf[n][0] = __builtin_convertvector(w, frag);
+        if constexpr (__is_same(T, __bf16)) {              // each pair rounded once, and taken apart
+          u32x4 x = __builtin_bit_cast(u32x4, pf[n][0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          pf[n][0][e] = (T)p[n][e >> 2][e & 3];
-          if constexpr (WPARTS == 2) pf[n][1][e] = (T)(p[n][e >> 2][e & 3] - (float)pf[n][0][e]);
+          for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(e & 1 ? x[e >> 1] & 0xffff0000u : x[e >> 1] << 16);
+          pf[n][1] = __builtin_convertvector(w, frag);
+        } else if constexpr (WPARTS == 2) {
+          pf[n][1] = __builtin_convertvector(w - __builtin_convertvector(pf[n][0], f32x8), frag);
         }
       }
     }
