@@ -789,9 +789,10 @@ __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt
     f32x4 v[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      int at = s0 + GROUPS * s;
-      p[s] = at < parts ? a.pl[from + at * step] : -__builtin_inff();
-      v[s] = at < parts && f < a.dv4 ? *(const f32x4*)(a.pO + (from + at * step) * a.dv4 + f) : f32x4{0.f, 0.f, 0.f, 0.f};
+      int at = s0 + GROUPS * s, there = min(at, parts - 1); // loads without branches, behind the last part of that again
+      p[s] = a.pl[from + there * step];
+      v[s] = *(const f32x4*)(a.pO + (from + there * step) * a.dv4 + min(f, a.dv4 - 4));
+      if (at >= parts) p[s] = -__builtin_inff();
     }
     float best = top;
 #pragma unroll
