@@ -6,7 +6,7 @@
 // 16 kb + 4 (lane / 16) + r in its registers, which are the second operand of O^T += V^T P^T as they stand.
 //   keys: a lane reads 16 bytes of key 16 kb + lane % 16 at piece 4 s + lane / 16; any order of the features serves that is the queries' too.
 //   values: a lane reads, of the eight keys whose weights it will meet, DP / 16 neighbouring features, 16 lanes a row.  Two-byte values then
-//           change places in pairs (one byte permutation per two values); fp32 values are operands as they stand.  No LDS before the join.
+//           change places in pairs (one byte permutation per two values); fp32 values are operands as they stand.  No LDS before the join, but for queries of 32 rows.
 // 8-bit rows become T on the way, by the instruction that applies their block's power of two.
 // Bound by memory with up to 16 rows a shared head: 8 requests of up to 32773 keys, 8 shared heads of 128, bf16, 660 MB in 117.8 us, 5.6 TB/s (a large
 // copy: 4.9); 16 of up to 65536 8-bit keys, 1.24 GB in 222 us, 5.6 TB/s; 64 with a window of 1024, fp16, d 64, 228 MB in 44.2 us, 5.2 TB/s.  With 32
