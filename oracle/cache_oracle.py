@@ -13,7 +13,7 @@ sums of n terms n u32) and outputs are rounded to the type once (unit u), weight
     dw         sum |n| (e_dz + |dz| (er + (terms + 2) u32)) + u |dw| + terms 2^-150 (sums of tiny terms)
     dx         r (|w| e_dz + |n| e_m + (2 er + 8 u32) (|w dz| + |n m|)) + u |dx|,   m the mean, e_m = mean |n| (|w| e_dz + |w dz| (er + (d + 4) u32))
     scores     ds = 2 (d + 8) u32 max_j (scale sum |q||k| + |lse|) + 16 u32 cap   (of a weight; tanh is off by less than 8 u32)
-    o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|
+    o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|   (up to 16 rows of a shared head in bf16: weights are three operands, u^2 stands for less than u32)
 fp16 adds half a step of its subnormal numbers (weights are lifted by 2^6 before they meet them).
 """
 from __future__ import annotations

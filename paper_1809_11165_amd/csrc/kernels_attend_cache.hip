@@ -184,7 +184,11 @@ template <typename T, bool E4M3, int DP, int NT, bool EVEN>
 __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void k_attend_cache(CacheArgs c, CacheAtt a) {
   constexpr bool kThree = sizeof(T) == 4 && E4M3;          // operands in three parts of bf16
   constexpr int PARTS = kThree ? 3 : 1;                    // of the queries, and of the weights:
-  constexpr int WPARTS = kThree ? 3 : sizeof(T) == 2 ? 2 : 1;   // what rounding to T leaves is a second operand, and costs nothing beside the reads
+  // Parts of the weights: what rounding to T leaves is a further operand.  bf16: three hold all 24 bits of a weight, which costs nothing beside the reads
+  // (one row, two parts / three: 8 requests of up to 32773 keys 124.0 / 124.5 us, 16 of 65536 8-bit keys 235.6 / 236.7; only with 8-bit rows of up to 64
+  // features 27.9 / 29.8).  With 32 rows products are the bound, and two parts leave 2^-16 of a weight (32 new rows of 4 sequences of 40000 keys 219 / 238,
+  // 8-bit pages 200 / 222).  fp16: two hold 22 bits.
+  constexpr int WPARTS = kThree ? 3 : sizeof(T) == 4 ? 1 : __is_same(T, __bf16) && NT == 1 ? 3 : 2;
   typedef std::conditional_t<kThree, __bf16, T> C;         // type of the operands
   typedef Mma<C> M;
   typedef typename M::frag frag;
@@ -476,10 +480,13 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
         f32x8 w = __builtin_shufflevector(p[n][0], p[n][1], 0, 1, 2, 3, 4, 5, 6, 7);
         pf[n][0] = __builtin_convertvector(w, frag);
         if constexpr (__is_same(T, __bf16)) {              // each pair rounded once, and taken apart
-          u32x4 x = __builtin_bit_cast(u32x4, pf[n][0]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(e & 1 ? x[e >> 1] & 0xffff0000u : x[e >> 1] << 16);
-          pf[n][1] = __builtin_convertvector(w, frag);
+          for (int part = 1; part < WPARTS; ++part) {
+            u32x4 x = __builtin_bit_cast(u32x4, pf[n][part - 1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(e & 1 ? x[e >> 1] & 0xffff0000u : x[e >> 1] << 16);
+            pf[n][part] = __builtin_convertvector(w, frag);
+          }
         } else if constexpr (WPARTS == 2) {
           pf[n][1] = __builtin_convertvector(w - __builtin_convertvector(pf[n][0], f32x8), frag);
         }
