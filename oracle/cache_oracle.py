@@ -12,7 +12,7 @@ sums of n terms n u32) and outputs are rounded to the type once (unit u), weight
     dz         e_dz = (|dy_a| + |dy_b|) (ec + 3 u32)
     dw         sum |n| (e_dz + |dz| (er + (terms + 2) u32)) + u |dw| + terms 2^-150 (sums of tiny terms)
     dx         r (|w| e_dz + |n| e_m + (2 er + 8 u32) (|w dz| + |n m|)) + u |dx|,   m the mean, e_m = mean |n| (|w| e_dz + |w dz| (er + (d + 4) u32))
-    scores     ds = 2 (d + 8) u32 max_j (scale sum |q||k| + |lse|) + 16 u32 cap   (of a weight; tanh is off by less than 8 u32)
+    scores     ds = 2 (d + 8) u32 max_j (scale sum |q||k| + |lse|) + 20 u32 max_j |s|   (of a weight; the last with a cap, whose tanh is off by less than 10 u32 of itself)
     o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|   (up to 16 rows of a shared head in bf16: weights are three operands, u^2 stands for less than u32)
 fp16 adds half a step of its subnormal numbers (weights are lifted by 2^6 before they meet them).
 """
@@ -168,7 +168,7 @@ def attend(kind, Q, K, V, scale, k_len, q_len=None, causal=True, window=0, cap=0
                 top = s.max()
                 lse = top + np.log(np.exp(s - top).sum())
                 p = np.exp(s - lse)
-                ds = 2 * (d + 8) * U32 * (big + abs(lse)) + 16 * U32 * cap
+                ds = 2 * (d + 8) * U32 * (big + abs(lse)) + (20 * U32 * np.abs(s).max() if cap else 0.0)
                 o = p @ v
                 val["o"][b, i, h], val["lse"][b, h, i] = o, lse
                 err["o"][b, i, h] = ((u if once else u * u) + ds + (len(at) + 1) * U32) * (p @ np.abs(v)) + u * np.abs(o) + tiny * (1 + 2.0 ** -4 * np.abs(v).sum(0))

@@ -90,6 +90,20 @@ __device__ __forceinline__ void in_three(const f32x8& x, bf16x8 (&p)[3]) {
   }
 }
 
+// cap tanh(scale x / cap) in units of the base-2 exponent, off by less than 10 u32 (2^-24) of itself however large the cap: scores that are small beside it
+// are c2 x (tanh y) / y, whose last factor nears one, so a y among fp32's subnormal numbers does no harm.  NEAR: every |y| < 1/2 here.
+template <bool NEAR>
+__device__ __forceinline__ float capped(float x, const CacheAtt& a) {
+  // |y| < 1/2: tanh y = y (1 + u P(u)), u = y^2, P of degree 3 with the least largest error, 0.3 u32
+  float y = x * a.cap_in, plain = x * a.c2, u = y * y, p = fmaf(0.01725541241466999f, u, -0.05305228754878044f);
+  p = fmaf(fmaf(p, u, 0.13325978815555573f), u, -0.33333149552345276f);
+  float near = fmaf(plain * u, p, plain);
+  if (NEAR) return near;
+  // 1 - 2 / (exp 2y + 1), off by less than 5 u32: its steps are 2^-24 absolutely, and tanh 1/2 = 0.46
+  float z = __builtin_amdgcn_exp2f(y * (2.f * kLog2e)), far = a.cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(z + 1.f));
+  return fabsf(y) < 0.5f ? near : far;
+}
+
 constexpr int kBlock = 32;                                 // keys of a wave's turn
 
 __device__ __forceinline__ int queries_of(const CacheAtt& a, int b) { return a.q_len ? uniform(min(max(a.q_len[b], 0), a.nq)) : a.nq; }
@@ -604,17 +618,17 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     // in units of the base-2 exponent
     if (a.cap2 != 0.f) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        float far = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float y = s[n][e >> 2][e & 3] * a.cap_in;
-          if constexpr (sizeof(T) == 4) {
-            s[n][e >> 2][e & 3] = a.cap2 * tanhf(y);
-          } else {                                         // 1 - 2 / (exp 2y + 1): off by 2^-23 of the cap, nothing beside a weight's rounding to T
-            float z = __builtin_amdgcn_exp2f(y * (2.f * kLog2e));
-            s[n][e >> 2][e & 3] = a.cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(z + 1.f));
-          }
-        }
+        for (int e = 0; e < 8; ++e) far = fmaxf(far, fabsf(s[n][e >> 2][e & 3]));
+        auto all = [&](auto near) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[n][e >> 2][e & 3] = capped<decltype(near)::value>(s[n][e >> 2][e & 3], a);
+        };
+        if (sizeof(T) == 4 || __any(far * a.cap_in >= 0.5f)) all(Const<0>{});   // (fp32: with two ways, others of the loop's registers went to scratch)
+        else all(Const<1>{});
+      }
     }
     float mul = a.cap2 != 0.f ? 1.f : a.c2;
     if (decltype(edge)::value || keep != ~0u) {

@@ -1,9 +1,10 @@
-"""GPU parity of the attention over a paged cache where numbers are out of the ordinary: weights whose lowest bits decide."""
+"""GPU parity of the attention over a paged cache where numbers are out of the ordinary: weights whose lowest bits decide, caps
+from far below the scores to fp32's largest numbers."""
 import numpy as np
 import pytest
 
 from oracle import cache_oracle as A
-from test_gpu_cache import DEV, TYPES, _bytes, _check, _filled, _host, _int, _new, _oracle, _rand
+from test_gpu_cache import DEV, TYPES, _attend_and_check, _filled, _host, _int, _new, _rand
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -49,4 +50,38 @@ def test_all_bits_of_a_weight_count_where_values_cancel(ctx, held):
     most = np.abs(o).max()
     assert most < 2.0 ** -10
     worst = (np.abs(_host(O)[:, 0, :, 0] - o) / lim).max()
+    assert worst <= 1
+
+
+@pytest.mark.parametrize("held", ["own", "e4m3"])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("cap", [1e-3, 0.3, 1e3, 1e5, 1e7, 1e9, 1e30, 1e38])
+def test_caps_of_any_size(ctx, kind, held, cap):
+    """A cap far above the scores leaves them as they are, one far below makes them plus or minus itself."""
+    rng = np.random.default_rng(21)
+    for shape in ((4, 1), (8, 5)):
+        k_len = [300, 90]
+        c = _filled(rng, kind, kind if held == "own" else held, k_len, 16, 2, 64, 64)
+        Q = _rand(rng, kind, 2, shape[1], shape[0], 64, spread=3.0)
+        _attend_and_check(ctx, kind, c, Q, k_len, cap=cap)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [0.01, 1.0, 50.0, 1e4, 1e20, 1e38])
+def test_a_capped_score_is_as_exact_as_it_is_small(ctx, kind, cap):
+    """Sequences of one key: lse is the score itself, which has to keep its relative error whatever its size beside the cap.
+
+    Off by less than 10 u32 for the tanh and its factors (see the oracle), 1 for the product of the features and 2 for the way from the base-2 exponent to e: 13 u32,
+    and steps of fp32's smallest numbers."""
+    from paper_1809_11165_amd import binding
+    B, H = 2048, 16
+    n = B * H
+    size = np.concatenate([np.linspace(0.4, 0.6, n // 4), np.geomspace(1e-6, 30, n - n // 4)]) * min(cap, 1e3)
+    k = torch.from_numpy((size * np.where(np.arange(n) % 2, 1, -1)).astype(np.float32)).to(TYPES[kind]).view(B, 1, H, 1)
+    c = _new(kind, B, 16, H, 1, 1, torch.arange(B, dtype=torch.int32, device=DEV)[:, None].contiguous(), 0)
+    ctx.bbmm_cache_write(c, k.to(DEV), torch.ones_like(k, device=DEV))
+    Q = torch.ones(B, 1, H, 1, dtype=TYPES[kind], device=DEV)
+    _, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int([1] * B), scale=1.0, cap=cap))
+    s = cap * np.tanh(_host(k)[:, 0, :, 0] / cap)
+    worst = (np.abs(_host(lse)[:, :, 0] - s) / (13 * A.U32 * np.abs(s) + 2.0 ** -140)).max()
     assert worst <= 1
