@@ -50,14 +50,14 @@ __device__ __forceinline__ float quarters_sum(float x) {
   return __int_as_float(r[0]) + __int_as_float(r[1]);
 }
 
-// c + a b where a, values, holds infinities or NaN that rows of weight zero must not meet: finite values are multiplied as ever; a column gets
-// an infinity or NaN where its weight for one is not zero.  b: the weights' parts.
+// c + a b where a, values, holds infinities or NaN: finite values are multiplied as ever; a column gets an infinity or NaN if it takes one (`took`, a bit
+// a key), whatever the weight, whose parts have either sign.  b: the weights' parts.
 template <typename T, int PARTS>
-__device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, const typename Mma<T>::frag (&b)[PARTS], f32x4 c) {
+__device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, const typename Mma<T>::frag (&b)[PARTS], unsigned took, f32x4 c) {
   const float odd[3] = {__builtin_inff(), -__builtin_inff(), __builtin_nanf("")};
-  typename Mma<T>::frag x = a;
+  typename Mma<T>::frag x = a, ones = a;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = fabsf((float)a[e]) < __builtin_inff() ? a[e] : (T)0.f;
+  for (int e = 0; e < 8; ++e) x[e] = fabsf((float)a[e]) < __builtin_inff() ? a[e] : (T)0.f, ones[e] = (took >> e) & 1 ? (T)1.f : (T)0.f;
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) c = Mma<T>::mma(x, b[p], c);
 #pragma unroll
@@ -67,9 +67,7 @@ __device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, const typename
       float y = (float)a[e];
       x[e] = (k == 2 ? y != y : y == odd[k]) ? (T)1.f : (T)0.f;
     }
-    f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) z = Mma<T>::mma(x, b[p], z);
+    f32x4 z = Mma<T>::mma(x, ones, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (z[r] != 0.f) c[r] += odd[k];
@@ -186,11 +184,12 @@ __device__ __forceinline__ Share share_of(const CacheArgs& c, const CacheAtt& a,
   return mine;
 }
 
-// Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.
+// Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.  (8-bit rows in bf16, one wave more / so: 4 requests of 40000 keys,
+// 4 shared heads, d 64 31.5 / 28.3 us, d 128 45.5 / 42.4, 16 of 65536 keys, 8 shared heads of 128, 249 / 240.)
 constexpr int waves_of(int size, bool e4m3, int dp, int nt, bool even) {
   if (nt == 2) return 2;
   if (size == 4) return dp == 64 && (even || !e4m3) ? 3 : 2;
-  return dp == 64 ? (even ? 4 : 3) : e4m3 && even ? 3 : 2;
+  return dp == 64 ? (even && !e4m3 ? 4 : 3) : 2;
 }
 
 // T held as such: a key's piece is 16 bytes, a value's 16 (two-byte values of up to 64 features: 8); E4M3: the same features in a half or a quarter.
@@ -483,8 +482,19 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
 #pragma unroll
   for (int n = 0; n < NT; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
 
+  // Keys of the block from j0 on that the lane's row takes, of those kept.
+  auto taken = [&](int n, int j0, unsigned keep) {
+    int64_t p = (int64_t)kn - qn + qi[n] - j0;             // the row's place in the block
+    if (a.causal) keep &= p < 0 ? 0u : p >= 31 ? ~0u : (2u << (int)p) - 1;
+    if (a.window) {
+      int64_t w = p - a.window + 1;                        // the first key
+      keep &= w <= 0 ? ~0u : w >= 32 ? 0u : ~0u << (int)w;
+    }
+    return keep;
+  };
+
   // O^T += V^T P^T; s[n][k][r]: weight of row n, key 16 k + 4 q4 + r.  fp32: eight single products make a step, of four keys each.
-  auto add_values = [&](const f32x4 (*p)[2], unsigned keep, auto odd) {
+  auto add_values = [&](const f32x4 (*p)[2], int j0, unsigned keep, auto odd) {
     frag pf[NT][WPARTS];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -506,11 +516,19 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
         }
       }
     }
+    unsigned took[NT];                                     // a bit each of the lane's eight keys
+    if constexpr (decltype(odd)::value) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        unsigned mine = taken(n, j0, keep);
+        took[n] = ((mine >> (4 * q4)) & 0xfu) | ((mine >> (12 + 4 * q4)) & 0xf0u);
+      }
+    }
     auto product = [&](frag v, int f) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         if constexpr (decltype(odd)::value) {
-          acc[n][f] = mma_odd<C, WPARTS>(v, pf[n], acc[n][f]);
+          acc[n][f] = mma_odd<C, WPARTS>(v, pf[n], took[n], acc[n][f]);
         } else {
 #pragma unroll
           for (int x = 0; x < WPARTS; ++x) acc[n][f] = M::mma(v, pf[n][x], acc[n][f]);
@@ -634,15 +652,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     if (decltype(edge)::value || keep != ~0u) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        unsigned mine = keep;
-        if constexpr (decltype(edge)::value) {
-          int64_t p = (int64_t)kn - qn + qi[n] - j0;       // the row's place in the block
-          if (a.causal) mine &= p < 0 ? 0u : p >= 31 ? ~0u : (2u << (int)p) - 1;
-          if (a.window) {
-            int64_t w = p - a.window + 1;                  // the first key
-            mine &= w <= 0 ? ~0u : w >= 32 ? 0u : ~0u << (int)w;
-          }
-        }
+        unsigned mine = decltype(edge)::value ? taken(n, j0, keep) : keep;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (!((mine >> (16 * (e >> 2) + 4 * q4 + (e & 3))) & 1)) s[n][e >> 2][e & 3] = -__builtin_inff();
@@ -698,7 +708,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
       fetch_k(next, keep_next);
       weights(t * kBlock, keep, Const<0>{});
       clear_values(keep);
-      add_values(s, keep, Const<0>{});
+      add_values(s, t * kBlock, keep, Const<0>{});
       fetch_v(next, keep_next);
       next = after;
       keep = keep_next;
@@ -706,7 +716,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     scores();
     weights(t * kBlock, keep, Const<0>{});
     clear_values(keep);
-    add_values(s, keep, Const<0>{});
+    add_values(s, t * kBlock, keep, Const<0>{});
   }
   // and the others, few: [t0, a0) and [a1, t1).  Infinities and NaN among their values are kept from rows that do not take them (an 8-bit value may
   // become infinite in fp16 as well).
@@ -719,8 +729,8 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     scores();
     weights(at * kBlock, keep, Const<1>{});
     clear_values(keep);
-    if (__any(odd_values()) || (E4M3 && __is_same(T, _Float16))) add_values(s, keep, Const<1>{});
-    else add_values(s, keep, Const<0>{});
+    if (__any(odd_values()) || (E4M3 && __is_same(T, _Float16))) add_values(s, at * kBlock, keep, Const<1>{});
+    else add_values(s, at * kBlock, keep, Const<0>{});
   }
 
   // the waves' sums: each scales its own to the largest reference; two leave theirs in LDS, the other two add them, all write
@@ -777,11 +787,38 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   if (!whole && !some) return;                             // parts without weight are not read
   const float* src = buf + row * (DP + 4);
   T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
+  float check = 0.f;                                       // NaN if an output is not finite
   for (int f = tid % TR * 4; f < DP; f += 4 * TR) {
     f32x4 y = (*(const f32x4*)(src + f) + *(const f32x4*)(src + kPart + f)) * inv;
     if (!some) y = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (f < c.dv) check = fmaf(y[0], 0.f, fmaf(y[1], 0.f, fmaf(y[2], 0.f, fmaf(y[3], 0.f, check))));
     if (whole) store4<T>(out, f, c.dv, a.ovec, y[0], y[1], y[2], y[3]);
     else if (f < a.dv4) *(f32x4*)(a.pO + at * a.dv4 + f) = y;
+  }
+  if (check == 0.f || lse2 != lse2) return;
+  // Infinities among the values that the row takes: its weights are positive, but a product with the weight's parts, which have either sign, or with a
+  // weight that rounds to zero is NaN.  So what is not finite is looked up in the values themselves (one thread a feature: slow, and rare).
+  int64_t p = (int64_t)kn - qn + i;
+  int from = max(t0 * kBlock, a.window ? (int)max(p - a.window + 1, (int64_t)0) : 0), to = (int)min((int64_t)t1 * kBlock, a.causal ? min(p + 1, (int64_t)kn) : (int64_t)kn);
+#pragma unroll 1
+  for (int z = 0; z < DP / TR; ++z) {
+    int f = 4 * (tid % TR + TR * (z >> 2)) + (z & 3);
+    if (f >= c.dv || fabsf((src[f] + src[kPart + f]) * inv) < __builtin_inff()) continue;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int j = from; j < to; ++j) {
+      uint32_t n = over((uint32_t)j, c.page);
+      int pg = table[n], row = j - (int)(n * c.page.d);
+      if ((unsigned)pg >= (unsigned)c.pages) continue;
+      const char* at = V + pg * vpage + (int64_t)row * vpitch + f * SB;
+      float y;
+      if constexpr (E4M3) y = (float)Wide<T>::template get<false>(*(const uint8_t*)at, block_scale(ve[pg * epage + (int64_t)row * 4 + f / 32], 0))[0];
+      else y = (float)*(const T*)at;
+      sum += fabsf(y) < __builtin_inff() ? 0.f : y;
+    }
+    if (sum == 0.f) continue;                              // (or NaN)
+    if (whole) out[f] = (T)sum;
+    else a.pO[at * a.dv4 + f] = sum;
   }
 }
 
@@ -853,6 +890,18 @@ __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt
   if (lane == 0) a.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
   T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
   store4<T>(out, f, c.dv, a.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+  // infinities of the parts come through whatever their weight, which may have rounded to zero
+  float check = fmaf(y[0], 0.f, fmaf(y[1], 0.f, fmaf(y[2], 0.f, y[3] * 0.f)));
+  if (check == 0.f || sum != sum) return;
+#pragma unroll 1
+  for (int e = f; e < min(f + 4, c.dv); ++e) {
+    float odd = 0.f;
+    for (int s = 0; s < parts; ++s) {
+      float v = a.pO[(from + s * step) * a.dv4 + e];
+      if (a.pl[from + s * step] != -__builtin_inff() && !(fabsf(v) < __builtin_inff())) odd += v;
+    }
+    if (odd != 0.f) out[e] = (T)odd;
+  }
 }
 
 template <typename T, bool E4M3, int DP, int NT>

@@ -1,10 +1,10 @@
 """GPU parity of the attention over a paged cache where numbers are out of the ordinary: weights whose lowest bits decide, caps
-from far below the scores to fp32's largest numbers."""
+from far below the scores to fp32's largest numbers, and infinite values that some rows take."""
 import numpy as np
 import pytest
 
 from oracle import cache_oracle as A
-from test_gpu_cache import DEV, TYPES, _attend_and_check, _filled, _host, _int, _new, _rand
+from test_gpu_cache import DEV, TYPES, _attend_and_check, _check, _filled, _host, _int, _new, _oracle, _rand
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -85,3 +85,95 @@ def test_a_capped_score_is_as_exact_as_it_is_small(ctx, kind, cap):
     s = cap * np.tanh(_host(k)[:, 0, :, 0] / cap)
     worst = (np.abs(_host(lse)[:, :, 0] - s) / (13 * A.U32 * np.abs(s) + 2.0 ** -140)).max()
     assert worst <= 1
+
+
+# k_len, heads, hk, nq, d, dv, page, pages of a table row, options of the call; then the keys (sequence, from its end) whose value is not finite
+ODD = {
+    "one_row": ([300, 90], 4, 2, 1, 64, 64, 16, None, {}, [(0, 1), (0, 20), (0, 299), (1, 40)]),
+    "one_row_page_of_twenty": ([300, 90], 4, 2, 1, 128, 128, 20, None, {}, [(0, 1), (0, 150), (1, 90)]),
+    "new_rows": ([300, 90], 4, 2, 5, 64, 64, 16, None, {}, [(0, 1), (0, 3), (0, 150), (1, 4), (1, 89)]),
+    "rows_40": ([300, 90], 8, 1, 5, 128, 128, 16, None, {}, [(0, 2), (0, 100), (0, 300), (1, 4), (1, 60)]),
+    "rows_40_page_of_twenty": ([300, 90], 8, 1, 5, 128, 128, 20, None, {}, [(0, 2), (0, 100), (1, 3)]),
+    "window": ([700, 90], 4, 2, 5, 64, 64, 16, None, dict(window=100), [(0, 3), (0, 50), (0, 102), (0, 104), (0, 300), (1, 85)]),
+    "all_keys": ([300, 90], 4, 2, 5, 64, 64, 16, None, dict(causal=False), [(0, 1), (1, 40)]),
+    "parts": ([5000, 1300], 4, 1, 1, 64, 64, 16, None, {}, [(0, 1), (0, 2500), (0, 4990), (1, 700)]),
+    "parts_rows_40": ([5000, 1300], 8, 1, 5, 128, 128, 16, None, {}, [(0, 3), (0, 2500), (1, 700)]),
+    "dealt": ([17000, 64, 700], 4, 2, 1, 64, 64, 16, 1100, {}, [(0, 9000), (1, 1), (2, 650)]),
+    "odd_features": ([150, 90], 3, 1, 2, 33, 7, 16, None, {}, [(0, 1), (0, 100), (1, 50)]),
+}
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("name", list(ODD))
+@pytest.mark.parametrize("value", ["inf", "-inf", "nan", "both"])
+def test_infinite_values_come_through_where_they_are_taken(ctx, name, kind, value):
+    """One feature of some values is infinite (or NaN, or infinities of both signs in turn): it is so in the outputs of the rows that take the key, wherever that
+    lies among the blocks, and nothing else changes."""
+    from paper_1809_11165_amd import binding
+    k_len, heads, hk, nq, d, dv, page, most, opt, places = ODD[name]
+    rng = np.random.default_rng(sum(map(ord, name)))
+    c = _filled(rng, kind, kind, k_len, page, hk, d, dv, most)
+    Q = _rand(rng, kind, len(k_len), nq, heads, d)
+    val, err = _oracle(kind, c, Q, k_len, **opt)
+    for at, (b, back) in enumerate(places):
+        j, f = k_len[b] - back, at % min(dv, 3)
+        x = float(value) if value != "both" else (-1.0) ** (at // min(dv, 3)) * float("inf")
+        c.V[int(c.table[b, j // page]), j % page, at % hk, f] = x
+        takes = A.taken(k_len[b], nq, k_len[b], opt.get("causal", True), opt.get("window", 0))[:, j]
+        heads_of = np.arange(heads) // (heads // hk) == at % hk
+        with np.errstate(invalid="ignore"):
+            val["o"][b, :, :, f][np.outer(takes, heads_of)] += x
+    O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int(k_len), **opt))
+    _check(lse, val, err, "lse")
+    got = _host(O)
+    off = ~np.isfinite(val["o"])
+    assert off.any() and np.array_equal(got[off], val["o"][off], equal_nan=True)
+    assert np.all(np.abs(got[~off] - val["o"][~off]) <= err["o"][~off])
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n", [90, 5000])
+@pytest.mark.parametrize("first", [True, False])
+def test_an_infinite_value_whose_weight_rounds_to_zero(ctx, kind, n, first):
+    """A weight is positive however small, in whatever order the keys come and whether or not they lie in one part.  The other values are those of the key that
+    outweighs all, times its weight and divided by it: 4 u32, and rounded; lse is off by 4 u32 of itself (the factor to base 2 and back, twice rounded)."""
+    from paper_1809_11165_amd import binding
+    rng = np.random.default_rng(22)
+    c = _filled(rng, kind, kind, [n], 16, 1, 64, 64)
+    Q = torch.zeros(1, 1, 4, 64, dtype=TYPES[kind], device=DEV)
+    Q[..., 0] = 16.0
+    at = torch.arange(n, device=DEV)
+    page, row = c.table[0].long()[at // 16], at % 16
+    c.K[page, row, 0, 0] = 0.0
+    far, top = (3, n - 3) if first else (n - 3, 3)
+    c.K[page[top], row[top], 0, 0] = 100.0                   # 1600 above all others
+    c.V[page[far], row[far], 0, 5] = float("inf")
+    O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int([n]), scale=1.0))
+    want, got = _host(c.V[page[top], row[top], 0]), _host(O)[0, 0]
+    assert np.all(got[:, 5] == np.inf)
+    got[:, 5] = want[5]
+    assert np.all(np.abs(got - want) <= (4 * A.U32 + A.UNIT[kind]) * np.abs(want))
+    assert np.all(np.abs(_host(lse) - 1600) <= 4 * A.U32 * 1600)
+
+
+@pytest.mark.parametrize("nq", [1, 5])
+@pytest.mark.parametrize("back", [1, 200])
+def test_8_bit_values_beyond_fp16_are_infinite_there(ctx, nq, back):
+    """As they are where they are read back in fp16; in the other types they are numbers."""
+    from paper_1809_11165_amd import binding
+    for kind in TYPES:
+        rng = np.random.default_rng(23)
+        k_len = [300, 90]
+        c = _filled(rng, kind, "e4m3", k_len, 16, 2, 64, 64)
+        Q = _rand(rng, kind, 2, nq, 4, 64)
+        j = k_len[0] - back
+        page, row = int(c.table[0, j // 16]), j % 16
+        c.V.view(torch.uint8)[page, row, :, :32] = 0x38      # ones
+        c.v_exp[page, :, row, 0] = 127 + 17
+        val, err = _oracle(kind, c, Q, k_len)
+        if kind == "f16":
+            takes = A.taken(300, nq, 300)[:, j]
+            val["o"][0, takes, :, :32] = np.inf
+        O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int(k_len)))
+        _check(O, val, err, "o")
+        _check(lse, val, err, "lse")
