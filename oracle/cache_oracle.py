@@ -10,7 +10,8 @@ sums of n terms n u32) and outputs are rounded to the type once (unit u), weight
     r          er = (d / 2 + 8) u32 of itself: d squares, the root;   cos, sin   ec = 6 u32 + 2^-51 |angle|, absolutely
     y          (|z_a| + |z_b|) (ec + er + 5 u32) + u |y|
     dz         e_dz = (|dy_a| + |dy_b|) (ec + 3 u32)
-    dw         sum |n| (e_dz + |dz| (er + (terms + 2) u32)) + u |dw| + terms 2^-150 (sums of tiny terms)
+    dw         sum |n| (e_dz + |dz| (er + (min(terms, 64) + 10) u32)) + u |dw| + terms 2^-150 (sums of tiny terms): a lane adds up some of its workgroup's
+               rows, 64 of them at most wherever this is compared, eight steps add the lanes of a workgroup, and workgroups are joined in 64 bits
     dx         r (|w| e_dz + |n| e_m + (2 er + 8 u32) (|w dz| + |n m|)) + u |dx|,   m the mean, e_m = mean |n| (|w| e_dz + |w dz| (er + (d + 4) u32))
     scores     ds = 2 (d + 8) u32 max_j (scale sum |q||k| + |lse|) + 20 u32 max_j |s|   (of a weight; the last with a cap, whose tanh is off by less than 10 u32 of itself)
     o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|   (up to 16 rows of a shared head in bf16: weights are three operands, u^2 stands for less than u32)
@@ -86,7 +87,7 @@ def rotate(kind, x, angle, neighbours=False, eps=None, weight=None, dy=None, row
     if weight is not None:
         terms = x.shape[0] * x.shape[1] * x.shape[2]
         val["dw"] = (dz * n).sum((0, 1, 2))
-        lim["dw"] = (np.abs(n) * (e_dz + np.abs(dz) * (er + (terms + 2) * U32))).sum((0, 1, 2)) + u * np.abs(val["dw"]) + tiny
+        lim["dw"] = (np.abs(n) * (e_dz + np.abs(dz) * (er + (min(terms, 64) + 10) * U32))).sum((0, 1, 2)) + u * np.abs(val["dw"]) + tiny
         lim["dw"] += terms * 2.0 ** -150                     # an addition of fp32 numbers is off by half a step of their subnormal ones
     dx, e = dz, e_dz + 3 * U32 * np.abs(dz)
     if eps is not None:
