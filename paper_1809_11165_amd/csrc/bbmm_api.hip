@@ -2645,7 +2645,8 @@ int cached_args(bbmm_ctx* c, const bbmm_cache* cache, const bbmm_cached_attentio
   int64_t rows = in->nq * t->G, tile = cache_rows(in->type, rows);
   t->blocks = (int)((rows + tile - 1) / tile);
   int64_t wgs = cache->batch * cache->kv_heads * ((rows + 15) / 16);
-  if (cache->batch * in->heads * in->nq > kMaxRows || wgs > kAttMaxGrid) return fail(c, BBMM_EINVAL, "cached attention: more than 2^27 rows in one call");
+  if (cache->batch * in->heads * in->nq > kMaxRows) return fail(c, BBMM_EINVAL, "cached attention: more than 2^27 rows in one call");
+  if (wgs > kAttMaxGrid) return fail(c, BBMM_EINVAL, "cached attention: more than 2^23 blocks of up to 16 rows of a shared head in one call");
   int64_t reach = t->window ? std::min<int64_t>(a->rows_most, (int64_t)t->window + t->nq) : a->rows_most;
   cache_parts(c->num_cus, cache_held(in->type, cache->type == BBMM_TYPE_E4M3, *a, rows), a->B, std::max<int64_t>((int64_t)a->HK * t->blocks, 1), reach, t);
   t->dv4 = (a->dv + 3) / 4 * 4;

@@ -177,3 +177,22 @@ def test_8_bit_values_beyond_fp16_are_infinite_there(ctx, nq, back):
         O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int(k_len)))
         _check(O, val, err, "o")
         _check(lse, val, err, "lse")
+
+
+def test_a_refusal_names_the_limit_that_is_passed(ctx):
+    import ctypes as C
+    from paper_1809_11165_amd import binding
+    c = _new("f16", 1, 16, 1, 64, 64, torch.zeros(1, 1, dtype=torch.int32, device=DEV))
+    s, a = binding.CachedAttention(c, torch.zeros(1, 1, 1, 64, dtype=torch.float16, device=DEV), _int([1])).to_c(ctx.device)
+    n = C.c_int64(0)
+
+    def refused(batch, kv_heads, heads, nq):
+        s.batch, s.kv_heads, a.heads, a.nq = batch, kv_heads, heads, nq
+        rc = ctx.lib.bbmm_attend_cache_workspace(ctx.h, C.byref(s), C.byref(a), C.byref(n))
+        return None if rc == 0 else ctx.lib.bbmm_last_error(ctx.h).decode()
+
+    assert refused(4096, 2048, 2048, 1) is None
+    assert "2^23" in refused(4097, 2048, 2048, 1)          # 2^23 rows and as many blocks, each of a shared head of its own
+    assert "2^23" in refused(4096, 4096, 4096, 1)
+    assert refused(128, 1, 16, 65536) is None
+    assert "2^27" in refused(129, 1, 16, 65536)
