@@ -12,6 +12,7 @@ import os
 import struct
 from array import array
 from dataclasses import dataclass, field
+from operator import index
 from typing import Optional
 
 import numpy as np
@@ -457,8 +458,8 @@ class Rotation:
             pp = pos.data_ptr()
         if self.axis is not None:
             try:
-                axis = array("B", bytes(self.axis))
-            except (ValueError, TypeError):
+                axis = array("B", self.axis if isinstance(self.axis, (list, tuple, bytes)) else [index(a) for a in self.axis])
+            except (ValueError, TypeError, OverflowError):
                 raise ValueError("axis must hold whole numbers of axes") from None
             if len(axis) != half:
                 raise ValueError("axis has %d entries, expected %d" % (len(axis), half))
