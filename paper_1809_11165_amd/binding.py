@@ -446,11 +446,11 @@ class Rotation:
         half = fp = pp = qw = kw = lp = ap = 0
         axes, axis = 1, None
         if freq is not None:
-            half = len(freq)
+            half = freq.shape[0] if getattr(freq, "ndim", 0) else 0
             _check_same(freq, (half,), float64, device, "freq")
             fp = freq.data_ptr()
         if pos is not None:
-            if pos.ndim == 3:
+            if getattr(pos, "ndim", 0) == 3:
                 axes = pos.shape[0]
                 _check_same(pos, (axes, b, rows), int64, device, "pos")
             else:
@@ -474,8 +474,11 @@ class Rotation:
             _check_same(self.row_len, (b,), int32, device, "row_len")
             lp = self.row_len.data_ptr()
         norm = self.eps is not None
-        r = _Rotation.from_buffer_copy(_Rotation.pack(code, bool(self.neighbours), norm, axes, self.eps if norm else 0.0, b, rows, qh, kh, d, 2 * half,
-                                                      qp, kp, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], qw, kw, pp, ap, fp, lp))
+        try:
+            r = _Rotation.from_buffer_copy(_Rotation.pack(code, bool(self.neighbours), norm, axes, self.eps if norm else 0.0, b, rows, qh, kh, d,
+                                                          2 * half, qp, kp, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], qw, kw, pp, ap, fp, lp))
+        except struct.error:
+            raise TypeError("eps must be a number") from None
         r.keep = axis
         return r
 
@@ -592,9 +595,12 @@ class CachedAttention:
             _check_same(self.q_len, (b,), int32, device, "q_len")
             ql = self.q_len.data_ptr()
         qs = Q.stride()
-        return c, _CachedAttention.from_buffer_copy(_CachedAttention.pack(
-            code, bool(self.causal), h, nq, _int64(self.window), max(d, 1) ** -0.5 if self.scale is None else self.scale, self.cap, Q.data_ptr(),
-            qs[0], qs[1], qs[2], ql, self.k_len.data_ptr()))
+        try:
+            return c, _CachedAttention.from_buffer_copy(_CachedAttention.pack(
+                code, bool(self.causal), h, nq, _int64(self.window), max(d, 1) ** -0.5 if self.scale is None else self.scale, self.cap, Q.data_ptr(),
+                qs[0], qs[1], qs[2], ql, self.k_len.data_ptr()))
+        except (struct.error, TypeError, ValueError, OverflowError):
+            raise TypeError("scale and cap must be numbers, window a whole one") from None
 
 
 @dataclass
