@@ -578,7 +578,7 @@ int bbmm_cache_read(bbmm_ctx* ctx, const bbmm_cache* cache, int32_t type, int64_
  *   p_i = k_len_b - q_len_b + i is the row's own place (the new rows are the sequence's last).
  * Rows that nothing is left for, and rows at or behind q_len_b, have o_i = 0 and lse_i = -infinity; what takes no part may hold
  * anything.  An infinity among the values that a row takes comes through as such, however small its weight; NaN and infinities of both signs as NaN
- * (a call with such values is slow: they are looked up one by one).  Scores, statistics and sums are fp32; weights are operands of parts in the products' type, each what rounding the ones before leaves:
+ * (calls with such values are slow: their rows are gone through key by key).  Large values keep to their mean where the sum leaves fp32 (and as slowly).  Scores, statistics and sums are fp32; weights are operands of parts in the products' type, each what rounding the ones before leaves:
  * three of bf16 (with more than 16 rows nq heads / kv_heads of a shared head over bf16 rows, two: 16 bits of a weight), two of fp16 (22 bits).
  *
  *   type          of Q and O; the cache's own unless that is E4M3.  heads: a multiple of the cache's kv_heads, head h reads

@@ -796,29 +796,59 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
     else if (f < a.dv4) *(f32x4*)(a.pO + at * a.dv4 + f) = y;
   }
   if (check == 0.f || lse2 != lse2) return;
-  // Infinities among the values that the row takes: its weights are positive, but a product with the weight's parts, which have either sign, or with a
-  // weight that rounds to zero is NaN.  So what is not finite is looked up in the values themselves (one thread a feature: slow, and rare).
+  // What is not finite is formed anew, key by key (a thread's features at once: slow, and rare).  Infinities among the values that the row takes come through: its
+  // weights are positive, but a product with the weight's parts, which have either sign, or with a weight that rounds to zero is NaN.  Without one, it was
+  // the sum that left fp32 before its division: with weights of the whole sum it is a mean, no larger than the values.
+  constexpr int N = DP / TR;                               // features of a thread: 4 neighbours, 4 TR apart
   int64_t p = (int64_t)kn - qn + i;
   int from = max(t0 * kBlock, a.window ? (int)max(p - a.window + 1, (int64_t)0) : 0), to = (int)min((int64_t)t1 * kBlock, a.causal ? min(p + 1, (int64_t)kn) : (int64_t)kn);
+  auto feature = [&](int z) { return 4 * (tid % TR + TR * (z >> 2)) + (z & 3); };
+  auto value = [&](const char* row, unsigned exps, int f) {   // an element of a held row
+    if constexpr (E4M3) return (float)Wide<T>::template get<false>(((const uint8_t*)row)[f], block_scale(exps, f / 32))[0];
+    else return (float)((const T*)row)[f];
+  };
+  const T* query = (const T*)a.Q + b * a.qs[0] + (int64_t)i * a.qs[1] + (int64_t)h * a.qs[2];
+  float odd[N], mean[N];
+#pragma unroll
+  for (int z = 0; z < N; ++z) odd[z] = mean[z] = 0.f;
 #pragma unroll 1
-  for (int z = 0; z < DP / TR; ++z) {
-    int f = 4 * (tid % TR + TR * (z >> 2)) + (z & 3);
-    if (f >= c.dv || fabsf((src[f] + src[kPart + f]) * inv) < __builtin_inff()) continue;
-    float sum = 0.f;
-#pragma unroll 4
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
     for (int j = from; j < to; ++j) {
       uint32_t n = over((uint32_t)j, c.page);
       int pg = table[n], row = j - (int)(n * c.page.d);
       if ((unsigned)pg >= (unsigned)c.pages) continue;
-      const char* at = V + pg * vpage + (int64_t)row * vpitch + f * SB;
-      float y;
-      if constexpr (E4M3) y = (float)Wide<T>::template get<false>(*(const uint8_t*)at, block_scale(ve[pg * epage + (int64_t)row * 4 + f / 32], 0))[0];
-      else y = (float)*(const T*)at;
-      sum += fabsf(y) < __builtin_inff() ? 0.f : y;
+      unsigned vexps = 0, kexps = 0;
+      if constexpr (E4M3) vexps = *(const unsigned*)(ve + pg * epage + (int64_t)row * 4), kexps = *(const unsigned*)(ke + pg * epage + (int64_t)row * 4);
+      float w = 0.f;
+      if (pass) {
+        const char* key = K + pg * kpage + (int64_t)row * kpitch;
+        float dot = 0.f;
+#pragma unroll 8
+        for (int x = 0; x < c.d; ++x) dot = fmaf((float)query[x], value(key, kexps, x), dot);
+        w = __builtin_amdgcn_exp2f((a.cap2 != 0.f ? capped<false>(dot, a) : dot * a.c2) - lse2);
+      }
+#pragma unroll
+      for (int z = 0; z < N; ++z) {
+        if (feature(z) >= c.dv) continue;
+        float y = value(V + pg * vpage + (int64_t)row * vpitch, vexps, feature(z));
+        if (pass) mean[z] = fmaf(w, y, mean[z]);
+        else odd[z] += fabsf(y) < __builtin_inff() ? 0.f : y;
+      }
     }
-    if (sum == 0.f) continue;                              // (or NaN)
-    if (whole) out[f] = (T)sum;
-    else a.pO[at * a.dv4 + f] = sum;
+    bool more = false;
+#pragma unroll
+    for (int z = 0; z < N; ++z) more |= feature(z) < c.dv && odd[z] == 0.f && !(fabsf((src[feature(z)] + src[kPart + feature(z)]) * inv) < __builtin_inff());
+    if (!more) break;
+  }
+  constexpr float most = __is_same(T, __bf16) ? 0x1.fep127f : 0x1.fffffep127f;
+#pragma unroll
+  for (int z = 0; z < N; ++z) {
+    int f = feature(z);
+    if (f >= c.dv || fabsf((src[f] + src[kPart + f]) * inv) < __builtin_inff()) continue;
+    float y = odd[z] != 0.f ? odd[z] : fminf(fmaxf(mean[z], -most), most);
+    if (whole) out[f] = (T)y;
+    else a.pO[at * a.dv4 + f] = y;
   }
 }
 
@@ -890,17 +920,21 @@ __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt
   if (lane == 0) a.lse[row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
   T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
   store4<T>(out, f, c.dv, a.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-  // infinities of the parts come through whatever their weight, which may have rounded to zero
+  // What is not finite is formed anew: infinities of the parts come through whatever their weight, which may have rounded to zero; else the sum left fp32.
   float check = fmaf(y[0], 0.f, fmaf(y[1], 0.f, fmaf(y[2], 0.f, y[3] * 0.f)));
   if (check == 0.f || sum != sum) return;
 #pragma unroll 1
   for (int e = f; e < min(f + 4, c.dv); ++e) {
-    float odd = 0.f;
+    float odd = 0.f, mean = 0.f;
+#pragma unroll 1
     for (int s = 0; s < parts; ++s) {
-      float v = a.pO[(from + s * step) * a.dv4 + e];
-      if (a.pl[from + s * step] != -__builtin_inff() && !(fabsf(v) < __builtin_inff())) odd += v;
+      float lse2 = a.pl[from + s * step], v = a.pO[(from + s * step) * a.dv4 + e];
+      if (lse2 == -__builtin_inff()) continue;
+      if (fabsf(v) < __builtin_inff()) mean = fmaf(__builtin_amdgcn_exp2f(lse2 - top) * inv, v, mean);
+      else odd += v;
     }
-    if (odd != 0.f) out[e] = (T)odd;
+    constexpr float most = __is_same(T, __bf16) ? 0x1.fep127f : 0x1.fffffep127f;
+    out[e] = (T)(odd != 0.f ? odd : fminf(fmaxf(mean, -most), most));
   }
 }
 

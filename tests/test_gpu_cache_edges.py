@@ -1,5 +1,6 @@
 """GPU parity of the attention over a paged cache where numbers are out of the ordinary: weights whose lowest bits decide, caps
-from far below the scores to fp32's largest numbers, and infinite values that some rows take."""
+from far below the scores to fp32's largest numbers, infinite values that some rows
+take, and values whose sums leave fp32."""
 import numpy as np
 import pytest
 
@@ -177,6 +178,25 @@ def test_8_bit_values_beyond_fp16_are_infinite_there(ctx, nq, back):
         O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int(k_len)))
         _check(O, val, err, "o")
         _check(lse, val, err, "lse")
+
+
+@pytest.mark.parametrize("kind,held", [("f32", "f32"), ("f32", "e4m3"), ("bf16", "bf16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("k_len,heads,hk,nq,most,opt", [([300, 90], 4, 2, 1, None, {}), ([300, 90], 8, 1, 5, None, dict(cap=2.0)), ([700, 90], 4, 2, 3, None, dict(window=50)),
+                                                        ([5000, 1300], 4, 1, 1, None, {}), ([17000, 64, 700], 4, 2, 1, 1100, {})])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 20)])
+def test_means_of_values_whose_sums_leave_fp32(ctx, kind, held, k_len, heads, hk, nq, most, opt, d, page):
+    """Values of 2^127: a sum of two is too large, a mean of any number is not."""
+    rng = np.random.default_rng(24)
+    c = _filled(rng, kind, held, k_len, page, hk, d, d, most)
+    if held == "e4m3":
+        c.V.view(torch.uint8).bitwise_and_(0x7f)
+        c.v_exp.fill_(127 + 119)
+    else:
+        c.V.copy_(c.V.abs().clamp(0.5, 1) * 2.0 ** 127)
+    Q = _rand(rng, kind, len(k_len), nq, heads, d)
+    val, _ = _oracle(kind, c, Q, k_len, **opt)
+    assert np.abs(val["o"]).max() > 2.0 ** (126 if held != "e4m3" else 118)
+    _attend_and_check(ctx, kind, c, Q, k_len, **opt)
 
 
 def test_a_refusal_names_the_limit_that_is_passed(ctx):
