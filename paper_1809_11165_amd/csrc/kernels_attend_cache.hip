@@ -75,7 +75,7 @@ __device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, const typename
   return c;
 }
 
-// fp32 numbers as three of bf16, 8 bits each: what is left is 2^-25 of them.  Products with 8-bit rows, which bf16 holds exactly, then run at a
+// fp32 numbers (no signalling NaN, whose only set bits may be cut off) as three of bf16, 8 bits each: what is left is 2^-25 of them.  Products with 8-bit rows, which bf16 holds exactly, then run at a
 // fifth of the fp32 instructions' time.
 __device__ __forceinline__ void in_three(const f32x8& x, bf16x8 (&p)[3]) {
 #pragma unroll
@@ -428,8 +428,11 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
           v1 = load16<T>(row, f1, c.d, a.qvec);
         }
         f32x8 x = __builtin_shufflevector(__builtin_bit_cast(f32x4, v0), __builtin_bit_cast(f32x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
-        if constexpr (kThree) in_three(x, qf[n][s]);
-        else qf[n][s][0] = x;
+        if constexpr (kThree) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = __builtin_canonicalizef(x[e]);
+          in_three(x, qf[n][s]);
+        } else qf[n][s][0] = x;
       }
     }
   }

@@ -199,6 +199,26 @@ def test_means_of_values_whose_sums_leave_fp32(ctx, kind, held, k_len, heads, hk
     _attend_and_check(ctx, kind, c, Q, k_len, **opt)
 
 
+@pytest.mark.parametrize("bits", [0x7f800001, 0x7fc00000, -0x7fffff, -0x400000])
+@pytest.mark.parametrize("held", ["f32", "e4m3"])
+def test_a_query_of_any_nan_gives_nan(ctx, held, bits):
+    """Also of one whose upper half is that of an infinity, which keys of one sign would make a score of -infinity."""
+    from paper_1809_11165_amd import binding
+    c = _filled(np.random.default_rng(25), "f32", held, [90], 16, 1, 64, 64)
+    at = torch.arange(90, device=DEV)
+    page, row = c.table[0].long()[at // 16], at % 16
+    first = c.K.view(torch.uint8 if held == "e4m3" else torch.float32)
+    first[page, row, 0, 0] = 0x38 if held == "e4m3" else 1.0
+    for sign in (1, -1):
+        if sign < 0:
+            first[page, row, 0, 0] = 0xb8 if held == "e4m3" else -1.0
+        Q = torch.zeros(1, 1, 2, 64, device=DEV)
+        Q.view(torch.int32)[0, 0, 0, 0] = bits
+        O, lse = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int([90])))
+        assert torch.isnan(O[0, 0, 0]).all() and torch.isnan(lse[0, 0]).all()
+        assert torch.isfinite(O[0, 0, 1]).all() and torch.isfinite(lse[0, 1]).all()
+
+
 def test_a_refusal_names_the_limit_that_is_passed(ctx):
     import ctypes as C
     from paper_1809_11165_amd import binding
