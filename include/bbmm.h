@@ -533,7 +533,7 @@ int bbmm_rotate_grad(bbmm_ctx* ctx, const bbmm_rotation* in, const void* dQr, co
  *
  *   type          BBMM_TYPE_F32, _F16, _BF16, or BBMM_TYPE_E4M3: 8-bit floats (4 exponent and 3 mantissa bits, largest 448) with a
  *                 power of two for every 32 features of a row (the last block may be shorter): the smallest 2^e, e >= -117, by which
- *                 the block's largest finite magnitude becomes at most 448.  Stored is x / 2^e rounded to nearest even (but not
+ *                 the block's largest finite magnitude becomes at most 448 (1 where that is 0).  Stored is x / 2^e rounded to nearest even (but not
  *                 beyond the type that x came in: 240 2^e is the last value then), infinities and NaN as NaN.  A value
  *                 read back is exact in fp32 and bf16, and rounded to fp16 where that type's range is left
  *   pages, page_rows   pages in 0 .. 2^31 - 1, page_rows in 1 .. 2^30, max_pages page_rows <= 2^30
@@ -577,9 +577,10 @@ int bbmm_cache_read(bbmm_ctx* ctx, const bbmm_cache* cache, int32_t type, int64_
  *   over rows j < k_len_b of pages that are there; with `causal` j <= p_i, with window > 0 j > p_i - window, where
  *   p_i = k_len_b - q_len_b + i is the row's own place (the new rows are the sequence's last).
  * Rows that nothing is left for, and rows at or behind q_len_b, have o_i = 0 and lse_i = -infinity; what takes no part may hold
- * anything.  An infinity among the values that a row takes comes through as such, however small its weight; NaN and infinities of both signs as NaN
- * (calls with such values are slow: their rows are gone through key by key).  Large values keep to their mean where the sum leaves fp32 (and as slowly).  Scores, statistics and sums are fp32; weights are operands of parts in the products' type, each what rounding the ones before leaves:
- * three of bf16 (with more than 16 rows nq heads / kv_heads of a shared head over bf16 rows, two: 16 bits of a weight), two of fp16 (22 bits).
+ * anything.  An infinity among the values that a row takes comes through as such, however small its weight; NaN, and infinities of both
+ * signs, as NaN.  Large values keep to their mean where the sum leaves fp32.  (Rows of such values are slow: they are gone through key by key.)
+ * Scores, statistics and sums are fp32; weights are operands of parts in the products' type, each what rounding the ones before leaves: three of
+ * bf16 (two, 16 bits of a weight, with more than 16 rows nq heads / kv_heads of a shared head where rows are bf16), two of fp16 (22 bits).
  *
  *   type          of Q and O; the cache's own unless that is E4M3.  heads: a multiple of the cache's kv_heads, head h reads
  *                 shared head h / (heads / kv_heads)

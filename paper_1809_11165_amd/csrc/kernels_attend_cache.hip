@@ -8,10 +8,11 @@
 //   values: a lane reads, of the eight keys whose weights it will meet, DP / 16 neighbouring features, 16 lanes a row.  Two-byte values then
 //           change places in pairs (one byte permutation per two values); fp32 values are operands as they stand.  No LDS before the join, but for queries of 32 rows.
 // 8-bit rows become T on the way, by the instruction that applies their block's power of two.
-// Bound by memory with up to 16 rows a shared head: 8 requests of up to 32773 keys, 8 shared heads of 128, bf16, 660 MB in 117.8 us, 5.6 TB/s (a large
-// copy: 4.9); 16 of up to 65536 8-bit keys, 1.24 GB in 222 us, 5.6 TB/s; 64 with a window of 1024, fp16, d 64, 228 MB in 44.2 us, 5.2 TB/s.  With 32
-// rows and more by the products and the vector work beside them: 2 x 512 new rows of 32 heads on 8 over 8192 keys 298 us, 460 TFLOP/s.
-// Few keys: the chain length, page, keys, scores, join (77 keys 5.1 us); 3 rows over 10000 keys in fp32, pages of 20 rows: 24.3 us, see the loop.
+// Bound by memory with up to 16 rows a shared head (all from HBM, other data each time): 8 requests of up to 32773 keys, 8 shared heads of 128, bf16, 660 MB in 120 us,
+// 5.5 TB/s (a large copy: 4.9); 16 of up to 65536 8-bit keys, 1.24 GB in 232 us, 5.3 TB/s; 64 with a window of 1024, fp16, d 64, 228 MB in 46.8 us,
+// 4.9 TB/s.  With 32 rows and more by the products and the vector work beside them: 2 x 512 new rows of 32 heads on 8 over 8192 keys 295 us, 466 TFLOP/s
+// (8-bit pages 263 us; fp32, 16 rows a workgroup, 1229 us, 112 TFLOP/s of 153).  Few keys: the chain length, page, keys, scores, join (77 keys 5.1 us).  3 rows
+// over 10000 keys in fp32, pages of 20 rows: 27.7 us with the join, see the loop.  Up to 64 features take the width of 64, so narrower rows leave lanes idle.
 #include <type_traits>
 
 #include "cache_dev.h"
@@ -185,7 +186,9 @@ __device__ __forceinline__ Share share_of(const CacheArgs& c, const CacheAtt& a,
 }
 
 // Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.  (8-bit rows in bf16, one wave more / so: 4 requests of 40000 keys,
-// 4 shared heads, d 64 31.5 / 28.3 us, d 128 45.5 / 42.4, 16 of 65536 keys, 8 shared heads of 128, 249 / 240.)
+// 4 shared heads, d 64 31.5 / 28.3 us, d 128 45.5 / 42.4, 16 of 65536 keys, 8 shared heads of 128, 249 / 240.)  Left in scratch at two waves: 40 to 64 bytes a lane
+// where page rows are no multiple of 16, of rows of 128 features in fp32, and of 32 rows of them in bf16 and, own type, fp16.  8-bit pages, fp16, 64 features and 32 rows
+// would fit three.
 constexpr int waves_of(int size, bool e4m3, int dp, int nt, bool even) {
   if (nt == 2) return 2;
   if (size == 4) return dp == 64 && (even || !e4m3) ? 3 : 2;

@@ -184,7 +184,8 @@ __device__ __forceinline__ void fill_trig(const RotArgs& a, float2* trig, int64_
 
 // Rows of the workgroup's tokens, a group of LPR lanes a row at a time; the next one is on its way meanwhile (a prompt of 8192 x 40 heads of 128, bf16, one
 // row in hand / so: 42.0 / 41.0 us a call).  That prompt, 168 MB: 35.3 us, 4.75 TB/s, the rate of a copy.  2 x 2309 x 32 heads of 80 in fp16, three axes,
-// neighbouring pairs: 13.7 us, 3.5 TB/s, of which the launch and a workgroup's chain (positions, angles, rows) are 4.  One token: 4 us, that chain.
+// neighbouring pairs: 14.9 us from HBM (13.4 of data read just before), 3.2 TB/s, of which the launch and a workgroup's chain (positions, angles, rows) are 4.  One token:
+// 4 us, that chain.  Halves of the turned features that are no whole 16 bytes take single elements: 8192 x 40 heads of 40, bf16, 29.7 us, floor 10.7.
 template <typename T, int E, int LPR, int KS, bool NB>
 __global__ __launch_bounds__(256) void k_rotate(RotArgs a) {
   typedef Row<T, E, LPR, KS, NB> Rows;
