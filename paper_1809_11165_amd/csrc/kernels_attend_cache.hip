@@ -185,6 +185,15 @@ __device__ __forceinline__ Share share_of(const CacheArgs& c, const CacheAtt& a,
   return mine;
 }
 
+// NaN if one of the four features from f on is not finite (those behind the last are whatever the rows' memory holds), else 0.
+__device__ __forceinline__ float odd_of(f32x4 y, int f, int width) {
+  if (f + 4 > width) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = f + e < width ? y[e] : 0.f;
+  }
+  return fmaf(y[0], 0.f, fmaf(y[1], 0.f, fmaf(y[2], 0.f, y[3] * 0.f)));
+}
+
 // Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.  (8-bit rows in bf16, one wave more / so: 4 requests of 40000 keys,
 // 4 shared heads, d 64 31.5 / 28.3 us, d 128 45.5 / 42.4, 16 of 65536 keys, 8 shared heads of 128, 249 / 240.)  Left in scratch at two waves: 40 to 64 bytes a lane
 // where page rows are no multiple of 16, of rows of 128 features in fp32, and of 32 rows of them in bf16 and, own type, fp16.  8-bit pages, fp16, 64 features and 32 rows
@@ -797,7 +806,7 @@ __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void 
   for (int f = tid % TR * 4; f < DP; f += 4 * TR) {
     f32x4 y = (*(const f32x4*)(src + f) + *(const f32x4*)(src + kPart + f)) * inv;
     if (!some) y = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (f < c.dv) check = fmaf(y[0], 0.f, fmaf(y[1], 0.f, fmaf(y[2], 0.f, fmaf(y[3], 0.f, check))));
+    check += odd_of(y, f, c.dv);
     if (whole) store4<T>(out, f, c.dv, a.ovec, y[0], y[1], y[2], y[3]);
     else if (f < a.dv4) *(f32x4*)(a.pO + at * a.dv4 + f) = y;
   }
@@ -927,8 +936,7 @@ __global__ __launch_bounds__(256) void k_attend_cache_join(CacheArgs c, CacheAtt
   T* out = (T*)a.O + (((size_t)b * a.nq + i) * a.H + h) * c.dv;
   store4<T>(out, f, c.dv, a.ovec, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
   // What is not finite is formed anew: infinities of the parts come through whatever their weight, which may have rounded to zero; else the sum left fp32.
-  float check = fmaf(y[0], 0.f, fmaf(y[1], 0.f, fmaf(y[2], 0.f, y[3] * 0.f)));
-  if (check == 0.f || sum != sum) return;
+  if (odd_of(y, f, c.dv) == 0.f || sum != sum) return;
 #pragma unroll 1
   for (int e = f; e < min(f + 4, c.dv); ++e) {
     float odd = 0.f, mean = 0.f;

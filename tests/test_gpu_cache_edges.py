@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from oracle import cache_oracle as A
-from test_gpu_cache import DEV, TYPES, _attend_and_check, _check, _filled, _host, _int, _new, _oracle, _rand
+from test_gpu_cache import DEV, TYPES, _attend_and_check, _bytes, _check, _filled, _host, _int, _new, _oracle, _rand
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -197,6 +197,24 @@ def test_means_of_values_whose_sums_leave_fp32(ctx, kind, held, k_len, heads, hk
     val, _ = _oracle(kind, c, Q, k_len, **opt)
     assert np.abs(val["o"]).max() > 2.0 ** (126 if held != "e4m3" else 118)
     _attend_and_check(ctx, kind, c, Q, k_len, **opt)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("held", ["own", "e4m3"])
+@pytest.mark.parametrize("k_len,page", [([300, 90], 16), ([300, 90], 5), ([5000, 1300], 16)])
+def test_what_follows_the_last_feature_may_hold_anything(ctx, kind, held, k_len, page):
+    """Pages that the caller has filled, up to each row's next 16 bytes, and exponents of blocks that are not there."""
+    rng = np.random.default_rng(26)
+    held = kind if held == "own" else held
+    c = _filled(rng, kind, held, k_len, page, 2, 33, 7)
+    Q = _rand(rng, kind, 2, 2, 4, 33)
+    want = _oracle(kind, c, Q, k_len)
+    for x, width in ((c.K, 33), (c.V, 7)):
+        size = x.element_size()
+        _bytes(x).view(-1, (width * size + 15) // 16 * 16)[:, width * size:] = 0x7f if held == "e4m3" else 0xff
+    if held == "e4m3":
+        c.k_exp[..., 2:], c.v_exp[..., 1:] = 255, 255
+    _attend_and_check(ctx, kind, c, Q, k_len, want=want)
 
 
 @pytest.mark.parametrize("bits", [0x7f800001, 0x7fc00000, -0x7fffff, -0x400000])
