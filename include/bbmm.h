@@ -580,7 +580,7 @@ int bbmm_cache_read(bbmm_ctx* ctx, const bbmm_cache* cache, int32_t type, int64_
  * anything.  An infinity among the values that a row takes comes through as such, however small its weight; NaN, and infinities of both
  * signs, as NaN.  Large values keep to their mean where the sum leaves fp32.  (Rows of such values are slow: they are gone through key by key.)
  * Scores, statistics and sums are fp32; weights are operands of parts in the products' type, each what rounding the ones before leaves: three of
- * bf16 (two, 16 bits of a weight, with more than 16 rows nq heads / kv_heads of a shared head where rows are bf16), two of fp16 (22 bits).
+ * bf16 (24 bits), two of fp16 (22 bits).
  *
  *   type          of Q and O; the cache's own unless that is E4M3.  heads: a multiple of the cache's kv_heads, head h reads
  *                 shared head h / (heads / kv_heads)

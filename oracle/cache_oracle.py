@@ -6,7 +6,7 @@
     attention  s_ij = scale q_i.k_j or cap tanh(scale q_i.k_j / cap) over the keys that row i takes; o_i = sum softmax(s_i)_j v_j
 
 Beside every value stands an elementwise bound on what rounding may do to it when norms, functions, scores and sums are fp32 (unit u32 = 2^-24;
-sums of n terms n u32) and outputs are rounded to the type once (unit u), weights as operands twice (what the first rounding leaves is a second operand):
+sums of n terms n u32) and outputs are rounded to the type once (unit u), weights as operands twice or more (what a rounding leaves is a further operand):
     r          er = (d / 2 + 8) u32 of itself: d squares, the root;   cos, sin   ec = 6 u32 + 2^-51 |angle|, absolutely
     y          (|z_a| + |z_b|) (ec + er + 5 u32) + u |y|
     dz         e_dz = (|dy_a| + |dy_b|) (ec + 3 u32)
@@ -14,7 +14,7 @@ sums of n terms n u32) and outputs are rounded to the type once (unit u), weight
                rows, 64 of them at most wherever this is compared, eight steps add the lanes of a workgroup, and workgroups are joined in 64 bits
     dx         r (|w| e_dz + |n| e_m + (2 er + 8 u32) (|w dz| + |n m|)) + u |dx|,   m the mean, e_m = mean |n| (|w| e_dz + |w dz| (er + (d + 4) u32))
     scores     ds = 2 (d + 8) u32 max_j (scale sum |q||k| + |lse|) + 20 u32 max_j |s|   (of a weight; the last with a cap, whose tanh is off by less than 10 u32 of itself)
-    o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|   (up to 16 rows of a shared head in bf16: weights are three operands, u^2 stands for less than u32)
+    o          (u^2 + ds + (n + 1) u32) sum p|v| + u |o|   (bf16: weights are three operands, u^2 stands for less than u32)
 fp16 adds half a step of its subnormal numbers (weights are lifted by 2^6 before they meet them).
 """
 from __future__ import annotations

@@ -10,8 +10,8 @@
 // 8-bit rows become T on the way, by the instruction that applies their block's power of two.
 // Bound by memory with up to 16 rows a shared head (all from HBM, other data each time): 8 requests of up to 32773 keys, 8 shared heads of 128, bf16, 660 MB in 120 us,
 // 5.5 TB/s (a large copy: 4.9); 16 of up to 65536 8-bit keys, 1.24 GB in 232 us, 5.3 TB/s; 64 with a window of 1024, fp16, d 64, 228 MB in 46.8 us,
-// 4.9 TB/s.  With 32 rows and more by the products and the vector work beside them: 2 x 512 new rows of 32 heads on 8 over 8192 keys 295 us, 466 TFLOP/s
-// (8-bit pages 263 us; fp32, 16 rows a workgroup, 1229 us, 112 TFLOP/s of 153).  Few keys: the chain length, page, keys, scores, join (77 keys 5.1 us).  3 rows
+// 4.9 TB/s.  With 32 rows and more by the products and the vector work beside them: 2 x 512 new rows of 32 heads on 8 over 8192 keys 304 us, 452 TFLOP/s
+// (8-bit pages 305 us; fp32, 16 rows a workgroup, 1229 us, 112 TFLOP/s of 153).  Few keys: the chain length, page, keys, scores, join (77 keys 5.1 us).  3 rows
 // over 10000 keys in fp32, pages of 20 rows: 27.7 us with the join, see the loop.  Up to 64 features take the width of 64, so narrower rows leave lanes idle.
 #include <type_traits>
 
@@ -209,11 +209,12 @@ template <typename T, bool E4M3, int DP, int NT, bool EVEN>
 __global__ __launch_bounds__(256, waves_of(sizeof(T), E4M3, DP, NT, EVEN)) void k_attend_cache(CacheArgs c, CacheAtt a) {
   constexpr bool kThree = sizeof(T) == 4 && E4M3;          // operands in three parts of bf16
   constexpr int PARTS = kThree ? 3 : 1;                    // of the queries, and of the weights:
-  // Parts of the weights: what rounding to T leaves is a further operand.  bf16: three hold all 24 bits of a weight, which costs nothing beside the reads
-  // (one row, two parts / three: 8 requests of up to 32773 keys 124.0 / 124.5 us, 16 of 65536 8-bit keys 235.6 / 236.7; only with 8-bit rows of up to 64
-  // features 27.9 / 29.8).  With 32 rows products are the bound, and two parts leave 2^-16 of a weight (32 new rows of 4 sequences of 40000 keys 219 / 238,
-  // 8-bit pages 200 / 222).  fp16: two hold 22 bits.
-  constexpr int WPARTS = kThree ? 3 : sizeof(T) == 4 ? 1 : __is_same(T, __bf16) && NT == 1 ? 3 : 2;
+  // Parts of the weights: what rounding to T leaves is a further operand, until a weight is as good as in fp32: three of bf16 hold all 24 bits, two of
+  // fp16 22 and what the second's sign adds.  Outputs then fall on the wrong side of their own rounding less often than those of a plain softmax in fp32 (8
+  // requests of up to 32773 keys, bf16: 0.5 of 1000 against 1.0, and 1.8 with two parts; 2 of 20000, fp16: 2.0 against 4.0).  The third part costs nothing where reads are the bound (that
+  // call, two / three: 124.0 / 124.5 us; 16 of 65536 8-bit keys 235.6 / 236.7; 32 rows of 4 sequences of 40000 keys 67.3 / 67.5), else up to a sixth
+  // (8-bit rows of 64 features 27.9 / 29.8; 2 x 512 new rows over 8192 keys 295 / 304, 8-bit pages 264 / 305).
+  constexpr int WPARTS = kThree ? 3 : sizeof(T) == 4 ? 1 : __is_same(T, __bf16) ? 3 : 2;
   typedef std::conditional_t<kThree, __bf16, T> C;         // type of the operands
   typedef Mma<C> M;
   typedef typename M::frag frag;

@@ -19,8 +19,9 @@ def ctx():
     c.close()
 
 
+@pytest.mark.parametrize("rows", [1, 32, 40])
 @pytest.mark.parametrize("held", ["bf16", "e4m3"])
-def test_all_bits_of_a_weight_count_where_values_cancel(ctx, held):
+def test_all_bits_of_a_weight_count_where_values_cancel(ctx, held, rows):
     """Values of which less than 2^-10 of the size is left over, so that the output's own rounding is far below what weights of 16 bits would miss.
 
     A weight is off by less than 8 u32 (2 |s| log2 e for the steps before the exponential, 2 for it, 1 for its parts), the sums of n terms and the
@@ -44,13 +45,13 @@ def test_all_bits_of_a_weight_count_where_values_cancel(ctx, held):
     c = _new(held, pages, page, H, 1, 1, table, 0)
     as_rows = lambda x: torch.from_numpy(x).to(DEV).bfloat16()[..., None]
     ctx.bbmm_cache_write(c, as_rows(k), as_rows(v))
-    Q = torch.ones(B, 1, H, 1, dtype=torch.bfloat16, device=DEV)
+    Q = torch.ones(B, 1, rows * H, 1, dtype=torch.bfloat16, device=DEV)
     O, _ = ctx.bbmm_attend_cache(binding.CachedAttention(c, Q, _int([n] * B), scale=1.0))
     o = (p * v).sum(1)
     lim = (n + 10) * A.U32 * (p * np.abs(v)).sum(1) + A.UNIT["bf16"] * np.abs(o)
     most = np.abs(o).max()
     assert most < 2.0 ** -10
-    worst = (np.abs(_host(O)[:, 0, :, 0] - o) / lim).max()
+    worst = (np.abs(_host(O).reshape(B, H, rows) - o[:, :, None]) / lim[:, :, None]).max()
     assert worst <= 1
 
 
