@@ -76,8 +76,8 @@ __device__ __forceinline__ f32x4 mma_odd(typename Mma<T>::frag a, const typename
   return c;
 }
 
-// fp32 numbers (no signalling NaN, whose only set bits may be cut off) as three of bf16, 8 bits each: what is left is 2^-25 of them.  Products with 8-bit rows, which bf16 holds exactly, then run at a
-// fifth of the fp32 instructions' time.
+// fp32 numbers (no signalling NaN, whose only set bits may be cut off) as three of bf16, 8 bits each: what is left is 2^-25 of them.  Products with
+// 8-bit rows, which bf16 holds exactly, then run at a fifth of the fp32 instructions' time.
 __device__ __forceinline__ void in_three(const f32x8& x, bf16x8 (&p)[3]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -195,9 +195,9 @@ __device__ __forceinline__ float odd_of(f32x4 y, int f, int width) {
 }
 
 // Waves per SIMD: what the registers admit without keeping any of the loop's in scratch.  (8-bit rows in bf16, one wave more / so: 4 requests of 40000 keys,
-// 4 shared heads, d 64 31.5 / 28.3 us, d 128 45.5 / 42.4, 16 of 65536 keys, 8 shared heads of 128, 249 / 240.)  Left in scratch at two waves: 40 to 64 bytes a lane
-// where page rows are no multiple of 16, of rows of 128 features in fp32, and of 32 rows of them in bf16 and, own type, fp16.  8-bit pages, fp16, 64 features and 32 rows
-// would fit three.
+// 4 shared heads, d 64 31.5 / 28.3 us, d 128 45.5 / 42.4, 16 of 65536 keys, 8 shared heads of 128, 249 / 240.)  Left in scratch at two waves: 40 to 72 bytes a lane
+// where page rows are no multiple of 16, of rows of 128 features in fp32 and of 32 rows of them in own type or, bf16, 8 bits; 8 bytes of 32 bf16 rows of them elsewhere.  8-bit
+// pages, fp16, 64 features and 32 rows would fit three.
 constexpr int waves_of(int size, bool e4m3, int dp, int nt, bool even) {
   if (nt == 2) return 2;
   if (size == 4) return dp == 64 && (even || !e4m3) ? 3 : 2;
